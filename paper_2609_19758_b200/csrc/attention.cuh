@@ -1,0 +1,81 @@
+// Shared by the attention operators (norm_rope.cu, paged_attention.cu): element types, four-element loads and stores,
+// and the place of a token in a paged cache.
+#pragma once
+#include "fpsk_common.cuh"
+#include "fpsk_attention.h"
+
+namespace fpsk {
+
+constexpr size_t kAttnSyncBytes = 256;         // synchronisation words at the start of a workspace
+
+__host__ __device__ __forceinline__ int elem_size(int type) { return type == FPSK_ELEM_FP32 ? 4 : 2; }
+
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+    static __device__ __forceinline__ float to_f(float x) { return x; }
+    static __device__ __forceinline__ float from_f(float x) { return x; }
+};
+template <> struct Elem<__half> {
+    static __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+    static __device__ __forceinline__ __half from_f(float x) { return __float2half_rn(x); }
+};
+template <> struct Elem<__nv_bfloat16> {
+    static __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+    static __device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __float2bfloat16_rn(x); }
+};
+
+__device__ __forceinline__ uint32_t pack2(__half a, __half b)
+{
+    return (uint32_t)__half_as_ushort(a) | ((uint32_t)__half_as_ushort(b) << 16);
+}
+__device__ __forceinline__ uint32_t pack2(__nv_bfloat16 a, __nv_bfloat16 b)
+{
+    return (uint32_t)__bfloat16_as_ushort(a) | ((uint32_t)__bfloat16_as_ushort(b) << 16);
+}
+
+// Four consecutive elements as FP32; `wide`: the address is a multiple of four elements.
+__device__ __forceinline__ float4 load4(const float *p, bool wide)
+{
+    if (wide) return __ldg(reinterpret_cast<const float4 *>(p));
+    return make_float4(__ldg(p), __ldg(p + 1), __ldg(p + 2), __ldg(p + 3));
+}
+template <typename T> __device__ __forceinline__ float4 load4(const T *p, bool wide)
+{
+    if (wide) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2 *>(p));
+        const float2 a = HalfTraits<T>::unpack2(u.x), b = HalfTraits<T>::unpack2(u.y);
+        return make_float4(a.x, a.y, b.x, b.y);
+    }
+    return make_float4(Elem<T>::to_f(p[0]), Elem<T>::to_f(p[1]), Elem<T>::to_f(p[2]), Elem<T>::to_f(p[3]));
+}
+__device__ __forceinline__ void store4(float *p, float4 x, bool wide)
+{
+    if (wide) { *reinterpret_cast<float4 *>(p) = x; return; }
+    p[0] = x.x; p[1] = x.y; p[2] = x.z; p[3] = x.w;
+}
+template <typename T> __device__ __forceinline__ void store4(T *p, float4 x, bool wide)
+{
+    const T a = Elem<T>::from_f(x.x), b = Elem<T>::from_f(x.y), c = Elem<T>::from_f(x.z), d = Elem<T>::from_f(x.w);
+    if (wide) { *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(a, b), pack2(c, d)); return; }
+    p[0] = a; p[1] = b; p[2] = c; p[3] = d;
+}
+// four weights of a run-time type (they are read once per thread)
+__device__ __forceinline__ float4 load4_any(const void *p, int type, int at)
+{
+    if (type == FPSK_ELEM_FP32) return load4(static_cast<const float *>(p) + at, false);
+    if (type == FPSK_ELEM_FP16) return load4(static_cast<const __half *>(p) + at, false);
+    return load4(static_cast<const __nv_bfloat16 *>(p) + at, false);
+}
+
+__device__ __forceinline__ void report_status(int32_t *d_status, int code)
+{
+    if (d_status) atomicMax(d_status, code);
+}
+
+// Checks shared by the entry points (attention_api.cu).
+bool elem_ok(int type);
+bool head_dim_ok(int dim);
+fpsk_status check_cache(const fpsk_paged_cache *c);
+fpsk_status check_batch(const fpsk_paged_batch *b);
+
+}  // namespace fpsk
