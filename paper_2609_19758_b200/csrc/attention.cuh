@@ -72,6 +72,36 @@ __device__ __forceinline__ void report_status(int32_t *d_status, int code)
     if (d_status) atomicMax(d_status, code);
 }
 
+struct AttnArgs {
+    const void *q, *k, *v;
+    void *out;
+    float *lse;
+    long long qts, qhs, ots, ohs;
+    long long kps, kts, khs, vps, vts, vhs;
+    const int *cu_q, *kv_len, *table;
+    long long table_stride, n_pages;
+    int n_seqs, max_pages, page_size;
+    int n_tokens, hq, hk, group, dim;
+    int causal, window;
+    float scale_log2;                  // scores in units of ln 2: exponentials are powers of two
+    int32_t *status;
+};
+
+constexpr float kLn2 = 0.693147180559945309f;
+
+// The keys [lo, hi) that the token at position p may see.
+__device__ __forceinline__ void key_range(const AttnArgs &g, long long p, int kv_len, int &lo, int &hi)
+{
+    hi = g.causal ? (int)(p + 1 < kv_len ? p + 1 : kv_len) : kv_len;
+    lo = g.window >= 0 && p > g.window ? (int)(p - g.window) : 0;
+    if (hi < 0 || p < 0) hi = 0;
+}
+
+// paged_attention_tc.cu
+bool attention_tc_takes(const AttnArgs &g);
+size_t attention_tc_workspace_bytes();
+fpsk_status attention_tc_launch(const AttnArgs &g, int type, int max_q_len, void *ws, cudaStream_t st);
+
 // Checks shared by the entry points (attention_api.cu).
 bool elem_ok(int type);
 bool head_dim_ok(int dim);

@@ -10,31 +10,6 @@
 
 namespace fpsk {
 
-struct AttnArgs {
-    const void *q, *k, *v;
-    void *out;
-    float *lse;
-    long long qts, qhs, ots, ohs;
-    long long kps, kts, khs, vps, vts, vhs;
-    const int *cu_q, *kv_len, *table;
-    long long table_stride, n_pages;
-    int n_seqs, max_pages, page_size;
-    int n_tokens, hq, hk, group, dim;
-    int causal, window;
-    float scale_log2;                  // scores in units of ln 2: exponentials are powers of two
-    int32_t *status;
-};
-
-constexpr float kLn2 = 0.693147180559945309f;
-
-// The keys [lo, hi) that the token at position p may see.
-__device__ __forceinline__ void key_range(const AttnArgs &g, long long p, int kv_len, int &lo, int &hi)
-{
-    hi = g.causal ? (int)(p + 1 < kv_len ? p + 1 : kv_len) : kv_len;
-    lo = g.window >= 0 && p > g.window ? (int)(p - g.window) : 0;
-    if (hi < 0 || p < 0) hi = 0;
-}
-
 // One block per token and query head; its warps take every fourth key, a lane every 32nd channel.
 constexpr int kPlainWarps = 4;
 template <typename T>
@@ -114,7 +89,7 @@ __global__ void __launch_bounds__(32 * kPlainWarps) attention_rows_kernel(const 
 
 using namespace fpsk;
 
-extern "C" size_t fpsk_paged_attention_workspace_bytes(void) { return kAttnSyncBytes; }
+extern "C" size_t fpsk_paged_attention_workspace_bytes(void) { return kAttnSyncBytes + attention_tc_workspace_bytes(); }
 
 extern "C" fpsk_status fpsk_paged_attention(const fpsk_paged_cache *cache, const fpsk_paged_batch *batch, const fpsk_attention *a,
                                             void *workspace, size_t ws_bytes, int32_t *d_status, void *stream)
@@ -143,6 +118,8 @@ extern "C" fpsk_status fpsk_paged_attention(const fpsk_paged_cache *cache, const
     g.scale_log2 = (a->scale > 0.f ? a->scale : (float)(1.0 / sqrt((double)g.dim))) * 1.44269504088896341f;
     g.status = d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (attention_tc_takes(g))
+        return attention_tc_launch(g, cache->type, a->max_q_len, static_cast<char *>(workspace) + kAttnSyncBytes, st);
     const dim3 grid((unsigned)g.n_tokens, (unsigned)g.hq);
     if (cache->type == FPSK_ELEM_FP16) attention_rows_kernel<__half><<<grid, 32 * kPlainWarps, 0, st>>>(g);
     else attention_rows_kernel<__nv_bfloat16><<<grid, 32 * kPlainWarps, 0, st>>>(g);
