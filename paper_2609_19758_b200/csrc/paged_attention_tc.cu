@@ -12,8 +12,8 @@
 // Two workers per CTA, a warpgroup each, a thread per row, with accumulators S and O of their own in TMEM.  In
 // a PAIR item they hold different query tiles and share every key tile; in a SPLIT item they hold the same queries and take
 // alternate key tiles, and meet at the item's end.  While one computes its softmax, the tensor cores work for the other.
-// A loader warp brings Q tiles and the pages of K and V by TMA into a ring of tiles, 128-byte swizzled; one warp issues
-// the MMAs.  Maximum: the reference maximum of a row follows the true one only when that has grown by more than 2^8 (P then
+// Two loader warps bring Q and K tiles and V tiles, page by page, by TMA into a ring of tiles, 128-byte swizzled; one warp
+// issues the MMAs.  Maximum: the reference maximum of a row follows the true one only when that has grown by more than 2^8 (P then
 // stays below 256, exact enough in 16 bits whatever its size), so O in TMEM is rescaled rarely.
 // Every wait is bounded: a role whose wait gave up stops waiting and issuing, walks through its loops, reports
 // FPSK_ERR_TIMEOUT and the CTA frees its TMEM and leaves.
@@ -27,18 +27,22 @@
 namespace fpsk {
 
 constexpr int kRowsPerTile = 128, kKeysPerTile = 128;
-constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8: MMA issue, 9: loader
+constexpr int kPairKeys = 64;                    // keys of a PAIR worker's step: two S accumulators fit its TMEM columns
+constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8: MMA issue, 9 and 10: loaders
 constexpr int kHalfBytes = 128 * 128;            // 128 rows of one 64-channel half of a tile
 constexpr int kTcaMaxSeqs = 16384;
+#ifndef FPSK_POLY
+#define FPSK_POLY 0
+#endif
+constexpr int kPoly = FPSK_POLY;                 // of eight pairs of exponentials, computed on the FMA pipe
 constexpr float kLazy = 8.f;                     // growth of the maximum (in powers of two) that O is not rescaled for
 
-// 32 consecutive columns of this thread's accumulator row; the values are there when the statement ends
-__device__ __forceinline__ void tm_ld32(uint32_t taddr, uint32_t (&v)[32])
+// 32 consecutive columns of this thread's accumulator row; valid after tm_wait32 on the same array
+__device__ __forceinline__ void tm_load32(uint32_t taddr, uint32_t (&v)[32])
 {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
         :
         "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
         "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
@@ -47,38 +51,22 @@ __device__ __forceinline__ void tm_ld32(uint32_t taddr, uint32_t (&v)[32])
         : "r"(taddr)
         : "memory");
 }
-// 128 consecutive columns of this thread's accumulator row; the values are there when the statement ends
-__device__ __forceinline__ void tm_ld128(uint32_t taddr, uint32_t (&v)[128])
+// all loads of this thread are complete (the array goes through, so that no use of it can move in front)
+__device__ __forceinline__ void tm_wait32(uint32_t (&v)[32])
 {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x128.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, "
-        "%38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, "
-        "%60, %61, %62, %63, %64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, %79, %80, %81, "
-        "%82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, %96, %97, %98, %99, %100, %101, %102, "
-        "%103, %104, %105, %106, %107, %108, %109, %110, %111, %112, %113, %114, %115, %116, %117, %118, %119, %120, "
-        "%121, %122, %123, %124, %125, %126, %127}, [%128];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
         :
-        "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
-        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
-        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]), "=r"(v[32]),
-        "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]),
-        "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]),
-        "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]),
-        "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63]), "=r"(v[64]),
-        "=r"(v[65]), "=r"(v[66]), "=r"(v[67]), "=r"(v[68]), "=r"(v[69]), "=r"(v[70]), "=r"(v[71]), "=r"(v[72]),
-        "=r"(v[73]), "=r"(v[74]), "=r"(v[75]), "=r"(v[76]), "=r"(v[77]), "=r"(v[78]), "=r"(v[79]), "=r"(v[80]),
-        "=r"(v[81]), "=r"(v[82]), "=r"(v[83]), "=r"(v[84]), "=r"(v[85]), "=r"(v[86]), "=r"(v[87]), "=r"(v[88]),
-        "=r"(v[89]), "=r"(v[90]), "=r"(v[91]), "=r"(v[92]), "=r"(v[93]), "=r"(v[94]), "=r"(v[95]), "=r"(v[96]),
-        "=r"(v[97]), "=r"(v[98]), "=r"(v[99]), "=r"(v[100]), "=r"(v[101]), "=r"(v[102]), "=r"(v[103]), "=r"(v[104]),
-        "=r"(v[105]), "=r"(v[106]), "=r"(v[107]), "=r"(v[108]), "=r"(v[109]), "=r"(v[110]), "=r"(v[111]),
-        "=r"(v[112]), "=r"(v[113]), "=r"(v[114]), "=r"(v[115]), "=r"(v[116]), "=r"(v[117]), "=r"(v[118]),
-        "=r"(v[119]), "=r"(v[120]), "=r"(v[121]), "=r"(v[122]), "=r"(v[123]), "=r"(v[124]), "=r"(v[125]),
-        "=r"(v[126]), "=r"(v[127])
-        : "r"(taddr)
+        "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+        "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+        "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+        "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+        :
         : "memory");
+}
+__device__ __forceinline__ void tm_ld32(uint32_t taddr, uint32_t (&v)[32])
+{
+    tm_load32(taddr, v);
+    tm_wait32(v);
 }
 __device__ __forceinline__ void tm_st32(uint32_t taddr, const uint32_t (&v)[32])
 {
@@ -93,33 +81,80 @@ __device__ __forceinline__ void tm_st32(uint32_t taddr, const uint32_t (&v)[32])
         "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
         : "memory");
 }
-__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D[tmem] (+)= A[tmem] * B[smem desc], 16-bit operands
-__device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void tm_st16(uint32_t taddr, const uint32_t (&v)[16])
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate)
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16};"
+        :
+        : "r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
         : "memory");
 }
-// operand descriptors of tiles with 128-byte rows, 128-byte swizzle: eight rows are 1024 bytes.  K-major (Q, K): the
-// rows are M or N, the row's channels the inner dimension.  MN-major (V): the rows are the inner dimension (keys), the
-// row's 64 channels one block of N, and the next block lies kHalfBytes further.
-__device__ __forceinline__ uint64_t sw128_desc(uint32_t saddr, uint32_t lbo_bytes)
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// D[tmem] (+)= A * B, 16-bit operands, A in shared memory or in TMEM.  Descriptors come as low words (address, leading offset)
+// next to one high word: with everything uniform over the warp the steps of a tile are additions in uniform registers, and
+// a step takes a few cycles to issue instead of about a hundred.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate)
 {
-    return tc_smem_desc(saddr, lbo_bytes, 1024) | ((uint64_t)2 << 61);
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
+// a value that all lanes hold, told to the compiler
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+// Operand descriptors of tiles with 128-byte rows, 128-byte swizzle.  K-major (Q, K): the rows are M or N, the row's channels the
+// inner dimension.  MN-major (V): the rows are the inner dimension (keys), the row's 64 channels one block of N.  Low word:
+// address and the offset between blocks of 64 channels (MN-major); high word: the offset between groups of eight rows.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t block_bytes) { return (saddr >> 4) | ((block_bytes >> 4) << 16); }
+__device__ __forceinline__ uint32_t desc_hi(uint32_t group_bytes) { return (group_bytes >> 4) | (1u << 14) | (2u << 29); }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, int v, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v) : "memory");
+}
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// Bounded wait on an mbarrier phase (about a second), without a call: a call's register conventions would spill the rows
+// that the workers hold.
+__device__ __forceinline__ bool bar_wait_inline(uint32_t bar, uint32_t parity)
+{
+    if (mbar_try(bar, parity)) return true;
+    const long long t_end = clock64() + 2000000000LL;
+#pragma unroll 1
+    while (!mbar_try(bar, parity))
+        if (clock64() > t_end) return false;
+    return true;
 }
 __device__ __forceinline__ void named_bar_sync(int id, int threads)
 {
@@ -129,6 +164,35 @@ __device__ __forceinline__ float ex2(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 2^x for x <= 100 on the FMA pipe, two at a time: x = n + f with n the nearest whole number, 2^f by the polynomial of degree 4
+// that minimises the largest relative error on [-1/2, 1/2] (Remez exchange: 2.6e-6; in FP32 2.7e-6), n added to the exponent.
+// Below -126 it stays at 2^-126; NaN comes out as some number (the callers see to both).
+__device__ __forceinline__ float2 ex2_poly(float2 x)
+{
+    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+    const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);   // 1.5 * 2^23
+    const float2 t = __fadd2_rn(x, magic);
+    const float2 f = __ffma2_rn(__fadd2_rn(t, unmagic), make_float2(-1.f, -1.f), x);
+    float2 p = __ffma2_rn(make_float2(0.009570102207362652f, 0.009570102207362652f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
+    p = __ffma2_rn(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
+    p = __ffma2_rn(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+    p = __ffma2_rn(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+// maxima that pass a NaN on
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ float max2(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
 template <typename T> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
@@ -146,10 +210,18 @@ template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float l
 }
 
 // ---------------------------------------------------------------- items
+// How a K or V tile lies in shared memory, and by which tensor map it comes.  Both halves of a row (64 channels each) in one
+// load: groups of eight rows, [group][half][8 rows][128 bytes].  Half by half: [half][128 rows][128 bytes].
+enum { kByHalves = 0, kGroupsOfAllPages = 1, kHeadsOfAllPages = 2 };
+struct TileLayout {
+    int map;                           // one of the three above
+    uint32_t half_bytes, group_bytes;  // offsets of the second half, of the next eight rows
+};
 struct TcaArgs {
     AttnArgs a;
-    int tile_tokens;                   // tokens of a 128-row tile: 128 / group
+    int tile_tokens;                   // tokens of a query tile: its rows / group
     int box_rows;                      // keys of one TMA box: the largest power of two that divides a page, at most 128
+    TileLayout kl, vl;
     float *part_o;                     // [2 slots per CTA][rows][DP]
     float2 *part_ml;                   // [2 slots per CTA][rows]: maximum (powers of two), sum
     struct SplitRecord *records;       // [CTA]
@@ -192,18 +264,18 @@ __device__ __forceinline__ Item make_item(const AttnArgs &g, int cu, int q_len, 
     return it;
 }
 
-// PAIR: the key tiles of [tile_a, tile_b) that worker w's own tokens may see, [a, b).
-__device__ __forceinline__ void worker_tiles(const AttnArgs &g, const Item &it, int w, int tile_tokens, int tile_a, int tile_b, int &a, int &b)
+// PAIR: the steps (64 keys) of [step_a, step_b) that worker w's own tokens may see, [a, b).
+__device__ __forceinline__ void worker_steps(const AttnArgs &g, const Item &it, int w, int tile_tokens, int step_a, int step_b, int &a, int &b)
 {
     const int t0 = w * tile_tokens, n = min(it.n_tok - t0, tile_tokens);
-    a = b = tile_a;
+    a = b = step_a;
     if (n <= 0) return;
     int lo, hi, skip;
     key_range(g, it.p0 + t0 + n - 1, it.kv_len, skip, hi);
     key_range(g, max(it.p0 + t0, 0), it.kv_len, lo, skip);
     if (hi <= lo) return;
-    a = max(tile_a, lo / kKeysPerTile);
-    b = max(a, min(tile_b, (hi + kKeysPerTile - 1) / kKeysPerTile));
+    a = max(step_a, lo / kPairKeys);
+    b = max(a, min(step_b, (hi + kPairKeys - 1) / kPairKeys));
 }
 
 // Walks the items of a CTA's range; every role walks for itself.
@@ -229,30 +301,38 @@ struct Walk {
     }
 };
 
-template <int DP, bool PAIR> struct Tca {
+// Kinds of items: see above.  COPIES: a SPLIT item of at most 32 rows with its queries four times in the tile, once for each
+// quarter of the TMEM lanes.
+enum Mode { kPair = 0, kSplit = 1, kCopies = 4 };
+
+template <int DP, int MODE> struct Tca {
+    static constexpr bool kIsPair = MODE == kPair;
+    static constexpr int kTileRows = MODE == kCopies ? 32 : kRowsPerTile;      // rows of a query tile
     static constexpr int kTile = kRowsPerTile * DP * 2;
     static constexpr int kHalves = DP / 64;
-    static constexpr int kQTiles = PAIR ? 2 : 1;
-    static constexpr int kSlots = DP == 128 ? (PAIR ? 5 : 6) : 8;
-    static constexpr int kBars = (kQTiles + kSlots) * kTile;           // barriers, start state, SPLIT: row statistics
+    static constexpr int kQTiles = kIsPair ? 2 : 1;
+    static constexpr int kSlots = DP == 128 ? (MODE == kSplit ? 6 : 5) : 8;
+    static constexpr int kStage = MODE == kCopies ? 4 * 8 * (DP + 4) * 4 : 0;  // eight rows of the four copies' outputs
+    static constexpr int kBars = (kQTiles + kSlots) * kTile + kStage;          // barriers, start state, SPLIT: row statistics
     static constexpr int kSmem = kBars + 3072;
-    static constexpr int kRows = kQTiles * kRowsPerTile;               // of a partial result
+    static constexpr int kRows = kQTiles * kTileRows;                          // of a partial result
 };
 
 struct TcaBars {                       // shared memory, after the tiles
-    unsigned long long q_full, q_empty, done, s_full[2], p_ready[2], o_done[2], kv_full[8], kv_empty[8];
+    unsigned long long q_full, q_empty, done, s_full[4], p_ready[4], o_done[4], kv_full[8], kv_empty[8];
     uint32_t tmem;
     int b, kvh, qi, u, left;
     long long totals[kTcaThreads / 32];
 };
 static_assert(sizeof(TcaBars) <= 1024, "barriers fit before the row statistics");
 
-template <typename T, int DP, bool PAIR>
+template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(kTcaThreads, 1)
 attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v)
 {
-    using Cfg = Tca<DP, PAIR>;
+    using Cfg = Tca<DP, MODE>;
+    constexpr bool PAIR = MODE == kPair;
     extern __shared__ __align__(1024) unsigned char smem[];
     const AttnArgs &g = ga.a;
     TcaBars *sh = reinterpret_cast<TcaBars *>(smem + Cfg::kBars);
@@ -265,7 +345,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         mbar_init(smem_u32(&sh->q_full), 1);
         mbar_init(smem_u32(&sh->q_empty), 1);
         mbar_init(smem_u32(&sh->done), 1);
-        for (int w = 0; w < 2; ++w) {
+        for (int w = 0; w < 4; ++w) {                                  // worker w & 1, even and odd steps
             mbar_init(smem_u32(&sh->s_full[w]), 1);
             mbar_init(smem_u32(&sh->p_ready[w]), 4);
             mbar_init(smem_u32(&sh->o_done[w]), 1);
@@ -367,7 +447,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     if (left > 0) walk.open(g, item_tokens);
     bool ok = true;                    // of this role
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !mbar_wait_bounded(bar, parity)) ok = false;
+        if (ok && !bar_wait_inline(bar, parity)) ok = false;
         __syncwarp();                  // the tcgen05 instructions behind it want the warp together
     };
 
@@ -386,156 +466,210 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         ga.records[blockIdx.x] = r;
     }
 
-    if (warp == 9) {
-        // ------------------------------------------------------------ loader
+    // Registers: 384 threads x 168 at launch = 64512; afterwards 256 x 208 + 128 x 80 = 63488.  (Each role's instruction stands
+    // in its own branch: the compiler takes the smaller number behind a join.)
+    if (warp == 9 || warp == 10) {
+        // ------------------------------------------------------------ loaders: Q and K tiles, V tiles
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         fence_proxy_async();
+        const bool is_v = warp == 10;
+        const CUtensorMap *map = is_v ? &map_v : &map_k;
+        const TileLayout tl = is_v ? ga.vl : ga.kl;
         const int page_size = g.page_size, R = ga.box_rows;
-        int slot = 0, fills = 0;
-        uint32_t phase = 0, q_phase = 0;
+        const int halves = tl.map == kByHalves ? Cfg::kHalves : 1;
+        const uint32_t box_bytes = (uint32_t)(R * 128 * Cfg::kHalves) / halves;
+        left = uniform(left);
+        u = uniform(u);
+        int seq = 0;                                                   // tiles of K and V that went before this item
+        int last = -1;                                                 // this warp's last one
+        uint32_t q_phase = 0;
         bool q_used = false;
         while (left > 0) {
             const Item it = make_item(g, walk.cu, walk.q_len, walk.kv_len, walk.qi, item_tokens);
-            const int n = min(left, it.units - u);
-            if (it.hi > it.lo) {
-                wait(smem_u32(&sh->q_empty), q_phase ^ 1u);
-                if (ok && lane == 0) {
-                    mbar_expect_tx(smem_u32(&sh->q_full), (uint32_t)(Cfg::kQTiles * Cfg::kHalves * tile_tokens * g.group * 128));
-                    for (int w = 0; w < Cfg::kQTiles; ++w)
-                        for (int h = 0; h < Cfg::kHalves; ++h)
-                            tma_load_3d(q_smem + w * Cfg::kTile + h * kHalfBytes, &map_q, h * 64, walk.kvh * g.group, it.token0 + w * tile_tokens,
-                                        smem_u32(&sh->q_full));
-                }
-                q_phase ^= 1u;
-                q_used = true;
-                const int *row = g.table + (long long)walk.b * g.table_stride;
-                const int tile_a = it.tile0 + u, tile_b = tile_a + n;
-                // a tile of K or V: its boxes that hold a visible key
-                auto load = [&](int tile, const CUtensorMap *map) {
-                    const int k0 = tile * kKeysPerTile;
-                    const int r0 = max(0, it.lo - k0) / R, r1 = (min(kKeysPerTile, it.hi - k0) + R - 1) / R;
-                    const uint32_t full = smem_u32(&sh->kv_full[slot]), dst = ring + slot * Cfg::kTile;
-                    wait(smem_u32(&sh->kv_empty[slot]), phase ^ 1u);
+            const int lo = uniform(it.lo), hi = uniform(it.hi), n = min(left, uniform(it.units) - u);
+            if (hi > lo) {
+                const int kvh = uniform(walk.kvh), tile_a = uniform(it.tile0) + u;
+                if (!is_v) {
+                    const int token0 = uniform(it.token0);
+                    wait(smem_u32(&sh->q_empty), q_phase ^ 1u);
                     ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) return;
-                    if (lane == 0) mbar_expect_tx(full, (uint32_t)((r1 - r0) * R * 128 * Cfg::kHalves));
-                    __syncwarp();
-                    for (int i = lane; i < (r1 - r0) * Cfg::kHalves; i += 32) {
-                        const int box = r0 + i / Cfg::kHalves, h = i % Cfg::kHalves;
-                        const int key = k0 + box * R, col = key / page_size;
-                        long long page = col < g.max_pages ? __ldg(row + col) : -1;
-                        if (page < 0 || page >= g.n_pages) {
-                            report_status(g.status, FPSK_ERR_PARAM);
-                            page = g.n_pages;                          // outside the tensor map: zeros
-                        }
-                        tma_load_4d(dst + h * kHalfBytes + box * R * 128, map, h * 64, key - col * page_size, walk.kvh, (int)page, full);
+                    if (ok && elect_one()) {
+                        constexpr int kLoads = MODE == kCopies ? 4 : Cfg::kQTiles;
+                        mbar_expect_tx(smem_u32(&sh->q_full), (uint32_t)(kLoads * Cfg::kHalves * tile_tokens * g.group * 128));
+                        for (int w = 0; w < kLoads; ++w)
+                            for (int h = 0; h < Cfg::kHalves; ++h)
+                                tma_load_3d(q_smem + (PAIR ? w * Cfg::kTile : w * 32 * 128) + h * kHalfBytes, &map_q, h * 64, kvh * g.group,
+                                            token0 + (PAIR ? w * tile_tokens : 0), smem_u32(&sh->q_full));
                     }
-                    ++fills;
-                    if (++slot == Cfg::kSlots) { slot = 0; phase ^= 1u; }
+                    q_phase ^= 1u;
+                    q_used = true;
+                }
+                const int *table = g.table + (long long)walk.b * g.table_stride;
+                // the pages of a tile's boxes that hold a visible key, one box per lane (up to 16)
+                auto first_box = [&](int tile) { return max(0, lo - tile * kKeysPerTile) / R; };
+                auto end_box = [&](int tile) { return (min(kKeysPerTile, hi - tile * kKeysPerTile) + R - 1) / R; };
+                auto pages = [&](int tile) {
+                    const int box = first_box(tile) + lane;
+                    int page = 0;
+                    if (box < end_box(tile)) {
+                        const int col = (tile * kKeysPerTile + box * R) / page_size;
+                        page = col < g.max_pages ? __ldg(table + col) : -1;
+                    }
+                    return page;
                 };
-                if constexpr (PAIR) {
-                    for (int t = tile_a; t < tile_b; ++t) {
-                        load(t, &map_k);
-                        load(t, &map_v);
+                int next = pages(tile_a);
+                for (int i = 0; i < n; ++i) {
+                    const int tile = tile_a + i;
+                    int page = next;
+                    if (i + 1 < n) next = pages(tile + 1);             // its latency passes behind the wait
+                    // this tile's place in the order in which the MMAs use the ring
+                    const int at = seq + (PAIR ? 2 * i + is_v : is_v ? min(2 * i + 2, 2 * n - 1) : max(2 * i - 1, 0));
+                    const int slot = at % Cfg::kSlots;
+                    const uint32_t phase = (uint32_t)(at / Cfg::kSlots) & 1u;
+                    const uint32_t full = smem_u32(&sh->kv_full[slot]), dst = ring + slot * Cfg::kTile;
+                    const int b0 = first_box(tile), b1 = end_box(tile);
+                    wait(smem_u32(&sh->kv_empty[slot]), phase ^ 1u);
+                    if (page < 0 || page >= g.n_pages) {
+                        report_status(g.status, FPSK_ERR_PARAM);
+                        page = (int)g.n_pages;                         // outside the tensor map: zeros
                     }
-                } else {
-                    load(tile_a, &map_k);
-                    if (n > 1) load(tile_a + 1, &map_k);
-                    for (int t = tile_a; t < tile_b; ++t) {
-                        load(t, &map_v);
-                        if (t + 2 < tile_b) load(t + 2, &map_k);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (ok) {
+                        if (elect_one()) mbar_expect_tx(full, (uint32_t)((b1 - b0) * halves) * box_bytes);
+                        __syncwarp();
+                        for (int box = b0; box < b1; ++box) {
+                            const int pg = __shfl_sync(0xFFFFFFFFu, page, box - b0);
+                            const int row = (tile * kKeysPerTile + box * R) % page_size;
+                            if (elect_one()) {
+                                if (tl.map == kGroupsOfAllPages)
+                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, kvh, (pg * page_size + row) >> 3, full);
+                                else if (tl.map == kHeadsOfAllPages)
+                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, row >> 3, pg * g.hk + kvh, full);
+                                else
+                                    for (int h = 0; h < Cfg::kHalves; ++h)
+                                        tma_load_4d(dst + h * kHalfBytes + box * box_bytes, map, h * 64, row, kvh, pg, full);
+                            }
+                            __syncwarp();
+                        }
+                        last = at;
                     }
                 }
+                if (ok) seq += 2 * n;
             }
             left -= n;
             u = 0;
             if (left > 0) walk.next(g, item_tokens);
         }
-        // own copies still in flight (only after a wait that gave up)
-        const int own = min(fills, Cfg::kSlots);
-        for (int i = 0; i < own; ++i) {
-            if (--slot < 0) { slot = Cfg::kSlots - 1; phase ^= 1u; }
-            if (!mbar_wait_bounded(smem_u32(&sh->kv_full[slot]), phase)) ok = false;
-        }
-        if (q_used && !mbar_wait_bounded(smem_u32(&sh->q_full), q_phase ^ 1u)) ok = false;
+        // The last fill of every slot: in flight still only if the MMA warp's waits gave up.
+        for (int at = last; at >= 0 && at >= seq - Cfg::kSlots; --at)
+            if (!bar_wait_inline(smem_u32(&sh->kv_full[at % Cfg::kSlots]), (uint32_t)(at / Cfg::kSlots) & 1u)) ok = false;
+        if (q_used && !bar_wait_inline(smem_u32(&sh->q_full), q_phase ^ 1u)) ok = false;
     } else if (warp == 8) {
         // ------------------------------------------------------------ MMA issue
-        const uint32_t fmt = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        const uint32_t fmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
         const uint32_t base_desc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(kRowsPerTile >> 4) << 24);
-        const uint32_t idesc_s = base_desc | ((uint32_t)(kKeysPerTile >> 3) << 17);
+        constexpr int kStepKeys = PAIR ? kPairKeys : kKeysPerTile;
+        const uint32_t idesc_s = base_desc | ((uint32_t)(kStepKeys >> 3) << 17);
         const uint32_t idesc_o = base_desc | (1u << 16) | ((uint32_t)(DP >> 3) << 17);
+        const uint32_t tm = (uint32_t)uniform((int)tmem);
+        const uint32_t q_hi = desc_hi(1024), k_hi = desc_hi(ga.kl.group_bytes), v_hi = desc_hi(ga.vl.group_bytes);
+        left = uniform(left);
+        u = uniform(u);
         int slot = 0;
-        uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0};
+        uint32_t phase = 0, q_phase = 0;
+        uint32_t s_count[2] = {0, 0}, o_count[2] = {0, 0};             // steps issued for each worker so far
         auto next_slot = [&]() {
             if (++slot == Cfg::kSlots) { slot = 0; phase ^= 1u; }
         };
+        auto all_wait = [&](uint32_t bar, uint32_t parity) {
+            wait(bar, parity);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            tc_fence_after();
+        };
+        // TMEM columns of a worker's S (and P) in a step
+        auto s_col = [&](int w, uint32_t count) { return tm + w * 128 + (PAIR ? (count & 1u) * kPairKeys : 0u); };
         auto issue_s = [&](int w, uint32_t k_addr) {
-            if (ok && lane == 0) {
-                const uint32_t qa = q_smem + (PAIR ? w * Cfg::kTile : 0);
+            const uint32_t c = s_count[w]++;
+            if (ok && elect_one()) {
+                const uint32_t qa = desc_lo(q_smem + (PAIR ? w * Cfg::kTile : 0), 16), kb = desc_lo(k_addr, 16);
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t off = (k / 4) * kHalfBytes + (k % 4) * 32;
-                    tc_mma(tmem + w * 128, sw128_desc(qa + off, 16), sw128_desc(k_addr + off, 16), idesc_s, k > 0);
-                }
-                tc_commit(smem_u32(&sh->s_full[w]));
+                for (int k = 0; k < DP / 16; ++k)
+                    mma_ss(s_col(w, c), qa + ((k / 4) * kHalfBytes + (k % 4) * 32) / 16, q_hi,
+                           kb + (k / 4) * (ga.kl.half_bytes / 16) + (k % 4) * 2, k_hi, idesc_s, k > 0);
+                tc_commit(smem_u32(&sh->s_full[w + 2 * (c & 1u)]));
             }
+            __syncwarp();
         };
         auto issue_o = [&](int w, uint32_t v_addr, bool accumulate) {
-            wait(smem_u32(&sh->p_ready[w]), p_phase[w]);
-            p_phase[w] ^= 1u;
-            tc_fence_after();
-            if (ok && lane == 0) {
+            const uint32_t c = o_count[w]++;
+            all_wait(smem_u32(&sh->p_ready[w + 2 * (c & 1u)]), (c >> 1) & 1u);
+            if (ok && elect_one()) {
+                const uint32_t vb = desc_lo(v_addr, ga.vl.half_bytes), step = ga.vl.group_bytes / 8;
 #pragma unroll
-                for (int k = 0; k < kKeysPerTile / 16; ++k)
-                    tc_mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, sw128_desc(v_addr + k * 2048, kHalfBytes), idesc_o,
-                              accumulate || k > 0);
-                tc_commit(smem_u32(&sh->o_done[w]));
+                for (int k = 0; k < kStepKeys / 16; ++k)
+                    mma_ts(tm + 256 + w * 128, s_col(w, c) + k * 8, vb + k * step, v_hi, idesc_o, accumulate || k > 0);
+                tc_commit(smem_u32(&sh->o_done[w + 2 * (c & 1u)]));
             }
+            __syncwarp();
         };
         auto release = [&](int s) {
-            if (ok && lane == 0) tc_commit(smem_u32(&sh->kv_empty[s]));
-        };
-        // rows of a V tile that no token of the item may see: zeros, for 0 * (what lies there) must not be NaN
-        auto clean_v = [&](const Item &it, int tile, uint32_t v_addr) {
-            const int k0 = tile * kKeysPerTile, r0 = max(0, it.lo - k0), r1 = min(kKeysPerTile, it.hi - k0);
-            if (r0 == 0 && r1 == kKeysPerTile) return;
-            for (int i = lane; i < kKeysPerTile * 8 * Cfg::kHalves; i += 32) {
-                const int r = (i >> 3) & (kKeysPerTile - 1);
-                if (r < r0 || r >= r1)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_addr + i * 16), "r"(0) : "memory");
-            }
-            fence_proxy_async();
+            if (ok && elect_one()) tc_commit(smem_u32(&sh->kv_empty[s]));
             __syncwarp();
         };
         while (left > 0) {
             const Item it = make_item(g, walk.cu, walk.q_len, walk.kv_len, walk.qi, item_tokens);
-            const int n = min(left, it.units - u);
-            if (it.hi > it.lo) {
-                const int tile_a = it.tile0 + u, tile_b = tile_a + n;
-                wait(smem_u32(&sh->q_full), q_phase);
-                q_phase ^= 1u;
-                auto wait_full = [&]() {
-                    wait(smem_u32(&sh->kv_full[slot]), phase);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    tc_fence_after();
+            const int lo = uniform(it.lo), hi = uniform(it.hi), n = min(left, uniform(it.units) - u);
+            if (hi > lo) {
+                const int tile_a = uniform(it.tile0) + u, tile_b = tile_a + n;
+                // rows of a V tile that no token of the item may see: zeros, for 0 * (what lies there) must not be NaN
+                auto clean_v = [&](int tile, uint32_t v_addr) {
+                    const int k0 = tile * kKeysPerTile, r0 = max(0, lo - k0), r1 = min(kKeysPerTile, hi - k0);
+                    if (r0 == 0 && r1 == kKeysPerTile) return;
+                    for (int i = lane; i < kKeysPerTile * 8 * Cfg::kHalves; i += 32) {
+                        const int r = i >> (2 + Cfg::kHalves), h = Cfg::kHalves == 2 ? (i >> 3) & 1 : 0;
+                        if (r < r0 || r >= r1)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_addr + (r >> 3) * ga.vl.group_bytes + h * ga.vl.half_bytes + (r & 7) * 128 + (i & 7) * 16), "r"(0) : "memory");
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
                 };
+                all_wait(smem_u32(&sh->q_full), q_phase);
+                q_phase ^= 1u;
+                auto wait_full = [&]() { all_wait(smem_u32(&sh->kv_full[slot]), phase); };
                 if constexpr (PAIR) {
+                    // S of a worker is two steps ahead of its P V, so that a softmax never waits for its scores
                     int wa[2], wb[2];
-                    for (int w = 0; w < 2; ++w) worker_tiles(g, it, w, tile_tokens, tile_a, tile_b, wa[w], wb[w]);
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        worker_steps(g, it, w, tile_tokens, 2 * tile_a, 2 * tile_b, wa[w], wb[w]);
+                        wa[w] = uniform(wa[w]);
+                        wb[w] = uniform(wb[w]);
+                    }
+                    const uint32_t k_half = 8 * ga.kl.group_bytes, v_half = 8 * ga.vl.group_bytes;   // the tile's second 64 keys
                     wait_full();
-                    for (int w = 0; w < 2; ++w)
-                        if (tile_a >= wa[w] && tile_a < wb[w]) issue_s(w, ring + slot * Cfg::kTile);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int w = 0; w < 2; ++w)
+                            if (2 * tile_a + h >= wa[w] && 2 * tile_a + h < wb[w]) issue_s(w, ring + slot * Cfg::kTile + h * k_half);
                     release(slot);
                     next_slot();
                     for (int t = tile_a; t < tile_b; ++t) {
                         const int v_slot = slot;
                         wait_full();
                         next_slot();
-                        const uint32_t v_addr = ring + v_slot * Cfg::kTile;
-                        if (ok) clean_v(it, t, v_addr);
+                        const uint32_t v_addr = ring + v_slot * Cfg::kTile, k_addr = ring + slot * Cfg::kTile;
+                        if (ok) clean_v(t, v_addr);
                         if (t + 1 < tile_b) wait_full();
-                        for (int w = 0; w < 2; ++w) {
-                            if (t >= wa[w] && t < wb[w]) issue_o(w, v_addr, t > wa[w]);
-                            if (t + 1 >= wa[w] && t + 1 < wb[w]) issue_s(w, ring + slot * Cfg::kTile);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int st = 2 * t + h;
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) {
+                                if (st >= wa[w] && st < wb[w]) issue_o(w, v_addr + h * v_half, st > wa[w]);
+                                if (st + 2 < 2 * tile_b && st + 2 >= wa[w] && st + 2 < wb[w]) issue_s(w, k_addr + h * k_half);
+                            }
                         }
                         release(v_slot);
                         if (t + 1 < tile_b) {
@@ -550,40 +684,50 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         release(slot);
                         next_slot();
                     }
-                    for (int i = 0; i < n; ++i) {
-                        wait_full();
-                        const uint32_t v_addr = ring + slot * Cfg::kTile;
-                        if (ok) clean_v(it, tile_a + i, v_addr);
-                        issue_o(i & 1, v_addr, i > 1);
-                        release(slot);
-                        next_slot();
-                        if (i + 2 < n) {
+                    for (int i = 0; i < n; i += 2) {
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            if (i + w >= n) break;
                             wait_full();
-                            issue_s(i & 1, ring + slot * Cfg::kTile);
+                            const uint32_t v_addr = ring + slot * Cfg::kTile;
+                            if (ok) clean_v(tile_a + i + w, v_addr);
+                            issue_o(w, v_addr, i > 0);
                             release(slot);
                             next_slot();
+                            if (i + w + 2 < n) {
+                                wait_full();
+                                issue_s(w, ring + slot * Cfg::kTile);
+                                release(slot);
+                                next_slot();
+                            }
                         }
                     }
                 }
-                if (ok && lane == 0) tc_commit(smem_u32(&sh->q_empty));
+                if (ok && elect_one()) tc_commit(smem_u32(&sh->q_empty));
+                __syncwarp();
             }
             left -= n;
             u = 0;
             if (left > 0) walk.next(g, item_tokens);
         }
-        if (lane == 0) {
-            tc_commit(smem_u32(&sh->done));
-            if (!mbar_wait_bounded(smem_u32(&sh->done), 0)) ok = false;
-        }
+        if (elect_one()) tc_commit(smem_u32(&sh->done));
+        __syncwarp();
+        if (!bar_wait_inline(smem_u32(&sh->done), 0)) ok = false;
         __syncwarp();
     } else if (warp < 8) {
         // ------------------------------------------------------------ workers: a thread per row
-        const int w = warp >> 2, rloc = tid & 127;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t ts = tmem + lanes + w * 128, to = tmem + lanes + 256 + w * 128;
-        const int tok_in_tile = rloc / g.group, head_in_group = rloc - tok_in_tile * g.group;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        constexpr int kCols = MODE == kCopies ? 32 : PAIR ? kPairKeys : 128;   // keys of a step that a thread weighs
+        const int w = warp >> 2, rloc = tid & 127, quarter = warp & 3;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t to = tmem + lanes + 256 + w * 128;
+        const int row = MODE == kCopies ? lane : rloc;                 // in the query tile
+        const int tok_in_tile = row / g.group, head_in_group = row - tok_in_tile * g.group;
+        const int col0 = MODE == kCopies ? quarter * 32 : 0;
         const float sl2 = g.scale_log2;
-        uint32_t s_phase = 0, o_count = 0;
+        uint32_t count = 0;                                            // steps so far
+        // the barrier (of its four) and the parity of step c
+        auto step_bar = [&](unsigned long long *bars, uint32_t c) { return smem_u32(&bars[w + 2 * (c & 1u)]); };
         while (left > 0) {
             const Item it = make_item(g, walk.cu, walk.q_len, walk.kv_len, walk.qi, item_tokens);
             const int n = min(left, it.units - u);
@@ -595,39 +739,85 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             int ta = 0, tb = 0, step = 1;
             if (it.hi > it.lo) {
                 const int tile_a = it.tile0 + u, tile_b = tile_a + n;
-                if constexpr (PAIR) worker_tiles(g, it, w, tile_tokens, tile_a, tile_b, ta, tb);
+                if constexpr (PAIR) worker_steps(g, it, w, tile_tokens, 2 * tile_a, 2 * tile_b, ta, tb);
                 else { ta = tile_a + w; tb = tile_b; step = 2; }
             }
             float m = -INFINITY, l = 0.f;
             bool have_o = false;
             for (int t = ta; t < tb; t += step) {
-                wait(smem_u32(&sh->s_full[w]), s_phase);
-                s_phase ^= 1u;
+                const int k0 = t * (PAIR ? kPairKeys : kKeysPerTile) + col0;
+                const uint32_t ts = tmem + lanes + w * 128 + (PAIR ? (count & 1u) * kPairKeys : 0u);
+                const bool masked = __any_sync(0xFFFFFFFFu, k0 < lo || k0 + kCols > hi);
+                wait(step_bar(sh->s_full, count), (count >> 1) & 1u);
                 tc_fence_after();
                 if (warp_on) {
-                    uint32_t s[128];
-                    tm_ld128(ts, s);
-                    const int k0 = t * kKeysPerTile;
-                    if (__any_sync(0xFFFFFFFFu, k0 < lo || k0 + kKeysPerTile > hi)) {
+                    constexpr int kChunks = kCols / 32;
+                    auto load_scores = [&](uint32_t (&s)[kChunks][32]) {
 #pragma unroll
-                        for (int i = 0; i < 128; ++i)
-                            if (k0 + i < lo || k0 + i >= hi) s[i] = 0xFF800000u;
-                    }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        for (int c = 0; c < kChunks; ++c) tm_load32(ts + col0 + c * 32, s[c]);
 #pragma unroll
-                    for (int i = 0; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(s[i]));
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
+                        for (int c = 0; c < kChunks; ++c) tm_wait32(s[c]);
+                        if (masked) {
+#pragma unroll
+                            for (int i = 0; i < kCols; ++i)
+                                if (k0 + i < lo || k0 + i >= hi) s[i / 32][i % 32] = 0xFF800000u;
+                        }
+                    };
+                    auto top32 = [&](const uint32_t (&s)[32], float top) {
+                        float a = top, b = __uint_as_float(s[0]);
+#pragma unroll
+                        for (int i = 1; i < 29; i += 4) {
+                            a = max3(a, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+                            b = max3(b, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
+                        }
+                        return max2(max3(a, __uint_as_float(s[29]), __uint_as_float(s[30])), max2(b, __uint_as_float(s[31])));
+                    };
+                    // a row that has met NaN or +inf is NaN, whatever its other scores are
+                    auto reference = [](float top) { return top < INFINITY ? top : __int_as_float(0x7FC00000); };
                     if (!have_o) {
-                        m = top;
-                    } else {
-                        const bool grow = valid && top > m + kLazy;
-                        if (__any_sync(0xFFFFFFFFu, grow)) {
-                            const float alpha = grow ? ex2(m - top) : 1.f;
-                            if (grow) m = top;
-                            l *= alpha;
-                            wait(smem_u32(&sh->o_done[w]), (o_count - 1u) & 1u);
-                            tc_fence_after();
+                        // the item's first tile sets the reference maximum
+                        uint32_t s[kChunks][32];
+                        load_scores(s);
+                        float top = -INFINITY;
 #pragma unroll
+                        for (int c = 0; c < kChunks; ++c) top = top32(s[c], top);
+                        m = reference(top * sl2);
+                    }
+                    // Weights against the reference maximum, the tile's own maximum beside them: where that has grown too far
+                    // (rare), the reference follows, O is rescaled and the weights are computed once more.  kPoly of eight pairs of
+                    // exponentials go to the FMA pipe, the others to the special-function unit, which alone would be what bounds it.
+                    uint32_t p[kCols / 2];
+                    float2 sum[2];
+#pragma unroll 1
+                    for (int pass = 0;; ++pass) {
+                        const float base = m == -INFINITY ? 0.f : m;
+                        const float2 sc = make_float2(sl2, sl2), nb = make_float2(-base, -base);
+                        float top = -INFINITY;
+                        sum[0] = sum[1] = make_float2(0.f, 0.f);
+                        uint32_t s[kChunks][32];
+                        load_scores(s);
+#pragma unroll
+                        for (int c = 0; c < kChunks; ++c) {
+                            top = top32(s[c], top);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                float2 x = make_float2(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1]));
+                                x = __ffma2_rn(x, sc, nb);
+                                x = ((i + 1) * kPoly) / 8 != (i * kPoly) / 8 ? ex2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
+                                sum[i & 1] = __fadd2_rn(sum[i & 1], x);
+                                p[c * 16 + i] = pack_pair<T>(x.x, x.y);
+                            }
+                        }
+                        top *= sl2;
+                        const bool grow = valid && !(top <= m + kLazy);
+                        if (pass || !__any_sync(0xFFFFFFFFu, grow)) break;
+                        const float m2 = grow ? reference(top) : m, alpha = grow ? ex2(m - m2) : 1.f;
+                        m = m2;
+                        l *= alpha;
+                        if (have_o) {
+                            wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
+                            tc_fence_after();
+#pragma unroll 1
                             for (int c = 0; c < DP / 32; ++c) {
                                 uint32_t o[32];
                                 tm_ld32(to + c * 32, o);
@@ -638,89 +828,138 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             tm_wait_st();
                         }
                     }
-                    const float base = m == -INFINITY ? 0.f : m;
-                    const float2 sc = make_float2(sl2, sl2), nb = make_float2(-base, -base);
-                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t p[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            float2 x = make_float2(__uint_as_float(s[64 * h + 2 * i]), __uint_as_float(s[64 * h + 2 * i + 1]));
-                            x = __ffma2_rn(x, sc, nb);
-                            x = make_float2(ex2(x.x), ex2(x.y));
-                            sum[i & 1] = __fadd2_rn(sum[i & 1], x);
-                            p[i] = pack_pair<T>(x.x, x.y);
-                        }
-                        tm_st32(ts + 32 * h, p);
-                    }
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    if constexpr (MODE == kCopies) {
+                        // zeros for the other quarters' keys
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            uint32_t x[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x[i] = q == quarter ? p[i] : 0u;
+                            tm_st16(ts + q * 16, x);
+                        }
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < kCols / 64; ++h) {
+                            uint32_t x[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = p[h * 32 + i];
+                            tm_st32(ts + h * 32, x);
+                        }
+                    }
                     tm_wait_st();
                 }
                 have_o = true;
-                ++o_count;
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[w]));
+                if (lane == 0) mbar_arrive(step_bar(sh->p_ready, count));
+                ++count;
             }
             if (have_o) {
-                wait(smem_u32(&sh->o_done[w]), (o_count - 1u) & 1u);
+                wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
                 tc_fence_after();
             }
+            if (m == -INFINITY) l = 0.f;                              // (2^-126 is not zero)
             // ---- the item's end: finished here, or a partial result
             const bool whole = u == 0 && n == it.units;
-            float wt0 = 1.f, wt1 = 0.f;                               // SPLIT: weights of the two workers' outputs
-            bool have1 = false;
+            const bool any = it.hi > it.lo, have1 = any && n > 1;     // SPLIT: outputs of the two workers
+            float wt0 = 1.f, wt1 = 0.f;                               // and their weights
             if constexpr (!PAIR) {
                 row_ml[w * 128 + rloc] = make_float2(m, l);
                 tc_fence_before();
                 named_bar_sync(1, 256);                               // both outputs are complete
                 tc_fence_after();
                 const float2 a = row_ml[rloc], b = row_ml[128 + rloc];
-                have1 = n > 1 && it.hi > it.lo;
                 m = fmaxf(a.x, b.x);
+                if constexpr (MODE == kCopies) {
+                    for (int q = 0; q < 4; ++q) m = max3(m, row_ml[q * 32 + lane].x, row_ml[128 + q * 32 + lane].x);
+                }
                 const float base = m == -INFINITY ? 0.f : m;
                 wt0 = ex2(a.x - base);
                 wt1 = ex2(b.x - base);
                 l = a.y * wt0 + b.y * wt1;
-            }
-            const bool have0 = PAIR ? have_o : it.hi > it.lo;
-            if (warp_on) {
-                const int row = (PAIR ? w * 128 : 0) + rloc;
-                const int pslot = 2 * blockIdx.x + (u == 0 ? 1 : 0);
-                const float inv = l != 0.f ? 1.f / l : 0.f;
-                const long long head = walk.kvh * g.group + head_in_group;
-                T *dst = static_cast<T *>(g.out) + (long long)(it.token0 + t_in_item) * g.ots + head * g.ohs;
-                float *pdst = ga.part_o + ((long long)pslot * Cfg::kRows + row) * DP;
-                if (valid && (PAIR || w == 0)) {
-                    if (whole) {
-                        if (g.lse)
-                            g.lse[(long long)(it.token0 + t_in_item) * g.hq + head] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-                    } else {
-                        ga.part_ml[(long long)pslot * Cfg::kRows + row] = make_float2(m, l);
+                if constexpr (MODE == kCopies) {
+                    l = 0.f;
+                    for (int q = 0; q < 4; ++q) {
+                        const float2 x = row_ml[q * 32 + lane], y = row_ml[128 + q * 32 + lane];
+                        l += x.y * ex2(x.x - base) + y.y * ex2(y.x - base);
                     }
                 }
-                // SPLIT: each worker brings one half of the channels of both outputs
-                const int c0 = PAIR ? 0 : w * (DP / 64), c1 = PAIR ? DP / 32 : c0 + DP / 64;
+            }
+            const bool have0 = PAIR ? have_o : any;
+            const int pslot = 2 * blockIdx.x + (u == 0 ? 1 : 0);
+            // 32 channels of this row: the worker's own (PAIR) or both workers'
+            auto outputs = [&](int c, float (&o)[32]) {
 #pragma unroll
-                for (int c = 0; c < DP / 32; ++c) {
-                    if (c < c0 || c >= c1) continue;
+                for (int i = 0; i < 32; ++i) o[i] = 0.f;
+                const uint32_t tc = tmem + lanes + 256 + (PAIR ? w * 128 : 0) + c * 32;
+                if (have0) {
+                    uint32_t x[32];
+                    tm_ld32(tc, x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]) * wt0;
+                }
+                if (!PAIR && have1) {
+                    uint32_t x[32];
+                    tm_ld32(tc + 128, x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = fmaf(__uint_as_float(x[i]), wt1, o[i]);
+                }
+            };
+            const float inv = l != 0.f ? 1.f / l : 0.f;
+            if (warp_on && valid && (PAIR || w == 0) && (MODE != kCopies || quarter == 0)) {
+                if (!whole) ga.part_ml[(long long)pslot * Cfg::kRows + (PAIR ? w * 128 : 0) + row] = make_float2(m, l);
+                else if (g.lse)
+                    g.lse[(long long)(it.token0 + t_in_item) * g.hq + walk.kvh * g.group + head_in_group] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+            }
+            if constexpr (MODE == kCopies) {
+                // The four copies' shares meet in shared memory, eight rows at a time; then a thread per four channels writes.
+                float *stage = reinterpret_cast<float *>(smem + (Cfg::kQTiles + Cfg::kSlots) * Cfg::kTile);
+                constexpr int kLine = DP + 4;
+                const int rows = it.n_tok * g.group;
+                for (int r0 = 0; r0 < rows; r0 += 8) {
+                    const bool mine = row >= r0 && row < r0 + 8 && valid;
+#pragma unroll
+                    for (int cc = 0; cc < DP / 64; ++cc) {
+                        const int c = w * (DP / 64) + cc;             // each worker brings one half of the channels
+                        float o[32];
+                        outputs(c, o);
+                        if (mine) {
+                            float *dst = stage + (quarter * 8 + row - r0) * kLine + c * 32;
+                            const float f = whole ? inv : 1.f;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                *reinterpret_cast<float4 *>(dst + i) = make_float4(o[i] * f, o[i + 1] * f, o[i + 2] * f, o[i + 3] * f);
+                        }
+                        __syncwarp();
+                    }
+                    named_bar_sync(3, 256);
+                    const int wtid = tid & 255, r = wtid / (DP / 4), ch = wtid % (DP / 4) * 4;
+                    if (r < 8 && r0 + r < rows) {
+                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float4 y = *reinterpret_cast<const float4 *>(stage + (q * 8 + r) * kLine + ch);
+                            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+                        }
+                        const int rr = r0 + r, tk = rr / g.group;
+                        if (!whole)
+                            *reinterpret_cast<float4 *>(ga.part_o + ((long long)pslot * Cfg::kRows + rr) * DP + ch) = x;
+                        else if (ch < g.dim)
+                            *reinterpret_cast<uint2 *>(static_cast<T *>(g.out) + (long long)(it.token0 + tk) * g.ots +
+                                                       (walk.kvh * g.group + rr - tk * g.group) * g.ohs + ch) =
+                                make_uint2(pack_pair<T>(x.x, x.y), pack_pair<T>(x.z, x.w));
+                    }
+                    named_bar_sync(2, 256);
+                }
+            } else if (warp_on) {
+                T *dst = static_cast<T *>(g.out) + (long long)(it.token0 + t_in_item) * g.ots + (walk.kvh * g.group + head_in_group) * g.ohs;
+                float *pdst = ga.part_o + ((long long)pslot * Cfg::kRows + (PAIR ? w * 128 : 0) + row) * DP;
+#pragma unroll
+                for (int cc = 0; cc < (PAIR ? DP / 32 : DP / 64); ++cc) {
+                    const int c = PAIR ? cc : w * (DP / 64) + cc;     // SPLIT: each worker brings one half of the channels
                     float o[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0.f;
-                    const uint32_t tc = tmem + lanes + 256 + (PAIR ? w * 128 : 0) + c * 32;
-                    if (have0) {
-                        uint32_t x[32];
-                        tm_ld32(tc, x);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]) * wt0;
-                    }
-                    if (!PAIR && have1) {
-                        uint32_t x[32];
-                        tm_ld32(tc + 128, x);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = fmaf(__uint_as_float(x[i]), wt1, o[i]);
-                    }
+                    outputs(c, o);
                     if (!valid) {
                     } else if (whole) {
 #pragma unroll
@@ -736,13 +975,15 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                     }
                     __syncwarp();
                 }
-                tc_fence_before();
             }
-            if constexpr (!PAIR) named_bar_sync(2, 256);
+            tc_fence_before();
+            if constexpr (MODE == kSplit) named_bar_sync(2, 256);
             left -= n;
             u = 0;
             if (left > 0) walk.next(g, item_tokens);
         }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     }
     if (!ok && lane == 0) report_status(g.status, FPSK_ERR_TIMEOUT);
     tc_fence_before();
@@ -751,10 +992,10 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
 }
 
 // Joins the parts of the divided items: a warp per row, four channels per lane.
-template <typename T, int DP, bool PAIR>
+template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcaArgs ga)
 {
-    constexpr int kRows = Tca<DP, PAIR>::kRows;
+    constexpr int kRows = Tca<DP, MODE>::kRows;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const AttnArgs &g = ga.a;
     const SplitRecord r = ga.records[blockIdx.x];
@@ -814,7 +1055,7 @@ static EncodeFn encode_fn()
 }
 static bool encode(CUtensorMap *map, int type, int rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box)
 {
-    static const cuuint32_t ones[4] = {1, 1, 1, 1};
+    static const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     const EncodeFn fn = encode_fn();
     return fn && fn(map, type == FPSK_ELEM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
                     const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -853,14 +1094,15 @@ bool attention_tc_takes(const AttnArgs &g)
            aligned16(g.out, g.ots, g.ohs, 0) && aligned16(g.k, g.kps, g.kts, g.khs) && aligned16(g.v, g.vps, g.vts, g.vhs);
 }
 
-template <typename T, int DP, bool PAIR> static fpsk_status launch_tc(const AttnArgs &a, int type, void *ws, cudaStream_t st)
+template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnArgs &a, int type, void *ws, cudaStream_t st)
 {
-    using Cfg = Tca<DP, PAIR>;
+    using Cfg = Tca<DP, MODE>;
+    constexpr bool PAIR = MODE == kPair;
     const int ctas = sm_count();
     if (ctas < 1) return FPSK_ERR_CUDA;
     TcaArgs g;
     g.a = a;
-    g.tile_tokens = kRowsPerTile / a.group;
+    g.tile_tokens = Cfg::kTileRows / a.group;
     g.box_rows = a.page_size & -a.page_size;
     if (g.box_rows > kKeysPerTile) g.box_rows = kKeysPerTile;
     char *p = static_cast<char *>(ws);
@@ -878,21 +1120,42 @@ template <typename T, int DP, bool PAIR> static fpsk_status launch_tc(const Attn
         const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)g.tile_tokens};
         if (!encode(&mq, type, 3, a.q, dims, str, box)) return FPSK_ERR_CUDA;
     }
-    const cuuint64_t dims[4] = {(cuuint64_t)a.dim, (cuuint64_t)a.page_size, (cuuint64_t)a.hk, (cuuint64_t)a.n_pages};
-    const cuuint32_t box[4] = {64, (cuuint32_t)g.box_rows, 1, 1};
-    const cuuint64_t ks[3] = {bytes(a.kts, a.page_size), bytes(a.khs, a.hk), bytes(a.kps, a.n_pages)};
-    const cuuint64_t vs[3] = {bytes(a.vts, a.page_size), bytes(a.vhs, a.hk), bytes(a.vps, a.n_pages)};
-    if (!encode(&mk, type, 4, a.k, dims, ks, box) || !encode(&mv, type, 4, a.v, dims, vs, box)) return FPSK_ERR_CUDA;
+    // A box of K or V holds the rows of one head and page.  Heads of 128 channels come with both halves in one load where two of
+    // the outer dimensions merge into one: the eight-row groups of all pages (a page is page_size rows long), or the heads of all
+    // pages (a page is its heads long).
+    auto kv_map = [&](CUtensorMap *m, TileLayout &tl, const void *base, long long ps, long long ts, long long hs) {
+        const cuuint32_t R = (cuuint32_t)g.box_rows;
+        tl.map = kByHalves;
+        if (a.dim == 128 && (a.n_pages == 1 || ps == a.page_size * ts) && a.n_pages * (a.page_size / 8) <= 0x7FFFFFFFLL) tl.map = kGroupsOfAllPages;
+        else if (a.dim == 128 && (a.n_pages == 1 || ps == a.hk * hs) && a.n_pages * a.hk <= 0x7FFFFFFFLL) tl.map = kHeadsOfAllPages;
+        if (tl.map == kByHalves) {
+            tl.half_bytes = kHalfBytes;
+            tl.group_bytes = 1024;
+            const cuuint64_t dims[4] = {(cuuint64_t)a.dim, (cuuint64_t)a.page_size, (cuuint64_t)a.hk, (cuuint64_t)a.n_pages};
+            const cuuint64_t str[3] = {bytes(ts, a.page_size), bytes(hs, a.hk), bytes(ps, a.n_pages)};
+            const cuuint32_t box[4] = {64, R, 1, 1};
+            return encode(m, type, 4, base, dims, str, box);
+        }
+        tl.half_bytes = 1024;
+        tl.group_bytes = 2048;
+        const bool groups = tl.map == kGroupsOfAllPages;
+        const cuuint64_t n_groups = (cuuint64_t)(a.page_size / 8);
+        const cuuint64_t dims[5] = {64, 8, 2, groups ? (cuuint64_t)a.hk : n_groups, groups ? n_groups * (cuuint64_t)a.n_pages : (cuuint64_t)(a.n_pages * a.hk)};
+        const cuuint64_t str[4] = {bytes(ts, 8), 128, groups ? bytes(hs, a.hk) : bytes(8 * ts, n_groups), groups ? bytes(8 * ts, dims[4]) : bytes(hs, dims[4])};
+        const cuuint32_t box[5] = {64, 8, 2, groups ? 1 : R / 8, groups ? R / 8 : 1};
+        return encode(m, type, 5, base, dims, str, box);
+    };
+    if (!kv_map(&mk, g.kl, a.k, a.kps, a.kts, a.khs) || !kv_map(&mv, g.vl, a.v, a.vps, a.vts, a.vhs)) return FPSK_ERR_CUDA;
 
     static std::atomic<unsigned long long> prepared{0};               // one bit per device
     int dev = 0;
     FPSK_CUDA_OK(cudaGetDevice(&dev));
     const unsigned long long bit = 1ull << (dev & 63);
     if (!(prepared.load(std::memory_order_acquire) & bit)) {
-        FPSK_CUDA_OK(cudaFuncSetAttribute(attention_tc_kernel<T, DP, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+        FPSK_CUDA_OK(cudaFuncSetAttribute(attention_tc_kernel<T, DP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
         prepared.fetch_or(bit, std::memory_order_release);
     }
-    attention_tc_kernel<T, DP, PAIR><<<ctas, kTcaThreads, Cfg::kSmem, st>>>(g, mq, mk, mv);
+    attention_tc_kernel<T, DP, MODE><<<ctas, kTcaThreads, Cfg::kSmem, st>>>(g, mq, mk, mv);
     FPSK_LAUNCH_CHECK();
     // the join's launch overlaps the end of the kernel before it
     cudaLaunchConfig_t cfg = {};
@@ -904,19 +1167,21 @@ template <typename T, int DP, bool PAIR> static fpsk_status launch_tc(const Attn
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_join_kernel<T, DP, PAIR>, g));
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_join_kernel<T, DP, MODE>, g));
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
 
-// PAIR where a sequence may have more tokens than one tile holds.
+// COPIES while the rows of every sequence's new tokens fit a quarter of the TMEM lanes, SPLIT while they fit one tile, else PAIR.
 fpsk_status attention_tc_launch(const AttnArgs &a, int type, int max_q_len, void *ws, cudaStream_t st)
 {
-    const bool pair = max_q_len > kRowsPerTile / a.group;
-#define FPSK_TCA(TT)                                                                                                              \
-    (a.dim <= 64 ? (pair ? launch_tc<TT, 64, true>(a, type, ws, st) : launch_tc<TT, 64, false>(a, type, ws, st))                  \
-                 : (pair ? launch_tc<TT, 128, true>(a, type, ws, st) : launch_tc<TT, 128, false>(a, type, ws, st)))
-    return type == FPSK_ELEM_FP16 ? FPSK_TCA(__half) : FPSK_TCA(__nv_bfloat16);
+    const long long rows = (long long)(max_q_len < 1 ? 1 : max_q_len) * a.group;
+#define FPSK_TCA(TT, DD)                                                        \
+    (rows <= 32 ? launch_tc<TT, DD, kCopies>(a, type, ws, st)                   \
+                : rows <= kRowsPerTile ? launch_tc<TT, DD, kSplit>(a, type, ws, st) : launch_tc<TT, DD, kPair>(a, type, ws, st))
+#define FPSK_TCA_DIM(TT) (a.dim <= 64 ? FPSK_TCA(TT, 64) : FPSK_TCA(TT, 128))
+    return type == FPSK_ELEM_FP16 ? FPSK_TCA_DIM(__half) : FPSK_TCA_DIM(__nv_bfloat16);
+#undef FPSK_TCA_DIM
 #undef FPSK_TCA
 }
 
