@@ -13,8 +13,8 @@
 // a PAIR item they hold different query tiles and share every key tile; in a SPLIT item they hold the same queries and take
 // alternate key tiles, and meet at the item's end.  While one computes its softmax, the tensor cores work for the other.
 // Two loader warps bring Q and K tiles and V tiles, page by page, by TMA into a ring of tiles, 128-byte swizzled; one warp
-// issues the MMAs.  Maximum: the reference maximum of a row follows the true one only when that has grown by more than 2^8 (P then
-// stays below 256, exact enough in 16 bits whatever its size), so O in TMEM is rescaled rarely.
+// issues the MMAs.  Maximum: the reference maximum of a row follows the true one only when the weights of a step outgrow it by 2^12 (P
+// is exact to 16-bit rounding whatever its size), so O in TMEM is rescaled rarely and most steps take no maximum at all.
 // Every wait is bounded: a role whose wait gave up stops waiting and issuing, walks through its loops, reports
 // FPSK_ERR_TIMEOUT and the CTA frees its TMEM and leaves.
 #include "attention.cuh"
@@ -31,11 +31,7 @@ constexpr int kPairKeys = 64;                    // keys of a PAIR worker's step
 constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8: MMA issue, 9 and 10: loaders
 constexpr int kHalfBytes = 128 * 128;            // 128 rows of one 64-channel half of a tile
 constexpr int kTcaMaxSeqs = 16384;
-#ifndef FPSK_POLY
-#define FPSK_POLY 0
-#endif
-constexpr int kPoly = FPSK_POLY;                 // of eight pairs of exponentials, computed on the FMA pipe
-constexpr float kLazy = 8.f;                     // growth of the maximum (in powers of two) that O is not rescaled for
+constexpr float kMostSum = 4096.f;               // of a step's weights, before a row's reference maximum is renewed
 
 // 32 consecutive columns of this thread's accumulator row; valid after tm_wait32 on the same array
 __device__ __forceinline__ void tm_load32(uint32_t taddr, uint32_t (&v)[32])
@@ -61,6 +57,16 @@ __device__ __forceinline__ void tm_wait32(uint32_t (&v)[32])
         "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
         "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
         :
+        : "memory");
+}
+__device__ __forceinline__ void tm_ld16(uint32_t taddr, uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
         : "memory");
 }
 __device__ __forceinline__ void tm_ld32(uint32_t taddr, uint32_t (&v)[32])
@@ -165,22 +171,6 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-// 2^x for x <= 100 on the FMA pipe, two at a time: x = n + f with n the nearest whole number, 2^f by the polynomial of degree 4
-// that minimises the largest relative error on [-1/2, 1/2] (Remez exchange: 2.6e-6; in FP32 2.7e-6), n added to the exponent.
-// Below -126 it stays at 2^-126; NaN comes out as some number (the callers see to both).
-__device__ __forceinline__ float2 ex2_poly(float2 x)
-{
-    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
-    const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);   // 1.5 * 2^23
-    const float2 t = __fadd2_rn(x, magic);
-    const float2 f = __ffma2_rn(__fadd2_rn(t, unmagic), make_float2(-1.f, -1.f), x);
-    float2 p = __ffma2_rn(make_float2(0.009570102207362652f, 0.009570102207362652f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
-    p = __ffma2_rn(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
-    p = __ffma2_rn(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
-    p = __ffma2_rn(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 // maxima that pass a NaN on
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -774,61 +764,62 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                     };
                     // a row that has met NaN or +inf is NaN, whatever its other scores are
                     auto reference = [](float top) { return top < INFINITY ? top : __int_as_float(0x7FC00000); };
-                    if (!have_o) {
-                        // the item's first tile sets the reference maximum
-                        uint32_t s[kChunks][32];
-                        load_scores(s);
+                    auto top_score = [&](uint32_t (&s)[kChunks][32]) {
                         float top = -INFINITY;
 #pragma unroll
                         for (int c = 0; c < kChunks; ++c) top = top32(s[c], top);
-                        m = reference(top * sl2);
-                    }
-                    // Weights against the reference maximum, the tile's own maximum beside them: where that has grown too far
-                    // (rare), the reference follows, O is rescaled and the weights are computed once more.  kPoly of eight pairs of
-                    // exponentials go to the FMA pipe, the others to the special-function unit, which alone would be what bounds it.
+                        return top * sl2;
+                    };
+                    // Weights against the reference maximum, which the item's first step sets.  The sum of a step's weights tells whether
+                    // a score has outgrown it: while the sum is at most kMostSum no weight is larger, and no maximum is taken.  Else
+                    // (rare) the reference follows, O is rescaled and the weights are computed once more.
                     uint32_t p[kCols / 2];
-                    float2 sum[2];
+                    float step_sum;
+                    bool again = !have_o;
 #pragma unroll 1
-                    for (int pass = 0;; ++pass) {
-                        const float base = m == -INFINITY ? 0.f : m;
-                        const float2 sc = make_float2(sl2, sl2), nb = make_float2(-base, -base);
-                        float top = -INFINITY;
-                        sum[0] = sum[1] = make_float2(0.f, 0.f);
+                    for (;;) {
                         uint32_t s[kChunks][32];
                         load_scores(s);
+                        if (again) {
+                            const float top = top_score(s);
+                            const bool grow = valid && !(top <= m);
+                            const float m2 = grow ? reference(top) : m, alpha = grow ? ex2(m - m2) : 1.f;
+                            m = m2;
+                            l *= alpha;
+                            if (have_o) {
+                                wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
+                                tc_fence_after();
+#pragma unroll 1
+                                for (int c = 0; c < DP / 16; ++c) {
+                                    uint32_t o[16];
+                                    tm_ld16(to + c * 16, o);
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                    tm_st16(to + c * 16, o);
+                                }
+                                tm_wait_st();
+                            }
+                        }
+                        const float base = m == -INFINITY ? 0.f : m;
+                        const float2 sc = make_float2(sl2, sl2), nb = make_float2(-base, -base);
+                        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                         for (int c = 0; c < kChunks; ++c) {
-                            top = top32(s[c], top);
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
                                 float2 x = make_float2(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1]));
                                 x = __ffma2_rn(x, sc, nb);
-                                x = ((i + 1) * kPoly) / 8 != (i * kPoly) / 8 ? ex2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
+                                x = make_float2(ex2(x.x), ex2(x.y));
                                 sum[i & 1] = __fadd2_rn(sum[i & 1], x);
                                 p[c * 16 + i] = pack_pair<T>(x.x, x.y);
                             }
                         }
-                        top *= sl2;
-                        const bool grow = valid && !(top <= m + kLazy);
-                        if (pass || !__any_sync(0xFFFFFFFFu, grow)) break;
-                        const float m2 = grow ? reference(top) : m, alpha = grow ? ex2(m - m2) : 1.f;
-                        m = m2;
-                        l *= alpha;
-                        if (have_o) {
-                            wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
-                            tc_fence_after();
-#pragma unroll 1
-                            for (int c = 0; c < DP / 32; ++c) {
-                                uint32_t o[32];
-                                tm_ld32(to + c * 32, o);
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tm_st32(to + c * 32, o);
-                            }
-                            tm_wait_st();
-                        }
+                        step_sum = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                        // (a row without a reference so far, all of its scores hidden, gets one with its first weight)
+                        if (again || __all_sync(0xFFFFFFFFu, !valid || step_sum <= (m == -INFINITY ? 0.f : kMostSum))) break;
+                        again = true;
                     }
-                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    l += step_sum;
                     if constexpr (MODE == kCopies) {
                         // zeros for the other quarters' keys
 #pragma unroll
@@ -859,7 +850,6 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
                 tc_fence_after();
             }
-            if (m == -INFINITY) l = 0.f;                              // (2^-126 is not zero)
             // ---- the item's end: finished here, or a partial result
             const bool whole = u == 0 && n == it.units;
             const bool any = it.hi > it.lo, have1 = any && n > 1;     // SPLIT: outputs of the two workers
