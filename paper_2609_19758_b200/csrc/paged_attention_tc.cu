@@ -12,8 +12,8 @@
 // Two workers per CTA, a warpgroup each, a thread per row, with accumulators S and O of their own in TMEM.  In
 // a PAIR item they hold different query tiles and share every key tile; in a SPLIT item they hold the same queries and take
 // alternate key tiles, and meet at the item's end.  While one computes its softmax, the tensor cores work for the other.
-// Two loader warps bring Q and K tiles and V tiles, page by page, by TMA into a ring of tiles, 128-byte swizzled; one warp
-// issues the MMAs.  Maximum: the reference maximum of a row follows the true one only when the weights of a step outgrow it by 2^12 (P
+// Two loader warps bring Q and K tiles and V tiles, page by page, by TMA into a ring of tiles, 128-byte swizzled; a warp for
+// each worker issues its MMAs.  Maximum: the reference maximum of a row follows the true one only when the weights of a step outgrow it by 2^12 (P
 // is exact to 16-bit rounding whatever its size), so O in TMEM is rescaled rarely and most steps take no maximum at all.
 // Every wait is bounded: a role whose wait gave up stops waiting and issuing, walks through its loops, reports
 // FPSK_ERR_TIMEOUT and the CTA frees its TMEM and leaves.
@@ -28,9 +28,13 @@ namespace fpsk {
 
 constexpr int kRowsPerTile = 128, kKeysPerTile = 128;
 constexpr int kPairKeys = 64;                    // keys of a PAIR worker's step: two S accumulators fit its TMEM columns
-constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8: MMA issue, 9 and 10: loaders
+constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8 and 11: their MMAs, 9 and 10: loaders
 constexpr int kHalfBytes = 128 * 128;            // 128 rows of one 64-channel half of a tile
 constexpr int kTcaMaxSeqs = 16384;
+#ifndef FPSK_POLY
+#define FPSK_POLY 0
+#endif
+constexpr int kPoly = FPSK_POLY;                 // of eight pairs of exponentials, computed on the FMA pipe
 constexpr float kMostSum = 4096.f;               // of a step's weights, before a row's reference maximum is renewed
 
 // 32 consecutive columns of this thread's accumulator row; valid after tm_wait32 on the same array
@@ -151,16 +155,15 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-// Bounded wait on an mbarrier phase (about a second), without a call: a call's register conventions would spill the rows
-// that the workers hold.
+// Bounded wait on an mbarrier phase, without a call (a call's register conventions would spill the rows that the workers hold)
+// and without the clock: the limit counts polls, each of which sleeps in hardware for a while.
+constexpr int kMostPolls = 1 << 22;
 __device__ __forceinline__ bool bar_wait_inline(uint32_t bar, uint32_t parity)
 {
-    if (mbar_try(bar, parity)) return true;
-    const long long t_end = clock64() + 2000000000LL;
 #pragma unroll 1
-    while (!mbar_try(bar, parity))
-        if (clock64() > t_end) return false;
-    return true;
+    for (int i = 0; i < kMostPolls; ++i)
+        if (mbar_try(bar, parity)) return true;
+    return false;
 }
 __device__ __forceinline__ void named_bar_sync(int id, int threads)
 {
@@ -171,6 +174,23 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// 2^x on the FMA pipe, two at a time: x = n + f with n the nearest whole number, 2^f by the polynomial of degree 4 that minimises
+// the largest relative error on [-1/2, 1/2] (Remez exchange: 2.6e-6; evaluated in FP32 2.7e-6), n added to the exponent.  Within
+// [-126, 127]; beyond, the value at the end.  NaN comes out as FLT_MAX or NaN, which no sum of weights passes for small.
+__device__ __forceinline__ float2 ex2_poly(float2 x)
+{
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;\n\tmin.NaN.f32 %0, %0, 0f42FE0000;" : "+f"(x.x));
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;\n\tmin.NaN.f32 %0, %0, 0f42FE0000;" : "+f"(x.y));
+    const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);   // 1.5 * 2^23
+    const float2 t = __fadd2_rn(x, magic);
+    const float2 f = __ffma2_rn(__fadd2_rn(t, unmagic), make_float2(-1.f, -1.f), x);
+    float2 p = __ffma2_rn(make_float2(0.009570102207362652f, 0.009570102207362652f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
+    p = __ffma2_rn(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
+    p = __ffma2_rn(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+    p = __ffma2_rn(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 // maxima that pass a NaN on
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -210,7 +230,8 @@ struct TileLayout {
 struct TcaArgs {
     AttnArgs a;
     int tile_tokens;                   // tokens of a query tile: its rows / group
-    int box_rows;                      // keys of one TMA box: the largest power of two that divides a page, at most 128
+    int box_log;                       // keys of one TMA box, 2^box_log: the largest power of two that divides a page, at most 128
+    int tile_pages, tile_rest;         // a tile further: so many pages and rows
     TileLayout kl, vl;
     float *part_o;                     // [2 slots per CTA][rows][DP]
     float2 *part_ml;                   // [2 slots per CTA][rows]: maximum (powers of two), sum
@@ -333,8 +354,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
 
     if (tid == 0) {
         mbar_init(smem_u32(&sh->q_full), 1);
-        mbar_init(smem_u32(&sh->q_empty), 1);
-        mbar_init(smem_u32(&sh->done), 1);
+        mbar_init(smem_u32(&sh->q_empty), 2);
+        mbar_init(smem_u32(&sh->done), 2);
         for (int w = 0; w < 4; ++w) {                                  // worker w & 1, even and odd steps
             mbar_init(smem_u32(&sh->s_full[w]), 1);
             mbar_init(smem_u32(&sh->p_ready[w]), 4);
@@ -342,7 +363,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         }
         for (int s = 0; s < Cfg::kSlots; ++s) {
             mbar_init(smem_u32(&sh->kv_full[s]), 1);
-            mbar_init(smem_u32(&sh->kv_empty[s]), 1);
+            mbar_init(smem_u32(&sh->kv_empty[s]), 2);                  // both MMA warps pass every tile
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -465,7 +486,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         const bool is_v = warp == 10;
         const CUtensorMap *map = is_v ? &map_v : &map_k;
         const TileLayout tl = is_v ? ga.vl : ga.kl;
-        const int page_size = g.page_size, R = ga.box_rows;
+        const int page_size = g.page_size, R = 1 << ga.box_log;
         const int halves = tl.map == kByHalves ? Cfg::kHalves : 1;
         const uint32_t box_bytes = (uint32_t)(R * 128 * Cfg::kHalves) / halves;
         left = uniform(left);
@@ -495,29 +516,30 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                     q_used = true;
                 }
                 const int *table = g.table + (long long)walk.b * g.table_stride;
-                // the pages of a tile's boxes that hold a visible key, one box per lane (up to 16)
-                auto first_box = [&](int tile) { return max(0, lo - tile * kKeysPerTile) / R; };
-                auto end_box = [&](int tile) { return (min(kKeysPerTile, hi - tile * kKeysPerTile) + R - 1) / R; };
-                auto pages = [&](int tile) {
-                    const int box = first_box(tile) + lane;
-                    int page = 0;
-                    if (box < end_box(tile)) {
-                        const int col = (tile * kKeysPerTile + box * R) / page_size;
-                        page = col < g.max_pages ? __ldg(table + col) : -1;
-                    }
-                    return page;
+                // A tile's boxes (up to 16), one per lane: column of the table and row of the page.  They are carried from tile to tile;
+                // a division here would wait for the special-function unit, which the workers keep busy.
+                int key = tile_a * kKeysPerTile + lane * R;
+                int col = key / page_size, row = key - col * page_size;
+                auto fetch = [&]() {
+                    const bool wanted = key + R > lo && key < hi && lane * R < kKeysPerTile;
+                    return !wanted ? 0 : col < g.max_pages ? __ldg(table + col) : -1;
                 };
-                int next = pages(tile_a);
+                int next = fetch();
                 for (int i = 0; i < n; ++i) {
-                    const int tile = tile_a + i;
+                    const int tile = tile_a + i, k0 = tile * kKeysPerTile;
                     int page = next;
-                    if (i + 1 < n) next = pages(tile + 1);             // its latency passes behind the wait
+                    const int page_row = row;
+                    key += kKeysPerTile;
+                    col += ga.tile_pages;
+                    row += ga.tile_rest;
+                    if (row >= page_size) { row -= page_size; ++col; }
+                    if (i + 1 < n) next = fetch();                     // its latency passes behind the wait
                     // this tile's place in the order in which the MMAs use the ring
                     const int at = seq + (PAIR ? 2 * i + is_v : is_v ? min(2 * i + 2, 2 * n - 1) : max(2 * i - 1, 0));
                     const int slot = at % Cfg::kSlots;
                     const uint32_t phase = (uint32_t)(at / Cfg::kSlots) & 1u;
                     const uint32_t full = smem_u32(&sh->kv_full[slot]), dst = ring + slot * Cfg::kTile;
-                    const int b0 = first_box(tile), b1 = end_box(tile);
+                    const int b0 = max(0, lo - k0) >> ga.box_log, b1 = (min(kKeysPerTile, hi - k0) + R - 1) >> ga.box_log;
                     wait(smem_u32(&sh->kv_empty[slot]), phase ^ 1u);
                     if (page < 0 || page >= g.n_pages) {
                         report_status(g.status, FPSK_ERR_PARAM);
@@ -528,16 +550,15 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         if (elect_one()) mbar_expect_tx(full, (uint32_t)((b1 - b0) * halves) * box_bytes);
                         __syncwarp();
                         for (int box = b0; box < b1; ++box) {
-                            const int pg = __shfl_sync(0xFFFFFFFFu, page, box - b0);
-                            const int row = (tile * kKeysPerTile + box * R) % page_size;
+                            const int pg = __shfl_sync(0xFFFFFFFFu, page, box), at_row = __shfl_sync(0xFFFFFFFFu, page_row, box);
                             if (elect_one()) {
                                 if (tl.map == kGroupsOfAllPages)
-                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, kvh, (pg * page_size + row) >> 3, full);
+                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, kvh, (pg * page_size + at_row) >> 3, full);
                                 else if (tl.map == kHeadsOfAllPages)
-                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, row >> 3, pg * g.hk + kvh, full);
+                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, at_row >> 3, pg * g.hk + kvh, full);
                                 else
                                     for (int h = 0; h < Cfg::kHalves; ++h)
-                                        tma_load_4d(dst + h * kHalfBytes + box * box_bytes, map, h * 64, row, kvh, pg, full);
+                                        tma_load_4d(dst + h * kHalfBytes + box * box_bytes, map, h * 64, at_row, kvh, pg, full);
                             }
                             __syncwarp();
                         }
@@ -554,9 +575,11 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         for (int at = last; at >= 0 && at >= seq - Cfg::kSlots; --at)
             if (!bar_wait_inline(smem_u32(&sh->kv_full[at % Cfg::kSlots]), (uint32_t)(at / Cfg::kSlots) & 1u)) ok = false;
         if (q_used && !bar_wait_inline(smem_u32(&sh->q_full), q_phase ^ 1u)) ok = false;
-    } else if (warp == 8) {
-        // ------------------------------------------------------------ MMA issue
+    } else if (warp == 8 || warp == 11) {
+        // ------------------------------------------------------------ MMA issue, a warp for each worker: while one waits for its
+        // worker or works through its barriers, the tensor core has the other's
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        const int w = warp == 11;
         const uint32_t fmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
         const uint32_t base_desc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(kRowsPerTile >> 4) << 24);
         constexpr int kStepKeys = PAIR ? kPairKeys : kKeysPerTile;
@@ -566,45 +589,44 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         const uint32_t q_hi = desc_hi(1024), k_hi = desc_hi(ga.kl.group_bytes), v_hi = desc_hi(ga.vl.group_bytes);
         left = uniform(left);
         u = uniform(u);
-        int slot = 0;
-        uint32_t phase = 0, q_phase = 0;
-        uint32_t s_count[2] = {0, 0}, o_count[2] = {0, 0};             // steps issued for each worker so far
-        auto next_slot = [&]() {
-            if (++slot == Cfg::kSlots) { slot = 0; phase ^= 1u; }
-        };
+        int seq = 0;                                                   // tiles of K and V that went before this item
+        uint32_t q_phase = 0, s_count = 0, o_count = 0;                // steps issued so far
         auto all_wait = [&](uint32_t bar, uint32_t parity) {
             wait(bar, parity);
             ok = __all_sync(0xFFFFFFFFu, ok);
             tc_fence_after();
         };
-        // TMEM columns of a worker's S (and P) in a step
-        auto s_col = [&](int w, uint32_t count) { return tm + w * 128 + (PAIR ? (count & 1u) * kPairKeys : 0u); };
-        auto issue_s = [&](int w, uint32_t k_addr) {
-            const uint32_t c = s_count[w]++;
+        // TMEM columns of the worker's S (and P) in a step
+        auto s_col = [&](uint32_t count) { return tm + w * 128 + (PAIR ? (count & 1u) * kPairKeys : 0u); };
+        auto issue_s = [&](uint32_t k_addr) {
+            const uint32_t c = s_count++;
             if (ok && elect_one()) {
                 const uint32_t qa = desc_lo(q_smem + (PAIR ? w * Cfg::kTile : 0), 16), kb = desc_lo(k_addr, 16);
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
-                    mma_ss(s_col(w, c), qa + ((k / 4) * kHalfBytes + (k % 4) * 32) / 16, q_hi,
+                    mma_ss(s_col(c), qa + ((k / 4) * kHalfBytes + (k % 4) * 32) / 16, q_hi,
                            kb + (k / 4) * (ga.kl.half_bytes / 16) + (k % 4) * 2, k_hi, idesc_s, k > 0);
                 tc_commit(smem_u32(&sh->s_full[w + 2 * (c & 1u)]));
             }
             __syncwarp();
         };
-        auto issue_o = [&](int w, uint32_t v_addr, bool accumulate) {
-            const uint32_t c = o_count[w]++;
+        auto issue_o = [&](uint32_t v_addr, bool accumulate) {
+            const uint32_t c = o_count++;
             all_wait(smem_u32(&sh->p_ready[w + 2 * (c & 1u)]), (c >> 1) & 1u);
             if (ok && elect_one()) {
                 const uint32_t vb = desc_lo(v_addr, ga.vl.half_bytes), step = ga.vl.group_bytes / 8;
 #pragma unroll
                 for (int k = 0; k < kStepKeys / 16; ++k)
-                    mma_ts(tm + 256 + w * 128, s_col(w, c) + k * 8, vb + k * step, v_hi, idesc_o, accumulate || k > 0);
+                    mma_ts(tm + 256 + w * 128, s_col(c) + k * 8, vb + k * step, v_hi, idesc_o, accumulate || k > 0);
                 tc_commit(smem_u32(&sh->o_done[w + 2 * (c & 1u)]));
             }
             __syncwarp();
         };
-        auto release = [&](int s) {
-            if (ok && elect_one()) tc_commit(smem_u32(&sh->kv_empty[s]));
+        // a tile by its place in the ring's order
+        auto tile_addr = [&](int at) { return ring + (uint32_t)(at % Cfg::kSlots) * Cfg::kTile; };
+        auto wait_tile = [&](int at) { all_wait(smem_u32(&sh->kv_full[at % Cfg::kSlots]), (uint32_t)(at / Cfg::kSlots) & 1u); };
+        auto release = [&](unsigned long long *bar) {
+            if (ok && elect_one()) tc_commit(smem_u32(bar));
             __syncwarp();
         };
         while (left > 0) {
@@ -612,7 +634,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             const int lo = uniform(it.lo), hi = uniform(it.hi), n = min(left, uniform(it.units) - u);
             if (hi > lo) {
                 const int tile_a = uniform(it.tile0) + u, tile_b = tile_a + n;
-                // rows of a V tile that no token of the item may see: zeros, for 0 * (what lies there) must not be NaN
+                // rows of a V tile that no token of the item may see: zeros, for 0 * (what lies there) must not be NaN (in a PAIR
+                // item both warps write them, each before its own MMAs)
                 auto clean_v = [&](int tile, uint32_t v_addr) {
                     const int k0 = tile * kKeysPerTile, r0 = max(0, lo - k0), r1 = min(kKeysPerTile, hi - k0);
                     if (r0 == 0 && r1 == kKeysPerTile) return;
@@ -626,75 +649,61 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 };
                 all_wait(smem_u32(&sh->q_full), q_phase);
                 q_phase ^= 1u;
-                auto wait_full = [&]() { all_wait(smem_u32(&sh->kv_full[slot]), phase); };
                 if constexpr (PAIR) {
-                    // S of a worker is two steps ahead of its P V, so that a softmax never waits for its scores
-                    int wa[2], wb[2];
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        worker_steps(g, it, w, tile_tokens, 2 * tile_a, 2 * tile_b, wa[w], wb[w]);
-                        wa[w] = uniform(wa[w]);
-                        wb[w] = uniform(wb[w]);
-                    }
+                    // S is two steps ahead of P V, so that a softmax never waits for its scores
+                    int sa, sb;
+                    worker_steps(g, it, w, tile_tokens, 2 * tile_a, 2 * tile_b, sa, sb);
+                    sa = uniform(sa);
+                    sb = uniform(sb);
                     const uint32_t k_half = 8 * ga.kl.group_bytes, v_half = 8 * ga.vl.group_bytes;   // the tile's second 64 keys
-                    wait_full();
+                    wait_tile(seq);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int w = 0; w < 2; ++w)
-                            if (2 * tile_a + h >= wa[w] && 2 * tile_a + h < wb[w]) issue_s(w, ring + slot * Cfg::kTile + h * k_half);
-                    release(slot);
-                    next_slot();
+                        if (2 * tile_a + h >= sa && 2 * tile_a + h < sb) issue_s(tile_addr(seq) + h * k_half);
+                    release(&sh->kv_empty[seq % Cfg::kSlots]);
                     for (int t = tile_a; t < tile_b; ++t) {
-                        const int v_slot = slot;
-                        wait_full();
-                        next_slot();
-                        const uint32_t v_addr = ring + v_slot * Cfg::kTile, k_addr = ring + slot * Cfg::kTile;
-                        if (ok) clean_v(t, v_addr);
-                        if (t + 1 < tile_b) wait_full();
+                        const int vt = seq + 1, kt = seq + 2;
+                        const bool more = t + 1 < tile_b;
+                        wait_tile(vt);
+                        if (ok) clean_v(t, tile_addr(vt));
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const int st = 2 * t + h;
-#pragma unroll
-                            for (int w = 0; w < 2; ++w) {
-                                if (st >= wa[w] && st < wb[w]) issue_o(w, v_addr + h * v_half, st > wa[w]);
-                                if (st + 2 < 2 * tile_b && st + 2 >= wa[w] && st + 2 < wb[w]) issue_s(w, k_addr + h * k_half);
-                            }
+                            if (st >= sa && st < sb) issue_o(tile_addr(vt) + h * v_half, st > sa);
+                            if (h == 1) release(&sh->kv_empty[vt % Cfg::kSlots]);
+                            if (more && h == 0) wait_tile(kt);
+                            if (more && st + 2 >= sa && st + 2 < sb) issue_s(tile_addr(kt) + h * k_half);
                         }
-                        release(v_slot);
-                        if (t + 1 < tile_b) {
-                            release(slot);
-                            next_slot();
-                        }
+                        if (more) release(&sh->kv_empty[kt % Cfg::kSlots]);
+                        seq += 2;
                     }
                 } else {
-                    for (int i = 0; i < 2 && i < n; ++i) {
-                        wait_full();
-                        issue_s(i, ring + slot * Cfg::kTile);
-                        release(slot);
-                        next_slot();
-                    }
-                    for (int i = 0; i < n; i += 2) {
-#pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            if (i + w >= n) break;
-                            wait_full();
-                            const uint32_t v_addr = ring + slot * Cfg::kTile;
-                            if (ok) clean_v(tile_a + i + w, v_addr);
-                            issue_o(w, v_addr, i > 0);
-                            release(slot);
-                            next_slot();
-                            if (i + w + 2 < n) {
-                                wait_full();
-                                issue_s(w, ring + slot * Cfg::kTile);
-                                release(slot);
-                                next_slot();
-                            }
+                    // Every other tile is this worker's.  Both warps go through the ring in its order and pass every tile on, their own
+                    // or not: a warp that waited for its own alone could take the parity of an older fill of a slot for the one it wants.
+                    auto step = [&](bool is_v, int i) {
+                        const int at = seq++;
+                        wait_tile(at);
+                        if ((i & 1) != w) {
+                            if (ok && elect_one()) mbar_arrive(smem_u32(&sh->kv_empty[at % Cfg::kSlots]));
+                            __syncwarp();
+                            return;
                         }
+                        if (is_v) {
+                            if (ok) clean_v(tile_a + i, tile_addr(at));
+                            issue_o(tile_addr(at), i > w);
+                        } else {
+                            issue_s(tile_addr(at));
+                        }
+                        release(&sh->kv_empty[at % Cfg::kSlots]);
+                    };
+                    step(false, 0);
+                    if (n > 1) step(false, 1);
+                    for (int i = 0; i < n; ++i) {
+                        step(true, i);
+                        if (i + 2 < n) step(false, i + 2);
                     }
                 }
-                if (ok && elect_one()) tc_commit(smem_u32(&sh->q_empty));
-                __syncwarp();
+                release(&sh->q_empty);
             }
             left -= n;
             u = 0;
@@ -704,7 +713,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         __syncwarp();
         if (!bar_wait_inline(smem_u32(&sh->done), 0)) ok = false;
         __syncwarp();
-    } else if (warp < 8) {
+    } else {
         // ------------------------------------------------------------ workers: a thread per row
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         constexpr int kCols = MODE == kCopies ? 32 : PAIR ? kPairKeys : 128;   // keys of a step that a thread weighs
@@ -809,7 +818,9 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             for (int i = 0; i < 16; ++i) {
                                 float2 x = make_float2(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1]));
                                 x = __ffma2_rn(x, sc, nb);
-                                x = make_float2(ex2(x.x), ex2(x.y));
+                                // (PAIR: the special-function unit alone would bound it)
+                                const bool poly = PAIR && ((i + 1) * kPoly) / 8 != (i * kPoly) / 8;
+                                x = poly ? ex2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
                                 sum[i & 1] = __fadd2_rn(sum[i & 1], x);
                                 p[c * 16 + i] = pack_pair<T>(x.x, x.y);
                             }
@@ -850,6 +861,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
                 tc_fence_after();
             }
+            if (m == -INFINITY) l = 0.f;                               // (hidden scores may have left 2^-126)
             // ---- the item's end: finished here, or a partial result
             const bool whole = u == 0 && n == it.units;
             const bool any = it.hi > it.lo, have1 = any && n > 1;     // SPLIT: outputs of the two workers
@@ -972,8 +984,6 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             u = 0;
             if (left > 0) walk.next(g, item_tokens);
         }
-    } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     }
     if (!ok && lane == 0) report_status(g.status, FPSK_ERR_TIMEOUT);
     tc_fence_before();
@@ -1093,8 +1103,9 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     TcaArgs g;
     g.a = a;
     g.tile_tokens = Cfg::kTileRows / a.group;
-    g.box_rows = a.page_size & -a.page_size;
-    if (g.box_rows > kKeysPerTile) g.box_rows = kKeysPerTile;
+    for (g.box_log = 3; g.box_log < 7 && a.page_size % (2 << g.box_log) == 0;) ++g.box_log;
+    g.tile_pages = kKeysPerTile / a.page_size;
+    g.tile_rest = kKeysPerTile % a.page_size;
     char *p = static_cast<char *>(ws);
     g.records = reinterpret_cast<SplitRecord *>(p);
     p += align_up((size_t)ctas * sizeof(SplitRecord), 256);
@@ -1114,7 +1125,7 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     // the outer dimensions merge into one: the eight-row groups of all pages (a page is page_size rows long), or the heads of all
     // pages (a page is its heads long).
     auto kv_map = [&](CUtensorMap *m, TileLayout &tl, const void *base, long long ps, long long ts, long long hs) {
-        const cuuint32_t R = (cuuint32_t)g.box_rows;
+        const cuuint32_t R = 1u << g.box_log;
         tl.map = kByHalves;
         if (a.dim == 128 && (a.n_pages == 1 || ps == a.page_size * ts) && a.n_pages * (a.page_size / 8) <= 0x7FFFFFFFLL) tl.map = kGroupsOfAllPages;
         else if (a.dim == 128 && (a.n_pages == 1 || ps == a.hk * hs) && a.n_pages * a.hk <= 0x7FFFFFFFLL) tl.map = kHeadsOfAllPages;
