@@ -477,11 +477,11 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         ga.records[blockIdx.x] = r;
     }
 
-    // Registers: 384 threads x 168 at launch = 64512; afterwards 256 x 208 + 128 x 80 = 63488.  (Each role's instruction stands
+    // Registers: 384 threads x 168 at launch = 64512; afterwards 256 x 192 + 128 x 112 = 63488.  (Each role's instruction stands
     // in its own branch: the compiler takes the smaller number behind a join.)
     if (warp == 9 || warp == 10) {
         // ------------------------------------------------------------ loaders: Q and K tiles, V tiles
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
         fence_proxy_async();
         const bool is_v = warp == 10;
         const CUtensorMap *map = is_v ? &map_v : &map_k;
@@ -578,7 +578,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     } else if (warp == 8 || warp == 11) {
         // ------------------------------------------------------------ MMA issue, a warp for each worker: while one waits for its
         // worker or works through its barriers, the tensor core has the other's
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
         const int w = warp == 11;
         const uint32_t fmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
         const uint32_t base_desc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(kRowsPerTile >> 4) << 24);
@@ -715,7 +715,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         __syncwarp();
     } else {
         // ------------------------------------------------------------ workers: a thread per row
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         constexpr int kCols = MODE == kCopies ? 32 : PAIR ? kPairKeys : 128;   // keys of a step that a thread weighs
         const int w = warp >> 2, rloc = tid & 127, quarter = warp & 3;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
