@@ -6,7 +6,7 @@
 
 namespace fpsk {
 
-constexpr size_t kAttnSyncBytes = 256;         // synchronisation words at the start of a workspace
+constexpr size_t kAttnSyncBytes = 4096;        // synchronisation words at the start of a workspace
 
 __host__ __device__ __forceinline__ int elem_size(int type) { return type == FPSK_ELEM_FP32 ? 4 : 2; }
 

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(32 * kPlainWarps) attention_rows_kernel(const 
 
 using namespace fpsk;
 
-extern "C" size_t fpsk_paged_attention_workspace_bytes(void) { return kAttnSyncBytes + attention_tc_workspace_bytes(); }
+extern "C" size_t fpsk_paged_attention_workspace_bytes(void) { return attention_tc_workspace_bytes(); }
 
 extern "C" fpsk_status fpsk_paged_attention(const fpsk_paged_cache *cache, const fpsk_paged_batch *batch, const fpsk_attention *a,
                                             void *workspace, size_t ws_bytes, int32_t *d_status, void *stream)
@@ -119,7 +119,7 @@ extern "C" fpsk_status fpsk_paged_attention(const fpsk_paged_cache *cache, const
     g.status = d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (attention_tc_takes(g))
-        return attention_tc_launch(g, cache->type, a->max_q_len, static_cast<char *>(workspace) + kAttnSyncBytes, st);
+        return attention_tc_launch(g, cache->type, a->max_q_len, workspace, st);
     const dim3 grid((unsigned)g.n_tokens, (unsigned)g.hq);
     if (cache->type == FPSK_ELEM_FP16) attention_rows_kernel<__half><<<grid, 32 * kPlainWarps, 0, st>>>(g);
     else attention_rows_kernel<__nv_bfloat16><<<grid, 32 * kPlainWarps, 0, st>>>(g);

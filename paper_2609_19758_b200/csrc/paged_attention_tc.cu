@@ -8,7 +8,7 @@
 // tile of queries, as in decoding) or two (PAIR: prompts), and measured in tiles of 128 keys.  All items lie on one
 // axis, (sequence, key head, query tile) ordered, which is cut into equal ranges, one per CTA: every SM gets the same
 // number of key tiles whatever the lengths are.  An item that a cut divides leaves partial results (running maximum, sum and
-// output, FP32) that a second, small kernel joins; all others are finished where they are computed.
+// output, FP32); the CTA whose part is the last to arrive joins them.  All other items are finished where they are computed.
 // Two workers per CTA, a warpgroup each, a thread per row, with accumulators S and O of their own in TMEM.  In
 // a PAIR item they hold different query tiles and share every key tile; in a SPLIT item they hold the same queries and take
 // alternate key tiles, and meet at the item's end.  While one computes its softmax, the tensor cores work for the other.
@@ -35,6 +35,7 @@ constexpr int kTcaMaxSeqs = 16384;
 #define FPSK_POLY 0
 #endif
 constexpr int kPoly = FPSK_POLY;                 // of eight pairs of exponentials, computed on the FMA pipe
+constexpr int kItemCost = 2;                     // an item's beginning and end, in key tiles
 constexpr float kMostSum = 4096.f;               // of a step's weights, before a row's reference maximum is renewed
 
 // 32 consecutive columns of this thread's accumulator row; valid after tm_wait32 on the same array
@@ -205,6 +206,12 @@ __device__ __forceinline__ float max2(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
+// a whole 32-byte sector
+__device__ __forceinline__ void store8(void *p, const uint32_t (&v)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                 "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
 template <typename T> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, float hi)
 {
@@ -233,15 +240,10 @@ struct TcaArgs {
     int box_log;                       // keys of one TMA box, 2^box_log: the largest power of two that divides a page, at most 128
     int tile_pages, tile_rest;         // a tile further: so many pages and rows
     TileLayout kl, vl;
+    int wide_out;                      // rows of the output are whole 32-byte sectors
     float *part_o;                     // [2 slots per CTA][rows][DP]
     float2 *part_ml;                   // [2 slots per CTA][rows]: maximum (powers of two), sum
-    struct SplitRecord *records;       // [CTA]
-};
-// A divided item, written by its second CTA: what the joining kernel needs.
-struct SplitRecord {
-    int parts;                         // 0: none
-    int first_cta, token0, n_tok, kvh;
-    int pad[3];
+    unsigned int *arrived;             // [CTA]: parts that are there of the divided item that begins in this CTA (returns to 0)
 };
 
 struct Item {
@@ -249,6 +251,7 @@ struct Item {
     int p0, kv_len;                    // position of the first token
     int lo, hi;                        // keys that some token of the item may see
     int tile0, units;                  // first key tile, key tiles (at least 1: an item without keys writes its zeros)
+    // on the axis an item takes some places for its beginning and end (kItemCost) and one for every key tile
 };
 
 __device__ __forceinline__ void seq_lengths(const AttnArgs &g, int b, int &cu, int &q_len, int &kv_len)
@@ -293,6 +296,12 @@ __device__ __forceinline__ void worker_steps(const AttnArgs &g, const Item &it, 
 struct Walk {
     int b, kvh, qi, n_items;
     int cu, q_len, kv_len;
+    // the CTA's key tiles [a, b) of the item at hand: `in` places of it lie before the CTA's range, `left` places are left of that
+    __device__ __forceinline__ static void share(const Item &it, int cost, int in, int left, int &a, int &b)
+    {
+        a = max(0, in - cost);
+        b = min(it.units, max(0, in + left - cost));
+    }
     __device__ __forceinline__ void open(const AttnArgs &g, int item_tokens)
     {
         seq_lengths(g, b, cu, q_len, kv_len);
@@ -332,10 +341,75 @@ template <int DP, int MODE> struct Tca {
 struct TcaBars {                       // shared memory, after the tiles
     unsigned long long q_full, q_empty, done, s_full[4], p_ready[4], o_done[4], kv_full[8], kv_empty[8];
     uint32_t tmem;
-    int b, kvh, qi, u, left;
-    long long totals[kTcaThreads / 32];
+    int b, kvh, qi, in, left, last;
+    long long totals[kTcaThreads / 32], items[kTcaThreads / 32];
 };
 static_assert(sizeof(TcaBars) <= 1024, "barriers fit before the row statistics");
+
+// Joins the parts of a divided item.  Each of eight warps has up to 32 rows, a lane the statistics of one; the outputs come four
+// rows by four parts at a time, four channels per lane.
+template <typename T, int DP, int MODE>
+__device__ __noinline__ void join_parts(const TcaArgs &ga, const Item &it, int kvh, int first, int parts, int warp)
+{
+    constexpr int kRows = Tca<DP, MODE>::kRows;
+    const AttnArgs &g = ga.a;
+    const int lane = threadIdx.x & 31;
+    const int rows = it.n_tok * g.group, mine = (rows + 7) / 8, row0 = warp * mine;
+    const int i = min(row0 + lane, rows - 1), t = i / g.group, h = i - t * g.group, tile = t / ga.tile_tokens;
+    const int row = tile * Tca<DP, MODE>::kTileRows + (t - tile * ga.tile_tokens) * g.group + h;
+    // the first part lies in the second slot of its CTA, the others in the first of theirs
+    auto slot = [&](int part) { return (long long)(2 * (first + part) + (part == 0 ? 1 : 0)) * kRows; };
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&ga.part_ml[slot(p) + row].x));
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const float2 ml = __ldcg(ga.part_ml + slot(p) + row);
+        l = fmaf(ml.y, ex2(ml.x - base), l);
+    }
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    const long long out_at = (long long)(it.token0 + t) * g.ots + (long long)(kvh * g.group + h) * g.ohs;
+    if (g.lse && lane < mine && row0 + lane < rows)
+        g.lse[(long long)(it.token0 + t) * g.hq + kvh * g.group + h] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    for (int r0 = 0; r0 < mine && row0 + r0 < rows; r0 += 4) {
+        float4 acc[4];
+        int at[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            at[j] = __shfl_sync(0xFFFFFFFFu, row, (r0 + j) & 31);
+        }
+        for (int p0 = 0; p0 < parts; p0 += 4) {
+            float wt[4];
+            float4 o[4][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool there = p0 + k < parts;
+                const long long s0 = slot(there ? p0 + k : 0);
+                wt[k] = there ? ex2(__ldcg(&ga.part_ml[s0 + row].x) - base) * inv : 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[j][k] = there && lane * 4 < DP ? __ldcg(reinterpret_cast<const float4 *>(ga.part_o + (s0 + at[j]) * DP + lane * 4))
+                                                     : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = __shfl_sync(0xFFFFFFFFu, wt[k], (r0 + j) & 31);
+                    if (p0 + k < parts)
+                        acc[j] = make_float4(fmaf(o[j][k].x, x, acc[j].x), fmaf(o[j][k].y, x, acc[j].y), fmaf(o[j][k].z, x, acc[j].z), fmaf(o[j][k].w, x, acc[j].w));
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const long long to = __shfl_sync(0xFFFFFFFFu, out_at, (r0 + j) & 31);
+            if (r0 + j < mine && row0 + r0 + j < rows && lane * 4 < g.dim)
+                *reinterpret_cast<uint2 *>(static_cast<T *>(g.out) + to + lane * 4) = make_uint2(pack_pair<T>(acc[j].x, acc[j].y), pack_pair<T>(acc[j].z, acc[j].w));
+        }
+    }
+}
 
 template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(kTcaThreads, 1)
@@ -352,6 +426,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int tile_tokens = ga.tile_tokens, item_tokens = tile_tokens * Cfg::kQTiles;
 
+    if (tid >= 352 && tid < 355)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(tid == 352 ? &map_q : tid == 353 ? &map_k : &map_v) : "memory");
     if (tid == 0) {
         mbar_init(smem_u32(&sh->q_full), 1);
         mbar_init(smem_u32(&sh->q_empty), 2);
@@ -374,8 +450,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     }
 
     // ---- this CTA's range: key tiles of every sequence (in the ring, before it is used), their total, the first item
-    unsigned int *seq_units = reinterpret_cast<unsigned int *>(smem + Cfg::kQTiles * Cfg::kTile);
-    long long mine = 0;
+    uint2 *seq_work = reinterpret_cast<uint2 *>(smem + Cfg::kQTiles * Cfg::kTile);    // key tiles and items of one key head
+    long long mine = 0, mine_items = 0;
     for (int base = 0; base < g.n_seqs; base += kTcaThreads) {
         const int b = base + tid;
         int cu = 0, q_len = 0, kv_len = 0, n = 0;
@@ -395,25 +471,48 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             t = __reduce_add_sync(0xFFFFFFFFu, t);
             if (lane == src) units = t;
         }
-        if (b < g.n_seqs) seq_units[b] = units;
+        if (b < g.n_seqs) seq_work[b] = make_uint2(units, (unsigned int)n);
         mine += units;
+        mine_items += n;
     }
-    for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
-    if (lane == 0) sh->totals[warp] = mine;
+    if (warp * 32 < g.n_seqs) {
+        for (int o = 16; o; o >>= 1) {
+            mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+            mine_items += __shfl_xor_sync(0xFFFFFFFFu, mine_items, o);
+        }
+    }
+    if (lane == 0) { sh->totals[warp] = mine; sh->items[warp] = mine_items; }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh->tmem;
-    long long total = 0;
-    for (int w = 0; w < kTcaThreads / 32; ++w) total += sh->totals[w];
+    long long total = 0, items = 0;
+    for (int w = 0; w < kTcaThreads / 32 && w * 32 < g.n_seqs; ++w) {
+        total += sh->totals[w];
+        items += sh->items[w];
+    }
     total *= g.hk;
-    const long long per = (total + gridDim.x - 1) / gridDim.x, start = per * blockIdx.x;
+    items *= g.hk;
+    // A small call is cut finely, a key tile for each worker; else an item's beginning and end count as well.
+    const bool small = total <= 2 * gridDim.x;
+    const int item_cost = small ? 0 : kItemCost;
+    const bool narrow = total + items * kItemCost < 0x40000000LL;      // (divisions of 64 bits cost hundreds of cycles)
+    long long per;
+    if (small) {
+        per = (total <= gridDim.x ? 1 : 2) * (!PAIR && total <= gridDim.x && total >= 2 * items ? 2 : 1);
+    } else {
+        total += items * kItemCost;
+        per = narrow ? (long long)(((unsigned int)total + gridDim.x - 1) / gridDim.x) : (total + gridDim.x - 1) / gridDim.x;
+    }
+    const long long start = per * blockIdx.x;
     if (warp == 0) {
         if (lane == 0) sh->left = (int)(start < total ? (total - start < per ? total - start : per) : 0);
         long long before = 0;
         bool found = start >= total;
         for (int base = 0; base < g.n_seqs && !found; base += 32) {
-            const long long u = base + lane < g.n_seqs ? (long long)seq_units[base + lane] * g.hk : 0;
+            const uint2 sw = base + lane < g.n_seqs ? seq_work[base + lane] : make_uint2(0u, 0u);
+            const int head_places = (int)(sw.x + sw.y * item_cost);
+            const long long u = (long long)head_places * g.hk;
             long long incl = u;
             for (int o = 1; o < 32; o <<= 1) {
                 const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
@@ -423,36 +522,35 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             if (hit) {
                 const int src = __ffs(hit) - 1;
                 const long long rest = start - before - __shfl_sync(0xFFFFFFFFu, incl - u, src);
-                const int b = base + src, per_head = (int)seq_units[b];
-                const int kvh = (int)(rest / per_head);
-                int u_in = (int)(rest - (long long)kvh * per_head), qi = 0;
-                int cu, q_len, kv_len;
-                seq_lengths(g, b, cu, q_len, kv_len);
-                const int n = (q_len + item_tokens - 1) / item_tokens;
-                for (int i0 = 0; i0 < n; i0 += 32) {
-                    const int un = i0 + lane < n ? make_item(g, cu, q_len, kv_len, i0 + lane, item_tokens).units : 0;
-                    int in = un;
+                const int b = base + src, per_head = __shfl_sync(0xFFFFFFFFu, head_places, src), n = __shfl_sync(0xFFFFFFFFu, (int)sw.y, src);
+                const int kvh = narrow ? (int)((unsigned int)rest / (unsigned int)per_head) : (int)(rest / per_head);
+                int in = (int)(rest - (long long)kvh * per_head), qi = 0;
+                int cu = 0, q_len = 0, kv_len = 0;
+                if (n > 1) seq_lengths(g, b, cu, q_len, kv_len);
+                for (int i0 = 0; n > 1 && i0 < n; i0 += 32) {
+                    const int un = i0 + lane < n ? make_item(g, cu, q_len, kv_len, i0 + lane, item_tokens).units + item_cost : 0;
+                    int sum = un;
                     for (int o = 1; o < 32; o <<= 1) {
-                        const int x = __shfl_up_sync(0xFFFFFFFFu, in, o);
-                        if (lane >= o) in += x;
+                        const int x = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                        if (lane >= o) sum += x;
                     }
-                    const unsigned int at = __ballot_sync(0xFFFFFFFFu, in > u_in);
+                    const unsigned int at = __ballot_sync(0xFFFFFFFFu, sum > in);
                     if (at) {
                         const int s2 = __ffs(at) - 1;
                         qi = i0 + s2;
-                        u_in -= __shfl_sync(0xFFFFFFFFu, in - un, s2);
+                        in -= __shfl_sync(0xFFFFFFFFu, sum - un, s2);
                         break;
                     }
-                    u_in -= __shfl_sync(0xFFFFFFFFu, in, 31);
+                    in -= __shfl_sync(0xFFFFFFFFu, sum, 31);
                 }
-                if (lane == 0) { sh->b = b; sh->kvh = kvh; sh->qi = qi; sh->u = u_in; }
+                if (lane == 0) { sh->b = b; sh->kvh = kvh; sh->qi = qi; sh->in = in; }
                 found = true;
             }
             before += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
     }
     __syncthreads();
-    int left = sh->left, u = sh->u;
+    int left = sh->left, in = sh->in;
     Walk walk;
     walk.b = sh->b; walk.kvh = sh->kvh; walk.qi = sh->qi;
     if (left > 0) walk.open(g, item_tokens);
@@ -461,21 +559,6 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         if (ok && !bar_wait_inline(bar, parity)) ok = false;
         __syncwarp();                  // the tcgen05 instructions behind it want the warp together
     };
-
-    if (tid == 0) {
-        // the record of a divided item: written by the CTA behind its first
-        SplitRecord r = {};
-        if (left > 0 && u > 0) {
-            const long long item0 = start - u;
-            if (item0 >= start - per) {
-                const Item it = make_item(g, walk.cu, walk.q_len, walk.kv_len, walk.qi, item_tokens);
-                r.first_cta = blockIdx.x - 1;
-                r.parts = (int)((item0 + it.units - 1) / per) - r.first_cta + 1;
-                r.token0 = it.token0; r.n_tok = it.n_tok; r.kvh = walk.kvh;
-            }
-        }
-        ga.records[blockIdx.x] = r;
-    }
 
     // Registers: 384 threads x 168 at launch = 64512; afterwards 256 x 192 + 128 x 112 = 63488.  (Each role's instruction stands
     // in its own branch: the compiler takes the smaller number behind a join.)
@@ -490,17 +573,20 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         const int halves = tl.map == kByHalves ? Cfg::kHalves : 1;
         const uint32_t box_bytes = (uint32_t)(R * 128 * Cfg::kHalves) / halves;
         left = uniform(left);
-        u = uniform(u);
+        in = uniform(in);
         int seq = 0;                                                   // tiles of K and V that went before this item
         int last = -1;                                                 // this warp's last one
         uint32_t q_phase = 0;
         bool q_used = false;
         while (left > 0) {
             const Item it = make_item(g, walk.cu, walk.q_len, walk.kv_len, walk.qi, item_tokens);
-            const int lo = uniform(it.lo), hi = uniform(it.hi), n = min(left, uniform(it.units) - u);
-            if (hi > lo) {
-                const int kvh = uniform(walk.kvh), tile_a = uniform(it.tile0) + u;
-                if (!is_v) {
+            int ua, ub;
+            Walk::share(it, item_cost, in, left, ua, ub);
+            ua = uniform(ua);
+            const int lo = uniform(it.lo), hi = uniform(it.hi), n = uniform(ub) - ua;
+            if (hi > lo && n > 0) {
+                const int kvh = uniform(walk.kvh), tile_a = uniform(it.tile0) + ua;
+                if (is_v) {                                            // (K tiles may come before the last item is through with its Q)
                     const int token0 = uniform(it.token0);
                     wait(smem_u32(&sh->q_empty), q_phase ^ 1u);
                     ok = __all_sync(0xFFFFFFFFu, ok);
@@ -567,8 +653,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 }
                 if (ok) seq += 2 * n;
             }
-            left -= n;
-            u = 0;
+            left -= uniform(it.units) + item_cost - in;
+            in = 0;
             if (left > 0) walk.next(g, item_tokens);
         }
         // The last fill of every slot: in flight still only if the MMA warp's waits gave up.
@@ -588,7 +674,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         const uint32_t tm = (uint32_t)uniform((int)tmem);
         const uint32_t q_hi = desc_hi(1024), k_hi = desc_hi(ga.kl.group_bytes), v_hi = desc_hi(ga.vl.group_bytes);
         left = uniform(left);
-        u = uniform(u);
+        in = uniform(in);
         int seq = 0;                                                   // tiles of K and V that went before this item
         uint32_t q_phase = 0, s_count = 0, o_count = 0;                // steps issued so far
         auto all_wait = [&](uint32_t bar, uint32_t parity) {
@@ -631,9 +717,12 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         };
         while (left > 0) {
             const Item it = make_item(g, walk.cu, walk.q_len, walk.kv_len, walk.qi, item_tokens);
-            const int lo = uniform(it.lo), hi = uniform(it.hi), n = min(left, uniform(it.units) - u);
-            if (hi > lo) {
-                const int tile_a = uniform(it.tile0) + u, tile_b = tile_a + n;
+            int ua, ub;
+            Walk::share(it, item_cost, in, left, ua, ub);
+            ua = uniform(ua);
+            const int lo = uniform(it.lo), hi = uniform(it.hi), n = uniform(ub) - ua;
+            if (hi > lo && n > 0) {
+                const int tile_a = uniform(it.tile0) + ua, tile_b = tile_a + n;
                 // rows of a V tile that no token of the item may see: zeros, for 0 * (what lies there) must not be NaN (in a PAIR
                 // item both warps write them, each before its own MMAs)
                 auto clean_v = [&](int tile, uint32_t v_addr) {
@@ -705,8 +794,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 }
                 release(&sh->q_empty);
             }
-            left -= n;
-            u = 0;
+            left -= uniform(it.units) + item_cost - in;
+            in = 0;
             if (left > 0) walk.next(g, item_tokens);
         }
         if (elect_one()) tc_commit(smem_u32(&sh->done));
@@ -725,11 +814,15 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         const int col0 = MODE == kCopies ? quarter * 32 : 0;
         const float sl2 = g.scale_log2;
         uint32_t count = 0;                                            // steps so far
+        long long pos = start - in;                                    // the item's place on the axis
         // the barrier (of its four) and the parity of step c
         auto step_bar = [&](unsigned long long *bars, uint32_t c) { return smem_u32(&bars[w + 2 * (c & 1u)]); };
         while (left > 0) {
             const Item it = make_item(g, walk.cu, walk.q_len, walk.kv_len, walk.qi, item_tokens);
-            const int n = min(left, it.units - u);
+            int ua, ub;
+            Walk::share(it, item_cost, in, left, ua, ub);
+            const int n = ub - ua;
+            if (n > 0) {
             const int t_in_item = (PAIR ? w * tile_tokens : 0) + tok_in_tile;
             const bool valid = tok_in_tile < tile_tokens && t_in_item < it.n_tok;
             const bool warp_on = __any_sync(0xFFFFFFFFu, valid);
@@ -737,7 +830,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             if (valid) key_range(g, it.p0 + t_in_item, it.kv_len, lo, hi);
             int ta = 0, tb = 0, step = 1;
             if (it.hi > it.lo) {
-                const int tile_a = it.tile0 + u, tile_b = tile_a + n;
+                const int tile_a = it.tile0 + ua, tile_b = tile_a + n;
                 if constexpr (PAIR) worker_steps(g, it, w, tile_tokens, 2 * tile_a, 2 * tile_b, ta, tb);
                 else { ta = tile_a + w; tb = tile_b; step = 2; }
             }
@@ -863,7 +956,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             }
             if (m == -INFINITY) l = 0.f;                               // (hidden scores may have left 2^-126)
             // ---- the item's end: finished here, or a partial result
-            const bool whole = u == 0 && n == it.units;
+            const bool whole = n == it.units;
             const bool any = it.hi > it.lo, have1 = any && n > 1;     // SPLIT: outputs of the two workers
             float wt0 = 1.f, wt1 = 0.f;                               // and their weights
             if constexpr (!PAIR) {
@@ -889,7 +982,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 }
             }
             const bool have0 = PAIR ? have_o : any;
-            const int pslot = 2 * blockIdx.x + (u == 0 ? 1 : 0);
+            const int pslot = 2 * blockIdx.x + (ua == 0 ? 1 : 0);        // divided: the part of the CTA where the item begins, or a later one
             // 32 channels of this row: the worker's own (PAIR) or both workers'
             auto outputs = [&](int c, float (&o)[32]) {
 #pragma unroll
@@ -963,6 +1056,15 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                     float o[32];
                     outputs(c, o);
                     if (!valid) {
+                    } else if (whole && ga.wide_out) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 16)
+                            if (c * 32 + i < g.dim) {
+                                uint32_t x[8];
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) x[k] = pack_pair<T>(o[i + 2 * k] * inv, o[i + 2 * k + 1] * inv);
+                                store8(dst + c * 32 + i, x);
+                            }
                     } else if (whole) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
@@ -972,16 +1074,39 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                                                pack_pair<T>(o[i + 4] * inv, o[i + 5] * inv), pack_pair<T>(o[i + 6] * inv, o[i + 7] * inv));
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<float4 *>(pdst + c * 32 + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t x[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) x[k] = __float_as_uint(o[i + k]);
+                            store8(pdst + c * 32 + i, x);
+                        }
                     }
                     __syncwarp();
                 }
             }
             tc_fence_before();
             if constexpr (MODE == kSplit) named_bar_sync(2, 256);
-            left -= n;
-            u = 0;
+            if (!whole) {
+                // The parts are joined by the CTA whose part is the last to arrive, in the order of the parts.
+                auto cta_of = [&](long long at) { return narrow ? (int)((unsigned int)at / (unsigned int)per) : (int)(at / per); };
+                const int first = cta_of(pos + item_cost), parts = cta_of(pos + item_cost + it.units - 1) - first + 1;
+                __threadfence();
+                named_bar_sync(4, 256);
+                if (tid == 0) {
+                    const bool last = atomicAdd(ga.arrived + first, 1u) == (unsigned int)(parts - 1);
+                    if (last) ga.arrived[first] = 0u;
+                    sh->last = last;
+                }
+                named_bar_sync(4, 256);
+                if (sh->last) {
+                    __threadfence();
+                    join_parts<T, DP, MODE>(ga, it, walk.kvh, first, parts, warp);
+                }
+            }
+            }
+            pos += it.units + item_cost;
+            left -= it.units + item_cost - in;
+            in = 0;
             if (left > 0) walk.next(g, item_tokens);
         }
     }
@@ -989,53 +1114,6 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     if (warp == 8) tc_dealloc(tmem, 512);
-}
-
-// Joins the parts of the divided items: a warp per row, four channels per lane.
-template <typename T, int DP, int MODE>
-__global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcaArgs ga)
-{
-    constexpr int kRows = Tca<DP, MODE>::kRows;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const AttnArgs &g = ga.a;
-    const SplitRecord r = ga.records[blockIdx.x];
-    if (r.parts == 0) return;
-    const int lane = threadIdx.x & 31;
-    for (int i = blockIdx.y * 8 + (threadIdx.x >> 5); i < r.n_tok * g.group; i += gridDim.y * 8) {
-        const int t = i / g.group, h = i - t * g.group, w = t / ga.tile_tokens;
-        const int row = w * 128 + (t - w * ga.tile_tokens) * g.group + h;
-        auto at = [&](int part) { return (long long)(2 * (r.first_cta + part) + (part == 0 ? 1 : 0)) * kRows + row; };
-        float m = -INFINITY;
-        for (int p = lane; p < r.parts; p += 32) m = fmaxf(m, ga.part_ml[at(p)].x);
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int p0 = 0; p0 < r.parts; p0 += 32) {
-            float wt = 0.f, lp = 0.f;
-            if (p0 + lane < r.parts) {
-                const float2 ml = ga.part_ml[at(p0 + lane)];
-                wt = ex2(ml.x - base);
-                lp = ml.y * wt;
-            }
-            for (int o = 16; o; o >>= 1) lp += __shfl_xor_sync(0xFFFFFFFFu, lp, o);
-            l += lp;
-            const int np = min(32, r.parts - p0);
-            for (int p = 0; p < np; ++p) {
-                const float x = __shfl_sync(0xFFFFFFFFu, wt, p);
-                if (lane * 4 < DP) {
-                    const float4 o = *reinterpret_cast<const float4 *>(ga.part_o + at(p0 + p) * DP + lane * 4);
-                    acc = make_float4(fmaf(o.x, x, acc.x), fmaf(o.y, x, acc.y), fmaf(o.z, x, acc.z), fmaf(o.w, x, acc.w));
-                }
-            }
-        }
-        const float inv = l != 0.f ? 1.f / l : 0.f;
-        const long long head = r.kvh * g.group + h, tok = r.token0 + t;
-        if (lane * 4 < g.dim)
-            *reinterpret_cast<uint2 *>(static_cast<T *>(g.out) + tok * g.ots + head * g.ohs + lane * 4) =
-                make_uint2(pack_pair<T>(acc.x * inv, acc.y * inv), pack_pair<T>(acc.z * inv, acc.w * inv));
-        if (g.lse && lane == 0) g.lse[tok * g.hq + head] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-    }
 }
 
 // ---------------------------------------------------------------- host side
@@ -1079,7 +1157,7 @@ constexpr int kMaxPartRows = 2 * kRowsPerTile, kMaxDP = 128;
 size_t attention_tc_workspace_bytes()
 {
     const size_t ctas = (size_t)sm_count();
-    return align_up(ctas * sizeof(SplitRecord), 256) + 2 * ctas * kMaxPartRows * (kMaxDP * sizeof(float) + sizeof(float2));
+    return kAttnSyncBytes + 2 * ctas * kMaxPartRows * (kMaxDP * sizeof(float) + sizeof(float2));
 }
 
 static bool aligned16(const void *p, long long s0, long long s1, long long s2)
@@ -1100,15 +1178,17 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     constexpr bool PAIR = MODE == kPair;
     const int ctas = sm_count();
     if (ctas < 1) return FPSK_ERR_CUDA;
+    if (ctas > (int)(kAttnSyncBytes / sizeof(unsigned int))) return FPSK_ERR_PARAM;
     TcaArgs g;
     g.a = a;
     g.tile_tokens = Cfg::kTileRows / a.group;
     for (g.box_log = 3; g.box_log < 7 && a.page_size % (2 << g.box_log) == 0;) ++g.box_log;
+    g.wide_out = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.ots % 16 == 0 && a.ohs % 16 == 0 && a.dim % 16 == 0;
     g.tile_pages = kKeysPerTile / a.page_size;
     g.tile_rest = kKeysPerTile % a.page_size;
     char *p = static_cast<char *>(ws);
-    g.records = reinterpret_cast<SplitRecord *>(p);
-    p += align_up((size_t)ctas * sizeof(SplitRecord), 256);
+    g.arrived = reinterpret_cast<unsigned int *>(p);
+    p += kAttnSyncBytes;
     g.part_o = reinterpret_cast<float *>(p);
     p += (size_t)2 * ctas * kMaxPartRows * kMaxDP * sizeof(float);
     g.part_ml = reinterpret_cast<float2 *>(p);
@@ -1157,18 +1237,6 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
         prepared.fetch_or(bit, std::memory_order_release);
     }
     attention_tc_kernel<T, DP, MODE><<<ctas, kTcaThreads, Cfg::kSmem, st>>>(g, mq, mk, mv);
-    FPSK_LAUNCH_CHECK();
-    // the join's launch overlaps the end of the kernel before it
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas, PAIR ? 8 : 4);
-    cfg.blockDim = dim3(256);
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_join_kernel<T, DP, MODE>, g));
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
