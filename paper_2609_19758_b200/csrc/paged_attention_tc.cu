@@ -8,7 +8,7 @@
 // tile of queries, as in decoding) or two (PAIR: prompts), and measured in tiles of 128 keys.  All items lie on one
 // axis, (sequence, key head, query tile) ordered, which is cut into equal ranges, one per CTA: every SM gets the same
 // number of key tiles whatever the lengths are.  An item that a cut divides leaves partial results (running maximum, sum and
-// output, FP32); the CTA whose part is the last to arrive joins them.  All other items are finished where they are computed.
+// output, FP32), joined in the order of the parts; all others are finished where they are computed.
 // Two workers per CTA, a warpgroup each, a thread per row, with accumulators S and O of their own in TMEM.  In
 // a PAIR item they hold different query tiles and share every key tile; in a SPLIT item they hold the same queries and take
 // alternate key tiles, and meet at the item's end.  While one computes its softmax, the tensor cores work for the other.
@@ -244,6 +244,13 @@ struct TcaArgs {
     float *part_o;                     // [2 slots per CTA][rows][DP]
     float2 *part_ml;                   // [2 slots per CTA][rows]: maximum (powers of two), sum
     unsigned int *arrived;             // [CTA]: parts that are there of the divided item that begins in this CTA (returns to 0)
+    struct SplitRecord *records;       // [CTA]
+};
+// A divided item of more than 32 rows, written by its second CTA: what the joining kernel needs.
+struct SplitRecord {
+    int parts;                         // 0: none
+    int first, token0, rows, kvh;
+    int pad[3];
 };
 
 struct Item {
@@ -346,69 +353,34 @@ struct TcaBars {                       // shared memory, after the tiles
 };
 static_assert(sizeof(TcaBars) <= 1024, "barriers fit before the row statistics");
 
-// Joins the parts of a divided item.  Each of eight warps has up to 32 rows, a lane the statistics of one; the outputs come four
-// rows by four parts at a time, four channels per lane.
+// Joins the parts of one row of a divided item: a warp, four channels per lane, four parts in flight.  Little code, because it runs
+// once in a launch, straight from L2.
 template <typename T, int DP, int MODE>
-__device__ __noinline__ void join_parts(const TcaArgs &ga, const Item &it, int kvh, int first, int parts, int warp)
+__device__ __forceinline__ void join_row(const TcaArgs &ga, int first, int parts, int token0, int kvh, int i)
 {
-    constexpr int kRows = Tca<DP, MODE>::kRows;
+    constexpr int kRows = Tca<DP, MODE>::kRows, kTileRows = Tca<DP, MODE>::kTileRows;
     const AttnArgs &g = ga.a;
-    const int lane = threadIdx.x & 31;
-    const int rows = it.n_tok * g.group, mine = (rows + 7) / 8, row0 = warp * mine;
-    const int i = min(row0 + lane, rows - 1), t = i / g.group, h = i - t * g.group, tile = t / ga.tile_tokens;
-    const int row = tile * Tca<DP, MODE>::kTileRows + (t - tile * ga.tile_tokens) * g.group + h;
-    // the first part lies in the second slot of its CTA, the others in the first of theirs
-    auto slot = [&](int part) { return (long long)(2 * (first + part) + (part == 0 ? 1 : 0)) * kRows; };
+    const int lane = threadIdx.x & 31, t = i / g.group, h = i - t * g.group, tile = MODE == kPair && t >= ga.tile_tokens;
+    const int row = tile * kTileRows + i - tile * ga.tile_tokens * g.group;
     float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&ga.part_ml[slot(p) + row].x));
-    const float base = m == -INFINITY ? 0.f : m;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int p = 0; p < parts; ++p) {
-        const float2 ml = __ldcg(ga.part_ml + slot(p) + row);
-        l = fmaf(ml.y, ex2(ml.x - base), l);
+        // the first part lies in the second slot of its CTA, the others in the first of theirs
+        const long long at = (long long)(2 * (first + p) + (p == 0 ? 1 : 0)) * kRows + row;
+        const float2 ml = __ldcg(ga.part_ml + at);
+        const float4 o = lane * 4 < DP ? __ldcg(reinterpret_cast<const float4 *>(ga.part_o + at * DP) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float m2 = fmaxf(m, ml.x), base = m2 == -INFINITY ? 0.f : m2, x = ex2(m - base), y = ex2(ml.x - base);
+        m = m2;
+        l = fmaf(l, x, ml.y * y);
+        acc = make_float4(fmaf(acc.x, x, o.x * y), fmaf(acc.y, x, o.y * y), fmaf(acc.z, x, o.z * y), fmaf(acc.w, x, o.w * y));
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;
-    const long long out_at = (long long)(it.token0 + t) * g.ots + (long long)(kvh * g.group + h) * g.ohs;
-    if (g.lse && lane < mine && row0 + lane < rows)
-        g.lse[(long long)(it.token0 + t) * g.hq + kvh * g.group + h] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-    for (int r0 = 0; r0 < mine && row0 + r0 < rows; r0 += 4) {
-        float4 acc[4];
-        int at[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-            at[j] = __shfl_sync(0xFFFFFFFFu, row, (r0 + j) & 31);
-        }
-        for (int p0 = 0; p0 < parts; p0 += 4) {
-            float wt[4];
-            float4 o[4][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool there = p0 + k < parts;
-                const long long s0 = slot(there ? p0 + k : 0);
-                wt[k] = there ? ex2(__ldcg(&ga.part_ml[s0 + row].x) - base) * inv : 0.f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    o[j][k] = there && lane * 4 < DP ? __ldcg(reinterpret_cast<const float4 *>(ga.part_o + (s0 + at[j]) * DP + lane * 4))
-                                                     : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float x = __shfl_sync(0xFFFFFFFFu, wt[k], (r0 + j) & 31);
-                    if (p0 + k < parts)
-                        acc[j] = make_float4(fmaf(o[j][k].x, x, acc[j].x), fmaf(o[j][k].y, x, acc[j].y), fmaf(o[j][k].z, x, acc[j].z), fmaf(o[j][k].w, x, acc[j].w));
-                }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long to = __shfl_sync(0xFFFFFFFFu, out_at, (r0 + j) & 31);
-            if (r0 + j < mine && row0 + r0 + j < rows && lane * 4 < g.dim)
-                *reinterpret_cast<uint2 *>(static_cast<T *>(g.out) + to + lane * 4) = make_uint2(pack_pair<T>(acc[j].x, acc[j].y), pack_pair<T>(acc[j].z, acc[j].w));
-        }
-    }
+    const long long tok = token0 + t, head = kvh * g.group + h;
+    if (lane * 4 < g.dim)
+        *reinterpret_cast<uint2 *>(static_cast<T *>(g.out) + tok * g.ots + head * g.ohs + lane * 4) =
+            make_uint2(pack_pair<T>(acc.x * inv, acc.y * inv), pack_pair<T>(acc.z * inv, acc.w * inv));
+    if (g.lse && lane == 0) g.lse[tok * g.hq + head] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int DP, int MODE>
@@ -426,6 +398,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int tile_tokens = ga.tile_tokens, item_tokens = tile_tokens * Cfg::kQTiles;
 
+    if (MODE != kCopies && tid == 351) ga.records[blockIdx.x].parts = 0;
     if (tid >= 352 && tid < 355)
         asm volatile("prefetch.tensormap [%0];" ::"l"(tid == 352 ? &map_q : tid == 353 ? &map_k : &map_v) : "memory");
     if (tid == 0) {
@@ -562,6 +535,14 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
 
     // Registers: 384 threads x 168 at launch = 64512; afterwards 256 x 192 + 128 x 112 = 63488.  (Each role's instruction stands
     // in its own branch: the compiler takes the smaller number behind a join.)
+    auto load_q = [&](int kvh, int token0) {
+        constexpr int kLoads = MODE == kCopies ? 4 : Cfg::kQTiles;
+        mbar_expect_tx(smem_u32(&sh->q_full), (uint32_t)(kLoads * Cfg::kHalves * tile_tokens * g.group * 128));
+        for (int w = 0; w < kLoads; ++w)
+            for (int h = 0; h < Cfg::kHalves; ++h)
+                tma_load_3d(q_smem + (PAIR ? w * Cfg::kTile : w * 32 * 128) + h * kHalfBytes, &map_q, h * 64, kvh * g.group,
+                            token0 + (PAIR ? w * tile_tokens : 0), smem_u32(&sh->q_full));
+    };
     if (warp == 9 || warp == 10) {
         // ------------------------------------------------------------ loaders: Q and K tiles, V tiles
         asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
@@ -586,17 +567,12 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             const int lo = uniform(it.lo), hi = uniform(it.hi), n = uniform(ub) - ua;
             if (hi > lo && n > 0) {
                 const int kvh = uniform(walk.kvh), tile_a = uniform(it.tile0) + ua;
+                const int token0 = uniform(it.token0);
                 if (is_v) {                                            // (K tiles may come before the last item is through with its Q)
-                    const int token0 = uniform(it.token0);
-                    wait(smem_u32(&sh->q_empty), q_phase ^ 1u);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (ok && elect_one()) {
-                        constexpr int kLoads = MODE == kCopies ? 4 : Cfg::kQTiles;
-                        mbar_expect_tx(smem_u32(&sh->q_full), (uint32_t)(kLoads * Cfg::kHalves * tile_tokens * g.group * 128));
-                        for (int w = 0; w < kLoads; ++w)
-                            for (int h = 0; h < Cfg::kHalves; ++h)
-                                tma_load_3d(q_smem + (PAIR ? w * Cfg::kTile : w * 32 * 128) + h * kHalfBytes, &map_q, h * 64, kvh * g.group,
-                                            token0 + (PAIR ? w * tile_tokens : 0), smem_u32(&sh->q_full));
+                    if (q_used) {
+                        wait(smem_u32(&sh->q_empty), q_phase ^ 1u);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (ok && elect_one()) load_q(kvh, token0);
                     }
                     q_phase ^= 1u;
                     q_used = true;
@@ -677,6 +653,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         in = uniform(in);
         int seq = 0;                                                   // tiles of K and V that went before this item
         uint32_t q_phase = 0, s_count = 0, o_count = 0;                // steps issued so far
+        bool first_item = true;
         auto all_wait = [&](uint32_t bar, uint32_t parity) {
             wait(bar, parity);
             ok = __all_sync(0xFFFFFFFFu, ok);
@@ -736,6 +713,13 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                     fence_proxy_async();
                     __syncwarp();
                 };
+                if (w == 1 && first_item) {                            // (the loader of V, which brings the others, has V to bring)
+                    fence_proxy_async();
+                    const int kvh = uniform(walk.kvh), token0 = uniform(it.token0);
+                    if (ok && elect_one()) load_q(kvh, token0);
+                    __syncwarp();
+                }
+                first_item = false;
                 all_wait(smem_u32(&sh->q_full), q_phase);
                 q_phase ^= 1u;
                 if constexpr (PAIR) {
@@ -1014,7 +998,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 const int rows = it.n_tok * g.group;
                 for (int r0 = 0; r0 < rows; r0 += 8) {
                     const bool mine = row >= r0 && row < r0 + 8 && valid;
-#pragma unroll
+#pragma unroll 1
                     for (int cc = 0; cc < DP / 64; ++cc) {
                         const int c = w * (DP / 64) + cc;             // each worker brings one half of the channels
                         float o[32];
@@ -1050,7 +1034,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             } else if (warp_on) {
                 T *dst = static_cast<T *>(g.out) + (long long)(it.token0 + t_in_item) * g.ots + (walk.kvh * g.group + head_in_group) * g.ohs;
                 float *pdst = ga.part_o + ((long long)pslot * Cfg::kRows + (PAIR ? w * 128 : 0) + row) * DP;
-#pragma unroll
+#pragma unroll 1
                 for (int cc = 0; cc < (PAIR ? DP / 32 : DP / 64); ++cc) {
                     const int c = PAIR ? cc : w * (DP / 64) + cc;     // SPLIT: each worker brings one half of the channels
                     float o[32];
@@ -1087,20 +1071,22 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             tc_fence_before();
             if constexpr (MODE == kSplit) named_bar_sync(2, 256);
             if (!whole) {
-                // The parts are joined by the CTA whose part is the last to arrive, in the order of the parts.
+                // COPIES: joined by the CTA whose part is the last to arrive, in the order of the parts.  Else by the kernel behind.
                 auto cta_of = [&](long long at) { return narrow ? (int)((unsigned int)at / (unsigned int)per) : (int)(at / per); };
                 const int first = cta_of(pos + item_cost), parts = cta_of(pos + item_cost + it.units - 1) - first + 1;
-                __threadfence();
+                if constexpr (MODE == kCopies) {
                 named_bar_sync(4, 256);
                 if (tid == 0) {
-                    const bool last = atomicAdd(ga.arrived + first, 1u) == (unsigned int)(parts - 1);
+                    const bool last = atom_acq_rel_add(ga.arrived + first) == (unsigned int)(parts - 1);
                     if (last) ga.arrived[first] = 0u;
                     sh->last = last;
                 }
                 named_bar_sync(4, 256);
-                if (sh->last) {
-                    __threadfence();
-                    join_parts<T, DP, MODE>(ga, it, walk.kvh, first, parts, warp);
+                if (sh->last)
+                    for (int i = warp; i < it.n_tok * g.group; i += 8) join_row<T, DP, MODE>(ga, first, parts, it.token0, walk.kvh, i);
+                } else if (tid == 0 && blockIdx.x == first + 1) {
+                    const SplitRecord r = {parts, first, it.token0, it.n_tok * g.group, walk.kvh, {0, 0, 0}};
+                    ga.records[blockIdx.x] = r;
                 }
             }
             }
@@ -1114,6 +1100,16 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     if (warp == 8) tc_dealloc(tmem, 512);
+}
+
+// A block for eight rows of a divided item.
+template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ TcaArgs ga)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const SplitRecord *r = ga.records + blockIdx.x;
+    const int i = blockIdx.y * 8 + (threadIdx.x >> 5), parts = __ldcg(&r->parts);
+    if (parts == 0 || i >= __ldcg(&r->rows)) return;
+    join_row<T, DP, MODE>(ga, __ldcg(&r->first), parts, __ldcg(&r->token0), __ldcg(&r->kvh), i);
 }
 
 // ---------------------------------------------------------------- host side
@@ -1157,7 +1153,7 @@ constexpr int kMaxPartRows = 2 * kRowsPerTile, kMaxDP = 128;
 size_t attention_tc_workspace_bytes()
 {
     const size_t ctas = (size_t)sm_count();
-    return kAttnSyncBytes + 2 * ctas * kMaxPartRows * (kMaxDP * sizeof(float) + sizeof(float2));
+    return kAttnSyncBytes + align_up(ctas * sizeof(SplitRecord), 256) + 2 * ctas * kMaxPartRows * (kMaxDP * sizeof(float) + sizeof(float2));
 }
 
 static bool aligned16(const void *p, long long s0, long long s1, long long s2)
@@ -1189,6 +1185,8 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     char *p = static_cast<char *>(ws);
     g.arrived = reinterpret_cast<unsigned int *>(p);
     p += kAttnSyncBytes;
+    g.records = reinterpret_cast<SplitRecord *>(p);
+    p += align_up((size_t)ctas * sizeof(SplitRecord), 256);
     g.part_o = reinterpret_cast<float *>(p);
     p += (size_t)2 * ctas * kMaxPartRows * kMaxDP * sizeof(float);
     g.part_ml = reinterpret_cast<float2 *>(p);
@@ -1238,6 +1236,20 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     }
     attention_tc_kernel<T, DP, MODE><<<ctas, kTcaThreads, Cfg::kSmem, st>>>(g, mq, mk, mv);
     FPSK_LAUNCH_CHECK();
+    if constexpr (MODE != kCopies) {
+        // the join's launch overlaps the end of the kernel before it
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)ctas, Cfg::kRows / 8);
+        cfg.blockDim = dim3(256);
+        cfg.stream = st;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_join_kernel<T, DP, MODE>, g));
+        FPSK_LAUNCH_CHECK();
+    }
     return FPSK_OK;
 }
 
