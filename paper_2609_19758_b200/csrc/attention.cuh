@@ -60,11 +60,11 @@ template <typename T> __device__ __forceinline__ void store4(T *p, float4 x, boo
     p[0] = a; p[1] = b; p[2] = c; p[3] = d;
 }
 // four weights of a run-time type (they are read once per thread)
-__device__ __forceinline__ float4 load4_any(const void *p, int type, int at)
+__device__ __forceinline__ float4 load4_any(const void *p, int type, int at, bool wide)
 {
-    if (type == FPSK_ELEM_FP32) return load4(static_cast<const float *>(p) + at, false);
-    if (type == FPSK_ELEM_FP16) return load4(static_cast<const __half *>(p) + at, false);
-    return load4(static_cast<const __nv_bfloat16 *>(p) + at, false);
+    if (type == FPSK_ELEM_FP32) return load4(static_cast<const float *>(p) + at, wide);
+    if (type == FPSK_ELEM_FP16) return load4(static_cast<const __half *>(p) + at, wide);
+    return load4(static_cast<const __nv_bfloat16 *>(p) + at, wide);
 }
 
 __device__ __forceinline__ void report_status(int32_t *d_status, int code)

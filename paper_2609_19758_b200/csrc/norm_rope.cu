@@ -9,6 +9,7 @@
 // i + rot/2, or eight neighbours when pairs are interleaved), so that the rotation needs no exchange.  The channels
 // behind rot_dim are paired the same way, (i, i + (D - rot)/2), and not rotated, which keeps one mapping for all.
 #include "attention.cuh"
+#include "stream_pipe.cuh"
 
 #include <mutex>
 
@@ -20,7 +21,7 @@ struct HeadsArg {
     const void *w;
     long long its, ihs, ots, ohs;      // strides of tokens and heads, input and output
     int n, wtype;
-    int wide_in, wide_out;
+    int wide_in, wide_out, wide_w;
 };
 
 struct PlaceArg {                      // where the new tokens' keys and values go
@@ -112,7 +113,8 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
     const int lane = threadIdx.x % L, slot = threadIdx.x / L;
     const LaneMap m(lane, g.dim, g.rot, g.interleaved);
     const long long v0 = (long long)blockIdx.x * (S * HPT);
-    const long long t0 = v0 / g.n_all;
+    // (a 64-bit division takes longer than a head)
+    const long long t0 = v0 < 0x7FFFFFFFLL ? (long long)((unsigned int)v0 / (unsigned int)g.n_all) : v0 / g.n_all;
     const int rem0 = (int)(v0 - t0 * g.n_all);
 
     int kind[HPT], head[HPT];
@@ -135,6 +137,17 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
             const X *p = static_cast<const X *>(H.in) + tok[i] * H.its + h * H.ihs;
             a[i] = load4(p + m.ia, H.wide_in);
             b[i] = load4(p + m.ib, H.wide_in);
+        }
+    }
+
+    // the weights of queries and of keys, once per thread
+    float4 wa[2], wb[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        wa[k] = wb[k] = splat4(1.f);
+        if (g.h[k].w && m.on) {
+            wa[k] = load4_any(g.h[k].w, g.h[k].wtype, m.ia, g.h[k].wide_w);
+            wb[k] = load4_any(g.h[k].w, g.h[k].wtype, m.ib, g.h[k].wide_w);
         }
     }
 
@@ -170,14 +183,15 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
             c = load4(g.cos + pos * (g.rot / 2) + m.cs, g.wide_tab);
             s = load4(g.sin + pos * (g.rot / 2) + m.cs, g.wide_tab);
         }
-        const void *w = kind[i] >= 0 ? g.h[kind[i]].w : nullptr;
+        const bool key = kind[i] == 1;
+        const bool normed = kind[i] >= 0 && kind[i] != 2 && (key ? g.h[1].w : g.h[0].w) != nullptr;
         float ss = dot4(b[i], b[i], dot4(a[i], a[i], 0.f));
         ss = sum_lanes<L>(ss);
         if (kind[i] < 0) continue;
-        if (w && kind[i] != 2 && m.on) {
+        if (normed) {
             const float r = rsqrtf(fmaf(ss, g.inv_dim, g.eps));
-            a[i] = mul4(scale4(a[i], r), load4_any(w, g.h[kind[i]].wtype, m.ia));
-            b[i] = mul4(scale4(b[i], r), load4_any(w, g.h[kind[i]].wtype, m.ib));
+            a[i] = mul4(scale4(a[i], r), key ? wa[1] : wa[0]);
+            b[i] = mul4(scale4(b[i], r), key ? wb[1] : wb[0]);
         }
         if (turn) {
             if (g.interleaved) to_pairs(a[i], b[i]);
@@ -222,7 +236,7 @@ struct HeadsGradArg {
     float *dw;
     long long its, ihs, dots, dohs, dits, dihs;
     int n, wtype;
-    int wide_in, wide_dout, wide_din;
+    int wide_in, wide_dout, wide_din, wide_w;
 };
 struct RopeGradArgs {
     HeadsGradArg h[2];
@@ -255,12 +269,12 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_grad_kernel(const __gr
     const long long n_vec = g.n_tok * H.n;
     float4 wa = splat4(1.f), wb = splat4(1.f), da = splat4(0.f), db = splat4(0.f);
     if (H.w && m.on) {
-        wa = load4_any(H.w, H.wtype, m.ia);
-        wb = load4_any(H.w, H.wtype, m.ib);
+        wa = load4_any(H.w, H.wtype, m.ia, H.wide_w);
+        wb = load4_any(H.w, H.wtype, m.ib, H.wide_w);
         if (g.interleaved) to_pairs(wa, wb);
     }
     for (long long v0 = (long long)block * (S * HPT); v0 < n_vec; v0 += (long long)blocks * (S * HPT)) {
-        const long long t0 = v0 / H.n;
+        const long long t0 = v0 < 0x7FFFFFFFLL ? (long long)((unsigned int)v0 / (unsigned int)H.n) : v0 / H.n;
         const int rem0 = (int)(v0 - t0 * H.n);
         float4 a[HPT], b[HPT], ua[HPT], ub[HPT];
         long long tok[HPT];
@@ -325,37 +339,42 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_grad_kernel(const __gr
             }
         }
     }
+    if (!g.h[0].dw && !g.h[1].dw) return;
     // the block's sums, in channel order
     const int dim = g.dim;
     if (g.interleaved) from_pairs(da, db);
     if (m.on) {
-        store4(sums + slot * dim + m.ia, da, false);
-        store4(sums + slot * dim + m.ib, db, false);
+        store4(sums + slot * dim + m.ia, da, true);
+        store4(sums + slot * dim + m.ib, db, true);
     }
     __syncthreads();
     for (int c = threadIdx.x; c < dim; c += kRopeThreads) {
         float t = 0.f;
+#pragma unroll
         for (int i = 0; i < S; ++i) t += sums[i * dim + c];
         g.part[(size_t)blockIdx.x * dim + c] = t;
     }
-    __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(g.count, 1u) == gridDim.x - 1;
+    if (threadIdx.x == 0) last = atom_acq_rel_add(g.count) == gridDim.x - 1;
     __syncthreads();
     if (!last) return;
-    __threadfence();
-    // rows of one kind split over 256 / (dim / 4) threads per channel group, then added in order
+    // The rows of one kind, split over the threads of a channel group, eight loads in flight; then the threads' sums in order.
     for (int k = 0; k < 2; ++k) {
         if (!g.h[k].dw) continue;
         const int b0 = k ? g.blocks0 : 0, b1 = k ? gridDim.x : g.blocks0;
         const int groups = dim / 4, parts = kRopeThreads / groups;
         const int c = threadIdx.x % groups, p = threadIdx.x / groups;
         float4 t = splat4(0.f);
-        if (p < parts)
-            for (int b = b0 + p; b < b1; b += parts) {
-                const float4 x = __ldcg(reinterpret_cast<const float4 *>(g.part + (size_t)b * dim) + c);
-                t = make_float4(t.x + x.x, t.y + x.y, t.z + x.z, t.w + x.w);
+        if (p < parts) {
+            for (int b = b0 + p; b < b1; b += 8 * parts) {
+                float4 x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] = b + j * parts < b1 ? __ldcg(reinterpret_cast<const float4 *>(g.part + (size_t)(b + j * parts) * dim) + c) : splat4(0.f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) t = make_float4(t.x + x[j].x, t.y + x[j].y, t.z + x[j].z, t.w + x[j].w);
             }
+        }
         __syncthreads();
         if (p < parts) store4(sums + p * dim + 4 * c, t, true);
         __syncthreads();
@@ -400,6 +419,7 @@ static HeadsArg heads_arg(const fpsk_heads *h, int in_size, int out_size)
     a.n = h->n_heads; a.wtype = h->weight_type;
     a.wide_in = wide(h->in, in_size, a.its, a.ihs);
     a.wide_out = wide(h->out, out_size, a.ots, a.ohs);
+    a.wide_w = wide(h->weight, elem_size(h->weight_type), 0, 0);
     return a;
 }
 template <typename G> static void rotary_arg(G &g, const fpsk_rotary *r)
@@ -449,7 +469,7 @@ template <bool APPEND> static fpsk_status launch_rope_typed(const RopeArgs &g, i
 #undef FPSK_IN
 }
 
-constexpr int kGradBlocks = 148 * 4;
+constexpr int kGradBlocks = 148 * 3;
 
 template <typename X, typename Y> static fpsk_status launch_grad(const RopeGradArgs &g, unsigned blocks, cudaStream_t st)
 {
@@ -565,6 +585,7 @@ extern "C" fpsk_status fpsk_qk_norm_rope_backward(const fpsk_heads_grad *q, cons
         a.wide_in = wide(a.in, in_size, a.its, a.ihs);
         a.wide_dout = wide(a.dout, gsize, a.dots, a.dohs);
         a.wide_din = wide(a.din, gsize, a.dits, a.dihs);
+        a.wide_w = wide(a.w, elem_size(a.wtype), 0, 0);
     }
     if (!workspace) return FPSK_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(workspace) % 256) return FPSK_ERR_ALIGN;
