@@ -24,47 +24,52 @@ template <> struct Elem<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __float2bfloat16_rn(x); }
 };
 
-__device__ __forceinline__ uint32_t pack2(__half a, __half b)
+// two values rounded to a pair
+template <typename T> __device__ __forceinline__ uint32_t round_pair(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t round_pair<__half>(float lo, float hi)
 {
-    return (uint32_t)__half_as_ushort(a) | ((uint32_t)__half_as_ushort(b) << 16);
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
-__device__ __forceinline__ uint32_t pack2(__nv_bfloat16 a, __nv_bfloat16 b)
+template <> __device__ __forceinline__ uint32_t round_pair<__nv_bfloat16>(float lo, float hi)
 {
-    return (uint32_t)__bfloat16_as_ushort(a) | ((uint32_t)__bfloat16_as_ushort(b) << 16);
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 
-// Four consecutive elements as FP32; `wide`: the address is a multiple of four elements.
-__device__ __forceinline__ float4 load4(const float *p, bool wide)
+// Four consecutive elements as FP32; WIDE: the address is a multiple of four elements.
+template <bool WIDE> __device__ __forceinline__ float4 load4(const float *p)
 {
-    if (wide) return __ldg(reinterpret_cast<const float4 *>(p));
+    if (WIDE) return __ldg(reinterpret_cast<const float4 *>(p));
     return make_float4(__ldg(p), __ldg(p + 1), __ldg(p + 2), __ldg(p + 3));
 }
-template <typename T> __device__ __forceinline__ float4 load4(const T *p, bool wide)
+template <bool WIDE, typename T> __device__ __forceinline__ float4 load4(const T *p)
 {
-    if (wide) {
+    if (WIDE) {
         const uint2 u = __ldg(reinterpret_cast<const uint2 *>(p));
         const float2 a = HalfTraits<T>::unpack2(u.x), b = HalfTraits<T>::unpack2(u.y);
         return make_float4(a.x, a.y, b.x, b.y);
     }
     return make_float4(Elem<T>::to_f(p[0]), Elem<T>::to_f(p[1]), Elem<T>::to_f(p[2]), Elem<T>::to_f(p[3]));
 }
-__device__ __forceinline__ void store4(float *p, float4 x, bool wide)
+template <bool WIDE> __device__ __forceinline__ void store4(float *p, float4 x)
 {
-    if (wide) { *reinterpret_cast<float4 *>(p) = x; return; }
+    if (WIDE) { *reinterpret_cast<float4 *>(p) = x; return; }
     p[0] = x.x; p[1] = x.y; p[2] = x.z; p[3] = x.w;
 }
-template <typename T> __device__ __forceinline__ void store4(T *p, float4 x, bool wide)
+template <bool WIDE, typename T> __device__ __forceinline__ void store4(T *p, float4 x)
 {
-    const T a = Elem<T>::from_f(x.x), b = Elem<T>::from_f(x.y), c = Elem<T>::from_f(x.z), d = Elem<T>::from_f(x.w);
-    if (wide) { *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(a, b), pack2(c, d)); return; }
-    p[0] = a; p[1] = b; p[2] = c; p[3] = d;
+    if (WIDE) { *reinterpret_cast<uint2 *>(p) = make_uint2(round_pair<T>(x.x, x.y), round_pair<T>(x.z, x.w)); return; }
+    p[0] = Elem<T>::from_f(x.x); p[1] = Elem<T>::from_f(x.y); p[2] = Elem<T>::from_f(x.z); p[3] = Elem<T>::from_f(x.w);
 }
 // four weights of a run-time type (they are read once per thread)
-__device__ __forceinline__ float4 load4_any(const void *p, int type, int at, bool wide)
+template <bool WIDE> __device__ __forceinline__ float4 load4_any(const void *p, int type, int at)
 {
-    if (type == FPSK_ELEM_FP32) return load4(static_cast<const float *>(p) + at, wide);
-    if (type == FPSK_ELEM_FP16) return load4(static_cast<const __half *>(p) + at, wide);
-    return load4(static_cast<const __nv_bfloat16 *>(p) + at, wide);
+    if (type == FPSK_ELEM_FP32) return load4<WIDE>(static_cast<const float *>(p) + at);
+    if (type == FPSK_ELEM_FP16) return load4<WIDE>(static_cast<const __half *>(p) + at);
+    return load4<WIDE>(static_cast<const __nv_bfloat16 *>(p) + at);
 }
 
 __device__ __forceinline__ void report_status(int32_t *d_status, int code)

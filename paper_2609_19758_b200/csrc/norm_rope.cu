@@ -33,10 +33,21 @@ struct PlaceArg {                      // where the new tokens' keys and values 
     int wide_k, wide_v;
 };
 
+// How a block walks tokens and heads.  A block has S = 256 / L head slots; a slot has kPer heads at a time: of one token (`tokens`
+// = 1: head, head + S, ..), or, where a token has fewer heads than slots, one head of kPer tokens, `tokens` apart.  What differs from
+// one step to the next is a pointer increment; with the addresses computed anew for every head the kernel was bound by them
+// (390 instructions for two heads, 0.8 issued per cycle, at half the memory's rate).
+constexpr int kRopeThreads = 256, kPer = 2;
+struct BlockMap {
+    int tokens;                        // of a block at a time, in the sense above
+    int step;                          // tokens a block covers in one step: 1 or kPer * tokens
+    int chunks;                        // of S * kPer heads (grid y)
+};
 struct RopeArgs {
     HeadsArg h[3];                     // queries, keys, values (values: append only, copied)
     int n_all;                         // heads of all kinds
-    long long n_vec;                   // tokens x heads
+    long long n_tok;
+    BlockMap map;
     int dim, rot, interleaved;
     const float *cos, *sin;
     const int *positions;
@@ -95,135 +106,181 @@ __device__ __forceinline__ float dot4(float4 a, float4 b, float acc)
     return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, acc))));
 }
 __device__ __forceinline__ float4 splat4(float x) { return make_float4(x, x, x, x); }
+// over the L lanes of a slot (whole slots take a branch, not whole warps)
 template <int L> __device__ __forceinline__ float sum_lanes(float x)
 {
+    const unsigned int mask = L == 32 ? 0xFFFFFFFFu : ((1u << L) - 1u) << (threadIdx.x & (32 - L) & 31);
 #pragma unroll
-    for (int o = L / 2; o; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    for (int o = L / 2; o; o >>= 1) x += __shfl_xor_sync(mask, x, o);
     return x;
 }
 
-constexpr int kRopeThreads = 256;
-
-// Block = 256 / L head slots, HPT consecutive rounds of them.  All loads of a thread's HPT heads are issued before the
-// first is used.
-template <typename X, typename Y, int L, int HPT, bool APPEND>
-__global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_constant__ RopeArgs g)
+template <int L> static BlockMap block_map(int heads)
 {
     constexpr int S = kRopeThreads / L;
-    const int lane = threadIdx.x % L, slot = threadIdx.x / L;
-    const LaneMap m(lane, g.dim, g.rot, g.interleaved);
-    const long long v0 = (long long)blockIdx.x * (S * HPT);
-    // (a 64-bit division takes longer than a head)
-    const long long t0 = v0 < 0x7FFFFFFFLL ? (long long)((unsigned int)v0 / (unsigned int)g.n_all) : v0 / g.n_all;
-    const int rem0 = (int)(v0 - t0 * g.n_all);
+    BlockMap m = {1, 1, 1};
+    if (heads < S) {
+        m.tokens = S / heads;
+        m.step = kPer * m.tokens;
+    } else {
+        m.chunks = (heads + S * kPer - 1) / (S * kPer);
+    }
+    return m;
+}
+// The head and the offset in tokens of a slot's i-th vector; head >= heads: none.
+struct SlotMap {
+    int head0, token0, head_step, token_step;
+    __device__ __forceinline__ SlotMap(const BlockMap &m, int heads, int slots, int slot, int chunk)
+    {
+        if (m.step == 1) {
+            head0 = chunk * slots * kPer + slot;
+            token0 = 0;
+            head_step = slots;
+            token_step = 0;
+        } else {
+            token0 = slot / heads;
+            head0 = token0 < m.tokens ? slot - token0 * heads : heads;
+            head_step = 0;
+            token_step = m.tokens;
+        }
+    }
+};
 
-    int kind[HPT], head[HPT];
-    long long tok[HPT];
-    float4 a[HPT], b[HPT];
+// WIDE: four elements at a time (all pointers and strides allow it), and 32-bit offsets into the tables.
+template <typename X, typename Y, int L, bool APPEND, bool WIDE>
+__global__ void __launch_bounds__(kRopeThreads, 3) norm_rope_kernel(const __grid_constant__ RopeArgs g)
+{
+    constexpr int S = kRopeThreads / L;
+    const int lane = threadIdx.x % L;
+    const LaneMap m(lane, g.dim, g.rot, g.interleaved);
+    const SlotMap sm(g.map, g.n_all, S, threadIdx.x / L, blockIdx.y);
+    // the slot's heads: what they are, where they lie (what the token adds comes with the token), their weights
+    int kind[kPer];
+    const X *src[kPer];
+    Y *dst[kPer];
+    float4 wa[kPer], wb[kPer];
+    bool normed[kPer];
+    const long long first = (long long)blockIdx.x * g.map.step, stride = (long long)gridDim.x * g.map.step;
 #pragma unroll
-    for (int i = 0; i < HPT; ++i) {
-        const int r = rem0 + slot + i * S;
-        const int dt = r / g.n_all;
-        int h = r - dt * g.n_all;
-        tok[i] = t0 + dt;
+    for (int i = 0; i < kPer; ++i) {
+        int h = sm.head0 + i * sm.head_step;
         kind[i] = 0;
         if (h >= g.h[0].n) { h -= g.h[0].n; kind[i] = 1; }
-        if (APPEND && kind[i] == 1 && h >= g.h[1].n) { h -= g.h[1].n; kind[i] = 2; }
-        head[i] = h;
-        a[i] = b[i] = splat4(0.f);
-        if (v0 + slot + i * S >= g.n_vec) { kind[i] = -1; continue; }
-        if (m.on) {
-            const HeadsArg &H = g.h[kind[i]];
-            const X *p = static_cast<const X *>(H.in) + tok[i] * H.its + h * H.ihs;
-            a[i] = load4(p + m.ia, H.wide_in);
-            b[i] = load4(p + m.ib, H.wide_in);
+        if (kind[i] == 1 && h >= g.h[1].n) { h -= g.h[1].n; kind[i] = 2; }
+        if (kind[i] == 2 && h >= g.h[2].n) kind[i] = -1;
+        const HeadsArg &H = g.h[max(kind[i], 0)];
+        const long long tok = first + sm.token0 + i * sm.token_step;
+        src[i] = static_cast<const X *>(H.in) + tok * H.its + h * H.ihs;
+        dst[i] = APPEND && kind[i] > 0 ? static_cast<Y *>(kind[i] == 1 ? g.at.k : g.at.v) + h * (kind[i] == 1 ? g.at.khs : g.at.vhs)
+                                       : static_cast<Y *>(H.out) + tok * H.ots + h * H.ohs;
+        normed[i] = H.w != nullptr && kind[i] != 2;
+        wa[i] = wb[i] = splat4(1.f);
+        if (normed[i] && m.on) {
+            wa[i] = load4_any<WIDE>(H.w, H.wtype, m.ia);
+            wb[i] = load4_any<WIDE>(H.w, H.wtype, m.ib);
         }
+        if (!m.on) kind[i] = -1;                                       // lanes behind the last channel only take part in the sums
     }
-
-    // the weights of queries and of keys, once per thread
-    float4 wa[2], wb[2];
+    long long in_step[kPer], out_step[kPer];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        wa[k] = wb[k] = splat4(1.f);
-        if (g.h[k].w && m.on) {
-            wa[k] = load4_any(g.h[k].w, g.h[k].wtype, m.ia, g.h[k].wide_w);
-            wb[k] = load4_any(g.h[k].w, g.h[k].wtype, m.ib, g.h[k].wide_w);
-        }
+    for (int i = 0; i < kPer; ++i) {
+        in_step[i] = stride * (kind[i] <= 0 ? g.h[0].its : kind[i] == 1 ? g.h[1].its : g.h[2].its);
+        out_step[i] = APPEND && kind[i] > 0 ? 0 : stride * (kind[i] == 1 ? g.h[1].ots : g.h[0].ots);
     }
-
-    // sequence of the block's first token: how many sequences end at or before it
+    float4 na[kPer], nb[kPer];                                         // the step ahead
+    auto fetch = [&](long long tok) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            na[i] = nb[i] = splat4(0.f);
+            if (kind[i] >= 0 && tok + sm.token0 + i * sm.token_step < g.n_tok) {
+                na[i] = load4<WIDE>(src[i] + m.ia);
+                nb[i] = load4<WIDE>(src[i] + m.ib);
+            }
+            src[i] += in_step[i];
+        }
+    };
+    if (first < g.n_tok) fetch(first);
     int seq0 = 0;
-    if (APPEND) {
-        const long long t_first = t0;
-        for (int base = 0; base < g.at.n_seqs; base += kRopeThreads) {
-            const int i = base + threadIdx.x;
-            const int before = __syncthreads_count(i < g.at.n_seqs && g.at.cu_q[i + 1] <= t_first);
-            seq0 += before;
-            if (before < kRopeThreads) break;
-        }
-    }
-
+    for (long long t0 = first; t0 < g.n_tok; t0 += stride) {
+        float4 a[kPer], b[kPer];
 #pragma unroll
-    for (int i = 0; i < HPT; ++i) {
-        long long pos = 0, place = 0;
-        int seq = seq0;
-        bool has_place = true;
-        if (APPEND && kind[i] >= 0) {
-            while (seq < g.at.n_seqs && g.at.cu_q[seq + 1] <= tok[i]) ++seq;
-            has_place = seq < g.at.n_seqs;
-            if (has_place) place = (long long)g.at.kv_len[seq] - (g.at.cu_q[seq + 1] - tok[i]);
-            has_place = has_place && place >= 0;
-            pos = place;
+        for (int i = 0; i < kPer; ++i) { a[i] = na[i]; b[i] = nb[i]; }
+        if (t0 + stride < g.n_tok) fetch(t0 + stride);
+        if (APPEND) {
+            // how many sequences end at or before the step's first token (the tokens ascend)
+            for (;;) {
+                const int i = seq0 + (threadIdx.x & 31);
+                const unsigned int before = __ballot_sync(0xFFFFFFFFu, i < g.at.n_seqs && __ldg(g.at.cu_q + i + 1) <= t0);
+                seq0 += __popc(before);
+                if (before != 0xFFFFFFFFu) break;
+            }
         }
-        if (g.positions && kind[i] >= 0) pos = g.positions[tok[i]];
-        const bool turn = kind[i] >= 0 && kind[i] != 2 && g.rot > 0;
-        const bool in_table = pos >= 0 && pos < g.n_pos;
+        long long place = -1, row_k = 0, row_v = 0;
+        bool in_table = true, stored = true;
         float4 c = splat4(1.f), s = splat4(0.f);
-        if (turn && in_table && m.on && m.rotated) {
-            c = load4(g.cos + pos * (g.rot / 2) + m.cs, g.wide_tab);
-            s = load4(g.sin + pos * (g.rot / 2) + m.cs, g.wide_tab);
-        }
-        const bool key = kind[i] == 1;
-        const bool normed = kind[i] >= 0 && kind[i] != 2 && (key ? g.h[1].w : g.h[0].w) != nullptr;
-        float ss = dot4(b[i], b[i], dot4(a[i], a[i], 0.f));
-        ss = sum_lanes<L>(ss);
-        if (kind[i] < 0) continue;
-        if (normed) {
-            const float r = rsqrtf(fmaf(ss, g.inv_dim, g.eps));
-            a[i] = mul4(scale4(a[i], r), key ? wa[1] : wa[0]);
-            b[i] = mul4(scale4(b[i], r), key ? wb[1] : wb[0]);
-        }
-        if (turn) {
-            if (g.interleaved) to_pairs(a[i], b[i]);
-            rotate4(a[i], b[i], c, s);
-            if (g.interleaved) from_pairs(a[i], b[i]);
-            if (!in_table) {
-                if (APPEND && !has_place && !g.positions) a[i] = b[i] = splat4(0.f);
-                else {
-                    a[i] = b[i] = splat4(__int_as_float(0x7FC00000));
-                    if (lane == 0) report_status(g.status, FPSK_ERR_PARAM);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const long long tok = t0 + sm.token0 + i * sm.token_step;
+            const bool live = kind[i] >= 0 && tok < g.n_tok;
+            if ((i == 0 || sm.token_step) && tok < g.n_tok) {          // what belongs to the token
+                int pos = 0;
+                if (APPEND) {
+                    int seq = seq0;
+                    if (sm.token_step || sm.token0)
+                        while (seq < g.at.n_seqs && __ldg(g.at.cu_q + seq + 1) <= tok) ++seq;
+                    place = -1;
+                    stored = false;
+                    if (seq < g.at.n_seqs) place = __ldg(g.at.kv_len + seq) - (__ldg(g.at.cu_q + seq + 1) - (int)tok);
+                    pos = (int)place;
+                    if (place >= 0) {
+                        const unsigned int col = (unsigned int)place / (unsigned int)g.at.page_size;
+                        const int row = (int)place - (int)(col * g.at.page_size);
+                        const int page = col < (unsigned int)g.at.max_pages ? __ldg(g.at.table + seq * g.at.table_stride + col) : -1;
+                        stored = page >= 0 && page < g.at.n_pages;
+                        if (!stored && lane == 0) report_status(g.status, FPSK_ERR_PARAM);
+                        row_k = page * g.at.kps + row * g.at.kts;
+                        row_v = page * g.at.vps + row * g.at.vts;
+                    }
+                }
+                if (g.positions) pos = __ldg(g.positions + tok);
+                if (g.rot > 0) {
+                    in_table = pos >= 0 && pos < g.n_pos;
+                    if (in_table && m.on && m.rotated) {
+                        if (WIDE) {
+                            const int at = pos * (g.rot / 2) + m.cs;
+                            c = load4<true>(g.cos + at);
+                            s = load4<true>(g.sin + at);
+                        } else {
+                            const long long at = (long long)pos * (g.rot / 2) + m.cs;
+                            c = load4<false>(g.cos + at);
+                            s = load4<false>(g.sin + at);
+                        }
+                    }
                 }
             }
-        }
-        if (!m.on) continue;
-        if (!APPEND || kind[i] == 0) {
-            const HeadsArg &H = g.h[kind[i]];
-            Y *p = static_cast<Y *>(H.out) + tok[i] * H.ots + head[i] * H.ohs;
-            store4(p + m.ia, a[i], H.wide_out);
-            store4(p + m.ib, b[i], H.wide_out);
-        } else if (has_place) {
-            const long long col = place / g.at.page_size;
-            const int row = (int)(place - col * g.at.page_size);
-            const long long page = col < g.at.max_pages ? g.at.table[seq * g.at.table_stride + col] : -1;
-            if (page < 0 || page >= g.at.n_pages) {
-                if (lane == 0) report_status(g.status, FPSK_ERR_PARAM);
-                continue;
+            if (normed[i]) {
+                const float ss = sum_lanes<L>(dot4(b[i], b[i], dot4(a[i], a[i], 0.f)));
+                const float r = rsqrtf(fmaf(ss, g.inv_dim, g.eps));
+                a[i] = mul4(scale4(a[i], r), wa[i]);
+                b[i] = mul4(scale4(b[i], r), wb[i]);
             }
-            const bool is_k = kind[i] == 1;
-            Y *p = is_k ? static_cast<Y *>(g.at.k) + page * g.at.kps + row * g.at.kts + head[i] * g.at.khs
-                        : static_cast<Y *>(g.at.v) + page * g.at.vps + row * g.at.vts + head[i] * g.at.vhs;
-            store4(p + m.ia, a[i], is_k ? g.at.wide_k : g.at.wide_v);
-            store4(p + m.ib, b[i], is_k ? g.at.wide_k : g.at.wide_v);
+            if (m.rotated && kind[i] != 2) {
+                if (g.interleaved) to_pairs(a[i], b[i]);
+                rotate4(a[i], b[i], c, s);
+                if (g.interleaved) from_pairs(a[i], b[i]);
+            }
+            if (!in_table && live && kind[i] != 2) {
+                const bool no_place = APPEND && place < 0 && !g.positions;
+                a[i] = b[i] = splat4(no_place ? 0.f : __int_as_float(0x7FC00000));
+                if (!no_place && lane == 0) report_status(g.status, FPSK_ERR_PARAM);
+            }
+            Y *p = dst[i];
+            if (APPEND && kind[i] > 0) p += kind[i] == 1 ? row_k : row_v;
+            dst[i] += out_step[i];
+            if (live && (!APPEND || kind[i] == 0 || stored)) {
+                store4<WIDE>(p + m.ia, a[i]);
+                store4<WIDE>(p + m.ib, b[i]);
+            }
         }
     }
 }
@@ -237,6 +294,7 @@ struct HeadsGradArg {
     long long its, ihs, dots, dohs, dits, dihs;
     int n, wtype;
     int wide_in, wide_dout, wide_din, wide_w;
+    BlockMap map;
 };
 struct RopeGradArgs {
     HeadsGradArg h[2];
@@ -255,88 +313,103 @@ struct RopeGradArgs {
 
 // Persistent blocks, each on the heads of one kind, so that a lane keeps one set of eight weight-gradient sums.  They
 // meet in shared memory, then in a partial row per block; the last block to arrive adds the rows in block order.
-template <typename X, typename Y, int L>
-__global__ void __launch_bounds__(kRopeThreads) norm_rope_grad_kernel(const __grid_constant__ RopeGradArgs g)
+template <typename X, typename Y, int L, bool WIDE>
+__global__ void __launch_bounds__(kRopeThreads, 2) norm_rope_grad_kernel(const __grid_constant__ RopeGradArgs g)
 {
-    constexpr int S = kRopeThreads / L, HPT = 2;
+    constexpr int S = kRopeThreads / L;
     __shared__ __align__(16) float sums[kRopeThreads * 8];
     __shared__ int last;
     const int lane = threadIdx.x % L, slot = threadIdx.x / L;
     const LaneMap m(lane, g.dim, g.rot, g.interleaved);
     const int kind = (int)blockIdx.x >= g.blocks0;
-    const int block = blockIdx.x - (kind ? g.blocks0 : 0), blocks = kind ? gridDim.x - g.blocks0 : g.blocks0;
     const HeadsGradArg &H = g.h[kind];
-    const long long n_vec = g.n_tok * H.n;
+    const int block = blockIdx.x - (kind ? g.blocks0 : 0), blocks = kind ? gridDim.x - g.blocks0 : g.blocks0;
+    const int chunk = block % H.map.chunks, lanes_of_blocks = blocks / H.map.chunks;   // (blocks: a multiple of the chunks)
+    const SlotMap sm(H.map, H.n, S, slot, chunk);
+    const long long first = (long long)(block / H.map.chunks) * H.map.step, stride = (long long)lanes_of_blocks * H.map.step;
     float4 wa = splat4(1.f), wb = splat4(1.f), da = splat4(0.f), db = splat4(0.f);
     if (H.w && m.on) {
-        wa = load4_any(H.w, H.wtype, m.ia, H.wide_w);
-        wb = load4_any(H.w, H.wtype, m.ib, H.wide_w);
+        wa = load4_any<WIDE>(H.w, H.wtype, m.ia);
+        wb = load4_any<WIDE>(H.w, H.wtype, m.ib);
         if (g.interleaved) to_pairs(wa, wb);
     }
-    for (long long v0 = (long long)block * (S * HPT); v0 < n_vec; v0 += (long long)blocks * (S * HPT)) {
-        const long long t0 = v0 < 0x7FFFFFFFLL ? (long long)((unsigned int)v0 / (unsigned int)H.n) : v0 / H.n;
-        const int rem0 = (int)(v0 - t0 * H.n);
-        float4 a[HPT], b[HPT], ua[HPT], ub[HPT];
-        long long tok[HPT];
-        int head[HPT];
-        bool live[HPT];
+    const X *src[kPer];
+    const Y *grad[kPer];
+    Y *dst[kPer];
+    bool there[kPer];
 #pragma unroll
-        for (int i = 0; i < HPT; ++i) {
-            const int r = rem0 + slot + i * S, dt = r / H.n;
-            head[i] = r - dt * H.n;
-            tok[i] = t0 + dt;
-            live[i] = v0 + slot + i * S < n_vec;
-            a[i] = b[i] = ua[i] = ub[i] = splat4(0.f);
-            if (live[i] && m.on) {
-                const X *p = static_cast<const X *>(H.in) + tok[i] * H.its + head[i] * H.ihs;
-                const Y *q = static_cast<const Y *>(H.dout) + tok[i] * H.dots + head[i] * H.dohs;
-                a[i] = load4(p + m.ia, H.wide_in);
-                b[i] = load4(p + m.ib, H.wide_in);
-                ua[i] = load4(q + m.ia, H.wide_dout);
-                ub[i] = load4(q + m.ib, H.wide_dout);
+    for (int i = 0; i < kPer; ++i) {
+        const int h = sm.head0 + i * sm.head_step;
+        const long long tok = first + sm.token0 + i * sm.token_step;
+        there[i] = h < H.n && m.on;
+        src[i] = static_cast<const X *>(H.in) + tok * H.its + h * H.ihs;
+        grad[i] = static_cast<const Y *>(H.dout) + tok * H.dots + h * H.dohs;
+        dst[i] = static_cast<Y *>(H.din) + tok * H.dits + h * H.dihs;
+    }
+    float4 na[kPer], nb[kPer], ga[kPer], gb[kPer];                     // the step ahead
+    auto fetch = [&](long long tok) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            na[i] = nb[i] = ga[i] = gb[i] = splat4(0.f);
+            if (there[i] && tok + sm.token0 + i * sm.token_step < g.n_tok) {
+                na[i] = load4<WIDE>(src[i] + m.ia);
+                nb[i] = load4<WIDE>(src[i] + m.ib);
+                ga[i] = load4<WIDE>(grad[i] + m.ia);
+                gb[i] = load4<WIDE>(grad[i] + m.ib);
             }
+            src[i] += stride * H.its;
+            grad[i] += stride * H.dots;
         }
+    };
+    if (first < g.n_tok) fetch(first);
+    for (long long t0 = first; t0 < g.n_tok; t0 += stride) {
+        float4 a[kPer], b[kPer], ua[kPer], ub[kPer];
 #pragma unroll
-        for (int i = 0; i < HPT; ++i) {
+        for (int i = 0; i < kPer; ++i) { a[i] = na[i]; b[i] = nb[i]; ua[i] = ga[i]; ub[i] = gb[i]; }
+        if (t0 + stride < g.n_tok) fetch(t0 + stride);
+        float4 c = splat4(1.f), s = splat4(0.f);
+        bool in_table = true;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const long long tok = t0 + sm.token0 + i * sm.token_step;
+            const bool live = there[i] && tok < g.n_tok;
+            if (g.rot > 0 && (i == 0 || sm.token_step) && tok < g.n_tok) {
+                const int pos = __ldg(g.positions + tok);
+                in_table = pos >= 0 && pos < g.n_pos;
+                if (in_table && m.on && m.rotated) {
+                    const long long at = WIDE ? (long long)(pos * (g.rot / 2) + m.cs) : (long long)pos * (g.rot / 2) + m.cs;
+                    c = load4<WIDE>(g.cos + at);
+                    s = scale4(load4<WIDE>(g.sin + at), -1.f);
+                }
+            }
             if (g.interleaved) {
                 to_pairs(a[i], b[i]);
                 to_pairs(ua[i], ub[i]);
             }
-            if (g.rot > 0 && live[i]) {
-                const long long pos = g.positions[tok[i]];
-                const bool in_table = pos >= 0 && pos < g.n_pos;
-                if (in_table && m.on && m.rotated) {
-                    const float4 c = load4(g.cos + pos * (g.rot / 2) + m.cs, g.wide_tab);
-                    const float4 s = load4(g.sin + pos * (g.rot / 2) + m.cs, g.wide_tab);
-                    rotate4(ua[i], ub[i], c, scale4(s, -1.f));
-                }
-                if (!in_table) {
-                    ua[i] = ub[i] = splat4(__int_as_float(0x7FC00000));
-                    if (lane == 0) report_status(g.status, FPSK_ERR_PARAM);
-                }
+            if (m.rotated) rotate4(ua[i], ub[i], c, s);
+            if (!in_table && live) {
+                ua[i] = ub[i] = splat4(__int_as_float(0x7FC00000));
+                if (lane == 0) report_status(g.status, FPSK_ERR_PARAM);
             }
             if (H.w) {
                 const float ss = sum_lanes<L>(dot4(b[i], b[i], dot4(a[i], a[i], 0.f)));
                 const float r = rsqrtf(fmaf(ss, g.inv_dim, g.eps));
-                a[i] = scale4(a[i], r);                             // n
+                a[i] = scale4(a[i], r);                             // n (zero where there is no vector: it adds nothing)
                 b[i] = scale4(b[i], r);
-                if (live[i] && m.on) {
-                    da = make_float4(fmaf(ua[i].x, a[i].x, da.x), fmaf(ua[i].y, a[i].y, da.y), fmaf(ua[i].z, a[i].z, da.z), fmaf(ua[i].w, a[i].w, da.w));
-                    db = make_float4(fmaf(ub[i].x, b[i].x, db.x), fmaf(ub[i].y, b[i].y, db.y), fmaf(ub[i].z, b[i].z, db.z), fmaf(ub[i].w, b[i].w, db.w));
-                }
+                da = make_float4(fmaf(ua[i].x, a[i].x, da.x), fmaf(ua[i].y, a[i].y, da.y), fmaf(ua[i].z, a[i].z, da.z), fmaf(ua[i].w, a[i].w, da.w));
+                db = make_float4(fmaf(ub[i].x, b[i].x, db.x), fmaf(ub[i].y, b[i].y, db.y), fmaf(ub[i].z, b[i].z, db.z), fmaf(ub[i].w, b[i].w, db.w));
                 ua[i] = mul4(ua[i], wa);                            // g = u w
                 ub[i] = mul4(ub[i], wb);
-                float dot = m.on ? dot4(ub[i], b[i], dot4(ua[i], a[i], 0.f)) : 0.f;
-                dot = sum_lanes<L>(dot) * g.inv_dim;
+                const float dot = sum_lanes<L>(dot4(ub[i], b[i], dot4(ua[i], a[i], 0.f))) * g.inv_dim;
                 ua[i] = make_float4(r * (ua[i].x - a[i].x * dot), r * (ua[i].y - a[i].y * dot), r * (ua[i].z - a[i].z * dot), r * (ua[i].w - a[i].w * dot));
                 ub[i] = make_float4(r * (ub[i].x - b[i].x * dot), r * (ub[i].y - b[i].y * dot), r * (ub[i].z - b[i].z * dot), r * (ub[i].w - b[i].w * dot));
             }
             if (g.interleaved) from_pairs(ua[i], ub[i]);
-            if (live[i] && m.on) {
-                Y *p = static_cast<Y *>(H.din) + tok[i] * H.dits + head[i] * H.dihs;
-                store4(p + m.ia, ua[i], H.wide_din);
-                store4(p + m.ib, ub[i], H.wide_din);
+            if (live) {
+                store4<WIDE>(dst[i] + m.ia, ua[i]);
+                store4<WIDE>(dst[i] + m.ib, ub[i]);
             }
+            dst[i] += stride * H.dits;
         }
     }
     if (!g.h[0].dw && !g.h[1].dw) return;
@@ -344,8 +417,8 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_grad_kernel(const __gr
     const int dim = g.dim;
     if (g.interleaved) from_pairs(da, db);
     if (m.on) {
-        store4(sums + slot * dim + m.ia, da, true);
-        store4(sums + slot * dim + m.ib, db, true);
+        store4<true>(sums + slot * dim + m.ia, da);
+        store4<true>(sums + slot * dim + m.ib, db);
     }
     __syncthreads();
     for (int c = threadIdx.x; c < dim; c += kRopeThreads) {
@@ -376,7 +449,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_grad_kernel(const __gr
             }
         }
         __syncthreads();
-        if (p < parts) store4(sums + p * dim + 4 * c, t, true);
+        if (p < parts) store4<true>(sums + p * dim + 4 * c, t);
         __syncthreads();
         for (int ch = threadIdx.x; ch < dim; ch += kRopeThreads) {
             float s = 0.f;
@@ -433,31 +506,28 @@ template <typename G> static void rotary_arg(G &g, const fpsk_rotary *r)
     g.wide_tab = g.rot && wide(r->cos, 4, r->rot_dim / 2, 0) && wide(r->sin, 4, r->rot_dim / 2, 0);
 }
 
-// Heads per thread: one while the call has fewer head slots than the card holds at once (latency), else four, whose loads
-// are in flight together.
-template <typename X, typename Y, bool APPEND> static fpsk_status launch_rope(const RopeArgs &g, cudaStream_t st)
+// Three blocks a multiprocessor walk the tokens.
+template <typename X, typename Y, int L, bool APPEND> static fpsk_status launch_rope_lanes(RopeArgs g, cudaStream_t st)
 {
-    const int L = g.dim <= 64 ? 8 : g.dim <= 128 ? 16 : 32, S = kRopeThreads / L;
-    const int hpt = g.n_vec > 148LL * 8 * S ? 4 : 1;
-    const long long blocks = (g.n_vec + S * hpt - 1) / (S * hpt);
-    if (blocks > 0x7FFFFFFFLL) return FPSK_ERR_SHAPE;
-#define FPSK_ROPE(LL, HH) norm_rope_kernel<X, Y, LL, HH, APPEND><<<(unsigned)blocks, kRopeThreads, 0, st>>>(g)
-    if (hpt == 1) {
-        if (L == 8) FPSK_ROPE(8, 1);
-        else if (L == 16) FPSK_ROPE(16, 1);
-        else FPSK_ROPE(32, 1);
-    } else {
-        if (L == 8) FPSK_ROPE(8, 4);
-        else if (L == 16) FPSK_ROPE(16, 4);
-        else FPSK_ROPE(32, 4);
-    }
-#undef FPSK_ROPE
+    g.map = block_map<L>(g.n_all);
+    const long long steps = (g.n_tok + g.map.step - 1) / g.map.step, most = (148 * 3 + g.map.chunks - 1) / g.map.chunks;
+    const dim3 grid((unsigned)(steps < most ? steps : most), (unsigned)g.map.chunks);
+    bool all = g.rot == 0 || (g.wide_tab && g.n_pos * (g.rot / 2) <= 0x7FFFFFFFLL);
+    for (int k = 0; k < 3; ++k)
+        if (g.h[k].n) all = all && g.h[k].wide_in && (APPEND && k > 0 ? (k == 1 ? g.at.wide_k : g.at.wide_v) : g.h[k].wide_out) && (!g.h[k].w || g.h[k].wide_w);
+    if (all) norm_rope_kernel<X, Y, L, APPEND, true><<<grid, kRopeThreads, 0, st>>>(g);
+    else norm_rope_kernel<X, Y, L, APPEND, false><<<grid, kRopeThreads, 0, st>>>(g);
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
+template <typename X, typename Y, bool APPEND> static fpsk_status launch_rope(const RopeArgs &g, cudaStream_t st)
+{
+    return g.dim <= 64 ? launch_rope_lanes<X, Y, 8, APPEND>(g, st) : g.dim <= 128 ? launch_rope_lanes<X, Y, 16, APPEND>(g, st)
+                                                                                  : launch_rope_lanes<X, Y, 32, APPEND>(g, st);
+}
 template <bool APPEND> static fpsk_status launch_rope_typed(const RopeArgs &g, int in, int out, cudaStream_t st)
 {
-    if (g.n_vec == 0) return FPSK_OK;
+    if (g.n_tok == 0 || g.n_all == 0) return FPSK_OK;
 #define FPSK_IN(Y)                                                                        \
     (in == FPSK_ELEM_FP32 ? launch_rope<float, Y, APPEND>(g, st)                          \
                           : in == FPSK_ELEM_FP16 ? launch_rope<__half, Y, APPEND>(g, st)  \
@@ -469,13 +539,22 @@ template <bool APPEND> static fpsk_status launch_rope_typed(const RopeArgs &g, i
 #undef FPSK_IN
 }
 
-constexpr int kGradBlocks = 148 * 3;
+constexpr int kGradBlocks = 148 * 2;
+constexpr int kMostGradBlocks = kGradBlocks + 2 * (65536 / 16 + 1);   // (a kind has at least a block for each chunk of its heads)
 
+template <typename X, typename Y, int L> static void launch_grad_lanes(const RopeGradArgs &g, unsigned blocks, cudaStream_t st)
+{
+    bool all = g.rot == 0 || (g.wide_tab && g.n_pos * (g.rot / 2) <= 0x7FFFFFFFLL);
+    for (int k = 0; k < 2; ++k)
+        if (g.h[k].n) all = all && g.h[k].wide_in && g.h[k].wide_dout && g.h[k].wide_din && (!g.h[k].w || g.h[k].wide_w);
+    if (all) norm_rope_grad_kernel<X, Y, L, true><<<blocks, kRopeThreads, 0, st>>>(g);
+    else norm_rope_grad_kernel<X, Y, L, false><<<blocks, kRopeThreads, 0, st>>>(g);
+}
 template <typename X, typename Y> static fpsk_status launch_grad(const RopeGradArgs &g, unsigned blocks, cudaStream_t st)
 {
-    if (g.dim <= 64) norm_rope_grad_kernel<X, Y, 8><<<blocks, kRopeThreads, 0, st>>>(g);
-    else if (g.dim <= 128) norm_rope_grad_kernel<X, Y, 16><<<blocks, kRopeThreads, 0, st>>>(g);
-    else norm_rope_grad_kernel<X, Y, 32><<<blocks, kRopeThreads, 0, st>>>(g);
+    if (g.dim <= 64) launch_grad_lanes<X, Y, 8>(g, blocks, st);
+    else if (g.dim <= 128) launch_grad_lanes<X, Y, 16>(g, blocks, st);
+    else launch_grad_lanes<X, Y, 32>(g, blocks, st);
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
@@ -503,7 +582,7 @@ extern "C" fpsk_status fpsk_qk_norm_rope(const fpsk_heads *q, const fpsk_heads *
     g.h[1] = heads_arg(k, elem_size(in_type), elem_size(out_type));
     g.n_all = g.h[0].n + g.h[1].n;
     if (n_tokens > (1LL << 40)) return FPSK_ERR_SHAPE;
-    g.n_vec = n_tokens * g.n_all;
+    g.n_tok = n_tokens;
     g.dim = head_dim;
     g.eps = eps;
     g.inv_dim = 1.f / (float)head_dim;
@@ -533,7 +612,7 @@ extern "C" fpsk_status fpsk_paged_append(const fpsk_paged_cache *cache, const fp
     g.h[1] = heads_arg(k, in_size, size);
     g.h[2] = heads_arg(v, in_size, size);
     g.n_all = g.h[0].n + g.h[1].n + g.h[2].n;
-    g.n_vec = batch->n_tokens * g.n_all;
+    g.n_tok = batch->n_tokens;
     g.dim = cache->head_dim;
     g.eps = eps;
     g.inv_dim = 1.f / (float)cache->head_dim;
@@ -554,7 +633,7 @@ extern "C" fpsk_status fpsk_paged_append(const fpsk_paged_cache *cache, const fp
 extern "C" size_t fpsk_norm_rope_workspace_bytes(int32_t head_dim)
 {
     if (!head_dim_ok(head_dim)) return 0;
-    return kAttnSyncBytes + (size_t)kGradBlocks * head_dim * sizeof(float);
+    return kAttnSyncBytes + (size_t)kMostGradBlocks * head_dim * sizeof(float);
 }
 
 extern "C" fpsk_status fpsk_qk_norm_rope_backward(const fpsk_heads_grad *q, const fpsk_heads_grad *k, int64_t n_tokens,
@@ -598,17 +677,16 @@ extern "C" fpsk_status fpsk_qk_norm_rope_backward(const fpsk_heads_grad *q, cons
     rotary_arg(g, rot);
     g.count = static_cast<unsigned int *>(workspace);
     g.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + kAttnSyncBytes);
-    // blocks of each kind in proportion to its heads, at least one where it has a weight gradient to write
-    const int L = head_dim <= 64 ? 8 : head_dim <= 128 ? 16 : 32, per = kRopeThreads / L * 2;
+    // Blocks of each kind in proportion to its heads, a multiple of its chunks of heads, at least one where it has a weight
+    // gradient to write.
     long long want[2];
     for (int i = 0; i < 2; ++i) {
-        want[i] = (n_tokens * g.h[i].n + per - 1) / per;
-        if (want[i] == 0 && g.h[i].dw) want[i] = 1;
-    }
-    if (want[0] + want[1] > kGradBlocks) {
-        const long long n0 = (long long)((double)kGradBlocks * (double)want[0] / (double)(want[0] + want[1]) + 0.5);
-        want[0] = want[0] ? (n0 < 1 ? 1 : n0 > kGradBlocks - (want[1] ? 1 : 0) ? kGradBlocks - (want[1] ? 1 : 0) : n0) : 0;
-        want[1] = want[1] ? kGradBlocks - want[0] : 0;
+        HeadsGradArg &a = g.h[i];
+        a.map = head_dim <= 64 ? block_map<8>(a.n ? a.n : 1) : head_dim <= 128 ? block_map<16>(a.n ? a.n : 1) : block_map<32>(a.n ? a.n : 1);
+        const long long steps = a.n ? (n_tokens + a.map.step - 1) / a.map.step : 0;
+        const long long most = (long long)kGradBlocks * a.n / (g.h[0].n + g.h[1].n > 0 ? g.h[0].n + g.h[1].n : 1) / a.map.chunks;
+        want[i] = (steps < most ? steps : most < 1 ? (steps < 1 ? steps : 1) : most) * a.map.chunks;
+        if (want[i] == 0 && a.dw) want[i] = a.map.chunks;
     }
     g.blocks0 = (int)want[0];
     const unsigned blocks = (unsigned)(want[0] + want[1]);

@@ -212,19 +212,6 @@ __device__ __forceinline__ void store8(void *p, const uint32_t (&v)[8])
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
                  "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
-template <typename T> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
-template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 
 // ---------------------------------------------------------------- items
 // How a K or V tile lies in shared memory, and by which tensor map it comes.  Both halves of a row (64 channels each) in one
@@ -379,7 +366,7 @@ __device__ __forceinline__ void join_row(const TcaArgs &ga, int first, int parts
     const long long tok = token0 + t, head = kvh * g.group + h;
     if (lane * 4 < g.dim)
         *reinterpret_cast<uint2 *>(static_cast<T *>(g.out) + tok * g.ots + head * g.ohs + lane * 4) =
-            make_uint2(pack_pair<T>(acc.x * inv, acc.y * inv), pack_pair<T>(acc.z * inv, acc.w * inv));
+            make_uint2(round_pair<T>(acc.x * inv, acc.y * inv), round_pair<T>(acc.z * inv, acc.w * inv));
     if (g.lse && lane == 0) g.lse[tok * g.hq + head] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
@@ -899,7 +886,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                                 const bool poly = PAIR && ((i + 1) * kPoly) / 8 != (i * kPoly) / 8;
                                 x = poly ? ex2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
                                 sum[i & 1] = __fadd2_rn(sum[i & 1], x);
-                                p[c * 16 + i] = pack_pair<T>(x.x, x.y);
+                                p[c * 16 + i] = round_pair<T>(x.x, x.y);
                             }
                         }
                         step_sum = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
@@ -1027,7 +1014,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         else if (ch < g.dim)
                             *reinterpret_cast<uint2 *>(static_cast<T *>(g.out) + (long long)(it.token0 + tk) * g.ots +
                                                        (walk.kvh * g.group + rr - tk * g.group) * g.ohs + ch) =
-                                make_uint2(pack_pair<T>(x.x, x.y), pack_pair<T>(x.z, x.w));
+                                make_uint2(round_pair<T>(x.x, x.y), round_pair<T>(x.z, x.w));
                     }
                     named_bar_sync(2, 256);
                 }
@@ -1046,7 +1033,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             if (c * 32 + i < g.dim) {
                                 uint32_t x[8];
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) x[k] = pack_pair<T>(o[i + 2 * k] * inv, o[i + 2 * k + 1] * inv);
+                                for (int k = 0; k < 8; ++k) x[k] = round_pair<T>(o[i + 2 * k] * inv, o[i + 2 * k + 1] * inv);
                                 store8(dst + c * 32 + i, x);
                             }
                     } else if (whole) {
@@ -1054,8 +1041,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         for (int i = 0; i < 32; i += 8)
                             if (c * 32 + i < g.dim)
                                 *reinterpret_cast<uint4 *>(dst + c * 32 + i) =
-                                    make_uint4(pack_pair<T>(o[i] * inv, o[i + 1] * inv), pack_pair<T>(o[i + 2] * inv, o[i + 3] * inv),
-                                               pack_pair<T>(o[i + 4] * inv, o[i + 5] * inv), pack_pair<T>(o[i + 6] * inv, o[i + 7] * inv));
+                                    make_uint4(round_pair<T>(o[i] * inv, o[i + 1] * inv), round_pair<T>(o[i + 2] * inv, o[i + 3] * inv),
+                                               round_pair<T>(o[i + 4] * inv, o[i + 5] * inv), round_pair<T>(o[i + 6] * inv, o[i + 7] * inv));
                     } else {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
