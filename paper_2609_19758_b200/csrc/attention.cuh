@@ -54,6 +54,14 @@ template <bool WIDE, typename T> __device__ __forceinline__ float4 load4(const T
     }
     return make_float4(Elem<T>::to_f(p[0]), Elem<T>::to_f(p[1]), Elem<T>::to_f(p[2]), Elem<T>::to_f(p[3]));
 }
+// the same from shared memory
+__device__ __forceinline__ float4 lds4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+template <typename T> __device__ __forceinline__ float4 lds4(const T *p)
+{
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    const float2 a = HalfTraits<T>::unpack2(u.x), b = HalfTraits<T>::unpack2(u.y);
+    return make_float4(a.x, a.y, b.x, b.y);
+}
 template <bool WIDE> __device__ __forceinline__ void store4(float *p, float4 x)
 {
     if (WIDE) { *reinterpret_cast<float4 *>(p) = x; return; }

@@ -8,112 +8,11 @@
 // so that the mean is a few shuffles, and a lane holds four channel PAIRS (two groups of four channels: i and
 // i + rot/2, or eight neighbours when pairs are interleaved), so that the rotation needs no exchange.  The channels
 // behind rot_dim are paired the same way, (i, i + (D - rot)/2), and not rotated, which keeps one mapping for all.
-#include "attention.cuh"
-#include "stream_pipe.cuh"
+#include "norm_rope.cuh"
 
 #include <mutex>
 
 namespace fpsk {
-
-struct HeadsArg {
-    const void *in;
-    void *out;
-    const void *w;
-    long long its, ihs, ots, ohs;      // strides of tokens and heads, input and output
-    int n, wtype;
-    int wide_in, wide_out, wide_w;
-};
-
-struct PlaceArg {                      // where the new tokens' keys and values go
-    const int *cu_q, *kv_len, *table;
-    long long table_stride, n_pages;
-    int n_seqs, max_pages, page_size;
-    long long kps, kts, khs, vps, vts, vhs;
-    void *k, *v;
-    int wide_k, wide_v;
-};
-
-// How a block walks tokens and heads.  A block has S = 256 / L head slots; a slot has kPer heads at a time: of one token (`tokens`
-// = 1: head, head + S, ..), or, where a token has fewer heads than slots, one head of kPer tokens, `tokens` apart.  What differs from
-// one step to the next is a pointer increment; with the addresses computed anew for every head the kernel was bound by them
-// (390 instructions for two heads, 0.8 issued per cycle, at half the memory's rate).
-constexpr int kRopeThreads = 256, kPer = 2;
-struct BlockMap {
-    int tokens;                        // of a block at a time, in the sense above
-    int step;                          // tokens a block covers in one step: 1 or kPer * tokens
-    int chunks;                        // of S * kPer heads (grid y)
-};
-struct RopeArgs {
-    HeadsArg h[3];                     // queries, keys, values (values: append only, copied)
-    int n_all;                         // heads of all kinds
-    long long n_tok;
-    BlockMap map;
-    int dim, rot, interleaved;
-    const float *cos, *sin;
-    const int *positions;
-    long long n_pos;
-    float eps, inv_dim;
-    int wide_tab;
-    PlaceArg at;
-    int32_t *status;
-};
-
-// What a lane of a head's L lanes holds: two groups of four channels.
-struct LaneMap {
-    int ia, ib, cs;
-    bool on, rotated;
-    __device__ __forceinline__ LaneMap(int lane, int dim, int rot, int interleaved)
-    {
-        const int p = 4 * lane;        // first of its four pairs
-        on = p < dim / 2;
-        rotated = p < rot / 2;
-        cs = p;
-        if (interleaved) {
-            ia = 8 * lane;
-            ib = ia + 4;
-        } else if (rotated) {
-            ia = p;
-            ib = p + rot / 2;
-        } else {
-            ia = rot + (p - rot / 2);
-            ib = ia + (dim - rot) / 2;
-        }
-    }
-};
-// eight neighbours (x0 x1 x2 x3)(x4 x5 x6 x7) <-> the four pairs' first and second members
-__device__ __forceinline__ void to_pairs(float4 &a, float4 &b)
-{
-    const float4 x = a, y = b;
-    a = make_float4(x.x, x.z, y.x, y.z);
-    b = make_float4(x.y, x.w, y.y, y.w);
-}
-__device__ __forceinline__ void from_pairs(float4 &a, float4 &b)
-{
-    const float4 x = a, y = b;
-    a = make_float4(x.x, y.x, x.y, y.y);
-    b = make_float4(x.z, y.z, x.w, y.w);
-}
-__device__ __forceinline__ void rotate4(float4 &a, float4 &b, const float4 &c, const float4 &s)
-{
-    const float4 x = a, y = b;
-    a = make_float4(x.x * c.x - y.x * s.x, x.y * c.y - y.y * s.y, x.z * c.z - y.z * s.z, x.w * c.w - y.w * s.w);
-    b = make_float4(y.x * c.x + x.x * s.x, y.y * c.y + x.y * s.y, y.z * c.z + x.z * s.z, y.w * c.w + x.w * s.w);
-}
-__device__ __forceinline__ float4 mul4(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
-__device__ __forceinline__ float4 scale4(float4 a, float r) { return make_float4(a.x * r, a.y * r, a.z * r, a.w * r); }
-__device__ __forceinline__ float dot4(float4 a, float4 b, float acc)
-{
-    return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, acc))));
-}
-__device__ __forceinline__ float4 splat4(float x) { return make_float4(x, x, x, x); }
-// over the L lanes of a slot (whole slots take a branch, not whole warps)
-template <int L> __device__ __forceinline__ float sum_lanes(float x)
-{
-    const unsigned int mask = L == 32 ? 0xFFFFFFFFu : ((1u << L) - 1u) << (threadIdx.x & (32 - L) & 31);
-#pragma unroll
-    for (int o = L / 2; o; o >>= 1) x += __shfl_xor_sync(mask, x, o);
-    return x;
-}
 
 template <int L> static BlockMap block_map(int heads)
 {
@@ -286,31 +185,6 @@ __global__ void __launch_bounds__(kRopeThreads, 3) norm_rope_kernel(const __grid
 }
 
 // ---------------------------------------------------------------- backward
-struct HeadsGradArg {
-    const void *in, *dout;
-    void *din;
-    const void *w;
-    float *dw;
-    long long its, ihs, dots, dohs, dits, dihs;
-    int n, wtype;
-    int wide_in, wide_dout, wide_din, wide_w;
-    BlockMap map;
-};
-struct RopeGradArgs {
-    HeadsGradArg h[2];
-    int blocks0;                       // the first blocks work on queries, the others on keys
-    long long n_tok;
-    int dim, rot, interleaved;
-    const float *cos, *sin;
-    const int *positions;
-    long long n_pos;
-    float eps, inv_dim;
-    int wide_tab;
-    float *part;                       // [blocks][dim]: every block's share of the weight gradient
-    unsigned int *count;               // arrivals (returns to 0)
-    int32_t *status;
-};
-
 // Persistent blocks, each on the heads of one kind, so that a lane keeps one set of eight weight-gradient sums.  They
 // meet in shared memory, then in a partial row per block; the last block to arrive adds the rows in block order.
 template <typename X, typename Y, int L, bool WIDE>
@@ -401,8 +275,8 @@ __global__ void __launch_bounds__(kRopeThreads, 2) norm_rope_grad_kernel(const _
                 ua[i] = mul4(ua[i], wa);                            // g = u w
                 ub[i] = mul4(ub[i], wb);
                 const float dot = sum_lanes<L>(dot4(ub[i], b[i], dot4(ua[i], a[i], 0.f))) * g.inv_dim;
-                ua[i] = make_float4(r * (ua[i].x - a[i].x * dot), r * (ua[i].y - a[i].y * dot), r * (ua[i].z - a[i].z * dot), r * (ua[i].w - a[i].w * dot));
-                ub[i] = make_float4(r * (ub[i].x - b[i].x * dot), r * (ub[i].y - b[i].y * dot), r * (ub[i].z - b[i].z * dot), r * (ub[i].w - b[i].w * dot));
+                ua[i] = norm_grad4(ua[i], a[i], dot, r);
+                ub[i] = norm_grad4(ub[i], b[i], dot, r);
             }
             if (g.interleaved) from_pairs(ua[i], ub[i]);
             if (live) {
@@ -431,32 +305,9 @@ __global__ void __launch_bounds__(kRopeThreads, 2) norm_rope_grad_kernel(const _
     if (threadIdx.x == 0) last = atom_acq_rel_add(g.count) == gridDim.x - 1;
     __syncthreads();
     if (!last) return;
-    // The rows of one kind, split over the threads of a channel group, eight loads in flight; then the threads' sums in order.
-    for (int k = 0; k < 2; ++k) {
-        if (!g.h[k].dw) continue;
-        const int b0 = k ? g.blocks0 : 0, b1 = k ? gridDim.x : g.blocks0;
-        const int groups = dim / 4, parts = kRopeThreads / groups;
-        const int c = threadIdx.x % groups, p = threadIdx.x / groups;
-        float4 t = splat4(0.f);
-        if (p < parts) {
-            for (int b = b0 + p; b < b1; b += 8 * parts) {
-                float4 x[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[j] = b + j * parts < b1 ? __ldcg(reinterpret_cast<const float4 *>(g.part + (size_t)(b + j * parts) * dim) + c) : splat4(0.f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t = make_float4(t.x + x[j].x, t.y + x[j].y, t.z + x[j].z, t.w + x[j].w);
-            }
-        }
-        __syncthreads();
-        if (p < parts) store4<true>(sums + p * dim + 4 * c, t);
-        __syncthreads();
-        for (int ch = threadIdx.x; ch < dim; ch += kRopeThreads) {
-            float s = 0.f;
-            for (int i = 0; i < parts; ++i) s += sums[i * dim + ch];
-            g.h[k].dw[ch] = s;
-        }
-    }
+    for (int k = 0; k < 2; ++k)
+        if (g.h[k].dw)
+            sum_rows<kRopeThreads>(g.part + (size_t)(k ? g.blocks0 : 0) * dim, dim, k ? (int)gridDim.x - g.blocks0 : g.blocks0, dim, sums, g.h[k].dw);
     if (threadIdx.x == 0) *g.count = 0u;
 }
 
@@ -528,6 +379,8 @@ template <typename X, typename Y, bool APPEND> static fpsk_status launch_rope(co
 template <bool APPEND> static fpsk_status launch_rope_typed(const RopeArgs &g, int in, int out, cudaStream_t st)
 {
     if (g.n_tok == 0 || g.n_all == 0) return FPSK_OK;
+    fpsk_status rc;
+    if (rope_ring(g, in, out, APPEND, st, &rc)) return rc;
 #define FPSK_IN(Y)                                                                        \
     (in == FPSK_ELEM_FP32 ? launch_rope<float, Y, APPEND>(g, st)                          \
                           : in == FPSK_ELEM_FP16 ? launch_rope<__half, Y, APPEND>(g, st)  \
@@ -692,6 +545,7 @@ extern "C" fpsk_status fpsk_qk_norm_rope_backward(const fpsk_heads_grad *q, cons
     const unsigned blocks = (unsigned)(want[0] + want[1]);
     if (blocks == 0) return FPSK_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (rope_grad_ring(g, in_type, grad_type, st, &rc)) return rc;
 #define FPSK_IN(Y)                                                               \
     (in_type == FPSK_ELEM_FP32 ? launch_grad<float, Y>(g, blocks, st)            \
                                : in_type == FPSK_ELEM_FP16 ? launch_grad<__half, Y>(g, blocks, st) : launch_grad<__nv_bfloat16, Y>(g, blocks, st))

@@ -115,6 +115,95 @@ def test_norm_rope_backward(case, wtype):
             assert bool((dwt == 7.0).all())      # no weight, no gradient written
 
 
+RING = [  # enough tokens for the ring of copied rows: tokens, query heads, key heads, dim, rot, interleaved, in, out
+    (4000, 3, 2, 128, 128, False, F32, BF16),
+    (15000, 2, 1, 64, 32, True, BF16, BF16),
+    (3001, 30, 2, 96, 96, False, F16, F16),
+    (2500, 5, 3, 256, 256, False, F32, F32),
+    (20011, 1, 1, 80, 40, True, F32, F16),
+]
+
+
+def _plain(x, w, c, s, rot, inter, eps):
+    """The forward pass in 64 bits with torch, for sizes that the loops of the definition are too slow for."""
+    x = x.double()
+    z = x if w is None else x * torch.rsqrt(x.square().mean(-1, keepdim=True) + eps) * w.double()
+    ia = torch.arange(0, rot, 2, device=x.device) if inter else torch.arange(rot // 2, device=x.device)
+    ib = ia + 1 if inter else ia + rot // 2
+    y = z.clone()
+    y[..., ia] = z[..., ia] * c[:, None] - z[..., ib] * s[:, None]
+    y[..., ib] = z[..., ib] * c[:, None] + z[..., ia] * s[:, None]
+    mag = z.abs()
+    mag[..., ia] = mag[..., ib] = z[..., ia].abs() + z[..., ib].abs()
+    return y, mag
+
+
+@pytest.mark.parametrize("case", RING, ids=str)
+def test_many_tokens_forward_and_backward(case):
+    tokens, hq, hk, dim, rot, inter, xin, yout = case
+    rng = np.random.default_rng(tokens)
+    q, k = projection(rng, tokens, (hq, hk), dim, xin)
+    gq, gk = projection(rng, tokens, (hq, hk), dim, yout)
+    cos, sin, _, _ = tables(300, rot)
+    pos = torch.from_numpy(rng.integers(0, 300, tokens).astype(np.int32)).cuda()
+    c, s = cos[pos.long()].double(), sin[pos.long()].double()
+    w = [torch.from_numpy((1 + 0.3 * rng.standard_normal(dim)).astype(np.float32)).cuda(), None]
+    outs = [torch.full((tokens, h, dim), 7.0, dtype=yout, device="cuda") for h in (hq, hk)]
+    A.qk_norm_rope(q, k, cos, sin, pos, *outs, w[0], w[1], eps=1e-5, interleaved=inter)
+    grads = [torch.full((tokens, h, dim), 7.0, dtype=yout, device="cuda") for h in (hq, hk)]
+    dw = torch.full((dim,), 7.0, device="cuda")
+    ws = A.norm_rope_workspace(dim)
+    A.qk_norm_rope_backward(q, k, gq, gk, cos, sin, pos, *grads, dw, None, ws, w[0], None, eps=1e-5, interleaved=inter)
+    first = [g.clone() for g in grads] + [dw.clone()]
+    A.qk_norm_rope_backward(q, k, gq, gk, cos, sin, pos, *grads, dw, None, ws, w[0], None, eps=1e-5, interleaved=inter)
+    assert all(torch.equal(a, b) for a, b in zip(first, grads + [dw]))       # the same bits again
+    for x, y, g, dx, wt in ((q, outs[0], gq, grads[0], w[0]), (k, outs[1], gk, grads[1], w[1])):
+        want, mag = _plain(x, wt, c, s, rot, inter, 1e-5)
+        assert bool(((y.double() - want).abs() <= UNIT[yout] * want.abs() + TINY[yout] + 32 * E32 * mag).all())
+        u, um = _plain(g, None, c, -s, rot, inter, 0.0)
+        if wt is None:
+            assert bool(((dx.double() - u).abs() <= UNIT[yout] * u.abs() + TINY[yout] + 64 * E32 * um).all())
+            continue
+        xd = x.double()
+        r = torch.rsqrt(xd.square().mean(-1, keepdim=True) + 1e-5)
+        n, gw = xd * r, u * wt.double()
+        want = r * (gw - n * (gw * n).mean(-1, keepdim=True))
+        mag = r * (um * wt.double().abs() + n.abs() * (um * wt.double().abs() * n.abs()).mean(-1, keepdim=True))
+        assert bool(((dx.double() - want).abs() <= UNIT[yout] * want.abs() + TINY[yout] + 64 * E32 * mag).all())
+        # chains of at most tokens * heads / (148 * 16) + 32 + 148 + 17 additions, and 32 roundings of a term
+        chain = tokens * hq / (148 * 16) + 32 + 148 + 17 + 32
+        assert bool(((dw.double() - (u * n).sum((0, 1))).abs() <= chain * E32 * (um * n.abs()).sum((0, 1))).all())
+
+
+@pytest.mark.parametrize("dim,page,dtype,rot", [(128, 16, BF16, 128), (64, 5, F16, 32), (96, 24, BF16, 0)])
+def test_append_of_many_tokens_equals_the_same_tokens_a_few_at_a_time(dim, page, dtype, rot):
+    rng = np.random.default_rng(dim)
+    seqs = [(900, 1500), (0, 7), (1, 1), (2200, 2200), (130, 100), (769, 800)]      # the fifth: 30 tokens without a place
+    hq, hk = 3, 2
+    kc, vc, cu, kv, table = make_cache(rng, seqs, hk, dim, page, dtype, "thd", fill=3.0)
+    n = int(cu[-1])
+    q, k, v = projection(rng, n, (hq, hk, hk), dim, F32)
+    cos, sin, _, _ = tables(3000, rot)
+    w = torch.from_numpy((1 + 0.3 * rng.standard_normal(dim)).astype(np.float32)).cuda()
+    whole = [torch.full((n, hq, dim), 7.0, dtype=dtype, device="cuda"), kc.clone(), vc.clone()]
+    dev = [torch.from_numpy(x).cuda() for x in (cu, kv, table)]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    A.paged_append(A.PagedCache(whole[1], whole[2]), k, v, *dev, cos, sin, w, q=q, q_out=whole[0], q_weight=w, status=status)
+    few = [torch.full((n, hq, dim), 7.0, dtype=dtype, device="cuda"), kc.clone(), vc.clone()]
+    cache = A.PagedCache(few[1], few[2])
+    for b, (new, keys) in enumerate(seqs):
+        for t in range(0, new, 97):
+            m = min(97, new - t)
+            lo = int(cu[b]) + t
+            at = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+            length = torch.tensor([keys - new + t + m], dtype=torch.int32, device="cuda")
+            A.paged_append(cache, k[lo:lo + m], v[lo:lo + m], at, length, dev[2][b:b + 1], cos, sin, w, q=q[lo:lo + m], q_out=few[0][lo:lo + m],
+                           q_weight=w, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    assert all(torch.equal(a, b) for a, b in zip(whole, few))
+
+
 def test_backward_repeats_bit_for_bit_over_many_blocks():
     rng = np.random.default_rng(5)
     q, k = projection(rng, 3000, (6, 2), 128, F32)
