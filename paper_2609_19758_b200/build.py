@@ -9,6 +9,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -39,21 +41,29 @@ def build(verbose: bool = False, force: bool = False, bounds: bool = False) -> s
     out = LIB_BOUNDS if bounds else LIB
     if not force and not needs_build(out):
         return out
-    cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
-           "-I", os.path.join(HERE, "csrc")]
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    flags = arch + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
+                    "-I", os.path.join(HERE, "csrc")]
     # extra flags, e.g. FPSK_NVCC_FLAGS=-DFPSK_MEASURE for the build that records in-kernel time stamps
-    cmd += os.environ.get("FPSK_NVCC_FLAGS", "").split()
+    flags += os.environ.get("FPSK_NVCC_FLAGS", "").split()
     if bounds:
-        cmd += ["-DFPSK_DEBUG_BOUNDS"]
+        flags += ["-DFPSK_DEBUG_BOUNDS"]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += sources() + ["-o", out]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed")
+        flags += ["-Xptxas", "-v"]
+
+    def run(cmd):
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if verbose or res.returncode != 0:
+            sys.stderr.write(res.stdout + res.stderr)
+        if res.returncode != 0:
+            raise RuntimeError("nvcc failed")
+
+    with tempfile.TemporaryDirectory() as tmp:
+        # one nvcc per source file, side by side
+        objs = [os.path.join(tmp, os.path.basename(f) + ".o") for f in sources()]
+        with ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as pool:
+            list(pool.map(lambda fo: run([nvcc_path()] + flags + ["-c", fo[0], "-o", fo[1]]), zip(sources(), objs)))
+        run([nvcc_path()] + arch + ["-shared", "-Xcompiler", "-fPIC"] + objs + ["-o", out])
     return out
 
 
