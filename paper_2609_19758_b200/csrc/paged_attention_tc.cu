@@ -385,9 +385,6 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int tile_tokens = ga.tile_tokens, item_tokens = tile_tokens * Cfg::kQTiles;
 
-    if (MODE != kCopies && tid == 351) ga.records[blockIdx.x].parts = 0;
-    if (tid >= 352 && tid < 355)
-        asm volatile("prefetch.tensormap [%0];" ::"l"(tid == 352 ? &map_q : tid == 353 ? &map_k : &map_v) : "memory");
     if (tid == 0) {
         mbar_init(smem_u32(&sh->q_full), 1);
         mbar_init(smem_u32(&sh->q_empty), 2);
@@ -408,6 +405,10 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
         tc_alloc(smem_u32(&sh->tmem), 512);
         tc_relinquish();
     }
+    asm volatile("griddepcontrol.wait;" ::: "memory");                 // what is above touches no global memory
+    if (MODE != kCopies && tid == 351) ga.records[blockIdx.x].parts = 0;
+    if (tid >= 352 && tid < 355)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(tid == 352 ? &map_q : tid == 353 ? &map_k : &map_v) : "memory");
 
     // ---- this CTA's range: key tiles of every sequence (in the ring, before it is used), their total, the first item
     uint2 *seq_work = reinterpret_cast<uint2 *>(smem + Cfg::kQTiles * Cfg::kTile);    // key tiles and items of one key head
@@ -1221,19 +1222,24 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
         FPSK_CUDA_OK(cudaFuncSetAttribute(attention_tc_kernel<T, DP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
         prepared.fetch_or(bit, std::memory_order_release);
     }
-    attention_tc_kernel<T, DP, MODE><<<ctas, kTcaThreads, Cfg::kSmem, st>>>(g, mq, mk, mv);
+    // Both launches may begin before the kernel in front has ended (they wait for it before they read): what a launch costs passes
+    // behind it.
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kTcaThreads);
+    cfg.dynamicSmemBytes = Cfg::kSmem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_tc_kernel<T, DP, MODE>, g, mq, mk, mv));
     FPSK_LAUNCH_CHECK();
     if constexpr (MODE != kCopies) {
-        // the join's launch overlaps the end of the kernel before it
-        cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)ctas, Cfg::kRows / 8);
         cfg.blockDim = dim3(256);
-        cfg.stream = st;
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr.val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
+        cfg.dynamicSmemBytes = 0;
         FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_join_kernel<T, DP, MODE>, g));
         FPSK_LAUNCH_CHECK();
     }
