@@ -2,8 +2,7 @@
 //
 // What bounds them is HBM, and what kept the plain form (norm_rope.cu) from it is what a thread has to hold and to compute to
 // have enough loads in flight.  Here one warp copies whole tokens - every kind's heads, the rows of the rotation tables - into a
-// ring of stages in shared memory, up to 200 KB in flight on every SM whatever the other warps do; sixteen warps read them from
-// there.  Where the new tokens go in the cache is looked up by the copying warp as well, 32 tokens at a time, so that the chain of
+// ring of stages in shared memory, up to 200 KB in flight on every SM whatever the other warps do; the others read them from there.  Where the new tokens go in the cache is looked up by the copying warp as well, 32 tokens at a time, so that the chain of
 // dependent loads (sequence, length, page) passes once for 32.
 #include "norm_rope.cuh"
 
@@ -12,8 +11,11 @@
 namespace fpsk {
 
 enum { kOpRope = 0, kOpAppend = 1, kOpGrad = 2 };
-constexpr int kRingThreads = 544;                // 16 warps of heads, one copying
-constexpr int kRingWorkers = 512, kRingMost = 8; // stages
+// Threads of heads, and one warp that copies.  The backward pass (92 registers) takes 512; the others 512, 640 or 768, the fewest with
+// which a stage takes the fewest rounds: 11112 tokens of 96 heads in 140 us with 512 (three rounds) and in 130 with 768 (two), 4096 tokens
+// of 64 heads in 44 us with 512 and in 48 with 768 (two rounds both).
+constexpr int kRingWorkers = 512, kRingMostWorkers = 768;
+constexpr int kRingMost = 8;                     // stages
 constexpr int kRingBytes = 200 * 1024, kRingStage = 32 * 1024;
 
 struct RingPiece {
@@ -29,6 +31,7 @@ struct RingArgs {
     int token_bytes, row_bytes;        // a token's block, and what of it the pieces fill; behind: cos, sin
     int cos_at, table_bytes;           // bytes of a row of a table
     int log_tokens, stages, stage_bytes;
+    int workers;
     unsigned int head_magic;           // ceil(2^32 / heads): a vector's token by a multiplication
     int n_all;
     long long n_tok, steps;
@@ -46,9 +49,9 @@ struct RingToken {                     // what the copying warp found out about 
 };
 
 template <typename X, typename Y, int L, int OP>
-__global__ void __launch_bounds__(kRingThreads, 1) norm_rope_ring_kernel(const __grid_constant__ RingArgs g)
+__global__ void __launch_bounds__((OP == kOpGrad ? kRingWorkers : kRingMostWorkers) + 32, 1) norm_rope_ring_kernel(const __grid_constant__ RingArgs g)
 {
-    constexpr int S = kRingWorkers / L;
+    const int workers = OP == kOpGrad ? kRingWorkers : g.workers, S = workers / L;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ unsigned long long full[kRingMost], empty[kRingMost];
     __shared__ RingToken info[kRingMost][32];
@@ -58,14 +61,14 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_rope_ring_kernel(const _
     if (tid == 0) {
         for (int s = 0; s < g.stages; ++s) {
             mbar_init(smem_u32(&full[s]), 1);
-            mbar_init(smem_u32(&empty[s]), kRingWorkers / 32);
+            mbar_init(smem_u32(&empty[s]), workers / 32);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
     bool ok = true;
 
-    if (warp == kRingWorkers / 32) {
+    if (warp == workers / 32) {
         // ------------------------------------------------------------ copies
         int slot = 0, in_batch = 32;
         uint32_t phase = 0;
@@ -288,7 +291,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_rope_ring_kernel(const _
     if (!last) return;
     float *sums = reinterpret_cast<float *>(smem);
     for (int k = 0; k < 2; ++k)
-        if (g.d.h[k].dw) sum_rows<kRingThreads>(g.d.part + k * g.dim, 2 * g.dim, (int)gridDim.x, g.dim, sums, g.d.h[k].dw);
+        if (g.d.h[k].dw) sum_rows<kRingWorkers + 32>(g.d.part + k * g.dim, 2 * g.dim, (int)gridDim.x, g.dim, sums, g.d.h[k].dw);
     if (tid == 0) *g.d.count = 0u;
 }
 
@@ -320,7 +323,7 @@ static bool plan_ring(RingArgs &g)
     g.head_magic = (unsigned int)((0x100000000ULL + g.n_all - 1) / g.n_all);
     return g.stages >= 2 && g.n_all >= 2 && g.n_all <= 2048 && g.steps >= 3 * kRingBlocks;
 }
-template <typename X, typename Y, int L, int OP> static fpsk_status launch_ring(const RingArgs &g, cudaStream_t st)
+template <typename X, typename Y, int L, int OP> static fpsk_status launch_ring(RingArgs &g, cudaStream_t st)
 {
     static std::atomic<unsigned long long> prepared{0};               // one bit per device
     int dev = 0;
@@ -330,15 +333,19 @@ template <typename X, typename Y, int L, int OP> static fpsk_status launch_ring(
         FPSK_CUDA_OK(cudaFuncSetAttribute(norm_rope_ring_kernel<X, Y, L, OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes));
         prepared.fetch_or(bit, std::memory_order_release);
     }
-    norm_rope_ring_kernel<X, Y, L, OP><<<kRingBlocks, kRingThreads, kRingBytes, st>>>(g);
+    const int vectors = g.n_all << g.log_tokens;
+    g.workers = kRingWorkers;
+    for (int w = kRingWorkers; OP != kOpGrad && w <= kRingMostWorkers; w += 128)
+        if ((vectors + w / L - 1) / (w / L) < (vectors + g.workers / L - 1) / (g.workers / L)) g.workers = w;
+    norm_rope_ring_kernel<X, Y, L, OP><<<kRingBlocks, g.workers + 32, kRingBytes, st>>>(g);
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
-template <typename X, typename Y, int OP> static fpsk_status launch_ring_dim(const RingArgs &g, cudaStream_t st)
+template <typename X, typename Y, int OP> static fpsk_status launch_ring_dim(RingArgs &g, cudaStream_t st)
 {
     return g.dim <= 64 ? launch_ring<X, Y, 8, OP>(g, st) : g.dim <= 128 ? launch_ring<X, Y, 16, OP>(g, st) : launch_ring<X, Y, 32, OP>(g, st);
 }
-template <int OP> static fpsk_status launch_ring_typed(const RingArgs &g, int in, int out, cudaStream_t st)
+template <int OP> static fpsk_status launch_ring_typed(RingArgs &g, int in, int out, cudaStream_t st)
 {
 #define FPSK_IN(Y)                                                                                                            \
     (in == FPSK_ELEM_FP32 ? launch_ring_dim<float, Y, OP>(g, st)                                                              \
