@@ -94,7 +94,7 @@ typedef struct {
 /* The sequences of one step.  Sequence b has the new tokens cu_q[b] .. cu_q[b+1] - 1 of the packed token axis and
  * kv_len[b] keys, the new tokens' own ones last: token t sits at p = kv_len[b] - (cu_q[b+1] - t), in slot p % page_size
  * of page block_table[b][p / page_size].  New tokens beyond kv_len (p < 0) have no place: they are not written and
- * attend to nothing.  Lengths of zero are allowed. */
+ * attend to nothing.  Lengths of zero are allowed.  Rows of the token axis behind cu_q[n_seqs] belong to no sequence. */
 typedef struct {
     const int32_t *cu_q;         /* device, n_seqs + 1, ascending from 0                               */
     const int32_t *kv_len;       /* device, n_seqs                                                     */
@@ -117,11 +117,16 @@ fpsk_status fpsk_paged_append(const fpsk_paged_cache *cache, const fpsk_paged_ba
  *   out_t = sum_j softmax_j(scale q_t . k_j) v_j over the keys j that token t (at position p) may see:
  *   j < kv_len[b];  j <= p when causal;  j >= p - window when window >= 0.
  * A token that may see nothing gets zeros and lse = -inf.  Query head h reads key head h / (n_heads_q / cache->n_heads).
- * Keys that no token may see are never used, whatever the memory holds (table entries behind the last page, NaN).
+ * Keys that no token of a sequence may see are never used, whatever the memory holds (table entries behind the last page,
+ * NaN).  A NaN or infinite value among keys that some tokens see and others do not can reach the others.  Rows that belong to no
+ * sequence are left alone.
  *   q, out     device, cache->type, (token, head) strides; lse: device FP32 n_tokens x n_heads_q, or NULL
- *   max_q_len, max_kv_len   upper bounds of the lengths: they choose the tiling, not the result's meaning
- *   workspace  fpsk_paged_attention_workspace_bytes() for the current device, 256-byte aligned; one call at a time
- * head_dim: a multiple of 8 up to FPSK_MAX_HEAD_DIM. */
+ *   max_q_len, max_kv_len   upper bounds of the lengths, known to the host: they choose tiles and grid (a bound that is
+ *              too small costs time only)
+ *   workspace  fpsk_paged_attention_workspace_bytes() for the current device, 256-byte aligned, initialised once by
+ *              fpsk_attention_workspace_init (and again after a FPSK_ERR_TIMEOUT); one call at a time
+ * head_dim: a multiple of 8 up to FPSK_MAX_HEAD_DIM.  Heads of up to 128 channels, up to 128 query heads to a key head, pages of a
+ * multiple of 8 tokens and 16-byte aligned rows run on the tensor cores; the rest on a plain kernel. */
 typedef struct {
     const void *q;
     void *out;

@@ -113,7 +113,7 @@ __device__ __forceinline__ void key_range(const AttnArgs &g, long long p, int kv
 // paged_attention_tc.cu
 bool attention_tc_takes(const AttnArgs &g);
 size_t attention_tc_workspace_bytes();
-fpsk_status attention_tc_launch(const AttnArgs &g, int type, int max_q_len, void *ws, cudaStream_t st);
+fpsk_status attention_tc_launch(const AttnArgs &g, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st);
 
 // Checks shared by the entry points (attention_api.cu).
 bool elem_ok(int type);

@@ -26,8 +26,9 @@ __global__ void __launch_bounds__(32 * kPlainWarps) attention_rows_kernel(const 
         seq += before;
         if (before < (int)blockDim.x) break;
     }
+    if (seq >= g.n_seqs) return;
     int lo = 0, hi = 0;
-    if (seq < g.n_seqs) key_range(g, (long long)g.kv_len[seq] - (g.cu_q[seq + 1] - tok), g.kv_len[seq], lo, hi);
+    key_range(g, (long long)g.kv_len[seq] - (g.cu_q[seq + 1] - tok), g.kv_len[seq], lo, hi);
     const T *qp = static_cast<const T *>(g.q) + tok * g.qts + head * g.qhs;
     float q[C], o[C];
 #pragma unroll
@@ -119,7 +120,7 @@ extern "C" fpsk_status fpsk_paged_attention(const fpsk_paged_cache *cache, const
     g.status = d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (attention_tc_takes(g))
-        return attention_tc_launch(g, cache->type, a->max_q_len, workspace, st);
+        return attention_tc_launch(g, cache->type, a->max_q_len, a->max_kv_len, workspace, st);
     const dim3 grid((unsigned)g.n_tokens, (unsigned)g.hq);
     if (cache->type == FPSK_ELEM_FP16) attention_rows_kernel<__half><<<grid, 32 * kPlainWarps, 0, st>>>(g);
     else attention_rows_kernel<__nv_bfloat16><<<grid, 32 * kPlainWarps, 0, st>>>(g);

@@ -31,10 +31,6 @@ constexpr int kPairKeys = 64;                    // keys of a PAIR worker's step
 constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8 and 11: their MMAs, 9 and 10: loaders
 constexpr int kHalfBytes = 128 * 128;            // 128 rows of one 64-channel half of a tile
 constexpr int kTcaMaxSeqs = 16384;
-#ifndef FPSK_POLY
-#define FPSK_POLY 0
-#endif
-constexpr int kPoly = FPSK_POLY;                 // of eight pairs of exponentials, computed on the FMA pipe
 constexpr int kItemCost = 2;                     // an item's beginning and end, in key tiles
 constexpr float kMostSum = 4096.f;               // of a step's weights, before a row's reference maximum is renewed
 
@@ -175,23 +171,6 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-// 2^x on the FMA pipe, two at a time: x = n + f with n the nearest whole number, 2^f by the polynomial of degree 4 that minimises
-// the largest relative error on [-1/2, 1/2] (Remez exchange: 2.6e-6; evaluated in FP32 2.7e-6), n added to the exponent.  Within
-// [-126, 127]; beyond, the value at the end.  NaN comes out as FLT_MAX or NaN, which no sum of weights passes for small.
-__device__ __forceinline__ float2 ex2_poly(float2 x)
-{
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;\n\tmin.NaN.f32 %0, %0, 0f42FE0000;" : "+f"(x.x));
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;\n\tmin.NaN.f32 %0, %0, 0f42FE0000;" : "+f"(x.y));
-    const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);   // 1.5 * 2^23
-    const float2 t = __fadd2_rn(x, magic);
-    const float2 f = __ffma2_rn(__fadd2_rn(t, unmagic), make_float2(-1.f, -1.f), x);
-    float2 p = __ffma2_rn(make_float2(0.009570102207362652f, 0.009570102207362652f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
-    p = __ffma2_rn(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
-    p = __ffma2_rn(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
-    p = __ffma2_rn(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 // maxima that pass a NaN on
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -603,7 +582,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             const int pg = __shfl_sync(0xFFFFFFFFu, page, box), at_row = __shfl_sync(0xFFFFFFFFu, page_row, box);
                             if (elect_one()) {
                                 if (tl.map == kGroupsOfAllPages)
-                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, kvh, (pg * page_size + at_row) >> 3, full);
+                                    tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, kvh, pg * (page_size >> 3) + (at_row >> 3), full);
                                 else if (tl.map == kHeadsOfAllPages)
                                     tma_load_5d(dst + box * box_bytes, map, 0, 0, 0, at_row >> 3, pg * g.hk + kvh, full);
                                 else
@@ -883,9 +862,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             for (int i = 0; i < 16; ++i) {
                                 float2 x = make_float2(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1]));
                                 x = __ffma2_rn(x, sc, nb);
-                                // (PAIR: the special-function unit alone would bound it)
-                                const bool poly = PAIR && ((i + 1) * kPoly) / 8 != (i * kPoly) / 8;
-                                x = poly ? ex2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
+                                x = make_float2(ex2(x.x), ex2(x.y));
                                 sum[i & 1] = __fadd2_rn(sum[i & 1], x);
                                 p[c * 16 + i] = round_pair<T>(x.x, x.y);
                             }
@@ -926,7 +903,6 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
                 tc_fence_after();
             }
-            if (m == -INFINITY) l = 0.f;                               // (hidden scores may have left 2^-126)
             // ---- the item's end: finished here, or a partial result
             const bool whole = n == it.units;
             const bool any = it.hi > it.lo, have1 = any && n > 1;     // SPLIT: outputs of the two workers
@@ -1156,16 +1132,20 @@ bool attention_tc_takes(const AttnArgs &g)
            aligned16(g.out, g.ots, g.ohs, 0) && aligned16(g.k, g.kps, g.kts, g.khs) && aligned16(g.v, g.vps, g.vts, g.vhs);
 }
 
-template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnArgs &a, int type, void *ws, cudaStream_t st)
+template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnArgs &a, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st)
 {
     using Cfg = Tca<DP, MODE>;
     constexpr bool PAIR = MODE == kPair;
-    const int ctas = sm_count();
-    if (ctas < 1) return FPSK_ERR_CUDA;
-    if (ctas > (int)(kAttnSyncBytes / sizeof(unsigned int))) return FPSK_ERR_PARAM;
+    const int sms = sm_count();
+    if (sms < 1) return FPSK_ERR_CUDA;
+    if (sms > (int)(kAttnSyncBytes / sizeof(unsigned int))) return FPSK_ERR_PARAM;
     TcaArgs g;
     g.a = a;
     g.tile_tokens = Cfg::kTileRows / a.group;
+    // a CTA on every SM, or for every key tile where the lengths promise fewer
+    const int item_tokens = g.tile_tokens * Cfg::kQTiles;
+    const double tiles = (double)a.n_seqs * a.hk * ((max_q_len + item_tokens - 1) / item_tokens) * ((max_kv_len + kKeysPerTile - 1) / kKeysPerTile);
+    const int ctas = tiles < 1.0 ? 1 : tiles < sms ? (int)tiles : sms;
     for (g.box_log = 3; g.box_log < 7 && a.page_size % (2 << g.box_log) == 0;) ++g.box_log;
     g.wide_out = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.ots % 16 == 0 && a.ohs % 16 == 0 && a.dim % 16 == 0;
     g.tile_pages = kKeysPerTile / a.page_size;
@@ -1174,9 +1154,9 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     g.arrived = reinterpret_cast<unsigned int *>(p);
     p += kAttnSyncBytes;
     g.records = reinterpret_cast<SplitRecord *>(p);
-    p += align_up((size_t)ctas * sizeof(SplitRecord), 256);
+    p += align_up((size_t)sms * sizeof(SplitRecord), 256);
     g.part_o = reinterpret_cast<float *>(p);
-    p += (size_t)2 * ctas * kMaxPartRows * kMaxDP * sizeof(float);
+    p += (size_t)2 * sms * kMaxPartRows * kMaxDP * sizeof(float);
     g.part_ml = reinterpret_cast<float2 *>(p);
     // strides of dimensions of one element are never used, but the encoder wants them valid
     auto bytes = [](long long s, long long n) { return (cuuint64_t)(n > 1 && s > 0 ? s * 2 : 16); };
@@ -1247,12 +1227,14 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
 }
 
 // COPIES while the rows of every sequence's new tokens fit a quarter of the TMEM lanes, SPLIT while they fit one tile, else PAIR.
-fpsk_status attention_tc_launch(const AttnArgs &a, int type, int max_q_len, void *ws, cudaStream_t st)
+fpsk_status attention_tc_launch(const AttnArgs &a, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st)
 {
-    const long long rows = (long long)(max_q_len < 1 ? 1 : max_q_len) * a.group;
+    if (max_q_len < 1) max_q_len = 1;
+    if (max_kv_len < 1) max_kv_len = 1;
+    const long long rows = (long long)max_q_len * a.group;
 #define FPSK_TCA(TT, DD)                                                        \
-    (rows <= 32 ? launch_tc<TT, DD, kCopies>(a, type, ws, st)                   \
-                : rows <= kRowsPerTile ? launch_tc<TT, DD, kSplit>(a, type, ws, st) : launch_tc<TT, DD, kPair>(a, type, ws, st))
+    (rows <= 32 ? launch_tc<TT, DD, kCopies>(a, type, max_q_len, max_kv_len, ws, st)                   \
+                : rows <= kRowsPerTile ? launch_tc<TT, DD, kSplit>(a, type, max_q_len, max_kv_len, ws, st) : launch_tc<TT, DD, kPair>(a, type, max_q_len, max_kv_len, ws, st))
 #define FPSK_TCA_DIM(TT) (a.dim <= 64 ? FPSK_TCA(TT, 64) : FPSK_TCA(TT, 128))
     return type == FPSK_ELEM_FP16 ? FPSK_TCA_DIM(__half) : FPSK_TCA_DIM(__nv_bfloat16);
 #undef FPSK_TCA_DIM
