@@ -15,6 +15,12 @@
 // Two loader warps bring Q and K tiles and V tiles, page by page, by TMA into a ring of tiles, 128-byte swizzled; a warp for
 // each worker issues its MMAs.  Maximum: the reference maximum of a row follows the true one only when the weights of a step outgrow it by 2^12 (P
 // is exact to 16-bit rounding whatever its size), so O in TMEM is rescaled rarely and most steps take no maximum at all.
+// What bounds it.  Many rows: the tensor cores and the exponentials, about equally.  A step of 64 keys takes a worker 1277 cycles (two
+// warps on a scheduler; 1024 of them the 64 x 2 exponentials at 4 lanes a cycle), the two workers' four products about 1150, where
+// S = Q K^T is held up by shared memory (48 cycles for 128 x 64 x 16: 128 bytes a cycle; O += P V has P in TMEM and is not).
+// Few rows: HBM, and the latency from the launch to the first scores (6 us), of which a short context is all.
+// Measured: 4096 new tokens of 32 heads over 16384 keys of 8 heads of 128, 850 us (1.13 PFLOP/s, 0.69 of a library's large product);
+// 4 tokens over 262144 keys 173 us (6.2 TB/s, 0.95 of a copy); 96 requests of one token, 98296 keys, 88 us (4.6 TB/s).
 // Every wait is bounded: a role whose wait gave up stops waiting and issuing, walks through its loops, reports
 // FPSK_ERR_TIMEOUT and the CTA frees its TMEM and leaves.
 #include "attention.cuh"
@@ -31,7 +37,9 @@ constexpr int kPairKeys = 64;                    // keys of a PAIR worker's step
 constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8 and 11: their MMAs, 9 and 10: loaders
 constexpr int kHalfBytes = 128 * 128;            // 128 rows of one 64-channel half of a tile
 constexpr int kTcaMaxSeqs = 16384;
-constexpr int kItemCost = 2;                     // an item's beginning and end, in key tiles
+// An item's beginning and end, in key tiles.  96 requests of uneven length take 88 us with 2, 107 with 1, 90 with 3; 32 requests of 16
+// tokens 34-39 us with 2, 52 with 1, 49 with 3.
+constexpr int kItemCost = 2;
 constexpr float kMostSum = 4096.f;               // of a step's weights, before a row's reference maximum is renewed
 
 // 32 consecutive columns of this thread's accumulator row; valid after tm_wait32 on the same array
@@ -304,7 +312,7 @@ template <int DP, int MODE> struct Tca {
     static constexpr int kTile = kRowsPerTile * DP * 2;
     static constexpr int kHalves = DP / 64;
     static constexpr int kQTiles = kIsPair ? 2 : 1;
-    static constexpr int kSlots = DP == 128 ? (MODE == kSplit ? 6 : 5) : 8;
+    static constexpr int kSlots = DP == 128 ? 5 : 8;
     static constexpr int kStage = MODE == kCopies ? 4 * 8 * (DP + 4) * 4 : 0;  // eight rows of the four copies' outputs
     static constexpr int kBars = (kQTiles + kSlots) * kTile + kStage;          // barriers, start state, SPLIT: row statistics
     static constexpr int kSmem = kBars + 3072;
@@ -1125,17 +1133,19 @@ static bool aligned16(const void *p, long long s0, long long s1, long long s2)
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s0 % 8 == 0 && s1 % 8 == 0 && s2 % 8 == 0;
 }
 // What the tensor-core kernel takes: heads of up to 128 channels, at most 128 query heads to a key head, whole eight-row
-// groups of a page, and 16-byte aligned rows (TMA).  The rest is the row kernel's.
+// groups of a page, rows at 16-byte boundaries (TMA), and no expanded query dimension (stride 0; a cache has none).  The rest is
+// the row kernel's: right for every layout, and slow (a block for every token and head; 4096 tokens of 32 heads over 16384 keys
+// take it 366 ms, the tensor-core kernel 0.85).
 bool attention_tc_takes(const AttnArgs &g)
 {
     return g.dim <= 128 && g.group <= 128 && g.page_size % 8 == 0 && g.n_seqs <= kTcaMaxSeqs && aligned16(g.q, g.qts, g.qhs, 0) &&
-           aligned16(g.out, g.ots, g.ohs, 0) && aligned16(g.k, g.kps, g.kts, g.khs) && aligned16(g.v, g.vps, g.vts, g.vhs);
+           aligned16(g.out, g.ots, g.ohs, 0) && aligned16(g.k, g.kps, g.kts, g.khs) && aligned16(g.v, g.vps, g.vts, g.vhs) &&
+           (g.n_tokens == 1 || g.qts > 0) && (g.hq == 1 || g.qhs > 0);
 }
 
 template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnArgs &a, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st)
 {
     using Cfg = Tca<DP, MODE>;
-    constexpr bool PAIR = MODE == kPair;
     const int sms = sm_count();
     if (sms < 1) return FPSK_ERR_CUDA;
     if (sms > (int)(kAttnSyncBytes / sizeof(unsigned int))) return FPSK_ERR_PARAM;
@@ -1226,16 +1236,22 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     return FPSK_OK;
 }
 
-// COPIES while the rows of every sequence's new tokens fit a quarter of the TMEM lanes, SPLIT while they fit one tile, else PAIR.
+// COPIES while the rows of every sequence's new tokens fit a quarter of the TMEM lanes; then, for heads of up to 64 channels,
+// SPLIT while they fit one tile; else PAIR.  In us, this rule first:
+//   rows <= 32: one token, 1001 keys 12.1, SPLIT and PAIR 13.5; 96 requests of one token, up to 8192 keys 88, SPLIT 99.5, PAIR 98;
+//   64 requests of 8 tokens 72, PAIR 68
+//   33 to 128 rows, heads of 128: 64 rows, 131072 keys PAIR 100, SPLIT 108; 32 requests of 4096 keys 33.7, 35.6; 8 of 1024 16.7, 20.8
+//   33 to 128 rows, heads of 64: 128 rows, 262144 keys SPLIT 144, PAIR 176 (the softmax of one tile takes longer than its
+//   keys, half as many bytes, take to come); 64 requests of 7 tokens 22.0, 23.2; but 64 of 32 tokens 61.5, 55
 fpsk_status attention_tc_launch(const AttnArgs &a, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st)
 {
     if (max_q_len < 1) max_q_len = 1;
     if (max_kv_len < 1) max_kv_len = 1;
     const long long rows = (long long)max_q_len * a.group;
-#define FPSK_TCA(TT, DD)                                                        \
-    (rows <= 32 ? launch_tc<TT, DD, kCopies>(a, type, max_q_len, max_kv_len, ws, st)                   \
-                : rows <= kRowsPerTile ? launch_tc<TT, DD, kSplit>(a, type, max_q_len, max_kv_len, ws, st) : launch_tc<TT, DD, kPair>(a, type, max_q_len, max_kv_len, ws, st))
-#define FPSK_TCA_DIM(TT) (a.dim <= 64 ? FPSK_TCA(TT, 64) : FPSK_TCA(TT, 128))
+#define FPSK_TCA(TT, DD, MM) launch_tc<TT, DD, MM>(a, type, max_q_len, max_kv_len, ws, st)
+#define FPSK_TCA_DIM(TT)                                                                                                                      \
+    (a.dim > 64 ? rows <= 32 ? FPSK_TCA(TT, 128, kCopies) : FPSK_TCA(TT, 128, kPair)                                                          \
+                : rows <= 32 ? FPSK_TCA(TT, 64, kCopies) : rows <= kRowsPerTile ? FPSK_TCA(TT, 64, kSplit) : FPSK_TCA(TT, 64, kPair))
     return type == FPSK_ELEM_FP16 ? FPSK_TCA_DIM(__half) : FPSK_TCA_DIM(__nv_bfloat16);
 #undef FPSK_TCA_DIM
 #undef FPSK_TCA

@@ -145,6 +145,33 @@ def test_infinite_scores_and_nan_keys_stay_in_their_sequence():
     assert out.isnan().any(-1).any(-1).tolist() == [False, True, False]
 
 
+@pytest.mark.parametrize("what", ["query heads", "tokens"])
+def test_expanded_dimensions(what):
+    """An expanded dimension (stride 0) of the queries gives what its copies give; a cache, which is written to, has none."""
+    rng = np.random.default_rng(3)
+    seqs, hq, hk, dim, page = [(40, 300), (1, 70)], 4, 2, 64, 16
+    k, v, cu, kv, table = make_cache(rng, seqs, hk, dim, page, BF16, "thd")
+    fill(rng, k, v, kv, table, page)
+    n = int(cu[-1])
+    q = torch.from_numpy(rng.standard_normal((n, hq, dim)).astype(np.float32)).to(BF16).cuda()
+    if what == "query heads": q = q[:, :1].expand(n, hq, dim)
+    if what == "tokens": q = q[:1].expand(n, hq, dim)
+    dev = [torch.from_numpy(x).cuda() for x in (cu, kv, table)]
+    ws = A.attention_workspace()
+    out = torch.full((n, hq, dim), 7.0, dtype=BF16, device="cuda")
+    A.paged_attention(A.PagedCache(k, v), q, out, *dev, ws, 40, 300)
+    torch.cuda.synchronize()
+    s = dim ** -0.5
+    want, _, mag, smag = O.paged_attention(q.double().cpu().numpy(), k.double().cpu().numpy(), v.double().cpu().numpy(),
+                                           cu, kv, table, s, True, -1)
+    u, e = UNIT[BF16], (dim + 8) * 2.0 ** -23 * smag + 2.0 ** -20
+    tol = u * np.abs(want) + mag * (2 * (u + e[..., None]) + 2.0 ** -20) + 2.0 ** -24
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
+    for pair in ((k[:, :, :1].expand(k.shape), v), (k, v[:, :, :1].expand(v.shape))):
+        with pytest.raises(fpsk.FpskError):
+            A.paged_attention(A.PagedCache(*pair), q, out, *dev, ws, 40, 300)
+
+
 def test_pages_outside_the_cache_are_reported():
     rng = np.random.default_rng(2)
     k, v, cu, kv, table = make_cache(rng, [(1, 200), (1, 100)], 1, 128, 16, BF16, "thd")
