@@ -697,17 +697,25 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                 first_item = false;
                 all_wait(smem_u32(&sh->q_full), q_phase);
                 q_phase ^= 1u;
+                // The tile of queries is free behind the item's last S: the next item's comes (and its V tiles behind it) while this
+                // one's weights, outputs and end are still to be done.
                 if constexpr (PAIR) {
                     // S is two steps ahead of P V, so that a softmax never waits for its scores
                     int sa, sb;
                     worker_steps(g, it, w, tile_tokens, 2 * tile_a, 2 * tile_b, sa, sb);
                     sa = uniform(sa);
                     sb = uniform(sb);
+                    if (sa >= sb) release(&sh->q_empty);
+                    auto next_s = [&](int st, uint32_t k_addr) {
+                        if (st < sa || st >= sb) return;
+                        issue_s(k_addr);
+                        if (st == sb - 1) release(&sh->q_empty);
+                    };
                     const uint32_t k_half = 8 * ga.kl.group_bytes, v_half = 8 * ga.vl.group_bytes;   // the tile's second 64 keys
                     wait_tile(seq);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        if (2 * tile_a + h >= sa && 2 * tile_a + h < sb) issue_s(tile_addr(seq) + h * k_half);
+                        next_s(2 * tile_a + h, tile_addr(seq) + h * k_half);
                     release(&sh->kv_empty[seq % Cfg::kSlots]);
                     for (int t = tile_a; t < tile_b; ++t) {
                         const int vt = seq + 1, kt = seq + 2;
@@ -720,7 +728,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             if (st >= sa && st < sb) issue_o(tile_addr(vt) + h * v_half, st > sa);
                             if (h == 1) release(&sh->kv_empty[vt % Cfg::kSlots]);
                             if (more && h == 0) wait_tile(kt);
-                            if (more && st + 2 >= sa && st + 2 < sb) issue_s(tile_addr(kt) + h * k_half);
+                            if (more) next_s(st + 2, tile_addr(kt) + h * k_half);
                         }
                         if (more) release(&sh->kv_empty[kt % Cfg::kSlots]);
                         seq += 2;
@@ -741,9 +749,11 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             issue_o(tile_addr(at), i > w);
                         } else {
                             issue_s(tile_addr(at));
+                            if (i + 2 >= n) release(&sh->q_empty);
                         }
                         release(&sh->kv_empty[at % Cfg::kSlots]);
                     };
+                    if (n <= w) release(&sh->q_empty);
                     step(false, 0);
                     if (n > 1) step(false, 1);
                     for (int i = 0; i < n; ++i) {
@@ -751,7 +761,6 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         if (i + 2 < n) step(false, i + 2);
                     }
                 }
-                release(&sh->q_empty);
             }
             left -= uniform(it.units) + item_cost - in;
             in = 0;
