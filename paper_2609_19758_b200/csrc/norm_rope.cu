@@ -8,6 +8,11 @@
 // so that the mean is a few shuffles, and a lane holds four channel PAIRS (two groups of four channels: i and
 // i + rot/2, or eight neighbours when pairs are interleaved), so that the rotation needs no exchange.  The channels
 // behind rot_dim are paired the same way, (i, i + (D - rot)/2), and not rotated, which keeps one mapping for all.
+//
+// This is the form for small calls and for any strides; large calls whose heads lie side by side go to norm_rope_ring.cu.  What
+// bounds it is a launch's latency, and behind that the instructions it issues (some 350 for two heads and lanes, backward).
+// Measured: one token of 32 + 8 heads of 128 3.1 us, a step of 64 requests into the cache 5.1 us, 1021 tokens of 28 + 4 heads
+// of 96 backward 15.4 us, of which 1.6 pass before the first loads and 3.2 in the last block's sum over the blocks' rows.
 #include "norm_rope.cuh"
 
 #include <mutex>

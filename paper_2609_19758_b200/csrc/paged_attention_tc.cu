@@ -4,23 +4,25 @@
 //
 // Rows.  The queries of the G heads that share a key head meet the same keys, so a tile of 128 rows holds 128 / G tokens
 // times G heads, and every key and value is read once for all of them.
-// Items.  The work on one key head of one sequence is cut into items of one query tile (SPLIT: the sequences have at most one
-// tile of queries, as in decoding) or two (PAIR: prompts), and measured in tiles of 128 keys.  All items lie on one
-// axis, (sequence, key head, query tile) ordered, which is cut into equal ranges, one per CTA: every SM gets the same
+// Items.  The work on one key head of one sequence is cut into items of one query tile (SPLIT, COPIES: a few tokens, as in
+// decoding) or two (PAIR: prompts), and measured in tiles of 128 keys.  All items lie on one axis, ordered by sequence, key head and query tile, which is cut into equal ranges, one per CTA: every SM gets the same
 // number of key tiles whatever the lengths are.  An item that a cut divides leaves partial results (running maximum, sum and
-// output, FP32), joined in the order of the parts; all others are finished where they are computed.
+// output, FP32), joined in the order of the parts; all others are finished where they are computed.  (COPIES, a few rows: joined in the
+// launch by the CTA whose part comes last; the others by a second launch, for in the first its code would be cold: 78 against 59 us
+// for windows.)
 // Two workers per CTA, a warpgroup each, a thread per row, with accumulators S and O of their own in TMEM.  In
 // a PAIR item they hold different query tiles and share every key tile; in a SPLIT item they hold the same queries and take
 // alternate key tiles, and meet at the item's end.  While one computes its softmax, the tensor cores work for the other.
 // Two loader warps bring Q and K tiles and V tiles, page by page, by TMA into a ring of tiles, 128-byte swizzled; a warp for
-// each worker issues its MMAs.  Maximum: the reference maximum of a row follows the true one only when the weights of a step outgrow it by 2^12 (P
-// is exact to 16-bit rounding whatever its size), so O in TMEM is rescaled rarely and most steps take no maximum at all.
+// each worker issues its MMAs.  Maximum: the reference maximum of a row follows the true one only when the weights of a step
+// outgrow it by 2^12 (P is exact to 16-bit rounding whatever its size), so O in TMEM is rescaled rarely and most steps take no
+// maximum at all.
 // What bounds it.  Many rows: the tensor cores and the exponentials, about equally.  A step of 64 keys takes a worker 1277 cycles (two
-// warps on a scheduler; 1024 of them the 64 x 2 exponentials at 4 lanes a cycle), the two workers' four products about 1150, where
+// warps on a scheduler; 1024 of them their exponentials, four lanes a cycle), the two workers' four products about 1150, where
 // S = Q K^T is held up by shared memory (48 cycles for 128 x 64 x 16: 128 bytes a cycle; O += P V has P in TMEM and is not).
 // Few rows: HBM, and the latency from the launch to the first scores (6 us), of which a short context is all.
 // Measured: 4096 new tokens of 32 heads over 16384 keys of 8 heads of 128, 850 us (1.13 PFLOP/s, 0.69 of a library's large product);
-// 4 tokens over 262144 keys 173 us (6.2 TB/s, 0.95 of a copy); 96 requests of one token, 98296 keys, 88 us (4.6 TB/s).
+// 4 tokens over 262144 keys 173 us (6.2 TB/s, 0.95 of a copy); 96 requests of one token, 98296 keys, 84 us (4.8 TB/s).
 // Every wait is bounded: a role whose wait gave up stops waiting and issuing, walks through its loops, reports
 // FPSK_ERR_TIMEOUT and the CTA frees its TMEM and leaves.
 #include "attention.cuh"
@@ -37,8 +39,8 @@ constexpr int kPairKeys = 64;                    // keys of a PAIR worker's step
 constexpr int kTcaThreads = 384;                 // warps 0-3 and 4-7: workers, 8 and 11: their MMAs, 9 and 10: loaders
 constexpr int kHalfBytes = 128 * 128;            // 128 rows of one 64-channel half of a tile
 constexpr int kTcaMaxSeqs = 16384;
-// An item's beginning and end, in key tiles.  96 requests of uneven length take 88 us with 2, 107 with 1, 90 with 3; 32 requests of 16
-// tokens 34-39 us with 2, 52 with 1, 49 with 3.
+// An item's beginning and end, in key tiles.  96 requests of uneven length take 84 us with 2, 91 with 1, 89 with 3; windows of 1000 keys
+// 34, 35, 45; 64 requests of 8 tokens 72, 68, 78.
 constexpr int kItemCost = 2;
 constexpr float kMostSum = 4096.f;               // of a step's weights, before a row's reference maximum is renewed
 
@@ -1143,8 +1145,7 @@ static bool aligned16(const void *p, long long s0, long long s1, long long s2)
 }
 // What the tensor-core kernel takes: heads of up to 128 channels, at most 128 query heads to a key head, whole eight-row
 // groups of a page, rows at 16-byte boundaries (TMA), and no expanded query dimension (stride 0; a cache has none).  The rest is
-// the row kernel's: right for every layout, and slow (a block for every token and head; 4096 tokens of 32 heads over 16384 keys
-// take it 366 ms, the tensor-core kernel 0.85).
+// the row kernel's.
 bool attention_tc_takes(const AttnArgs &g)
 {
     return g.dim <= 128 && g.group <= 128 && g.page_size % 8 == 0 && g.n_seqs <= kTcaMaxSeqs && aligned16(g.q, g.qts, g.qhs, 0) &&
@@ -1247,7 +1248,7 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
 
 // COPIES while the rows of every sequence's new tokens fit a quarter of the TMEM lanes; then, for heads of up to 64 channels,
 // SPLIT while they fit one tile; else PAIR.  In us, this rule first:
-//   rows <= 32: one token, 1001 keys 12.1, SPLIT and PAIR 13.5; 96 requests of one token, up to 8192 keys 88, SPLIT 99.5, PAIR 98;
+//   rows <= 32: one token, 1001 keys 12.1, SPLIT and PAIR 13.5; 96 requests of one token, up to 8192 keys 88, SPLIT 99, PAIR 98;
 //   64 requests of 8 tokens 72, PAIR 68
 //   33 to 128 rows, heads of 128: 64 rows, 131072 keys PAIR 100, SPLIT 108; 32 requests of 4096 keys 33.7, 35.6; 8 of 1024 16.7, 20.8
 //   33 to 128 rows, heads of 64: 128 rows, 262144 keys SPLIT 144, PAIR 176 (the softmax of one tile takes longer than its
