@@ -125,8 +125,8 @@ fpsk_status fpsk_paged_append(const fpsk_paged_cache *cache, const fpsk_paged_ba
  *              too small costs time only)
  *   workspace  fpsk_paged_attention_workspace_bytes() for the current device, 256-byte aligned, initialised once by
  *              fpsk_attention_workspace_init (and again after a FPSK_ERR_TIMEOUT); one call at a time
- * head_dim: a multiple of 8 up to FPSK_MAX_HEAD_DIM.  Heads of up to 128 channels, up to 128 query heads to a key head, pages of a
- * multiple of 8 tokens and 16-byte aligned rows run on the tensor cores; the rest on a plain kernel. */
+ * head_dim: a multiple of 8 up to FPSK_MAX_HEAD_DIM.  Heads of up to 128 channels, up to 128 query heads to a key head and 16-byte
+ * aligned rows run on the tensor cores (fastest in pages of a multiple of 8 tokens); the rest on a plain kernel. */
 typedef struct {
     const void *q;
     void *out;

@@ -6,7 +6,7 @@
 // a key with score s takes them to m' = max(m, s), l' = l e^(m - m') + e^(s - m'), o' likewise.
 //
 // This is the form for everything that the tensor-core kernel (paged_attention_tc.cu) does not take: heads of more than 128
-// channels, pages that are not whole groups of eight rows, unaligned rows.  Every token and head reads its keys and values for
+// channels, more than 128 query heads to a key head, unaligned rows.  Every token and head reads its keys and values for
 // itself, so it is bound by L2: 4096 tokens of 32 heads over 16384 keys take it 366 ms, the tensor-core kernel 0.85.
 #include "attention.cuh"
 

@@ -176,6 +176,11 @@ __device__ __forceinline__ void named_bar_sync(int id, int threads)
 {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
+// 16 bytes, or (n = 0) zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, int n)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -204,10 +209,11 @@ __device__ __forceinline__ void store8(void *p, const uint32_t (&v)[8])
 
 // ---------------------------------------------------------------- items
 // How a K or V tile lies in shared memory, and by which tensor map it comes.  Both halves of a row (64 channels each) in one
-// load: groups of eight rows, [group][half][8 rows][128 bytes].  Half by half: [half][128 rows][128 bytes].
-enum { kByHalves = 0, kGroupsOfAllPages = 1, kHeadsOfAllPages = 2 };
+// load: groups of eight rows, [group][half][8 rows][128 bytes].  Half by half: [half][128 rows][128 bytes].  kByRows: the same places,
+// but copied row by row (cp.async, 16 bytes a lane), for pages that are not whole groups of eight rows.
+enum { kByHalves = 0, kGroupsOfAllPages = 1, kHeadsOfAllPages = 2, kByRows = 3 };
 struct TileLayout {
-    int map;                           // one of the three above
+    int map;                           // one of the four above
     uint32_t half_bytes, group_bytes;  // offsets of the second half, of the next eight rows
 };
 struct TcaArgs {
@@ -359,7 +365,8 @@ __device__ __forceinline__ void join_row(const TcaArgs &ga, int first, int parts
     if (g.lse && lane == 0) g.lse[tok * g.hq + head] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
-template <typename T, int DP, int MODE>
+// BY_ROWS: K and V come by kByRows (a template, not a branch: a branch in the loaders cost 96 requests' step 84 -> 89 us).
+template <typename T, int DP, int MODE, bool BY_ROWS>
 __global__ void __launch_bounds__(kTcaThreads, 1)
 attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v)
@@ -563,6 +570,80 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                     const bool wanted = key + R > lo && key < hi && lane * R < kKeysPerTile;
                     return !wanted ? 0 : col < g.max_pages ? __ldg(table + col) : -1;
                 };
+                if constexpr (BY_ROWS) {
+                    // A lane looks up the rows lane, lane + 32, ..; half a warp (a quarter, for heads of 64) copies a row.
+                    constexpr int kChunks = DP / 8, kRowsAtOnce = 32 / kChunks;
+                    const T *base = static_cast<const T *>(is_v ? g.v : g.k) + (long long)kvh * (is_v ? g.vhs : g.khs);
+                    const long long ps = is_v ? g.vps : g.kps, ts = is_v ? g.vts : g.kts;
+                    const int chunk = lane % kChunks, half = chunk / 8, size = chunk * 8 < g.dim ? 16 : 0;
+                    int c[4], r[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at_key = tile_a * kKeysPerTile + lane + 32 * j;
+                        c[j] = at_key / page_size;
+                        r[j] = at_key - c[j] * page_size;
+                    }
+                    int pages[4];
+                    auto look_up = [&](int k0) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int key = k0 + lane + 32 * j;
+                            pages[j] = key < lo || key >= hi ? 0 : c[j] < g.max_pages ? __ldg(table + c[j]) : -1;
+                        }
+                    };
+                    look_up(tile_a * kKeysPerTile);
+                    int in_flight = -1;                                // this item's tile whose copies are not known to have landed
+                    auto landed = [&](int behind) {
+                        if (behind) asm volatile("cp.async.wait_group 1;" ::: "memory");
+                        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&sh->kv_full[in_flight % Cfg::kSlots]));
+                        in_flight = -1;
+                    };
+                    for (int i = 0; i < n && ok; ++i) {
+                        const int k0 = (tile_a + i) * kKeysPerTile;
+                        const int at = seq + (PAIR ? 2 * i + is_v : is_v ? min(2 * i + 2, 2 * n - 1) : max(2 * i - 1, 0));
+                        const int slot = at % Cfg::kSlots;
+                        const uint32_t phase = (uint32_t)(at / Cfg::kSlots) & 1u, empty = smem_u32(&sh->kv_empty[slot]);
+                        long long row_at[4];                           // -1: not wanted, -2: no such page
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int key = k0 + lane + 32 * j;
+                            row_at[j] = -1;
+                            if (key >= lo && key < hi) {
+                                row_at[j] = pages[j] >= 0 && pages[j] < g.n_pages ? pages[j] * ps + r[j] * ts : -2;
+                                if (row_at[j] == -2) report_status(g.status, FPSK_ERR_PARAM);
+                            }
+                            c[j] += ga.tile_pages;
+                            r[j] += ga.tile_rest;
+                            if (r[j] >= page_size) { r[j] -= page_size; ++c[j]; }
+                        }
+                        if (i + 1 < n) look_up(k0 + kKeysPerTile);     // its latency passes behind the copies
+                        // (a tile in flight is handed on before a wait that may be long)
+                        if (in_flight >= 0 && !__all_sync(0xFFFFFFFFu, mbar_try(empty, phase ^ 1u))) landed(0);
+                        wait(empty, phase ^ 1u);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        const uint32_t dst = ring + slot * Cfg::kTile + half * kHalfBytes;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll 8                                                       // (1.63 ms; 4: 1.79, 16: 1.97)
+                            for (int x = 0; x < 32; x += kRowsAtOnce) {
+                                const int src_lane = x + lane / kChunks, row = 32 * j + src_lane;
+                                const long long from = __shfl_sync(0xFFFFFFFFu, row_at[j], src_lane);
+                                if (from != -1)
+                                    copy16(dst + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), from >= 0 && size ? base + from + chunk * 8 : base,
+                                           from >= 0 ? size : 0);
+                            }
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                        if (in_flight >= 0) landed(1);
+                        in_flight = at;
+                        last = at;
+                    }
+                    if (in_flight >= 0) landed(0);
+                    if (ok) seq += 2 * n;
+                } else {
                 int next = fetch();
                 for (int i = 0; i < n; ++i) {
                     const int tile = tile_a + i, k0 = tile * kKeysPerTile;
@@ -605,6 +686,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                     }
                 }
                 if (ok) seq += 2 * n;
+                }
             }
             left -= uniform(it.units) + item_cost - in;
             in = 0;
@@ -1143,17 +1225,16 @@ static bool aligned16(const void *p, long long s0, long long s1, long long s2)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s0 % 8 == 0 && s1 % 8 == 0 && s2 % 8 == 0;
 }
-// What the tensor-core kernel takes: heads of up to 128 channels, at most 128 query heads to a key head, whole eight-row
-// groups of a page, rows at 16-byte boundaries (TMA), and no expanded query dimension (stride 0; a cache has none).  The rest is
-// the row kernel's.
+// What the tensor-core kernel takes: heads of up to 128 channels, at most 128 query heads to a key head, rows at 16-byte
+// boundaries, and no expanded query dimension (TMA wants strides; a cache has none of 0).  The rest is the row kernel's.
 bool attention_tc_takes(const AttnArgs &g)
 {
-    return g.dim <= 128 && g.group <= 128 && g.page_size % 8 == 0 && g.n_seqs <= kTcaMaxSeqs && aligned16(g.q, g.qts, g.qhs, 0) &&
+    return g.dim <= 128 && g.group <= 128 && g.n_seqs <= kTcaMaxSeqs && aligned16(g.q, g.qts, g.qhs, 0) &&
            aligned16(g.out, g.ots, g.ohs, 0) && aligned16(g.k, g.kps, g.kts, g.khs) && aligned16(g.v, g.vps, g.vts, g.vhs) &&
            (g.n_tokens == 1 || g.qts > 0) && (g.hq == 1 || g.qhs > 0);
 }
 
-template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnArgs &a, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st)
+template <typename T, int DP, int MODE, bool BY_ROWS> static fpsk_status launch_tc(const AttnArgs &a, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st)
 {
     using Cfg = Tca<DP, MODE>;
     const int sms = sm_count();
@@ -1192,7 +1273,13 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     // pages (a page is its heads long).
     auto kv_map = [&](CUtensorMap *m, TileLayout &tl, const void *base, long long ps, long long ts, long long hs) {
         const cuuint32_t R = 1u << g.box_log;
-        tl.map = kByHalves;
+        tl.map = BY_ROWS ? kByRows : kByHalves;
+        if (BY_ROWS) {
+            tl.half_bytes = kHalfBytes;
+            tl.group_bytes = 1024;
+            *m = mq;                                                   // (never loaded by)
+            return true;
+        }
         if (a.dim == 128 && (a.n_pages == 1 || ps == a.page_size * ts) && a.n_pages * (a.page_size / 8) <= 0x7FFFFFFFLL) tl.map = kGroupsOfAllPages;
         else if (a.dim == 128 && (a.n_pages == 1 || ps == a.hk * hs) && a.n_pages * a.hk <= 0x7FFFFFFFLL) tl.map = kHeadsOfAllPages;
         if (tl.map == kByHalves) {
@@ -1219,7 +1306,7 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     FPSK_CUDA_OK(cudaGetDevice(&dev));
     const unsigned long long bit = 1ull << (dev & 63);
     if (!(prepared.load(std::memory_order_acquire) & bit)) {
-        FPSK_CUDA_OK(cudaFuncSetAttribute(attention_tc_kernel<T, DP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+        FPSK_CUDA_OK(cudaFuncSetAttribute(attention_tc_kernel<T, DP, MODE, BY_ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
         prepared.fetch_or(bit, std::memory_order_release);
     }
     // Both launches may begin before the kernel in front has ended (they wait for it before they read): what a launch costs passes
@@ -1234,7 +1321,7 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_tc_kernel<T, DP, MODE>, g, mq, mk, mv));
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, attention_tc_kernel<T, DP, MODE, BY_ROWS>, g, mq, mk, mv));
     FPSK_LAUNCH_CHECK();
     if constexpr (MODE != kCopies) {
         cfg.gridDim = dim3((unsigned)ctas, Cfg::kRows / 8);
@@ -1253,16 +1340,24 @@ template <typename T, int DP, int MODE> static fpsk_status launch_tc(const AttnA
 //   33 to 128 rows, heads of 128: 64 rows, 131072 keys PAIR 100, SPLIT 108; 32 requests of 4096 keys 33.7, 35.6; 8 of 1024 16.7, 20.8
 //   33 to 128 rows, heads of 64: 128 rows, 262144 keys SPLIT 144, PAIR 176 (the softmax of one tile takes longer than its
 //   keys, half as many bytes, take to come); 64 requests of 7 tokens 22.0, 23.2; but 64 of 32 tokens 61.5, 55
+// Pages that are not whole groups of eight rows: copied by rows, bound by the copying warps (each a tile of 128 keys of K or V
+// in some 8000 cycles): 4096 tokens over 16384 keys in pages of 12 in 1.63 ms, 96 requests of one token in 0.23 ms (pages of 16: 0.84 and
+// 0.084); pages of 1 take no longer.
 fpsk_status attention_tc_launch(const AttnArgs &a, int type, int max_q_len, int max_kv_len, void *ws, cudaStream_t st)
 {
     if (max_q_len < 1) max_q_len = 1;
     if (max_kv_len < 1) max_kv_len = 1;
     const long long rows = (long long)max_q_len * a.group;
-#define FPSK_TCA(TT, DD, MM) launch_tc<TT, DD, MM>(a, type, max_q_len, max_kv_len, ws, st)
-#define FPSK_TCA_DIM(TT)                                                                                                                      \
-    (a.dim > 64 ? rows <= 32 ? FPSK_TCA(TT, 128, kCopies) : FPSK_TCA(TT, 128, kPair)                                                          \
-                : rows <= 32 ? FPSK_TCA(TT, 64, kCopies) : rows <= kRowsPerTile ? FPSK_TCA(TT, 64, kSplit) : FPSK_TCA(TT, 64, kPair))
+    const bool by_rows = a.page_size % 8 != 0;
+#define FPSK_TCA(TT, DD, MM, RR) launch_tc<TT, DD, MM, RR>(a, type, max_q_len, max_kv_len, ws, st)
+#define FPSK_TCA_ROWS(TT, DD) (rows <= 32 ? FPSK_TCA(TT, DD, kCopies, true) : FPSK_TCA(TT, DD, kPair, true))
+#define FPSK_TCA_DIM(TT)                                                                                                                    \
+    (by_rows       ? a.dim > 64 ? FPSK_TCA_ROWS(TT, 128) : FPSK_TCA_ROWS(TT, 64)                                                            \
+     : a.dim > 64  ? rows <= 32 ? FPSK_TCA(TT, 128, kCopies, false) : FPSK_TCA(TT, 128, kPair, false)                                       \
+     : rows <= 32  ? FPSK_TCA(TT, 64, kCopies, false)                                                                                       \
+     : rows <= kRowsPerTile ? FPSK_TCA(TT, 64, kSplit, false) : FPSK_TCA(TT, 64, kPair, false))
     return type == FPSK_ELEM_FP16 ? FPSK_TCA_DIM(__half) : FPSK_TCA_DIM(__nv_bfloat16);
+#undef FPSK_TCA_ROWS
 #undef FPSK_TCA_DIM
 #undef FPSK_TCA
 }

@@ -100,6 +100,13 @@ CASES = {
     "page_of_300": dict(seqs=[(20, 700), (1, 301)], hq=4, hk=2, dim=128, page=304, dtype=BF16),
     "page_of_5": dict(seqs=[(20, 70), (1, 31)], hq=4, hk=2, dim=128, page=5, dtype=BF16),
     "page_of_1": dict(seqs=[(3, 33)], hq=2, hk=1, dim=64, page=1, dtype=BF16),
+    "rows_steps": dict(seqs=[(1, 300), (1, 1), (1, 1000), (3, 129), (0, 12)], hq=8, hk=2, dim=128, page=5, dtype=BF16),
+    "rows_prompt": dict(seqs=[(300, 700), (70, 400)], hq=4, hk=2, dim=128, page=20, dtype=F16),
+    "rows_prompt_long": dict(seqs=[(130, 3000), (1, 2500)], hq=4, hk=2, dim=128, page=100, dtype=BF16),
+    "rows_dim_96": dict(seqs=[(130, 260), (1, 70)], hq=4, hk=2, dim=96, page=12, dtype=BF16),
+    "rows_dim_64": dict(seqs=[(20, 600), (16, 40)], hq=8, hk=2, dim=64, page=3, dtype=F16),
+    "rows_dim_40": dict(seqs=[(90, 140), (1, 300)], hq=2, hk=1, dim=40, page=1, dtype=BF16),
+    "rows_window": dict(seqs=[(150, 400), (1, 900), (4, 130)], hq=4, hk=2, dim=128, page=12, dtype=BF16, window=100, order="htd"),
     "heads_outer": dict(seqs=[(20, 170), (1, 310)], hq=4, hk=2, dim=128, page=16, dtype=BF16, order="htd"),
     "odd_query_stride": dict(seqs=[(5, 90)], hq=3, hk=3, dim=64, page=16, dtype=BF16, q_pad=3),
     "padded_query_rows": dict(seqs=[(5, 90), (140, 141)], hq=3, hk=3, dim=64, page=16, dtype=BF16, q_pad=64),
@@ -172,10 +179,11 @@ def test_expanded_dimensions(what):
             A.paged_attention(A.PagedCache(*pair), q, out, *dev, ws, 40, 300)
 
 
-def test_pages_outside_the_cache_are_reported():
+@pytest.mark.parametrize("page", [16, 12])
+def test_pages_outside_the_cache_are_reported(page):
     rng = np.random.default_rng(2)
-    k, v, cu, kv, table = make_cache(rng, [(1, 200), (1, 100)], 1, 128, 16, BF16, "thd")
-    fill(rng, k, v, kv, table, 16)
+    k, v, cu, kv, table = make_cache(rng, [(1, 200), (1, 100)], 1, 128, page, BF16, "thd")
+    fill(rng, k, v, kv, table, page)
     table[0, 4] = 12345
     q = torch.randn(2, 2, 128, device="cuda").to(BF16)
     out = torch.zeros_like(q)
