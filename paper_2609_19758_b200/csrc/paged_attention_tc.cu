@@ -1333,10 +1333,12 @@ template <typename T, int DP, int MODE, bool BY_ROWS> static fpsk_status launch_
     return FPSK_OK;
 }
 
-// COPIES while the rows of every sequence's new tokens fit a quarter of the TMEM lanes; then, for heads of up to 64 channels,
-// SPLIT while they fit one tile; else PAIR.  In us, this rule first:
-//   rows <= 32: one token, 1001 keys 12.1, SPLIT and PAIR 13.5; 96 requests of one token, up to 8192 keys 88, SPLIT 99, PAIR 98;
-//   64 requests of 8 tokens 72, PAIR 68
+// COPIES for a few rows of new tokens a sequence (its end goes by eight rows, and holds at most 32); then, for heads of up to 64
+// channels, SPLIT while they fit one tile; else PAIR.  In us, this rule first:
+//   4 rows: one token, 1001 keys 12.1, SPLIT and PAIR 13.5; 96 requests, up to 8192 keys 88, SPLIT 99, PAIR 98
+//   24 rows, heads of 128: 64 requests of 4096 keys 48, PAIR 51; 8 of 500 16.2, 15.1; one of 65536 62, 60
+//   32 rows, heads of 128: the same PAIR 58, 15.0, 60, COPIES 60, 17.6, 65; 262144 keys 181, 179
+//   32 rows, heads of 64: 49, 15.6, 58, SPLIT 57, 14.8, 53
 //   33 to 128 rows, heads of 128: 64 rows, 131072 keys PAIR 100, SPLIT 108; 32 requests of 4096 keys 33.7, 35.6; 8 of 1024 16.7, 20.8
 //   33 to 128 rows, heads of 64: 128 rows, 262144 keys SPLIT 144, PAIR 176 (the softmax of one tile takes longer than its
 //   keys, half as many bytes, take to come); 64 requests of 7 tokens 22.0, 23.2; but 64 of 32 tokens 61.5, 55
@@ -1348,13 +1350,13 @@ fpsk_status attention_tc_launch(const AttnArgs &a, int type, int max_q_len, int 
     if (max_q_len < 1) max_q_len = 1;
     if (max_kv_len < 1) max_kv_len = 1;
     const long long rows = (long long)max_q_len * a.group;
-    const bool by_rows = a.page_size % 8 != 0;
+    const bool by_rows = a.page_size % 8 != 0, copies = rows <= (a.dim > 64 ? 24 : 32);
 #define FPSK_TCA(TT, DD, MM, RR) launch_tc<TT, DD, MM, RR>(a, type, max_q_len, max_kv_len, ws, st)
-#define FPSK_TCA_ROWS(TT, DD) (rows <= 32 ? FPSK_TCA(TT, DD, kCopies, true) : FPSK_TCA(TT, DD, kPair, true))
-#define FPSK_TCA_DIM(TT)                                                                                                                    \
-    (by_rows       ? a.dim > 64 ? FPSK_TCA_ROWS(TT, 128) : FPSK_TCA_ROWS(TT, 64)                                                            \
-     : a.dim > 64  ? rows <= 32 ? FPSK_TCA(TT, 128, kCopies, false) : FPSK_TCA(TT, 128, kPair, false)                                       \
-     : rows <= 32  ? FPSK_TCA(TT, 64, kCopies, false)                                                                                       \
+#define FPSK_TCA_ROWS(TT, DD) (copies ? FPSK_TCA(TT, DD, kCopies, true) : FPSK_TCA(TT, DD, kPair, true))
+#define FPSK_TCA_DIM(TT)                                                                                  \
+    (by_rows       ? a.dim > 64 ? FPSK_TCA_ROWS(TT, 128) : FPSK_TCA_ROWS(TT, 64)                          \
+     : a.dim > 64  ? copies ? FPSK_TCA(TT, 128, kCopies, false) : FPSK_TCA(TT, 128, kPair, false)         \
+     : copies      ? FPSK_TCA(TT, 64, kCopies, false)                                                     \
      : rows <= kRowsPerTile ? FPSK_TCA(TT, 64, kSplit, false) : FPSK_TCA(TT, 64, kPair, false))
     return type == FPSK_ELEM_FP16 ? FPSK_TCA_DIM(__half) : FPSK_TCA_DIM(__nv_bfloat16);
 #undef FPSK_TCA_ROWS
