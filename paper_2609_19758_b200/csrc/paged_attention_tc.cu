@@ -888,6 +888,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
             }
             float m = -INFINITY, l = 0.f;
             bool have_o = false;
+            bool open = true;                                          // some row of the warp may have no reference maximum yet
             for (int t = ta; t < tb; t += step) {
                 const int k0 = t * (PAIR ? kPairKeys : kKeysPerTile) + col0;
                 const uint32_t ts = tmem + lanes + w * 128 + (PAIR ? (count & 1u) * kPairKeys : 0u);
@@ -924,12 +925,13 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         for (int c = 0; c < kChunks; ++c) top = top32(s[c], top);
                         return top * sl2;
                     };
-                    // Weights against the reference maximum, which the item's first step sets.  The sum of a step's weights tells whether
+                    // Weights against the reference maximum, which the first step that a row sees sets (with a window that need not be
+                    // the item's first; weights against anything else could all be zero).  The sum of a step's weights tells whether
                     // a score has outgrown it: while the sum is at most kMostSum no weight is larger, and no maximum is taken.  Else
                     // (rare) the reference follows, O is rescaled and the weights are computed once more.
                     uint32_t p[kCols / 2];
                     float step_sum;
-                    bool again = !have_o;
+                    bool again = !have_o || (open && __any_sync(0xFFFFFFFFu, valid && m == -INFINITY && max(k0, lo) < min(k0 + kCols, hi)));
 #pragma unroll 1
                     for (;;) {
                         uint32_t s[kChunks][32];
@@ -940,6 +942,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             const float m2 = grow ? reference(top) : m, alpha = grow ? ex2(m - m2) : 1.f;
                             m = m2;
                             l *= alpha;
+                            open = __any_sync(0xFFFFFFFFu, valid && m == -INFINITY);
                             if (have_o) {
                                 wait(step_bar(sh->o_done, count - 1u), ((count - 1u) >> 1) & 1u);
                                 tc_fence_after();
@@ -969,8 +972,8 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                             }
                         }
                         step_sum = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                        // (a row without a reference so far, all of its scores hidden, gets one with its first weight)
-                        if (again || __all_sync(0xFFFFFFFFu, !valid || step_sum <= (m == -INFINITY ? 0.f : kMostSum))) break;
+                        // (a row without a reference has seen no key, or scores of -inf alone: weights of zero)
+                        if (again || __all_sync(0xFFFFFFFFu, !valid || step_sum <= kMostSum)) break;
                         again = true;
                     }
                     l += step_sum;
