@@ -14,9 +14,10 @@
 // a PAIR item they hold different query tiles and share every key tile; in a SPLIT item they hold the same queries and take
 // alternate key tiles, and meet at the item's end.  While one computes its softmax, the tensor cores work for the other.
 // Two loader warps bring Q and K tiles and V tiles, page by page, by TMA into a ring of tiles, 128-byte swizzled; a warp for
-// each worker issues its MMAs.  Maximum: the reference maximum of a row follows the true one only when the weights of a step
-// outgrow it by 2^12 (P is exact to 16-bit rounding whatever its size), so O in TMEM is rescaled rarely and most steps take no
-// maximum at all.
+// each worker issues its MMAs.  Maximum: the reference of a row follows its maximum only when the weights of a step outgrow it (see
+// Reference), so O in TMEM is rescaled rarely and most steps take no maximum at all.
+// Roundings.  Weights meet the values as 16-bit numbers, which the tensor cores want: each is off by half a unit of the type at most,
+// the sum that divides them is not rounded.  Sums, maxima and outputs are FP32 up to the one rounding at the end.
 // What bounds it.  Many rows: the tensor cores and the exponentials, about equally.  A step of 64 keys takes a worker 1277 cycles (two
 // warps on a scheduler; 1024 of them their exponentials, four lanes a cycle), the two workers' four products about 1150, where
 // S = Q K^T is held up by shared memory (48 cycles for 128 x 64 x 16: 128 bytes a cycle; O += P V has P in TMEM and is not).
@@ -42,7 +43,17 @@ constexpr int kTcaMaxSeqs = 16384;
 // An item's beginning and end, in key tiles.  96 requests of uneven length take 84 us with 2, 91 with 1, 89 with 3; windows of 1000 keys
 // 34, 35, 45; 64 requests of 8 tokens 72, 68, 78.
 constexpr int kItemCost = 2;
-constexpr float kMostSum = 4096.f;               // of a step's weights, before a row's reference maximum is renewed
+// Weights are powers of two over a row's reference, which lies kBelow binary digits under its maximum when it is set, and is renewed
+// when the sum of a step's weights passes kMost.  BF16 has the exponents of FP32: any reference will do.  FP16 rounds weights below
+// 2^-14 to multiples of 2^-24, and a long tail of such weights counts (131071 keys at 2^-24.4 of a dominant one are 0.006 of
+// it, and would be off by a third of that): with the reference eight digits down that is 2^-33 of the largest weight each, 2^-13 of it for 2^20 keys.
+// 128 weights of 2^8 stay within kMost, so that equal scores take no maximum either, and no weight passes the largest FP16 number.
+template <typename T> struct Reference {
+    static constexpr float kBelow = 0.f, kMost = 4096.f;
+};
+template <> struct Reference<__half> {
+    static constexpr float kBelow = 8.f, kMost = 60000.f;
+};
 
 // 32 consecutive columns of this thread's accumulator row; valid after tm_wait32 on the same array
 __device__ __forceinline__ void tm_load32(uint32_t taddr, uint32_t (&v)[32])
@@ -923,11 +934,11 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         float top = -INFINITY;
 #pragma unroll
                         for (int c = 0; c < kChunks; ++c) top = top32(s[c], top);
-                        return top * sl2;
+                        return top * sl2 - Reference<T>::kBelow;
                     };
                     // Weights against the reference maximum, which the first step that a row sees sets (with a window that need not be
                     // the item's first; weights against anything else could all be zero).  The sum of a step's weights tells whether
-                    // a score has outgrown it: while the sum is at most kMostSum no weight is larger, and no maximum is taken.  Else
+                    // a score has outgrown it: while the sum is at most kMost no weight is larger, and no maximum is taken.  Else
                     // (rare) the reference follows, O is rescaled and the weights are computed once more.
                     uint32_t p[kCols / 2];
                     float step_sum;
@@ -973,7 +984,7 @@ attention_tc_kernel(const __grid_constant__ TcaArgs ga, const __grid_constant__ 
                         }
                         step_sum = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                         // (a row without a reference has seen no key, or scores of -inf alone: weights of zero)
-                        if (again || __all_sync(0xFFFFFFFFu, !valid || step_sum <= kMostSum)) break;
+                        if (again || __all_sync(0xFFFFFFFFu, !valid || step_sum <= Reference<T>::kMost)) break;
                         again = true;
                     }
                     l += step_sum;

@@ -1,5 +1,5 @@
 """Attention over pages where the scores lie far from zero or far from each other: windows whose keys all score very low (a row
-of a tile may see nothing in its item's first steps).
+of a tile may see nothing in its item's first steps), and a dominant key above a long tail of small weights.
 
 Tolerances: those of test_gpu_paged_attention.py, whose derivation holds for any scores."""
 import numpy as np
@@ -90,3 +90,24 @@ def test_windows_of_very_low_scores(name, level):
             v[pg, :m] = torch.from_numpy(rng.standard_normal((m, hk, dim)).astype(np.float32)).to(dtype).cuda()
     q = torch.from_numpy((a + 0.1 * rng.standard_normal((int(cu[-1]), hq, dim))).astype(np.float32)).to(dtype).cuda()
     compare(q, k, v, cu, kv, table, max(x for x, _ in c["seqs"]), 1 if c.get("whole") else max(x for _, x in c["seqs"]), c.get("causal", True), c["window"])
+
+
+@pytest.mark.parametrize("digits", [16, 23.4, 24.6, 26])
+@pytest.mark.parametrize("first", [True, False])
+@pytest.mark.parametrize("new,hq,dim,page,keys", [(1, 4, 128, 16, 131072), (1, 4, 64, 16, 131072), (9, 4, 64, 16, 65536), (26, 1, 128, 16, 65536),
+                                                  (1, 2, 128, 12, 65532)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_a_dominant_key_above_a_long_tail(dtype, new, hq, dim, page, keys, first, digits):
+    """One key with a score 2^digits above all others, whose values have a mean of 1: together they count."""
+    if new > 1 and dtype == BF16:
+        pytest.skip("one form is enough for the type with the wide exponent")
+    rng = np.random.default_rng(11)
+    k, v, cu, kv, table = make_cache(rng, [(new, keys)], 1, dim, page, dtype, "thd")
+    at = 0 if first else keys - 200                               # (every new token sees it)
+    top = (digits * np.log(2.0) * dim ** 0.5) ** 0.5
+    k[int(table[0, at // page]), at % page, 0, 0] = top
+    v.copy_(torch.from_numpy((1 + 0.25 * rng.standard_normal(v.shape)).astype(np.float32)))
+    v[int(table[0, at // page]), at % page] = torch.from_numpy(rng.standard_normal((1, dim)).astype(np.float32)).to(dtype).cuda()
+    q = torch.zeros(new, hq, dim, dtype=dtype, device="cuda")
+    q[..., 0] = top
+    compare(q, k, v, cu, kv, table, new, 1)                       # (one CTA: a part of its own would have a reference of its own)
