@@ -272,8 +272,9 @@ __global__ void __launch_bounds__(kRopeThreads, 2) norm_rope_grad_kernel(const _
             }
             if (H.w) {
                 const float ss = sum_lanes<L>(dot4(b[i], b[i], dot4(a[i], a[i], 0.f)));
-                const float r = rsqrtf(fmaf(ss, g.inv_dim, g.eps));
-                a[i] = scale4(a[i], r);                             // n (zero where there is no vector: it adds nothing)
+                // n; zero where there is no vector, so that it adds nothing (there the root is infinite when eps is 0)
+                const float r = live ? rsqrtf(fmaf(ss, g.inv_dim, g.eps)) : 0.f;
+                a[i] = scale4(a[i], r);
                 b[i] = scale4(b[i], r);
                 da = make_float4(fmaf(ua[i].x, a[i].x, da.x), fmaf(ua[i].y, a[i].y, da.y), fmaf(ua[i].z, a[i].z, da.z), fmaf(ua[i].w, a[i].w, da.w));
                 db = make_float4(fmaf(ub[i].x, b[i].x, db.x), fmaf(ub[i].y, b[i].y, db.y), fmaf(ub[i].z, b[i].z, db.z), fmaf(ub[i].w, b[i].w, db.w));
