@@ -202,6 +202,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) norm_rope_grad_kernel(const _
     const LaneMap m(lane, g.dim, g.rot, g.interleaved);
     const int kind = (int)blockIdx.x >= g.blocks0;
     const HeadsGradArg &H = g.h[kind];
+    const long long n_tok = H.n ? g.n_tok : 0;                         // a kind without heads only has its weight gradient of zero to write
     const int block = blockIdx.x - (kind ? g.blocks0 : 0), blocks = kind ? gridDim.x - g.blocks0 : g.blocks0;
     const int chunk = block % H.map.chunks, lanes_of_blocks = blocks / H.map.chunks;   // (blocks: a multiple of the chunks)
     const SlotMap sm(H.map, H.n, S, slot, chunk);
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) norm_rope_grad_kernel(const _
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             na[i] = nb[i] = ga[i] = gb[i] = splat4(0.f);
-            if (there[i] && tok + sm.token0 + i * sm.token_step < g.n_tok) {
+            if (there[i] && tok + sm.token0 + i * sm.token_step < n_tok) {
                 na[i] = load4<WIDE>(src[i] + m.ia);
                 nb[i] = load4<WIDE>(src[i] + m.ib);
                 ga[i] = load4<WIDE>(grad[i] + m.ia);
@@ -240,19 +241,19 @@ __global__ void __launch_bounds__(kRopeThreads, 2) norm_rope_grad_kernel(const _
             grad[i] += stride * H.dots;
         }
     };
-    if (first < g.n_tok) fetch(first);
-    for (long long t0 = first; t0 < g.n_tok; t0 += stride) {
+    if (first < n_tok) fetch(first);
+    for (long long t0 = first; t0 < n_tok; t0 += stride) {
         float4 a[kPer], b[kPer], ua[kPer], ub[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) { a[i] = na[i]; b[i] = nb[i]; ua[i] = ga[i]; ub[i] = gb[i]; }
-        if (t0 + stride < g.n_tok) fetch(t0 + stride);
+        if (t0 + stride < n_tok) fetch(t0 + stride);
         float4 c = splat4(1.f), s = splat4(0.f);
         bool in_table = true;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const long long tok = t0 + sm.token0 + i * sm.token_step;
-            const bool live = there[i] && tok < g.n_tok;
-            if (g.rot > 0 && (i == 0 || sm.token_step) && tok < g.n_tok) {
+            const bool live = there[i] && tok < n_tok;
+            if (g.rot > 0 && (i == 0 || sm.token_step) && tok < n_tok) {
                 const int pos = __ldg(g.positions + tok);
                 in_table = pos >= 0 && pos < g.n_pos;
                 if (in_table && m.on && m.rotated) {

@@ -1,4 +1,4 @@
-"""Norms and rotation at the edges of what the entry points take: eps = 0.  Tolerances as in test_gpu_norm_rope.py."""
+"""Norms and rotation at the edges of what the entry points take: eps = 0, kinds of heads without heads.  Tolerances as in test_gpu_norm_rope.py."""
 import numpy as np
 import pytest
 import torch
@@ -62,3 +62,26 @@ def test_many_tokens_backward_without_eps():
         n = x.double() * torch.rsqrt(x.double().square().mean(-1, keepdim=True))
         chain = tokens * x.shape[1] / (148 * 16) + 32 + 148 + 17 + 32
         assert bool(((dwt.double() - (u * n).sum((0, 1))).abs() <= chain * E32 * (um * n.abs()).sum((0, 1))).all())
+
+
+@pytest.mark.parametrize("empty", ["q", "k"])
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_a_kind_without_heads_has_a_weight_gradient_of_zero(empty, tokens):
+    rng = np.random.default_rng(2)
+    hq, hk = (0, 3) if empty == "q" else (3, 0)
+    q, k = projection(rng, tokens, (hq, hk), 64, F32)
+    gq, gk = projection(rng, tokens, (hq, hk), 64, BF16)
+    cos, sin, c64, s64 = tables(50, 64)
+    pos = torch.from_numpy(rng.integers(0, 50, tokens).astype(np.int32)).cuda()
+    w = torch.ones(64, device="cuda")
+    dq, dk = (torch.full((tokens, h, 64), 7.0, dtype=BF16, device="cuda") for h in (hq, hk))
+    dw = [torch.full((64,), 7.0, device="cuda") for _ in range(2)]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    A.qk_norm_rope_backward(q, k, gq, gk, cos, sin, pos, dq, dk, dw[0], dw[1], A.norm_rope_workspace(64), w, w, eps=1e-5, status=status)
+    assert int(status) == 0
+    x, g, dx, there, none = (k, gk, dk, dw[1], dw[0]) if empty == "q" else (q, gq, dq, dw[0], dw[1])
+    assert bool((none == 0).all())
+    p = pos.cpu().numpy()
+    want, mag, want_w, mag_w = O.norm_rope_grad(x.double().cpu().numpy(), np.ones(64), g.double().cpu().numpy(), c64[p], s64[p], 64, 1e-5)
+    close(dx, want, UNIT[BF16] * np.abs(want) + 64 * E32 * mag)
+    close(there, want_w, (256 + 32) * E32 * mag_w)
