@@ -12,6 +12,7 @@ import os
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import fpsk
 from .fpsk import ERR_SHAPE, STATUS_OK, FpskError
@@ -97,7 +98,8 @@ def qk_norm_rope_backward(q, k, dq_out, dk_out, cos, sin, positions, dq, dk, dq_
 
 class QKNormRope(torch.autograd.Function):
     """qk_norm_rope with its gradients for autograd: ``apply(q, k, q_weight, k_weight, cos, sin, positions, out_dtype, eps,
-    interleaved)`` returns the rotated queries and keys in out_dtype.  Gradients of q and k are computed in out_dtype."""
+    interleaved)`` returns the rotated queries and keys in out_dtype.  Gradients of q and k are computed in out_dtype.  A second
+    derivative is refused."""
 
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, out_dtype, eps, interleaved):
@@ -109,6 +111,7 @@ class QKNormRope(torch.autograd.Function):
         return q_out, k_out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
         out_dtype, eps, interleaved = ctx.more

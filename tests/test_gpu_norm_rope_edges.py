@@ -1,4 +1,5 @@
-"""Norms and rotation at the edges of what the entry points take: eps = 0, kinds of heads without heads.  Tolerances as in test_gpu_norm_rope.py."""
+"""Norms and rotation at the edges of what the entry points take: eps = 0, kinds of heads without heads, gradients of gradients.
+Tolerances as in test_gpu_norm_rope.py."""
 import numpy as np
 import pytest
 import torch
@@ -85,3 +86,14 @@ def test_a_kind_without_heads_has_a_weight_gradient_of_zero(empty, tokens):
     want, mag, want_w, mag_w = O.norm_rope_grad(x.double().cpu().numpy(), np.ones(64), g.double().cpu().numpy(), c64[p], s64[p], 64, 1e-5)
     close(dx, want, UNIT[BF16] * np.abs(want) + 64 * E32 * mag)
     close(there, want_w, (256 + 32) * E32 * mag_w)
+
+
+def test_a_second_derivative_is_refused():
+    q, k = (torch.randn(3, 2, 32, device="cuda", requires_grad=True) for _ in range(2))
+    w = torch.ones(32, device="cuda", requires_grad=True)
+    cos, sin, _, _ = tables(10, 32)
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")
+    qo, ko = A.QKNormRope.apply(q, k, w, w, cos, sin, pos, F32, 1e-5, False)
+    dq, = torch.autograd.grad(qo.square().sum() + ko.sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (dq.square().sum() + q.square().sum()).backward()          # (the first term alone would be left out in silence)
