@@ -98,8 +98,8 @@ def qk_norm_rope_backward(q, k, dq_out, dk_out, cos, sin, positions, dq, dk, dq_
 
 class QKNormRope(torch.autograd.Function):
     """qk_norm_rope with its gradients for autograd: ``apply(q, k, q_weight, k_weight, cos, sin, positions, out_dtype, eps,
-    interleaved)`` returns the rotated queries and keys in out_dtype.  Gradients of q and k are computed in out_dtype.  A second
-    derivative is refused."""
+    interleaved)`` returns the rotated queries and keys in out_dtype.  Gradients of q and k are computed and rounded once in
+    their own type (in FP32 where it differs from out_dtype).  A second derivative is refused."""
 
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, out_dtype, eps, interleaved):
@@ -115,9 +115,11 @@ class QKNormRope(torch.autograd.Function):
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
         out_dtype, eps, interleaved = ctx.more
-        dq_out, dk_out = (g if g.stride(-1) == 1 else g.contiguous() for g in (dq_out, dk_out))
-        dq = torch.empty(q.shape, dtype=out_dtype, device=q.device)
-        dk = torch.empty(k.shape, dtype=out_dtype, device=k.device)
+        # the library's gradients have one type: with an FP32 accumulator behind 16-bit outputs that is FP32, not the outputs'
+        grad_dtype = out_dtype if q.dtype == out_dtype else torch.float32
+        dq_out, dk_out = ((g if g.stride(-1) == 1 else g.contiguous()).to(grad_dtype) for g in (dq_out, dk_out))
+        dq = torch.empty(q.shape, dtype=grad_dtype, device=q.device)
+        dk = torch.empty(k.shape, dtype=grad_dtype, device=k.device)
         dw = [torch.empty(w.shape, dtype=torch.float32, device=w.device) if w is not None else None for w in (q_weight, k_weight)]
         qk_norm_rope_backward(q, k, dq_out, dk_out, cos, sin, positions, dq, dk, dw[0], dw[1],
                               norm_rope_workspace(q.shape[2], q.device), q_weight, k_weight, eps, interleaved)

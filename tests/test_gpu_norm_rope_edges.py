@@ -1,5 +1,5 @@
-"""Norms and rotation at the edges of what the entry points take: eps = 0, kinds of heads without heads, gradients of gradients.
-Tolerances as in test_gpu_norm_rope.py."""
+"""Norms and rotation at the edges of what the entry points take: eps = 0, kinds of heads without heads, gradients of gradients, and
+gradients of an FP32 accumulator.  Tolerances as in test_gpu_norm_rope.py."""
 import numpy as np
 import pytest
 import torch
@@ -97,3 +97,22 @@ def test_a_second_derivative_is_refused():
     dq, = torch.autograd.grad(qo.square().sum() + ko.sum(), q, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (dq.square().sum() + q.square().sum()).backward()          # (the first term alone would be left out in silence)
+
+
+@pytest.mark.parametrize("in_type,out_type", [(F32, BF16), (F32, F16), (BF16, F32), (F16, BF16), (BF16, BF16)])
+def test_autograd_gradients_have_the_precision_of_the_inputs(in_type, out_type):
+    """The gradient of an FP32 accumulator is not rounded to the type of the outputs on its way."""
+    rng = np.random.default_rng(4)
+    q, k = (t.contiguous().requires_grad_() for t in projection(rng, 9, (3, 2), 64, in_type))
+    w = torch.from_numpy((1 + 0.2 * rng.standard_normal(64)).astype(np.float32)).cuda()
+    cos, sin, c64, s64 = tables(50, 64)
+    pos = torch.from_numpy(rng.integers(0, 50, 9).astype(np.int32)).cuda()
+    gq, gk = projection(rng, 9, (3, 2), 64, out_type)
+    qo, ko = A.QKNormRope.apply(q, k, w, w, cos, sin, pos, out_type, 1e-5, False)
+    assert qo.dtype == ko.dtype == out_type
+    torch.autograd.backward((qo, ko), (gq, gk))
+    p = pos.cpu().numpy()
+    for x, g in ((q, gq), (k, gk)):
+        assert x.grad.dtype == in_type
+        want, mag, _, _ = O.norm_rope_grad(x.detach().double().cpu().numpy(), w.double().cpu().numpy(), g.double().cpu().numpy(), c64[p], s64[p], 64, 1e-5)
+        close(x.grad, want, UNIT[in_type] * np.abs(want) + TINY[in_type] + 64 * E32 * mag)
