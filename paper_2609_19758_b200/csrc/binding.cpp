@@ -108,7 +108,33 @@ int32_t *status_ptr(PyObject *o, int device)
         refuse(PyExc_ValueError, "status: an int32 tensor on cuda:%d expected", device);
     return static_cast<int32_t *>(t->data_ptr());
 }
-void *stream_ptr(PyObject *o) { return PyLong_AsVoidPtr(o); }
+void *stream_ptr(PyObject *o)
+{
+    void *p = PyLong_AsVoidPtr(o);
+    if (!p && PyErr_Occurred()) throw Refused{};
+    return p;
+}
+double number(PyObject *o)
+{
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw Refused{};
+    return x;
+}
+bool truth(PyObject *o)
+{
+    const int x = PyObject_IsTrue(o);
+    if (x < 0) throw Refused{};
+    return x != 0;
+}
+// A bound or a window: beyond 32 bits it limits as little (or is refused as much) as the widest that they hold.
+int32_t clamped(PyObject *o)
+{
+    int beyond = 0;
+    const long long x = PyLong_AsLongLongAndOverflow(o, &beyond);
+    if (x == -1 && !beyond && PyErr_Occurred()) throw Refused{};
+    if (beyond) return beyond > 0 ? INT32_MAX : INT32_MIN;
+    return x > INT32_MAX ? INT32_MAX : x < INT32_MIN ? INT32_MIN : (int32_t)x;
+}
 
 // One kind of heads and where they go; with no `out`, only what is read.
 fpsk_heads heads(const at::Tensor *x, const at::Tensor *out, const at::Tensor *w, const at::Tensor &like, at::ScalarType out_type, int device,
@@ -237,9 +263,9 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int device = device_of(like, "q, k"), in_type = elem(like, "q, k"), out_type = elem(*out, "the output");
         const fpsk_heads hq = heads(q, qo, tensor(a[7], "q_weight"), like, out->scalar_type(), device, "q", true);
         const fpsk_heads hk = heads(k, ko, tensor(a[8], "k_weight"), like, out->scalar_type(), device, "k", true);
-        const fpsk_rotary r = rotary(a[2], a[3], a[4], PyObject_IsTrue(a[10]), like.size(0), device);
+        const fpsk_rotary r = rotary(a[2], a[3], a[4], truth(a[10]), like.size(0), device);
         return lib.norm_rope(&hq, &hk, like.size(0), (int32_t)like.size(2), (fpsk_elem)in_type, (fpsk_elem)out_type, &r,
-                             (float)PyFloat_AsDouble(a[9]), status_ptr(a[11], device), stream_ptr(a[12]));
+                             (float)number(a[9]), status_ptr(a[11], device), stream_ptr(a[12]));
     });
 }
 // q, k, dq_out, dk_out, cos, sin, positions, dq, dk, dq_weight, dk_weight, ws, q_weight, k_weight, eps, interleaved, status, stream
@@ -254,9 +280,9 @@ PyObject *py_norm_rope_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (!ws.is_cuda() || ws.get_device() != device || !ws.is_contiguous()) refuse(PyExc_ValueError, "ws: on cuda:%d expected", device);
         const fpsk_heads_grad hq = heads_grad(q, a[2], a[7], tensor(a[12], "q_weight"), a[9], like, g.scalar_type(), device, "q");
         const fpsk_heads_grad hk = heads_grad(k, a[3], a[8], tensor(a[13], "k_weight"), a[10], like, g.scalar_type(), device, "k");
-        const fpsk_rotary r = rotary(a[4], a[5], a[6], PyObject_IsTrue(a[15]), like.size(0), device);
+        const fpsk_rotary r = rotary(a[4], a[5], a[6], truth(a[15]), like.size(0), device);
         return lib.norm_rope_backward(&hq, &hk, like.size(0), (int32_t)like.size(2), (fpsk_elem)in_type, (fpsk_elem)grad_type, &r,
-                                      (float)PyFloat_AsDouble(a[14]), ws.data_ptr(), (size_t)ws.nbytes(), status_ptr(a[16], device), stream_ptr(a[17]));
+                                      (float)number(a[14]), ws.data_ptr(), (size_t)ws.nbytes(), status_ptr(a[16], device), stream_ptr(a[17]));
     });
 }
 PyObject *py_check_cache(PyObject *, PyObject *const *a, Py_ssize_t n)
@@ -276,9 +302,9 @@ PyObject *py_append(PyObject *, PyObject *const *a, Py_ssize_t n)
         const fpsk_heads hk = heads(&k, nullptr, tensor(a[9], "k_weight"), k, c.type, c.device, "k", false);
         const fpsk_heads hv = heads(&v, nullptr, nullptr, k, c.type, c.device, "v", false);
         const fpsk_heads hq = heads(q, tensor(a[11], "q_out"), tensor(a[12], "q_weight"), k, c.type, c.device, "q", true);
-        const fpsk_rotary r = rotary(a[7], a[8], a[13], PyObject_IsTrue(a[15]), k.size(0), c.device);
+        const fpsk_rotary r = rotary(a[7], a[8], a[13], truth(a[15]), k.size(0), c.device);
         const fpsk_paged_batch b = batch(a[4], a[5], a[6], k.size(0), c.device);
-        return lib.append(&c.c, &b, &hk, &hv, &hq, (fpsk_elem)in_type, &r, (float)PyFloat_AsDouble(a[14]), status_ptr(a[16], c.device),
+        return lib.append(&c.c, &b, &hk, &hv, &hq, (fpsk_elem)in_type, &r, (float)number(a[14]), status_ptr(a[16], c.device),
                           stream_ptr(a[17]));
     });
 }
@@ -304,16 +330,15 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         t.q_token_stride = q.stride(0); t.q_head_stride = q.stride(1);
         t.out_token_stride = out.stride(0); t.out_head_stride = out.stride(1);
         t.n_heads = (int32_t)q.size(1);
-        t.causal = PyObject_IsTrue(a[11]);
-        t.window = (int32_t)PyLong_AsLong(a[12]);
-        t.max_q_len = (int32_t)PyLong_AsLong(a[8]);
-        t.max_kv_len = (int32_t)PyLong_AsLong(a[9]);
+        t.causal = truth(a[11]);
+        t.window = clamped(a[12]);
+        t.max_q_len = clamped(a[8]);
+        t.max_kv_len = clamped(a[9]);
         if (a[10] != Py_None) {
-            const double scale = PyFloat_AsDouble(a[10]);
+            const double scale = number(a[10]);
             if (!(scale > 0) || scale > 3.4e38) refuse(PyExc_ValueError, "scale must be positive and finite");
             t.scale = (float)scale;
         }
-        if (PyErr_Occurred()) throw Refused{};
         const fpsk_paged_batch b = batch(a[4], a[5], a[6], q.size(0), c.device);
         return lib.attention(&c.c, &b, &t, ws.data_ptr(), (size_t)ws.nbytes(), status_ptr(a[14], c.device), stream_ptr(a[15]));
     });

@@ -1,0 +1,91 @@
+"""What the Python entry points of the attention operators do with arguments that are no numbers or out of a C integer's range."""
+import pytest
+import torch
+
+from paper_2609_19758_b200 import attention as A
+from paper_2609_19758_b200 import build as B
+from paper_2609_19758_b200 import fpsk
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    B.build()
+
+
+class NoTruth:
+    def __bool__(self):
+        raise RuntimeError("no truth value")
+
+
+def rope_args(device="cuda", tokens=3):
+    q = torch.randn(tokens, 2, 32, device=device)
+    cos, sin = A.rotary_tables(10, 32, device=device)
+    pos = torch.arange(tokens, dtype=torch.int32, device=device)
+    return q, cos, sin, pos, torch.zeros(tokens, 2, 32, dtype=F16, device=device)
+
+
+def attention_args(device="cuda", keys=300):
+    g = torch.Generator(device=device).manual_seed(1)
+    k, v = (torch.randn(20, 16, 2, 64, generator=g, device=device).to(BF16) for _ in range(2))
+    q = torch.randn(1, 4, 64, generator=g, device=device).to(BF16)
+    cu, kv = (torch.tensor(t, dtype=torch.int32, device=device) for t in ([0, 1], [keys]))
+    table = torch.arange(20, dtype=torch.int32, device=device)[None]
+    return A.PagedCache(k, v), q, torch.full_like(q, 7.0), cu, kv, table
+
+
+@pytest.mark.parametrize("bad", ["x", None, object()])
+def test_numbers_that_are_none(bad):
+    q, cos, sin, pos, out = rope_args()
+    with pytest.raises(TypeError):
+        A.qk_norm_rope(q, None, cos, sin, pos, out, None, eps=bad)
+    with pytest.raises(TypeError):
+        A.qk_norm_rope_backward(q, None, out, None, cos, sin, pos, out.clone(), None, None, None, A.norm_rope_workspace(32), eps=bad)
+    cache, q, out, cu, kv, table = attention_args()
+    ws = A.attention_workspace()
+    k = torch.randn(1, 2, 64, device="cuda")
+    with pytest.raises(TypeError):
+        A.paged_append(cache, k, k, cu, kv, table, eps=bad)
+    with pytest.raises(TypeError):
+        A.paged_attention(cache, q, out, cu, kv, table, ws, bad, 300)
+    with pytest.raises(TypeError):
+        A.paged_attention(cache, q, out, cu, kv, table, ws, 1, bad)
+    with pytest.raises(TypeError):
+        A.paged_attention(cache, q, out, cu, kv, table, ws, 1, 300, window=bad)
+    if bad is not None:                          # (no scale: the usual one)
+        with pytest.raises(TypeError):
+            A.paged_attention(cache, q, out, cu, kv, table, ws, 1, 300, scale=bad)
+    assert bool((out == 7.0).all())
+
+
+def test_an_argument_without_a_truth_value():
+    q, cos, sin, pos, out = rope_args()
+    with pytest.raises(RuntimeError, match="no truth value"):
+        A.qk_norm_rope(q, None, cos, sin, pos, out, None, interleaved=NoTruth())
+    cache, q, out, cu, kv, table = attention_args()
+    with pytest.raises(RuntimeError, match="no truth value"):
+        A.paged_attention(cache, q, out, cu, kv, table, A.attention_workspace(), 1, 300, causal=NoTruth())
+
+
+@pytest.mark.parametrize("wide", [2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63, 2 ** 70])
+def test_wide_windows_and_bounds_are_no_limits(wide):
+    cache, q, out, cu, kv, table = attention_args()
+    ws = A.attention_workspace()
+    A.paged_attention(cache, q, out, cu, kv, table, ws, 1, 300)
+    for kw in (dict(window=wide), dict(max_kv_len=wide), dict(max_q_len=wide)):
+        again = torch.full_like(out, 7.0)
+        A.paged_attention(cache, q, again, cu, kv, table, ws, **{**dict(max_q_len=1, max_kv_len=300), **kw})
+        # (other bounds may choose another form: a unit of the type, from the order of the sums)
+        assert float((again.float() - out.float()).abs().max()) <= 2.0 ** -7 * float(out.float().abs().max())
+
+
+@pytest.mark.parametrize("low", [-2 ** 31, -2 ** 32 - 1, -2 ** 32 + 5, -2 ** 70])
+def test_negative_numbers_beyond_32_bits_are_refused(low):
+    cache, q, out, cu, kv, table = attention_args()
+    ws = A.attention_workspace()
+    for kw in (dict(window=low), dict(max_kv_len=low), dict(max_q_len=low)):
+        with pytest.raises(fpsk.FpskError):
+            A.paged_attention(cache, q, out, cu, kv, table, ws, **{**dict(max_q_len=1, max_kv_len=300), **kw})
