@@ -1259,7 +1259,8 @@ template <typename T, int DP, int MODE, bool BY_ROWS> static fpsk_status launch_
     g.tile_tokens = Cfg::kTileRows / a.group;
     // a CTA on every SM, or for every key tile where the lengths promise fewer
     const int item_tokens = g.tile_tokens * Cfg::kQTiles;
-    const double tiles = (double)a.n_seqs * a.hk * ((max_q_len + item_tokens - 1) / item_tokens) * ((max_kv_len + kKeysPerTile - 1) / kKeysPerTile);
+    auto pieces = [](int n, int of) { return (double)(((long long)n + of - 1) / of); };
+    const double tiles = (double)a.n_seqs * a.hk * pieces(max_q_len, item_tokens) * pieces(max_kv_len, kKeysPerTile);
     const int ctas = tiles < 1.0 ? 1 : tiles < sms ? (int)tiles : sms;
     for (g.box_log = 3; g.box_log < 7 && a.page_size % (2 << g.box_log) == 0;) ++g.box_log;
     g.wide_out = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.ots % 16 == 0 && a.ohs % 16 == 0 && a.dim % 16 == 0;

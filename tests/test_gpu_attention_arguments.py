@@ -89,3 +89,26 @@ def test_negative_numbers_beyond_32_bits_are_refused(low):
     for kw in (dict(window=low), dict(max_kv_len=low), dict(max_q_len=low)):
         with pytest.raises(fpsk.FpskError):
             A.paged_attention(cache, q, out, cu, kv, table, ws, **{**dict(max_q_len=1, max_kv_len=300), **kw})
+
+
+def test_the_widest_bound_of_the_keys_takes_every_multiprocessor():
+    """The bound chooses the grid: the widest one must not overflow into a grid of one block (148 times as long)."""
+    k, v = (torch.randn(4096, 16, 1, 128, device="cuda").to(BF16) for _ in range(2))
+    q = torch.randn(1, 8, 128, device="cuda").to(BF16)
+    cu, kv = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([0, 1], [65536]))
+    table = torch.arange(4096, dtype=torch.int32, device="cuda")[None]
+    cache, ws, out = A.PagedCache(k, v), A.attention_workspace(), torch.empty_like(q)
+
+    def fastest(bound):
+        times = []
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            A.paged_attention(cache, q, out, cu, kv, table, ws, 1, bound)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    fastest(65536)
+    assert fastest(2 ** 31 - 1) <= 5 * fastest(65536)
