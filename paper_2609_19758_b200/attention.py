@@ -2,7 +2,7 @@
 queries and keys with their backward pass, writes to a paged cache, and attention of new tokens over it.
 
 Argument marshalling only, like ``fpsk.py``, in C++ (``csrc/binding.cpp``): every step runs inside the CUDA library,
-asynchronously on the given (or the current) stream.  Outputs and workspaces are the caller's tensors; wrong shapes, types,
+asynchronously on the given (or the current) stream of the tensors' device.  Outputs and workspaces are the caller's tensors; wrong shapes, types,
 devices or strides raise ValueError or TypeError, what the library refuses raises FpskError.
 """
 from __future__ import annotations
@@ -52,9 +52,12 @@ def _stream(device: int, stream) -> int:
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
 
 
-def _workspace(nbytes: int, device, stream) -> torch.Tensor:
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device or "cuda")
-    _check(fpsk.lib().fpsk_attention_workspace_init(ws.data_ptr(), nbytes, _stream(ws.get_device(), stream)), "fpsk_attention_workspace_init")
+def _workspace(nbytes, device, stream) -> torch.Tensor:
+    """A workspace of nbytes() bytes on the device (None: the current one)."""
+    with torch.cuda.device(device):
+        n = nbytes()
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        _check(fpsk.lib().fpsk_attention_workspace_init(ws.data_ptr(), n, _stream(ws.get_device(), stream)), "fpsk_attention_workspace_init")
     return ws
 
 
@@ -82,7 +85,7 @@ def norm_rope_workspace(head_dim: int, device=None, stream=None) -> torch.Tensor
     n = int(fpsk.lib().fpsk_norm_rope_workspace_bytes(head_dim))
     if n == 0:
         raise FpskError(ERR_SHAPE, "fpsk_norm_rope_workspace_bytes")
-    return _workspace(n, device, stream)
+    return _workspace(lambda: n, device, stream)
 
 
 def qk_norm_rope_backward(q, k, dq_out, dk_out, cos, sin, positions, dq, dk, dq_weight, dk_weight, ws: torch.Tensor,
@@ -150,8 +153,7 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_q: torc
 def attention_workspace(device=None, stream=None) -> torch.Tensor:
     """Workspace of paged_attention, of one size for all calls on a device; serves one call at a time."""
     _bind()
-    with torch.cuda.device(device):
-        return _workspace(int(fpsk.lib().fpsk_paged_attention_workspace_bytes()), device, stream)
+    return _workspace(lambda: int(fpsk.lib().fpsk_paged_attention_workspace_bytes()), device, stream)
 
 
 def paged_attention(cache: PagedCache, q: torch.Tensor, out: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor,

@@ -3,6 +3,7 @@
 // marshalling: in Python it took 7 of the 10 us that the smallest norm and rotation call needs on the host, here well under one.
 // The library's functions come by address, from the build of it that the process has loaded.
 #include <Python.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "fpsk_attention.h"
@@ -219,6 +220,12 @@ fpsk_paged_batch batch(PyObject *cu_, PyObject *kv_, PyObject *table_, int64_t t
     return b;
 }
 
+// The library launches on the current device and sizes its grids by it: that is the tensors' for the time of a call.
+struct OnDevice {
+    c10::DeviceGuard guard;
+    explicit OnDevice(int device) : guard(c10::Device(c10::kCUDA, (c10::DeviceIndex)device)) {}
+};
+
 template <typename F> PyObject *call(Py_ssize_t given, Py_ssize_t wanted, F f)
 {
     if (given != wanted) {
@@ -264,6 +271,7 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
         const fpsk_heads hq = heads(q, qo, tensor(a[7], "q_weight"), like, out->scalar_type(), device, "q", true);
         const fpsk_heads hk = heads(k, ko, tensor(a[8], "k_weight"), like, out->scalar_type(), device, "k", true);
         const fpsk_rotary r = rotary(a[2], a[3], a[4], truth(a[10]), like.size(0), device);
+        const OnDevice on(device);
         return lib.norm_rope(&hq, &hk, like.size(0), (int32_t)like.size(2), (fpsk_elem)in_type, (fpsk_elem)out_type, &r,
                              (float)number(a[9]), status_ptr(a[11], device), stream_ptr(a[12]));
     });
@@ -281,6 +289,7 @@ PyObject *py_norm_rope_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const fpsk_heads_grad hq = heads_grad(q, a[2], a[7], tensor(a[12], "q_weight"), a[9], like, g.scalar_type(), device, "q");
         const fpsk_heads_grad hk = heads_grad(k, a[3], a[8], tensor(a[13], "k_weight"), a[10], like, g.scalar_type(), device, "k");
         const fpsk_rotary r = rotary(a[4], a[5], a[6], truth(a[15]), like.size(0), device);
+        const OnDevice on(device);
         return lib.norm_rope_backward(&hq, &hk, like.size(0), (int32_t)like.size(2), (fpsk_elem)in_type, (fpsk_elem)grad_type, &r,
                                       (float)number(a[14]), ws.data_ptr(), (size_t)ws.nbytes(), status_ptr(a[16], device), stream_ptr(a[17]));
     });
@@ -304,6 +313,7 @@ PyObject *py_append(PyObject *, PyObject *const *a, Py_ssize_t n)
         const fpsk_heads hq = heads(q, tensor(a[11], "q_out"), tensor(a[12], "q_weight"), k, c.type, c.device, "q", true);
         const fpsk_rotary r = rotary(a[7], a[8], a[13], truth(a[15]), k.size(0), c.device);
         const fpsk_paged_batch b = batch(a[4], a[5], a[6], k.size(0), c.device);
+        const OnDevice on(c.device);
         return lib.append(&c.c, &b, &hk, &hv, &hq, (fpsk_elem)in_type, &r, (float)number(a[14]), status_ptr(a[16], c.device),
                           stream_ptr(a[17]));
     });
@@ -340,6 +350,7 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
             t.scale = (float)scale;
         }
         const fpsk_paged_batch b = batch(a[4], a[5], a[6], q.size(0), c.device);
+        const OnDevice on(c.device);
         return lib.attention(&c.c, &b, &t, ws.data_ptr(), (size_t)ws.nbytes(), status_ptr(a[14], c.device), stream_ptr(a[15]));
     });
 }

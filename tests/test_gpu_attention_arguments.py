@@ -1,4 +1,5 @@
-"""What the Python entry points of the attention operators do with arguments that are no numbers or out of a C integer's range."""
+"""What the Python entry points of the attention operators do with arguments that are no numbers, out of a C integer's range, or of a
+device that is not the current one."""
 import pytest
 import torch
 
@@ -112,3 +113,35 @@ def test_the_widest_bound_of_the_keys_takes_every_multiprocessor():
 
     fastest(65536)
     assert fastest(2 ** 31 - 1) <= 5 * fastest(65536)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
+def test_tensors_of_a_device_that_is_not_current():
+    results = []
+    for device in ("cuda:0", "cuda:1"):
+        q, cos, sin, pos, out = (t.to(device) for t in rope_args("cuda:0"))
+        torch.manual_seed(0)
+        q = torch.randn(q.shape).to(device)
+        A.qk_norm_rope(q, None, cos, sin, pos, out, None)
+        dx = torch.empty_like(out)
+        A.qk_norm_rope_backward(q, None, out, None, cos, sin, pos, dx, None, None, None, A.norm_rope_workspace(32, device))
+        torch.cuda.synchronize(device)
+        results.append((out.cpu(), dx.cpu()))
+        assert torch.cuda.current_device() == 0
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    results = []
+    for device in ("cuda:0", "cuda:1"):
+        cache, q, out, cu, kv, table = attention_args("cuda:0")
+        cache = A.PagedCache(cache.k.to(device), cache.v.to(device))
+        q, out, cu, kv, table = (t.to(device) for t in (q, out, cu, kv, table))
+        A.paged_attention(cache, q, out, cu, kv, table, A.attention_workspace(device), 1, 300)
+        torch.cuda.synchronize(device)
+        results.append(out.cpu())
+        assert torch.cuda.current_device() == 0
+    assert torch.equal(*results)
+
+
+def test_workspaces_lie_on_the_device_that_is_asked_for():
+    for device in (0, "cuda:0", torch.device("cuda", 0), None):
+        for ws in (A.norm_rope_workspace(64, device), A.attention_workspace(device)):
+            assert ws.device == torch.device("cuda", torch.cuda.current_device() if device is None else 0)
