@@ -46,17 +46,15 @@ __global__ void __launch_bounds__(32 * kPlainWarps) attention_rows_kernel(const 
     for (int j = lo + warp; j < hi; j += kPlainWarps) {
         const int col = j / g.page_size, row = j - col * g.page_size;
         const long long page = col < g.max_pages ? g.table[seq * g.table_stride + col] : -1;
-        if (page < 0 || page >= g.n_pages) {
-            if (lane == 0) report_status(g.status, FPSK_ERR_PARAM);
-            continue;
-        }
-        const T *kp = static_cast<const T *>(g.k) + page * g.kps + row * g.kts + kvh * g.khs;
-        const T *vp = static_cast<const T *>(g.v) + page * g.vps + row * g.vts + kvh * g.vhs;
+        const bool there = page >= 0 && page < g.n_pages;              // else zeros, as in the tensor-core kernel
+        if (!there && lane == 0) report_status(g.status, FPSK_ERR_PARAM);
+        const T *kp = static_cast<const T *>(g.k) + (there ? page * g.kps + row * g.kts + kvh * g.khs : 0);
+        const T *vp = static_cast<const T *>(g.v) + (there ? page * g.vps + row * g.vts + kvh * g.vhs : 0);
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int c = lane + 32 * i;
-            if (c < g.dim) s = fmaf(q[i], Elem<T>::to_f(kp[c]), s);
+            if (there && c < g.dim) s = fmaf(q[i], Elem<T>::to_f(kp[c]), s);
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
@@ -67,7 +65,7 @@ __global__ void __launch_bounds__(32 * kPlainWarps) attention_rows_kernel(const 
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int c = lane + 32 * i;
-            if (c < g.dim) o[i] = fmaf(o[i], a, p * Elem<T>::to_f(vp[c]));
+            if (c < g.dim) o[i] = fmaf(o[i], a, there ? p * Elem<T>::to_f(vp[c]) : 0.f);
         }
     }
     if (lane == 0) { sm[warp] = m; sl[warp] = l; }
