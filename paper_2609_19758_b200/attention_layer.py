@@ -31,11 +31,20 @@ class PageTable:
         return len(self.rows) - 1
 
     def extend(self, seq: int, tokens: int) -> None:
-        self.length[seq] += tokens
-        while len(self.rows[seq]) * self.page_size < self.length[seq]:
-            if not self.free:
-                raise RuntimeError("the cache is full")
-            self.rows[seq].append(self.free.pop())
+        self.extend_all([seq], [tokens])
+
+    def extend_all(self, seqs: Sequence[int], tokens: Sequence[int]) -> None:
+        """Room for the new tokens of several sequences: for all of them, or an exception and none."""
+        if len(seqs) != len(tokens) or len(set(seqs)) != len(seqs):
+            raise ValueError("a number of tokens for each sequence, each sequence once")
+        if any(not 0 <= b < len(self.rows) for b in seqs) or any(n < 0 for n in tokens):
+            raise ValueError("an unknown sequence, or a negative number of tokens")
+        wanted = [-(-(self.length[b] + n) // self.page_size) - len(self.rows[b]) for b, n in zip(seqs, tokens)]
+        if sum(wanted) > len(self.free):
+            raise RuntimeError("the cache is full")
+        for b, n, pages in zip(seqs, tokens, wanted):
+            self.rows[b] += [self.free.pop() for _ in range(pages)]
+            self.length[b] += n
 
     def close(self, seq: int) -> None:
         self.free += self.rows[seq][::-1]
@@ -73,9 +82,12 @@ class VerifiedAttention:
         return c
 
     def step(self, x: torch.Tensor, seqs: Sequence[int], new: Sequence[int], fault=None) -> torch.Tensor:
-        """x (tokens, hidden): the new tokens of the sequences `seqs`, `new` of each.  Returns the layer's output, FP32."""
-        for b, n in zip(seqs, new):
-            self.pages.extend(b, n)
+        """x (tokens, hidden): the new tokens of the sequences `seqs`, `new` of each.  Returns the layer's output, FP32.  A step that is
+        refused (ValueError, or RuntimeError when the cache is full) changes nothing."""
+        w = self.qkv_weight
+        if x.dim() != 2 or x.shape[1] != w.shape[0] or x.shape[0] != sum(new) or x.shape[0] == 0 or x.dtype != w.dtype or x.device != w.device:
+            raise ValueError(f"x: ({sum(new)}, {w.shape[0]}) {w.dtype} on {w.device} expected, at least one token")
+        self.pages.extend_all(seqs, new)
         cu = [0]
         for n in new:
             cu.append(cu[-1] + n)

@@ -1,0 +1,52 @@
+"""Steps of the verified attention layer that go wrong: they are refused or reported, and leave the layer usable."""
+import pytest
+import torch
+
+from paper_2609_19758_b200 import attention_layer as L
+from paper_2609_19758_b200 import build as B
+
+pytestmark = pytest.mark.gpu
+
+HIDDEN, HQ, HK, DIM = 256, 4, 2, 64
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    B.build()
+
+
+def make(seed=0, **kw):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def rand(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+
+    cols = (HQ + 2 * HK) * DIM
+    layer = L.VerifiedAttention((rand(HIDDEN, cols) * HIDDEN ** -0.5).to(torch.bfloat16), (rand(HQ * DIM, HIDDEN) * (HQ * DIM) ** -0.5).to(torch.bfloat16),
+                                HQ, HK, DIM, 1 + 0.1 * rand(DIM), 1 + 0.1 * rand(DIM), **kw)
+    return layer, lambda n: rand(n, HIDDEN).to(torch.bfloat16)
+
+
+def pages(layer):
+    return (sorted(layer.pages.free), [list(r) for r in layer.pages.rows], list(layer.pages.length))
+
+
+def test_refused_steps_leave_the_pages_alone():
+    layer, x = make(n_pages=4, page_size=16)
+    a, b = layer.pages.open(), layer.pages.open()
+    layer.step(x(20), [a], [20])
+    before, cache = pages(layer), layer.cache.k.clone()
+    for rows, seqs, new in ((5, [a], [4]), (4, [a, b], [4]), (3, [a, a], [1, 2]), (1, [a, b], [2, -1]), (0, [a], [0]), (1, [], []), (1, [7], [1])):
+        with pytest.raises(ValueError):
+            layer.step(x(rows), seqs, new)
+        assert pages(layer) == before
+    with pytest.raises(ValueError):
+        layer.step(x(2)[:, :-8], [a], [2])
+    with pytest.raises(ValueError):
+        layer.step(x(2).float(), [a], [2])
+    with pytest.raises(RuntimeError, match="full"):
+        layer.step(x(45), [a, b], [10, 35])
+    assert pages(layer) == before and torch.equal(layer.cache.k, cache)
+    assert not layer.fired()
+    layer.step(x(44), [a, b], [12, 32])
+    assert layer.pages.length == [32, 32] and not layer.fired()
