@@ -33,12 +33,14 @@ class PageTable:
     def extend(self, seq: int, tokens: int) -> None:
         self.extend_all([seq], [tokens])
 
-    def extend_all(self, seqs: Sequence[int], tokens: Sequence[int]) -> None:
-        """Room for the new tokens of several sequences: for all of them, or an exception and none."""
+    def extend_all(self, seqs: Sequence[int], tokens: Sequence[int], most: Optional[int] = None) -> None:
+        """Room for the new tokens of several sequences, of at most `most` tokens each: for all of them, or an exception and none."""
         if len(seqs) != len(tokens) or len(set(seqs)) != len(seqs):
             raise ValueError("a number of tokens for each sequence, each sequence once")
         if any(not 0 <= b < len(self.rows) for b in seqs) or any(n < 0 for n in tokens):
             raise ValueError("an unknown sequence, or a negative number of tokens")
+        if most is not None and any(self.length[b] + n > most for b, n in zip(seqs, tokens)):
+            raise ValueError(f"a sequence of more than {most} tokens")
         wanted = [-(-(self.length[b] + n) // self.page_size) - len(self.rows[b]) for b, n in zip(seqs, tokens)]
         if sum(wanted) > len(self.free):
             raise RuntimeError("the cache is full")
@@ -65,6 +67,7 @@ class VerifiedAttention:
         self.pages = PageTable(n_pages, page_size)
         self.cos, self.sin = A.rotary_tables(n_pos, dim if rot_dim is None else rot_dim, device=dev)
         self.ws = A.attention_workspace(dev)
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.state = fpsk.new_probe_state(dev)
         self.result = fpsk.new_probe_result()
         self.probe_ws = {}
@@ -87,7 +90,7 @@ class VerifiedAttention:
         w = self.qkv_weight
         if x.dim() != 2 or x.shape[1] != w.shape[0] or x.shape[0] != sum(new) or x.shape[0] == 0 or x.dtype != w.dtype or x.device != w.device:
             raise ValueError(f"x: ({sum(new)}, {w.shape[0]}) {w.dtype} on {w.device} expected, at least one token")
-        self.pages.extend_all(seqs, new)
+        self.pages.extend_all(seqs, new, most=self.cos.shape[0] if self.cos.shape[1] else None)
         cu = [0]
         for n in new:
             cu.append(cu[-1] + n)
@@ -100,15 +103,21 @@ class VerifiedAttention:
         q, k, v = (t.unflatten(1, (-1, dim)) for t in c.split((hq * dim, hk * dim, hk * dim), dim=1))
         q_out = torch.empty(n, hq, dim, dtype=x.dtype, device=x.device)
         A.paged_append(self.cache, k, v, cu_q, kv_len, block_table, self.cos, self.sin, self.k_weight, q=q, q_out=q_out,
-                       q_weight=self.q_weight, eps=self.eps)
+                       q_weight=self.q_weight, eps=self.eps, status=self.status)
         out = torch.empty_like(q_out)
-        A.paged_attention(self.cache, q_out, out, cu_q, kv_len, block_table, self.ws, max(new), max(kv))
+        A.paged_attention(self.cache, q_out, out, cu_q, kv_len, block_table, self.ws, max(new), max(kv), status=self.status)
         return self._verified(out.flatten(1), self.out_weight)
 
     def fired(self) -> bool:
-        """Whether any product since the last call was dirty (the one host read of a step)."""
+        """Whether any product since the last call was dirty (where a step is read on the host).  What the kernels of the append and the
+        attention reported since then, a page outside the cache or a wait that gave up, is raised."""
         s = fpsk.read_probe_state(self.state)
         fpsk.reset_probe_state(self.state)
+        reported = int(self.status)
+        if reported != fpsk.STATUS_OK:
+            self.status.zero_()
+            self.ws = A.attention_workspace(self.ws.device)            # (a wait that gave up may leave its words)
+            raise fpsk.FpskError(reported, "attention layer")
         return bool(s.fired_any)
 
 

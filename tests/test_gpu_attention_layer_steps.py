@@ -4,6 +4,7 @@ import torch
 
 from paper_2609_19758_b200 import attention_layer as L
 from paper_2609_19758_b200 import build as B
+from paper_2609_19758_b200 import fpsk
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +51,32 @@ def test_refused_steps_leave_the_pages_alone():
     assert not layer.fired()
     layer.step(x(44), [a, b], [12, 32])
     assert layer.pages.length == [32, 32] and not layer.fired()
+
+
+def test_positions_beyond_the_tables_are_refused():
+    layer, x = make(n_pages=8, page_size=16, n_pos=40)
+    a = layer.pages.open()
+    layer.step(x(40), [a], [40])
+    before = pages(layer)
+    with pytest.raises(ValueError, match="40"):
+        layer.step(x(1), [a], [1])
+    assert pages(layer) == before and not layer.fired()
+    assert not layer.cache.k.isnan().any()
+    layer, x = make(n_pages=8, page_size=16, n_pos=40, rot_dim=0)
+    layer.step(x(41), [layer.pages.open()], [41])                # nothing is rotated: no tables to leave
+    assert not layer.fired()
+
+
+def test_what_only_the_device_sees_is_raised_with_the_verdict():
+    layer, x = make(n_pages=8, page_size=16)
+    a = layer.pages.open()
+    layer.step(x(20), [a], [20])
+    assert not layer.fired()
+    layer.pages.rows[a][0] = 77                  # (a table gone wrong: no such page)
+    layer.step(x(1), [a], [1])
+    with pytest.raises(fpsk.FpskError) as e:
+        layer.fired()
+    assert e.value.status == fpsk.ERR_PARAM
+    layer.pages.rows[a][0] = 7
+    layer.step(x(1), [a], [1])
+    assert not layer.fired()                     # reported once
