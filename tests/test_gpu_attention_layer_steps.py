@@ -80,3 +80,15 @@ def test_what_only_the_device_sees_is_raised_with_the_verdict():
     layer.pages.rows[a][0] = 7
     layer.step(x(1), [a], [1])
     assert not layer.fired()                     # reported once
+
+
+def test_workspaces_do_not_grow_with_the_calls():
+    layer, x = make(n_pages=64, page_size=16)
+    a = layer.pages.open()
+    for n in (3, 17, 1, 40, 2):
+        layer.step(x(n), [a], [n])
+    held = {t.data_ptr() for t in layer.probe_ws.values()}
+    assert len(held) == 2                        # one for each product, whatever the tokens
+    for n in (5, 90, 33):
+        layer.step(x(n), [a], [n])
+    assert {t.data_ptr() for t in layer.probe_ws.values()} == held and not layer.fired()
