@@ -3,7 +3,7 @@
 The QKV projection is a vendor GEMM with its FP32 accumulator delivered.  The probe checks it; then the accumulator itself is
 read by ``paged_append`` (queries and keys normed and rotated, keys and values written to the pages of the cache, rounded
 once), ``paged_attention`` runs the new tokens over the cache, and the output projection is checked like the first.  Verdicts
-are accumulated on the device and read once per step.
+are accumulated on the device and read once per step; a dirty step is retracted and repeated.
 """
 from __future__ import annotations
 
@@ -48,6 +48,17 @@ class PageTable:
             self.rows[b] += [self.free.pop() for _ in range(pages)]
             self.length[b] += n
 
+    def retract(self, seqs: Sequence[int], tokens: Sequence[int]) -> None:
+        """Takes the last tokens of the sequences out again, and their pages where nothing is left on them."""
+        if len(seqs) != len(tokens) or len(set(seqs)) != len(seqs):
+            raise ValueError("a number of tokens for each sequence, each sequence once")
+        if any(not 0 <= b < len(self.rows) for b in seqs) or any(not 0 <= n <= self.length[b] for b, n in zip(seqs, tokens)):
+            raise ValueError("an unknown sequence, or more tokens than it has")
+        for b, n in list(zip(seqs, tokens))[::-1]:                     # (the reverse of extend_all, page for page)
+            self.length[b] -= n
+            while (len(self.rows[b]) - 1) * self.page_size >= self.length[b] and self.rows[b]:
+                self.free.append(self.rows[b].pop())
+
     def close(self, seq: int) -> None:
         self.free += self.rows[seq][::-1]
         self.rows[seq], self.length[seq] = [], 0
@@ -71,6 +82,7 @@ class VerifiedAttention:
         self.state = fpsk.new_probe_state(dev)
         self.result = fpsk.new_probe_result()
         self.probe_ws = {}
+        self.last = None                                               # sequences and new tokens of the last step
 
     def _verified(self, x: torch.Tensor, w: torch.Tensor, fault=None) -> torch.Tensor:
         """x w with the accumulator in FP32, probed; `fault`: (row, column, what to add), for trying the probe."""
@@ -91,6 +103,15 @@ class VerifiedAttention:
         if x.dim() != 2 or x.shape[1] != w.shape[0] or x.shape[0] != sum(new) or x.shape[0] == 0 or x.dtype != w.dtype or x.device != w.device:
             raise ValueError(f"x: ({sum(new)}, {w.shape[0]}) {w.dtype} on {w.device} expected, at least one token")
         self.pages.extend_all(seqs, new, most=self.cos.shape[0] if self.cos.shape[1] else None)
+        try:
+            out = self._step(x, seqs, new, fault)
+        except BaseException:
+            self.pages.retract(seqs, new)
+            raise
+        self.last = (list(seqs), list(new))
+        return out
+
+    def _step(self, x, seqs, new, fault):
         cu = [0]
         for n in new:
             cu.append(cu[-1] + n)
@@ -107,6 +128,14 @@ class VerifiedAttention:
         out = torch.empty_like(q_out)
         A.paged_attention(self.cache, q_out, out, cu_q, kv_len, block_table, self.ws, max(new), max(kv), status=self.status)
         return self._verified(out.flatten(1), self.out_weight)
+
+    def retract(self) -> None:
+        """Takes the last step's tokens out of the cache again, whose keys and values are there before the verdict is: a step that
+        `fired` (or raised what the device reported) is retracted and repeated."""
+        if self.last is None:
+            raise RuntimeError("no step to retract")
+        self.pages.retract(*self.last)
+        self.last = None
 
     def fired(self) -> bool:
         """Whether any product since the last call was dirty (where a step is read on the host).  What the kernels of the append and the

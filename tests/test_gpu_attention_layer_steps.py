@@ -92,3 +92,45 @@ def test_workspaces_do_not_grow_with_the_calls():
     for n in (5, 90, 33):
         layer.step(x(n), [a], [n])
     assert {t.data_ptr() for t in layer.probe_ws.values()} == held and not layer.fired()
+
+
+def test_a_dirty_step_is_taken_back_and_repeated():
+    """The verdict comes after the keys and values of the step are in the cache: retract() takes them out again."""
+    layer, x = make(n_pages=16, page_size=16)
+    other, _ = make(n_pages=16, page_size=16)
+    a, b = layer.pages.open(), layer.pages.open()
+    other.pages.open(), other.pages.open()
+    first, second, third = x(30), x(19), x(2)
+    for one in (layer, other):
+        one.step(first, [a, b], [16, 14])
+        assert not one.fired()
+    before = pages(layer)
+    layer.step(second, [b, a], [18, 1], fault=(3, HQ * DIM + 5, 40.0))       # in the keys
+    assert layer.fired()
+    layer.retract()
+    assert pages(layer) == before
+    with pytest.raises(RuntimeError):
+        layer.retract()                          # once for a step
+    y = layer.step(second, [b, a], [18, 1])
+    assert not layer.fired()
+    assert torch.equal(y, other.step(second, [b, a], [18, 1]))
+    assert torch.equal(layer.step(third, [a, b], [1, 1]), other.step(third, [a, b], [1, 1]))
+    assert not layer.fired() and not other.fired()
+
+
+def test_a_step_that_raises_on_its_way_is_taken_back(monkeypatch):
+    layer, x = make(n_pages=16, page_size=16)
+    a = layer.pages.open()
+    layer.step(x(20), [a], [20])
+    before = pages(layer)
+
+    def fails(*args, **kw):
+        raise MemoryError("no room")
+
+    with monkeypatch.context() as m:
+        m.setattr(L.A, "paged_attention", fails)
+        with pytest.raises(MemoryError):
+            layer.step(x(20), [a], [20])
+    assert pages(layer) == before
+    layer.step(x(20), [a], [20])
+    assert not layer.fired()

@@ -45,3 +45,19 @@ def test_sequences_that_make_no_step(seqs, tokens):
     with pytest.raises(ValueError):
         t.extend_all(seqs, tokens)
     assert state(t) == before
+
+
+def test_tokens_are_taken_back():
+    t = PageTable(6, 4)
+    a, b = t.open(), t.open()
+    t.extend_all([a, b], [6, 1])
+    before = state(t)
+    t.extend_all([a, b], [7, 3])
+    t.retract([a, b], [7, 3])
+    assert state(t) == before
+    t.retract([a], [6])
+    assert t.length == [0, 1] and not t.rows[a]
+    for seqs, tokens in (([b], [2]), ([a], [1]), ([b], [-1]), ([b, b], [1, 1]), ([5], [0])):
+        with pytest.raises(ValueError):
+            t.retract(seqs, tokens)
+    assert t.length == [0, 1]
