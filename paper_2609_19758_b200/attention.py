@@ -14,7 +14,7 @@ from typing import Optional
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import fpsk
+from . import build, fpsk
 from .fpsk import ERR_SHAPE, STATUS_OK, FpskError
 
 _binding = None
@@ -26,6 +26,8 @@ def _bind():
     if _binding is None:
         if not os.path.exists(BINDING_PATH):
             raise FileNotFoundError(f"{BINDING_PATH} is missing: build it with `python -m paper_2609_19758_b200.build`")
+        if not build.binding_is_current():
+            raise RuntimeError(f"{BINDING_PATH} is not made for {build.binding_mark()} build it again with `python -m paper_2609_19758_b200.build`")
         from . import _binding as b
         L = fpsk.lib()
         vp, sz = C.c_void_p, C.c_size_t
@@ -39,7 +41,7 @@ def _bind():
     return _binding
 
 
-BINDING_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_binding.so")
+BINDING_PATH = build.BINDING
 
 
 def _check(rc: int, where: str) -> None:

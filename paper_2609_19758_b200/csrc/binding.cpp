@@ -368,4 +368,13 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__binding() { return PyModule_Create(&module); }
+// (kept in the file: by it a binding made against another torch is told)
+PyMODINIT_FUNC PyInit__binding()
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "made_for", FPSK_BINDING_MARK) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
