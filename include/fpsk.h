@@ -24,7 +24,7 @@
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).
  *   - Indices are 0-based.  The 1-based index weights of the paper are internal.
  *   - Errors are return codes.  Nothing throws, aborts or resets the device.  After
- *     FPSK_ERR_CUDA the CUDA error is left for the caller to query.
+ *     FPSK_ERR_CUDA the CUDA error is left for the caller to query; fpsk_last_cuda_error names it and the call.
  *   - Fast paths use 128-bit loads when the base pointers are 16-byte aligned and the
  *     leading dimensions are multiples of 8 (A, B) / 4 (C) elements; otherwise a scalar
  *     path with the same arithmetic order runs.
@@ -123,6 +123,9 @@ typedef struct {
 } fpsk_noise;
 
 const char *fpsk_status_string(fpsk_status s);
+/* The CUDA error behind the last FPSK_ERR_CUDA that this thread was given: its name, number and text, the source line and the
+ * call that failed ("" when there was none).  Valid until the thread's next call into the library. */
+const char *fpsk_last_cuda_error(void);
 void fpsk_default_params(fpsk_params *p);
 
 /* ---- host-only scalar planning (no device work) --------------------------------------- */

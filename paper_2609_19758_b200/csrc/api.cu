@@ -5,6 +5,7 @@
 #include "fpsk_test.h"
 
 #include <math.h>
+#include <stdio.h>
 #include <string.h>
 #include <algorithm>
 #include <mutex>
@@ -13,6 +14,15 @@
 namespace fpsk {
 std::atomic<unsigned long long> g_launches{0};
 std::atomic<unsigned long long> g_lazy_resources{0};
+
+static thread_local char g_cuda_error[384] = "";
+fpsk_status cuda_failed(cudaError_t error, const char *file, int line, const char *what)
+{
+    const char *name = strrchr(file, '/');
+    snprintf(g_cuda_error, sizeof(g_cuda_error), "%s (%d: %s) at %s:%d, %.160s", cudaGetErrorName(error), (int)error, cudaGetErrorString(error),
+             name ? name + 1 : file, line, what);
+    return FPSK_ERR_CUDA;
+}
 
 #ifdef FPSK_DEBUG_BOUNDS
 // the bounds records of the source files of the library (each registers its own at load)
@@ -580,6 +590,8 @@ const char *fpsk_status_string(fpsk_status s)
     return "unknown";
 }
 
+const char *fpsk_last_cuda_error(void) { return g_cuda_error; }
+
 void fpsk_default_params(fpsk_params *p)
 {
     if (!p) return;
@@ -1128,10 +1140,11 @@ fpsk_status fpsk_verify_repair(const void *A, int64_t lda, const void *B, int64_
     if (!restore.empty()) {
         PatchEntry *d = static_cast<PatchEntry *>(rep_ws);
         fpsk_status rc2 = FPSK_OK;
-        if (cudaMemcpyAsync(d, restore.data(), sizeof(PatchEntry) * restore.size(), cudaMemcpyHostToDevice, st) != cudaSuccess)
-            rc2 = FPSK_ERR_CUDA;
+        cudaError_t e = cudaMemcpyAsync(d, restore.data(), sizeof(PatchEntry) * restore.size(), cudaMemcpyHostToDevice, st);
+        if (e != cudaSuccess) rc2 = FPSK_CUDA_FAILED(e, "the copy of the entries to put back");
         if (rc2 == FPSK_OK) rc2 = patch_launch(C, ldc, d, (int)restore.size(), st);
-        if (cudaStreamSynchronize(st) != cudaSuccess && rc2 == FPSK_OK) rc2 = FPSK_ERR_CUDA;
+        e = cudaStreamSynchronize(st);
+        if (e != cudaSuccess && rc2 == FPSK_OK) rc2 = FPSK_CUDA_FAILED(e, "the wait for the entries put back");
         if (rc == FPSK_OK) rc = rc2;
     }
     if (rc != FPSK_OK) return rc;
@@ -1198,7 +1211,7 @@ fpsk_status fpsk_debug_bounds_clear(void)
 {
 #ifdef FPSK_DEBUG_BOUNDS
     for (const BoundsSource &src : bounds_sources())
-        if (src.clear() != cudaSuccess) return FPSK_ERR_CUDA;
+        FPSK_CUDA_OK(src.clear());
 #endif
     return FPSK_OK;
 }
@@ -1208,12 +1221,16 @@ fpsk_status fpsk_context_create(fpsk_context **out)
     if (!out) return FPSK_ERR_NULL;
     *out = nullptr;
     fpsk_context *c = new fpsk_context;
-    bool ok = sketch_aux_create(c->aux) == FPSK_OK;
-    ok = ok && cudaEventCreateWithFlags(&c->round_done, cudaEventDisableTiming) == cudaSuccess;
-    ok = ok && cudaHostAlloc(&c->pinned, kPackBytes, cudaHostAllocPortable) == cudaSuccess;
-    if (!ok) {
+    const fpsk_status rc = [&]() -> fpsk_status {
+        const fpsk_status aux = sketch_aux_create(c->aux);
+        if (aux != FPSK_OK) return aux;
+        FPSK_CUDA_OK(cudaEventCreateWithFlags(&c->round_done, cudaEventDisableTiming));
+        FPSK_CUDA_OK(cudaHostAlloc(&c->pinned, kPackBytes, cudaHostAllocPortable));
+        return FPSK_OK;
+    }();
+    if (rc != FPSK_OK) {
         fpsk_context_destroy(c);
-        return FPSK_ERR_CUDA;
+        return rc;
     }
     *out = c;
     return FPSK_OK;
@@ -1226,7 +1243,7 @@ fpsk_status fpsk_context_destroy(fpsk_context *c)
     if (c->round_done) ok = (cudaEventDestroy(c->round_done) == cudaSuccess) && ok;
     if (c->pinned) ok = (cudaFreeHost(c->pinned) == cudaSuccess) && ok;
     delete c;
-    return ok ? FPSK_OK : FPSK_ERR_CUDA;
+    return ok ? FPSK_OK : FPSK_CUDA_FAILED(cudaPeekAtLastError(), "the end of a context");
 }
 
 }  // extern "C"

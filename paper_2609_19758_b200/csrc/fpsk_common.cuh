@@ -14,16 +14,21 @@ namespace fpsk {
 extern std::atomic<unsigned long long> g_launches;   // kernels launched by this library
 inline void count_launch(int n = 1) { g_launches.fetch_add((unsigned long long)n, std::memory_order_relaxed); }
 
-#define FPSK_CUDA_OK(expr)                         \
-    do {                                           \
-        cudaError_t e__ = (expr);                  \
-        if (e__ != cudaSuccess) return FPSK_ERR_CUDA; \
+// Notes which CUDA call failed where (what fpsk_last_cuda_error tells) and returns FPSK_ERR_CUDA.
+fpsk_status cuda_failed(cudaError_t error, const char *file, int line, const char *what);
+#define FPSK_CUDA_FAILED(error, what) fpsk::cuda_failed((error), __FILE__, __LINE__, (what))
+
+#define FPSK_CUDA_OK(expr)                                                       \
+    do {                                                                         \
+        cudaError_t e__ = (expr);                                                \
+        if (e__ != cudaSuccess) return FPSK_CUDA_FAILED(e__, #expr);             \
     } while (0)
 
-#define FPSK_LAUNCH_CHECK()                                    \
-    do {                                                       \
-        fpsk::count_launch();                                  \
-        if (cudaPeekAtLastError() != cudaSuccess) return FPSK_ERR_CUDA; \
+#define FPSK_LAUNCH_CHECK()                                                      \
+    do {                                                                         \
+        fpsk::count_launch();                                                    \
+        const cudaError_t e__ = cudaPeekAtLastError();                           \
+        if (e__ != cudaSuccess) return FPSK_CUDA_FAILED(e__, "a kernel launch"); \
     } while (0)
 
 static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }

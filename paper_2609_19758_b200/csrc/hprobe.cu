@@ -1583,7 +1583,7 @@ fpsk_status hprobe_launch(const void *A, long long lda, const float *C, long lon
                 count_launch();
                 return FPSK_OK;
             }
-            if (le != cudaErrorCooperativeLaunchTooLarge) return FPSK_ERR_CUDA;
+            if (le != cudaErrorCooperativeLaunchTooLarge) return FPSK_CUDA_FAILED(le, "the cooperative launch");
             (void)cudaGetLastError();
             v.partAB = w.partAB; v.ksplit = 0; v.n_maxA = 0;
         }

@@ -1252,7 +1252,7 @@ template <typename T, int DP, int MODE, bool BY_ROWS> static fpsk_status launch_
 {
     using Cfg = Tca<DP, MODE>;
     const int sms = sm_count();
-    if (sms < 1) return FPSK_ERR_CUDA;
+    if (sms < 1) return FPSK_CUDA_FAILED(cudaErrorInvalidDevice, "the number of multiprocessors");
     if (sms > (int)(kAttnSyncBytes / sizeof(unsigned int))) return FPSK_ERR_PARAM;
     TcaArgs g;
     g.a = a;
@@ -1281,7 +1281,7 @@ template <typename T, int DP, int MODE, bool BY_ROWS> static fpsk_status launch_
         const cuuint64_t dims[3] = {(cuuint64_t)a.dim, (cuuint64_t)a.hq, (cuuint64_t)a.n_tokens};
         const cuuint64_t str[2] = {bytes(a.qhs, a.hq), bytes(a.qts, a.n_tokens)};
         const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)g.tile_tokens};
-        if (!encode(&mq, type, 3, a.q, dims, str, box)) return FPSK_ERR_CUDA;
+        if (!encode(&mq, type, 3, a.q, dims, str, box)) return FPSK_CUDA_FAILED(cudaErrorInvalidValue, "the tensor map of the queries");
     }
     // A box of K or V holds the rows of one head and page.  Heads of 128 channels come with both halves in one load where two of
     // the outer dimensions merge into one: the eight-row groups of all pages (a page is page_size rows long), or the heads of all
@@ -1314,7 +1314,8 @@ template <typename T, int DP, int MODE, bool BY_ROWS> static fpsk_status launch_
         const cuuint32_t box[5] = {64, 8, 2, groups ? 1 : R / 8, groups ? R / 8 : 1};
         return encode(m, type, 5, base, dims, str, box);
     };
-    if (!kv_map(&mk, g.kl, a.k, a.kps, a.kts, a.khs) || !kv_map(&mv, g.vl, a.v, a.vps, a.vts, a.vhs)) return FPSK_ERR_CUDA;
+    if (!kv_map(&mk, g.kl, a.k, a.kps, a.kts, a.khs) || !kv_map(&mv, g.vl, a.v, a.vps, a.vts, a.vhs))
+        return FPSK_CUDA_FAILED(cudaErrorInvalidValue, "the tensor maps of the cache");
 
     static std::atomic<unsigned long long> prepared{0};               // one bit per device
     int dev = 0;

@@ -1197,7 +1197,7 @@ static fpsk_status probe_grid(int &grid)
 {
     int dev = 0;
     FPSK_CUDA_OK(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return FPSK_ERR_CUDA;
+    if (dev < 0 || dev >= 64) return FPSK_CUDA_FAILED(cudaErrorInvalidDevice, "a device number beyond 63");
     std::lock_guard<std::mutex> lk(g_dev_mu);
     if (g_dev[dev].grid == 0) {
         int sms = 0, occ = 0, o2 = 0;
@@ -1210,7 +1210,7 @@ static fpsk_status probe_grid(int &grid)
         occ = occ < o2 ? occ : o2;
         FPSK_CUDA_OK(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o2, probe_kernel<__nv_bfloat16, false>, kProbeThreads, 0));
         occ = occ < o2 ? occ : o2;
-        if (occ < 1 || sms < 1) return FPSK_ERR_CUDA;
+        if (occ < 1 || sms < 1) return FPSK_CUDA_FAILED(cudaErrorLaunchOutOfResources, "no block of the probe fits a multiprocessor");
         if (occ > 2) occ = 2;
         g_dev[dev].sms = sms;
         g_dev[dev].grid = sms * occ;
@@ -1289,7 +1289,7 @@ static fpsk_status tma_grid(int &grid)
 {
     int dev = 0;
     FPSK_CUDA_OK(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return FPSK_ERR_CUDA;
+    if (dev < 0 || dev >= 64) return FPSK_CUDA_FAILED(cudaErrorInvalidDevice, "a device number beyond 63");
     std::lock_guard<std::mutex> lk(g_dev_mu);
     if (g_dev[dev].tma_grid == 0) {
         int sms = 0, occ = 0, o2 = 0;
@@ -1299,7 +1299,7 @@ static fpsk_status tma_grid(int &grid)
         FPSK_CUDA_OK(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, probe_tma_kernel<__half>, kTmaThreads, kTmaSmem));
         FPSK_CUDA_OK(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o2, probe_tma_kernel<__nv_bfloat16>, kTmaThreads, kTmaSmem));
         occ = occ < o2 ? occ : o2;
-        if (occ < 1 || sms < 1) return FPSK_ERR_CUDA;
+        if (occ < 1 || sms < 1) return FPSK_CUDA_FAILED(cudaErrorLaunchOutOfResources, "no block of the probe fits a multiprocessor");
         g_dev[dev].tma_grid = sms;        // one CTA per SM
     }
     grid = g_dev[dev].tma_grid;

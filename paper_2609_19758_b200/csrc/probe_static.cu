@@ -25,12 +25,12 @@ static fpsk_status scratch_address(void **out)
 {
     int dev = 0;
     FPSK_CUDA_OK(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return FPSK_ERR_CUDA;
+    if (dev < 0 || dev >= 64) return FPSK_CUDA_FAILED(cudaErrorInvalidDevice, "a device number beyond 63");
     std::lock_guard<std::mutex> lk(g_scratch_mu);
     if (!g_scratch_addr[dev]) {
         void *ptr = nullptr;
         FPSK_CUDA_OK(cudaGetSymbolAddress(&ptr, g_probe_scratch));
-        if (!ptr) return FPSK_ERR_CUDA;
+        if (!ptr) return FPSK_CUDA_FAILED(cudaErrorInvalidSymbol, "the address of the static scratch");
         g_scratch_addr[dev] = ptr;
     }
     *out = g_scratch_addr[dev];

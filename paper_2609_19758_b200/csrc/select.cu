@@ -794,10 +794,16 @@ long long rms_c_samples(const float *C, long long ldc, long long n1, long long n
     if (stride < 1) stride = 1;
     const long long nsamp = (total + stride - 1) / stride;
     sample_c_kernel<<<(unsigned)((nsamp + 255) / 256), 256, 0, st>>>(C, ldc, n3, total, stride, nsamp, samples);
-    if (cudaGetLastError() != cudaSuccess) return -1;
-    if (cudaMemsetAsync(w.counts, 0, 4 * 4, st) != cudaSuccess) return -1;
-    count_valid_kernel<<<64, 256, 0, st>>>(SEL_SAMPLE, samples, nsamp, w.scal, w.counts);
-    if (cudaGetLastError() != cudaSuccess) return -1;
+    cudaError_t e = cudaPeekAtLastError();
+    if (e == cudaSuccess) e = cudaMemsetAsync(w.counts, 0, 4 * 4, st);
+    if (e == cudaSuccess) {
+        count_valid_kernel<<<64, 256, 0, st>>>(SEL_SAMPLE, samples, nsamp, w.scal, w.counts);
+        e = cudaPeekAtLastError();
+    }
+    if (e != cudaSuccess) {
+        FPSK_CUDA_FAILED(e, "the samples of C");
+        return -1;
+    }
     return nsamp;
 }
 

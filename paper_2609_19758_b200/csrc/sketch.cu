@@ -1818,7 +1818,7 @@ static fpsk_status build_sketches_t(const SketchIn &in, uint64_t seed, int rnd, 
                 if (attr_err == cudaSuccess)
                     attr_err = cudaFuncSetAttribute(scatter_ring_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
             });
-            if (attr_err != cudaSuccess) return FPSK_ERR_CUDA;
+            FPSK_CUDA_OK(attr_err);
             SrArgs sa;
             sa.C = in.C; sa.ldc = in.ldc; sa.n1 = n1; sa.n3 = n3; sa.m_b = m_b; sa.nsplit = pl.nsplit; sa.n_units = m_b * pl.nsplit; sa.nst = kSrStages;
             sa.rowperm = w.rowperm; sa.colpos = w.colpos; sa.rowstart = w.rowstart; sa.colstart = w.colstart;

@@ -70,7 +70,8 @@ class ProbeState(C.Structure):
 class FpskError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
-        super().__init__(f"{where}: fpsk status {status} ({status_string(status)})")
+        detail = last_cuda_error() if status == ERR_CUDA else ""
+        super().__init__(f"{where}: fpsk status {status} ({status_string(status)}{': ' + detail if detail else ''})")
 
 
 _lib = None
@@ -87,6 +88,8 @@ def lib() -> C.CDLL:
         vp, i64, i32, u64, sz = C.c_void_p, C.c_int64, C.c_int32, C.c_uint64, C.c_size_t
         L.fpsk_status_string.restype = C.c_char_p
         L.fpsk_status_string.argtypes = [C.c_int]
+        L.fpsk_last_cuda_error.restype = C.c_char_p
+        L.fpsk_last_cuda_error.argtypes = []
         L.fpsk_default_params.restype = None
         L.fpsk_default_params.argtypes = [C.POINTER(Params)]
         L.fpsk_law_m_start.restype = i32
@@ -169,6 +172,11 @@ def lib() -> C.CDLL:
 
 def status_string(s: int) -> str:
     return lib().fpsk_status_string(int(s)).decode()
+
+
+def last_cuda_error() -> str:
+    """The CUDA error behind this thread's last ERR_CUDA: what failed, where and why."""
+    return lib().fpsk_last_cuda_error().decode()
 
 
 def default_params(**kw) -> Params:
