@@ -64,6 +64,12 @@ void check_heads(const at::Tensor &t, int64_t tokens, int64_t heads, int64_t dim
         refuse(PyExc_ValueError, "%s: expected (%lld, %lld, %lld) %s on cuda:%d with contiguous channels", what, (long long)tokens,
                (long long)heads, (long long)dim, c10::toString(type), device);
 }
+// what is written must not be expanded
+void check_written(const at::Tensor &t, const char *what)
+{
+    for (int d = 0; d < t.dim(); ++d)
+        if (t.size(d) > 1 && t.stride(d) == 0) refuse(PyExc_ValueError, "%s: elements of an output share memory (an expanded dimension)", what);
+}
 const void *weight(const at::Tensor *w, int64_t dim, int device, const char *what, int32_t &type)
 {
     if (!w) return nullptr;
@@ -152,6 +158,7 @@ fpsk_heads heads(const at::Tensor *x, const at::Tensor *out, const at::Tensor *w
     if (has_out) {
         if (!out) refuse(PyExc_ValueError, "%s_out is missing", what);
         check_heads(*out, x->size(0), x->size(1), x->size(2), out_type, device, what);
+        check_written(*out, what);
         h.out = out->data_ptr();
         h.out_token_stride = out->stride(0);
         h.out_head_stride = out->stride(1);
@@ -170,6 +177,7 @@ fpsk_heads_grad heads_grad(const at::Tensor *x, PyObject *dy_, PyObject *dx_, co
     check_heads(*x, n, x->size(1), dim, like.scalar_type(), device, what);
     check_heads(dy, n, x->size(1), dim, grad_type, device, what);
     check_heads(dx, n, x->size(1), dim, grad_type, device, what);
+    check_written(dx, what);
     h.in = x->data_ptr(); h.dout = dy.data_ptr(); h.din = dx.data_ptr();
     h.in_token_stride = x->stride(0); h.in_head_stride = x->stride(1);
     h.dout_token_stride = dy.stride(0); h.dout_head_stride = dy.stride(1);
@@ -328,6 +336,7 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (q.dim() != 3) refuse(PyExc_ValueError, "q: (tokens, heads, channels) expected");
         check_heads(q, q.size(0), q.size(1), c.c.head_dim, c.type, c.device, "q");
         check_heads(out, q.size(0), q.size(1), c.c.head_dim, c.type, c.device, "out");
+        check_written(out, "out");
         if (!ws.is_cuda() || ws.get_device() != c.device || !ws.is_contiguous()) refuse(PyExc_ValueError, "ws: on cuda:%d expected", c.device);
         fpsk_attention t = {};
         if (lse) {

@@ -145,3 +145,23 @@ def test_workspaces_lie_on_the_device_that_is_asked_for():
     for device in (0, "cuda:0", torch.device("cuda", 0), None):
         for ws in (A.norm_rope_workspace(64, device), A.attention_workspace(device)):
             assert ws.device == torch.device("cuda", torch.cuda.current_device() if device is None else 0)
+
+
+def test_outputs_whose_elements_share_memory_are_refused():
+    """An expanded output would be written by several threads at once."""
+    q, cos, sin, pos, out = rope_args()
+    for bad in (out[:1].expand(3, 2, 32), out[:, :1].expand(3, 2, 32)):
+        with pytest.raises(ValueError, match="share"):
+            A.qk_norm_rope(q, None, cos, sin, pos, bad, None)
+        with pytest.raises(ValueError, match="share"):
+            A.qk_norm_rope(q, q, cos, sin, pos, out, bad)
+        with pytest.raises(ValueError, match="share"):
+            A.qk_norm_rope_backward(q, None, out, None, cos, sin, pos, bad, None, None, None, A.norm_rope_workspace(32))
+    cache, q, out, cu, kv, table = attention_args()
+    with pytest.raises(ValueError, match="share"):
+        A.paged_attention(cache, q, out[:, :1].expand(1, 4, 64), cu, kv, table, A.attention_workspace(), 1, 300)
+    k = torch.randn(1, 2, 64, device="cuda").to(BF16)
+    with pytest.raises(ValueError, match="share"):
+        A.paged_append(cache, k, k, cu, kv, table, q=q, q_out=out[:, :1].expand(1, 4, 64))
+    q1, cos, sin, pos, out = rope_args(tokens=1)
+    A.qk_norm_rope(q1, None, cos, sin, pos, out.expand(1, 2, 32), None)          # one token: nothing is shared
