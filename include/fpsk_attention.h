@@ -119,9 +119,9 @@ fpsk_status fpsk_paged_append(const fpsk_paged_cache *cache, const fpsk_paged_ba
  * A token that may see nothing gets zeros and lse = -inf.  A page number outside [0, n_pages), or a key behind the last column of the
  * table, reads as zeros (a score of 0) and sets *d_status to FPSK_ERR_PARAM.  Query head h reads key head h / (n_heads_q / cache->n_heads).
  * Keys that no token of a sequence may see are never used, whatever the memory holds (table entries behind the last page,
- * NaN).  Scores, softmax and sums are FP32; on the tensor cores each weight exp(s - m) is rounded to cache->type, half a unit at most,
- * before it multiplies its value (the sum that divides is not rounded).  A NaN or infinite value among keys that some tokens see and others do not can reach the others.  Rows that belong to no
- * sequence are left alone.
+ * NaN).  A NaN or infinite value among keys that some tokens see and others do not can reach the others.  Rows that belong to no
+ * sequence are left alone.  Scores, softmax and sums are FP32; on the tensor cores each weight exp(s - m) is rounded to
+ * cache->type, half a unit at most, before it multiplies its value (the sum that divides is not rounded).
  *   q, out     device, cache->type, (token, head) strides; lse: device FP32 n_tokens x n_heads_q, or NULL
  *   max_q_len, max_kv_len   upper bounds of the lengths, known to the host: they choose tiles and grid (a bound that is
  *              too small costs time only)

@@ -11,11 +11,9 @@
 //
 // This is the form for small calls and for any strides; large calls whose heads lie side by side go to norm_rope_ring.cu.  What
 // bounds it is a launch's latency, and behind that the instructions it issues (some 350 for two heads and lanes, backward).
-// Measured: one token of 32 + 8 heads of 128 3.1 us, a step of 64 requests into the cache 5.1 us, 1021 tokens of 28 + 4 heads
-// of 96 backward 15.4 us, of which 1.6 pass before the first loads and 3.2 in the last block's sum over the blocks' rows.
+// Measured: one token of 32 + 8 heads of 128 3.4 us, a step of 64 requests into the cache 5.2 us, 1021 tokens of 28 + 4 heads
+// of 96 backward 16.0 us, of which 1.6 pass before the first loads and 3.2 in the last block's sum over the blocks' rows.
 #include "norm_rope.cuh"
-
-#include <mutex>
 
 namespace fpsk {
 

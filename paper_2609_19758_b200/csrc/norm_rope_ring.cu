@@ -10,7 +10,8 @@
 // (sequence, length, page) passes once for 32.
 //
 // Measured: 4096 tokens of 64 heads of 128, FP32 in and 16 bits out, 36.5 us (5.5 TB/s; 31.1 us at the rate of a copy), its
-// backward pass 62.7 us (4.3 TB/s: the instructions of two sums across lanes a head, 0.65 issued in a cycle); 11112 tokens with
+// backward pass 63.1 us (4.3 TB/s: the latency of two sums across lanes a head, one behind the other; 0.60 instructions are issued
+// in a cycle of a scheduler, so that their number is not the bound); 11112 tokens with
 // 96 heads of 128 into the cache 131 us (6.3 TB/s).
 #include "norm_rope.cuh"
 

@@ -22,8 +22,10 @@
 // warps on a scheduler; 1024 of them their exponentials, four lanes a cycle), the two workers' four products about 1150, where
 // S = Q K^T is held up by shared memory (48 cycles for 128 x 64 x 16: 128 bytes a cycle; O += P V has P in TMEM and is not).
 // Few rows: HBM, and the latency from the launch to the first scores (6 us), of which a short context is all.
-// Measured: 4096 new tokens of 32 heads over 16384 keys of 8 heads of 128, 850 us (1.13 PFLOP/s, 0.69 of a library's large product);
-// 4 tokens over 262144 keys 173 us (6.2 TB/s, 0.95 of a copy); 96 requests of one token, 98296 keys, 84 us (4.8 TB/s).
+// Measured, sustained: 4096 new tokens of 32 heads over 16384 keys of 8 heads of 128, 882 us (1.09 PFLOP/s, 0.66 of a library's large
+// product); 4 tokens over 262144 keys 213 us (5.0 TB/s, 0.77 of a copy); 96 requests of one token, 98296 keys, 98 us (4.1 TB/s).
+// In a burst of up to a hundred launches they take 850, 177 and 84 us: within some 0.1 s the load brings the chip to its power
+// limit, and the SM clock from 1965 to 1590 - 1740 MHz.  The other times in this file, both sides of a choice, are of bursts.
 // Every wait is bounded: a role whose wait gave up stops waiting and issuing, walks through its loops, reports
 // FPSK_ERR_TIMEOUT and the CTA frees its TMEM and leaves.
 #include "attention.cuh"
