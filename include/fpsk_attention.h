@@ -21,7 +21,7 @@
 extern "C" {
 #endif
 
-typedef enum { FPSK_ELEM_FP16 = 0, FPSK_ELEM_BF16 = 1, FPSK_ELEM_FP32 = 2 } fpsk_elem;
+typedef enum { FPSK_ELEM_FP16 = 0, FPSK_ELEM_BF16 = 1, FPSK_ELEM_FP32 = 2, FPSK_ELEM_E4M3 = 3 /* outputs of fpsk_decoder.h only */ } fpsk_elem;
 
 #define FPSK_MAX_HEAD_DIM 256
 

@@ -49,7 +49,7 @@ def needs_build(lib: str = LIB) -> bool:
         return True
     t = os.path.getmtime(lib)
     if lib == BINDING:
-        sources_ = [os.path.join(HERE, "csrc", "binding.cpp"), os.path.join(ROOT, "include", "fpsk_attention.h")]
+        sources_ = [os.path.join(HERE, "csrc", "binding.cpp")] + glob.glob(os.path.join(ROOT, "include", "*.h"))
         return any(os.path.getmtime(d) > t for d in sources_) or not binding_is_current()
     deps = sources() + glob.glob(os.path.join(HERE, "csrc", "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)

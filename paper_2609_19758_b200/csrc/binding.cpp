@@ -1,4 +1,4 @@
-// Python binding of the attention operators (fpsk_attention.h): reads the tensors, checks what the library cannot see (shapes, types,
+// Python binding of the attention operators (fpsk_attention.h) and the decoder's (fpsk_decoder.h): reads the tensors, checks what the library cannot see (shapes, types,
 // devices, contiguous channels), fills the structs of the header and calls the library.  In C++ because a small call's time is its
 // marshalling: in Python it took 7 of the 10 us that the smallest norm and rotation call needs on the host, here well under one.
 // The library's functions come by address, from the build of it that the process has loaded.
@@ -6,7 +6,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "fpsk_attention.h"
+#include "fpsk_decoder.h"
 
 #include <stdarg.h>
 #include <stdio.h>
@@ -18,6 +18,11 @@ struct Library {
     decltype(&fpsk_qk_norm_rope_backward) norm_rope_backward;
     decltype(&fpsk_paged_append) append;
     decltype(&fpsk_paged_attention) attention;
+    decltype(&fpsk_add_rms_norm) add_norm;
+    decltype(&fpsk_add_rms_norm_backward) add_norm_backward;
+    decltype(&fpsk_adjust_logits) adjust_logits;
+    decltype(&fpsk_distill_loss) distill;
+    decltype(&fpsk_distill_loss_backward) distill_backward;
 } lib;
 
 struct Refused {};                       // a Python error is set
@@ -251,11 +256,16 @@ template <typename F> PyObject *call(Py_ssize_t given, Py_ssize_t wanted, F f)
 
 PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return call(n, 4, [&] {
+    return call(n, 9, [&] {
         lib.norm_rope = reinterpret_cast<decltype(lib.norm_rope)>(PyLong_AsVoidPtr(a[0]));
         lib.norm_rope_backward = reinterpret_cast<decltype(lib.norm_rope_backward)>(PyLong_AsVoidPtr(a[1]));
         lib.append = reinterpret_cast<decltype(lib.append)>(PyLong_AsVoidPtr(a[2]));
         lib.attention = reinterpret_cast<decltype(lib.attention)>(PyLong_AsVoidPtr(a[3]));
+        lib.add_norm = reinterpret_cast<decltype(lib.add_norm)>(PyLong_AsVoidPtr(a[4]));
+        lib.add_norm_backward = reinterpret_cast<decltype(lib.add_norm_backward)>(PyLong_AsVoidPtr(a[5]));
+        lib.adjust_logits = reinterpret_cast<decltype(lib.adjust_logits)>(PyLong_AsVoidPtr(a[6]));
+        lib.distill = reinterpret_cast<decltype(lib.distill)>(PyLong_AsVoidPtr(a[7]));
+        lib.distill_backward = reinterpret_cast<decltype(lib.distill_backward)>(PyLong_AsVoidPtr(a[8]));
         return 0;
     });
 }
@@ -364,6 +374,217 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---------------------------------------------------------------- the decoder's operators
+// (rows, n) with contiguous rows; rows < 0: any number, n < 0: any width
+const at::Tensor &rows_of(PyObject *o, int64_t rows, int64_t n, int device, const char *what)
+{
+    const at::Tensor &t = needed(o, what);
+    if (t.dim() != 2 || !t.is_cuda() || t.get_device() != device || (rows >= 0 && t.size(0) != rows) || (n >= 0 && t.size(1) != n) ||
+        (t.size(1) > 1 && t.stride(1) != 1))
+        refuse(PyExc_ValueError, "%s: (%lld, %lld) on cuda:%d with contiguous rows expected (-1: any)", what, (long long)rows, (long long)n, device);
+    return t;
+}
+int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+// one number of a type for each row, or nothing
+template <typename T> T *row_values(PyObject *o, at::ScalarType type, int64_t rows, int device, const char *what)
+{
+    const at::Tensor *t = tensor(o, what);
+    if (!t) return nullptr;
+    if (t->dim() != 1 || t->size(0) != rows || t->scalar_type() != type || !t->is_contiguous() || !t->is_cuda() || t->get_device() != device)
+        refuse(PyExc_ValueError, "%s: contiguous (%lld,) %s on cuda:%d expected", what, (long long)rows, c10::toString(type), device);
+    return static_cast<T *>(t->data_ptr());
+}
+int32_t small(int64_t n, const char *what)
+{
+    if (n > INT32_MAX) refuse(PyExc_ValueError, "%s: too wide", what);
+    return (int32_t)n;
+}
+
+// x, residual, weight, y, residual_out, scale, group, eps, stream
+PyObject *py_add_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(n, 9, [&] {
+        const int device = device_of(needed(a[0], "x"), "x");
+        const at::Tensor &x = rows_of(a[0], -1, -1, device, "x");
+        const int64_t rows = x.size(0), dim = x.size(1);
+        fpsk_add_norm t = {};
+        t.x = x.data_ptr();
+        t.x_stride = row_stride(x);
+        t.x_type = elem(x, "x");
+        t.n_tokens = rows;
+        t.dim = small(dim, "x");
+        const at::Tensor &y = rows_of(a[3], rows, dim, device, "y");
+        check_written(y, "y");
+        t.y = y.data_ptr();
+        t.y_stride = row_stride(y);
+        t.y_type = y.scalar_type() == at::kFloat8_e4m3fn ? FPSK_ELEM_E4M3 : elem(y, "y");
+        if (a[1] != Py_None) {
+            const at::Tensor &r = rows_of(a[1], rows, dim, device, "residual");
+            t.residual = r.data_ptr();
+            t.residual_stride = row_stride(r);
+            t.residual_type = elem(r, "residual");
+        }
+        if (a[4] != Py_None) {
+            const at::Tensor &r = rows_of(a[4], rows, dim, device, "residual_out");
+            check_written(r, "residual_out");
+            const int type = elem(r, "residual_out");
+            if (t.residual && type != t.residual_type) refuse(PyExc_ValueError, "residual_out: the type of residual expected");
+            t.residual_out = r.data_ptr();
+            t.residual_out_stride = row_stride(r);
+            t.residual_type = type;
+        }
+        t.weight = weight(tensor(a[2], "weight"), dim, device, "weight", t.weight_type);
+        t.group = clamped(a[6]);
+        if (t.y_type == FPSK_ELEM_E4M3) {
+            const int64_t groups = t.group > 0 ? (dim + t.group - 1) / t.group : 1;
+            const at::Tensor &s = rows_of(a[5], rows, groups, device, "scale");
+            if (s.scalar_type() != at::kFloat) refuse(PyExc_TypeError, "scale: float32 expected");
+            check_written(s, "scale");
+            t.scale = static_cast<float *>(s.data_ptr());
+            t.scale_stride = row_stride(s);
+        } else if (a[5] != Py_None) {
+            refuse(PyExc_ValueError, "scale: of a float8_e4m3fn y only");
+        }
+        t.eps = (float)number(a[7]);
+        const OnDevice on(device);
+        return lib.add_norm(&t, stream_ptr(a[8]));
+    });
+}
+// h, dy, weight, dx, dweight, ws, dh, eps, stream
+PyObject *py_add_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(n, 9, [&] {
+        const int device = device_of(needed(a[0], "h"), "h");
+        const at::Tensor &h = rows_of(a[0], -1, -1, device, "h");
+        const int64_t rows = h.size(0), dim = h.size(1);
+        const at::Tensor &dy = rows_of(a[1], rows, dim, device, "dy"), &dx = rows_of(a[3], rows, dim, device, "dx");
+        check_written(dx, "dx");
+        fpsk_add_norm_grad t = {};
+        t.h = h.data_ptr(); t.dy = dy.data_ptr(); t.dx = dx.data_ptr();
+        t.h_stride = row_stride(h); t.dy_stride = row_stride(dy); t.dx_stride = row_stride(dx);
+        t.h_type = elem(h, "h");
+        t.grad_type = elem(dy, "dy");
+        if (dx.scalar_type() != dy.scalar_type()) refuse(PyExc_ValueError, "dx: the type of dy expected");
+        if (a[6] != Py_None) {
+            const at::Tensor &dh = rows_of(a[6], rows, dim, device, "dh");
+            if (dh.scalar_type() != dy.scalar_type()) refuse(PyExc_ValueError, "dh: the type of dy expected");
+            t.dh = dh.data_ptr();
+            t.dh_stride = row_stride(dh);
+        }
+        t.n_tokens = rows;
+        t.dim = small(dim, "h");
+        t.weight = weight(tensor(a[2], "weight"), dim, device, "weight", t.weight_type);
+        t.dweight = row_values<float>(a[4], at::kFloat, dim, device, "dweight");
+        const at::Tensor *ws = tensor(a[5], "ws");
+        if (ws && (!ws->is_cuda() || ws->get_device() != device || !ws->is_contiguous())) refuse(PyExc_ValueError, "ws: on cuda:%d expected", device);
+        t.eps = (float)number(a[7]);
+        const OnDevice on(device);
+        return lib.add_norm_backward(&t, ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->nbytes() : 0, stream_ptr(a[8]));
+    });
+}
+// logits, out, history, history_len, prompt_len, repetition, frequency, presence, bias pointers, tokens, values, mask, mask_row, token,
+// lse, status, stream
+PyObject *py_adjust_logits(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(n, 17, [&] {
+        const int device = device_of(needed(a[0], "logits"), "logits");
+        const at::Tensor &x = rows_of(a[0], -1, -1, device, "logits");
+        const int64_t rows = x.size(0), vocab = x.size(1);
+        fpsk_logits t = {};
+        t.logits = x.data_ptr();
+        t.logits_stride = row_stride(x);
+        t.logits_type = elem(x, "logits");
+        t.n_rows = rows;
+        t.vocab = small(vocab, "logits");
+        if (a[1] != Py_None) {
+            const at::Tensor &o = rows_of(a[1], rows, vocab, device, "out");
+            check_written(o, "out");
+            t.out = o.data_ptr();
+            t.out_stride = row_stride(o);
+            t.out_type = elem(o, "out");
+        }
+        if (a[2] != Py_None) {
+            const at::Tensor &h = rows_of(a[2], rows, -1, device, "history");
+            if (h.scalar_type() != at::kInt) refuse(PyExc_TypeError, "history: int32 expected");
+            t.history = static_cast<const int32_t *>(h.data_ptr());
+            t.history_stride = row_stride(h);
+            t.history_width = small(h.size(1), "history");
+            // (an empty tensor has no address: nothing to pass over)
+            static const int32_t none = -1;
+            if (!t.history) t.history = &none;
+        } else if (a[3] != Py_None || a[4] != Py_None || a[5] != Py_None || a[6] != Py_None || a[7] != Py_None) {
+            refuse(PyExc_ValueError, "lengths and penalties need a history");
+        }
+        t.history_len = row_values<int32_t>(a[3], at::kInt, rows, device, "history_len");
+        t.prompt_len = row_values<int32_t>(a[4], at::kInt, rows, device, "prompt_len");
+        t.repetition = row_values<float>(a[5], at::kFloat, rows, device, "repetition");
+        t.frequency = row_values<float>(a[6], at::kFloat, rows, device, "frequency");
+        t.presence = row_values<float>(a[7], at::kFloat, rows, device, "presence");
+        if (a[8] != Py_None) {
+            t.bias_ptr = row_values<int32_t>(a[8], at::kInt, rows + 1, device, "bias: the rows' first entries");
+            t.n_biases = needed(a[9], "bias: tokens").numel();
+            t.bias_token = row_values<int32_t>(a[9], at::kInt, t.n_biases, device, "bias: tokens");
+            t.bias_value = row_values<float>(a[10], at::kFloat, t.n_biases, device, "bias: values");
+            if (t.n_biases && !t.bias_value) refuse(PyExc_ValueError, "bias: values are missing");
+        }
+        if (a[11] != Py_None) {
+            const at::Tensor &m = rows_of(a[11], a[12] == Py_None ? rows : -1, (vocab + 31) / 32, device, "mask");
+            if (m.scalar_type() != at::kInt) refuse(PyExc_TypeError, "mask: int32 expected");
+            t.mask = static_cast<const int32_t *>(m.data_ptr());
+            t.mask_stride = row_stride(m);
+            t.n_masks = m.size(0);
+            static const int32_t none = 0;
+            if (!t.mask) t.mask = &none;                               // (no masks: mask_row has -1 or is reported)
+            t.mask_row = row_values<int32_t>(a[12], at::kInt, rows, device, "mask_row");
+        } else if (a[12] != Py_None) {
+            refuse(PyExc_ValueError, "mask_row needs a mask");
+        }
+        t.token = row_values<int32_t>(a[13], at::kInt, rows, device, "token");
+        t.lse = row_values<float>(a[14], at::kFloat, rows, device, "lse");
+        if (!t.out && a[1] == Py_None && a[13] == Py_None && a[14] == Py_None) refuse(PyExc_ValueError, "one of out, token and lse expected");
+        const OnDevice on(device);
+        return lib.adjust_logits(&t, status_ptr(a[15], device), stream_ptr(a[16]));
+    });
+}
+// logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, stream
+template <bool BACKWARD> PyObject *py_distill(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(n, 10, [&] {
+        const int device = device_of(needed(a[0], "logits"), "logits");
+        const at::Tensor &x = rows_of(a[0], -1, -1, device, "logits");
+        const int64_t rows = x.size(0), vocab = x.size(1);
+        fpsk_distill t = {};
+        t.logits = x.data_ptr();
+        t.logits_stride = row_stride(x);
+        t.logits_type = elem(x, "logits");
+        t.n_rows = rows;
+        t.vocab = small(vocab, "logits");
+        const at::Tensor &tok = rows_of(a[1], rows, -1, device, "teacher_token"), &tl = rows_of(a[2], rows, tok.size(1), device, "teacher_logit");
+        if (tok.scalar_type() != at::kInt && tok.scalar_type() != at::kLong) refuse(PyExc_TypeError, "teacher_token: int32 or int64 expected");
+        t.teacher_token = tok.data_ptr(); t.teacher_logit = tl.data_ptr();
+        t.token_stride = row_stride(tok); t.teacher_stride = row_stride(tl);
+        t.token_bytes = tok.scalar_type() == at::kInt ? 4 : 8;
+        t.teacher_type = elem(tl, "teacher_logit");
+        t.top = small(tok.size(1), "teacher_token");
+        t.row_weight = row_values<float>(a[4], at::kFloat, rows, device, "row_weight");
+        t.loss = row_values<float>(a[3], at::kFloat, rows, device, "loss");
+        t.lse = row_values<float>(a[5], at::kFloat, rows, device, "lse");
+        if (a[6] != Py_None) {
+            const at::Tensor &d = rows_of(a[6], rows, vocab, device, "dlogits");
+            check_written(d, "dlogits");
+            t.dlogits = d.data_ptr();
+            t.dlogits_stride = row_stride(d);
+            t.grad_type = elem(d, "dlogits");
+        }
+        const double tau = number(a[7]);
+        if (!(tau > 0) || tau > 3.4e38 || tau < 1e-38) refuse(PyExc_ValueError, "temperature must be positive and finite");
+        t.temperature = (float)tau;
+        t.normalize = truth(a[8]);
+        const OnDevice on(device);
+        return (BACKWARD ? lib.distill_backward : lib.distill)(&t, stream_ptr(a[9]));
+    });
+}
+
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(py_bind), METH_FASTCALL, nullptr},
     {"device", py_device, METH_O, nullptr},
@@ -372,6 +593,11 @@ PyMethodDef methods[] = {
     {"check_cache", reinterpret_cast<PyCFunction>(py_check_cache), METH_FASTCALL, nullptr},
     {"paged_append", reinterpret_cast<PyCFunction>(py_append), METH_FASTCALL, nullptr},
     {"paged_attention", reinterpret_cast<PyCFunction>(py_attention), METH_FASTCALL, nullptr},
+    {"add_rms_norm", reinterpret_cast<PyCFunction>(py_add_norm), METH_FASTCALL, nullptr},
+    {"add_rms_norm_backward", reinterpret_cast<PyCFunction>(py_add_norm_backward), METH_FASTCALL, nullptr},
+    {"adjust_logits", reinterpret_cast<PyCFunction>(py_adjust_logits), METH_FASTCALL, nullptr},
+    {"distill_loss", reinterpret_cast<PyCFunction>(py_distill<false>), METH_FASTCALL, nullptr},
+    {"distill_loss_backward", reinterpret_cast<PyCFunction>(py_distill<true>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
