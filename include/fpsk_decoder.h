@@ -9,7 +9,8 @@
  * The conventions of fpsk.h hold: the caller owns every buffer, nothing is allocated, every call is asynchronous on `stream`
  * without a host synchronisation, errors are return codes, nothing throws.  Strides are in ELEMENTS between rows; the elements
  * of a row are contiguous.  Types are fpsk_elem; a row may start anywhere that its type may.  Rows of 0 do nothing.  Sums, norms
- * and exponentials are FP32 in a fixed order: a call gives the same bits each time on one device.
+ * and exponentials are FP32 in a fixed order: a call gives the same bits each time on one device.  d_status is a device int32 or
+ * NULL, to which the kernels only ever write an fpsk_status other than FPSK_OK (FPSK_ERR_TIMEOUT: a device-side wait gave up).
  */
 #ifndef FPSK_DECODER_H
 #define FPSK_DECODER_H
@@ -63,7 +64,7 @@ typedef struct {
 size_t fpsk_add_norm_workspace_bytes(int32_t dim);
 fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, void *workspace, size_t ws_bytes, void *stream);
 
-#define FPSK_MAX_VOCAB (1 << 26)
+#define FPSK_MAX_VOCAB (1 << 23)
 
 /* What is done to a row of logits before a token is picked, in this order, in FP32:
  *   tokens that the row's history holds:      z > 0 ? z / repetition : z * repetition
@@ -124,8 +125,8 @@ typedef struct {
     int32_t normalize;
     float temperature;           /* positive and finite                                                */
 } fpsk_distill;
-fpsk_status fpsk_distill_loss(const fpsk_distill *a, void *stream);
-fpsk_status fpsk_distill_loss_backward(const fpsk_distill *a, void *stream);
+fpsk_status fpsk_distill_loss(const fpsk_distill *a, int32_t *d_status, void *stream);
+fpsk_status fpsk_distill_loss_backward(const fpsk_distill *a, int32_t *d_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -546,10 +546,10 @@ PyObject *py_adjust_logits(PyObject *, PyObject *const *a, Py_ssize_t n)
         return lib.adjust_logits(&t, status_ptr(a[15], device), stream_ptr(a[16]));
     });
 }
-// logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, stream
+// logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, status, stream
 template <bool BACKWARD> PyObject *py_distill(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return call(n, 10, [&] {
+    return call(n, 11, [&] {
         const int device = device_of(needed(a[0], "logits"), "logits");
         const at::Tensor &x = rows_of(a[0], -1, -1, device, "logits");
         const int64_t rows = x.size(0), vocab = x.size(1);
@@ -581,7 +581,7 @@ template <bool BACKWARD> PyObject *py_distill(PyObject *, PyObject *const *a, Py
         t.temperature = (float)tau;
         t.normalize = truth(a[8]);
         const OnDevice on(device);
-        return (BACKWARD ? lib.distill_backward : lib.distill)(&t, stream_ptr(a[9]));
+        return (BACKWARD ? lib.distill_backward : lib.distill)(&t, status_ptr(a[9], device), stream_ptr(a[10]));
     });
 }
 

@@ -35,21 +35,22 @@ def adjust_logits(logits: torch.Tensor, out: Optional[torch.Tensor] = None, hist
 
 def distill_loss(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, loss: torch.Tensor,
                  row_weight: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
-                 temperature: float = 1.0, normalize: bool = True, stream=None) -> None:
+                 temperature: float = 1.0, normalize: bool = True, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """loss (rows,): sum_j p_j (log p_j - log q_j) of each row of logits (rows, vocab), q = softmax(logits / temperature), against the
     teacher's logits for the tokens teacher_token (rows, top): p = softmax(teacher_logit / temperature) over them, or exp(teacher_logit)
     with normalize=False (logarithms of probabilities).  Tokens outside the vocabulary (-1) are left out.  dlogits (rows, vocab) gets the gradient of
     sum(row_weight * loss) in the same launch; it may be logits.  Rows of weight 0 are not read: loss 0, gradient 0."""
     b = A._binding or A._bind()
-    A._check(b.distill_loss(logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize,
+    A._check(b.distill_loss(logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, status,
                             A._stream(b.device(logits), stream)), "fpsk_distill_loss")
 
 
 def distill_loss_backward(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, lse: torch.Tensor,
-                          dloss: torch.Tensor, dlogits: torch.Tensor, temperature: float = 1.0, normalize: bool = True, stream=None) -> None:
+                          dloss: torch.Tensor, dlogits: torch.Tensor, temperature: float = 1.0, normalize: bool = True,
+                          status: Optional[torch.Tensor] = None, stream=None) -> None:
     """The gradient of distill_loss alone, from the lse of the forward pass and the gradients dloss (rows,) of the rows' losses."""
     b = A._binding or A._bind()
-    A._check(b.distill_loss_backward(logits, teacher_token, teacher_logit, None, dloss, lse, dlogits, temperature, normalize,
+    A._check(b.distill_loss_backward(logits, teacher_token, teacher_logit, None, dloss, lse, dlogits, temperature, normalize, status,
                                      A._stream(b.device(logits), stream)), "fpsk_distill_loss_backward")
 
 

@@ -20,7 +20,7 @@ def lib():
     L.fpsk_add_rms_norm_backward.argtypes = [vp, vp, sz, vp]
     L.fpsk_add_norm_workspace_bytes.argtypes, L.fpsk_add_norm_workspace_bytes.restype = [C.c_int32], sz
     L.fpsk_adjust_logits.argtypes = [vp, vp, vp]
-    L.fpsk_distill_loss.argtypes = L.fpsk_distill_loss_backward.argtypes = [vp, vp]
+    L.fpsk_distill_loss.argtypes = L.fpsk_distill_loss_backward.argtypes = [vp, vp, vp]
     return L
 
 
@@ -62,7 +62,7 @@ def test_adjust_logits(lib):
         return lib.fpsk_adjust_logits(s, None, None)
 
     assert lib.fpsk_adjust_logits(None, None, None) == fpsk.ERR_NULL
-    assert call(n=-1) == call(n=1 << 31) == call(vocab=0) == call(vocab=(1 << 26) + 1) == call(strides=(100, 99)) == call(strides=(-1, 100)) == fpsk.ERR_SHAPE
+    assert call(n=-1) == call(n=1 << 31) == call(vocab=0) == call(vocab=(1 << 23) + 1) == call(strides=(100, 99)) == call(strides=(-1, 100)) == fpsk.ERR_SHAPE
     assert call(types=(E4M3, F32)) == call(types=(F32, E4M3)) == fpsk.ERR_DTYPE
     assert call(x=0) == call(out=0) == call(penalties=(P, 0, 0)) == call(history=(0, P, 0)) == call(bias=(P, 0, P), n_biases=3) == call(mask=(0, P)) == fpsk.ERR_NULL
     assert call(history=(P, 0, 0), width=-1) == call(mask=(P, 0), mask_stride=-1) == fpsk.ERR_SHAPE
@@ -72,10 +72,10 @@ def test_adjust_logits(lib):
 
 def test_distill(lib):
     def call(f, x=P, tok=P, t=P, weight=0, loss=P, lse=P, dx=P, strides=(100, 4, 4, 100), n=2, vocab=100, top=4, types=(F32, 4, F32, F32), normalize=1, tau=1.0):
-        return f(struct.pack("@PPPPPPPqqqqqiiiiiiif", x, tok, t, weight, loss, lse, dx, *strides, n, vocab, top, *types, normalize, tau), None)
+        return f(struct.pack("@PPPPPPPqqqqqiiiiiiif", x, tok, t, weight, loss, lse, dx, *strides, n, vocab, top, *types, normalize, tau), None, None)
 
     for f in (lib.fpsk_distill_loss, lib.fpsk_distill_loss_backward):
-        assert f(None, None) == fpsk.ERR_NULL
+        assert f(None, None, None) == fpsk.ERR_NULL
         assert call(f, n=-1) == call(f, vocab=0) == call(f, top=-1) == call(f, top=1025) == call(f, strides=(100, 4, 4, 99)) == call(f, strides=(-1, 4, 4, 100)) == fpsk.ERR_SHAPE
         assert call(f, types=(E4M3, 4, F32, F32)) == call(f, types=(F32, 2, F32, F32)) == call(f, types=(F32, 8, E4M3, F32)) == call(f, types=(F32, 8, F32, E4M3)) == fpsk.ERR_DTYPE
         assert call(f, tau=0.0) == call(f, tau=-1.0) == call(f, tau=float("nan")) == call(f, tau=float("inf")) == call(f, tau=1e-39) == fpsk.ERR_PARAM
