@@ -35,9 +35,8 @@ struct DistillArgs {
     int32_t *status;
 };
 
-constexpr int kWorkers = 256, kDistillThreads = kWorkers + 64;
+constexpr int kWorkers = 128, kDistillThreads = kWorkers + 64;
 constexpr int kPiece = 8192, kPieceVecs = kPiece / 16, kMostStages = 27;
-constexpr float kFollow = 20.f;        // the reference follows a logit that stands out by 2^20: sums stay far from FP32's range
 constexpr float kNoReference = -3.4e38f;
 
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -46,13 +45,18 @@ __device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("
 // 2^((x - M) c) summed
 struct RefSum {
     float m, s;
-    __device__ __forceinline__ void join(float om, float os, float c)
-    {
-        const float top = fmaxf(m, om);
-        s = s * exp2_fast((m - top) * c) + os * exp2_fast((om - top) * c);
-        m = top;
-    }
 };
+// Joined over a warp's first LANES lanes (the others hold no reference), in a fixed order; every lane has the result.
+template <int LANES> __device__ __forceinline__ RefSum join_lanes(RefSum r, float c)
+{
+    float top = r.m;
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    float s = r.s * exp2_fast((r.m - top) * c);
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    return RefSum{top, s};
+}
 
 // A vector of 16 bytes as pairs.
 template <typename X> struct Vec;
@@ -76,6 +80,37 @@ template <typename X> struct Vec16 {
 };
 template <> struct Vec<__half> : Vec16<__half> {};
 template <> struct Vec<__nv_bfloat16> : Vec16<__nv_bfloat16> {};
+
+template <typename X> __device__ __forceinline__ float vec_max(const uint4 &u)
+{
+    float2 e[Vec<X>::n / 2];
+    Vec<X>::open(u, e);
+    float top = fmaxf(e[0].x, e[0].y);
+#pragma unroll
+    for (int j = 1; j < Vec<X>::n / 2; ++j) top = fmaxf(top, fmaxf(e[j].x, e[j].y));
+    return top;
+}
+// sum += 2^((x - M) c) of a vector's elements
+template <typename X> __device__ __forceinline__ void add_powers(const uint4 &u, float2 minus, float2 cc, float2 &sum)
+{
+    float2 e[Vec<X>::n / 2];
+    Vec<X>::open(u, e);
+#pragma unroll
+    for (int j = 0; j < Vec<X>::n / 2; ++j) {
+        const float2 y = __fmul2_rn(__fadd2_rn(e[j], minus), cc);
+        sum = __fadd2_rn(sum, make_float2(exp2_fast(y.x), exp2_fast(y.y)));
+    }
+}
+// f 2^((x - M) c)
+template <typename X> __device__ __forceinline__ void gradients(const uint4 &u, float2 minus, float2 cc, float2 ff, float2 (&e)[Vec<X>::n / 2])
+{
+    Vec<X>::open(u, e);
+#pragma unroll
+    for (int j = 0; j < Vec<X>::n / 2; ++j) {
+        const float2 y = __fmul2_rn(__fadd2_rn(e[j], minus), cc);
+        e[j] = __fmul2_rn(make_float2(exp2_fast(y.x), exp2_fast(y.y)), ff);
+    }
+}
 
 // Where the 16-byte vectors of a row lie: `a` elements in front of the first, `n` vectors, of which a block has [v0, v1).
 struct Slice {
@@ -342,30 +377,32 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 float2 s2 = make_float2(r.s, 0.f), minus = make_float2(-r.m, -r.m);
                 for (int v = sl.v0; v < sl.v1; v += kPieceVecs) {
                     wait(full[stage], phase);
-                    const uint4 *piece = reinterpret_cast<const uint4 *>(smem + stage * kPiece);
-                    const int vecs = min(kPieceVecs, sl.v1 - v);
-#pragma unroll
-                    for (int i = 0; i < kPieceVecs / kWorkers; ++i) {
-                        const int at = tid + i * kWorkers;
-                        if (at < vecs) {
-                            float2 e[VEC / 2];
-                            Vec<X>::open(piece[at], e);
-                            float top = fmaxf(e[0].x, e[0].y);
-#pragma unroll
-                            for (int j = 1; j < VEC / 2; ++j) top = fmaxf(top, fmaxf(e[j].x, e[j].y));
-                            if ((top + minus.x) * c > kFollow) {
-                                const float f = exp2_fast((-minus.x - top) * c);
-                                s2.x *= f;
-                                s2.y *= f;
-                                minus = make_float2(-top, -top);
-                            }
-#pragma unroll
-                            for (int j = 0; j < VEC / 2; ++j) {
-                                const float2 y = __fmul2_rn(__fadd2_rn(e[j], minus), cc);
-                                s2 = __fadd2_rn(s2, make_float2(exp2_fast(y.x), exp2_fast(y.y)));
-                            }
-                        }
+                    const uint4 *piece = reinterpret_cast<const uint4 *>(smem + stage * kPiece) + tid;
+                    const int vecs = sl.v1 - v;
+                    // The reference is the largest of the thread's first logits, and stays where it is unless a piece's powers add up to
+                    // 2^100 or more (an infinity, a NaN): then it moves to the piece's largest and the piece is summed anew.  A
+                    // reference below the row's largest costs no precision.
+                    if (v == sl.v0 && tid < vecs && loose < 0) {
+                        const float top = vec_max<X>(piece[0]);
+                        if (top != -INFINITY) minus = make_float2(-top, -top);
                     }
+                    float2 sum = make_float2(0.f, 0.f);
+                    if (vecs >= kPieceVecs) {
+#pragma unroll
+                        for (int i = 0; i < kPieceVecs / kWorkers; ++i) add_powers<X>(piece[i * kWorkers], minus, cc, sum);
+                    } else {
+                        for (int at = tid; at < vecs; at += kWorkers) add_powers<X>(piece[at - tid], minus, cc, sum);
+                    }
+                    if (!(sum.x + sum.y < 1.2676506e30f)) {
+                        float top = -minus.x;
+                        for (int at = tid; at < min(vecs, kPieceVecs); at += kWorkers) top = fmaxf(top, vec_max<X>(piece[at - tid]));
+                        const float f = exp2_fast((-minus.x - top) * c);
+                        s2 = make_float2(s2.x * f, s2.y * f);
+                        minus = make_float2(-top, -top);
+                        sum = make_float2(0.f, 0.f);
+                        for (int at = tid; at < min(vecs, kPieceVecs); at += kWorkers) add_powers<X>(piece[at - tid], minus, cc, sum);
+                    }
+                    s2 = __fadd2_rn(s2, sum);
                     if (MODE == kLossOnly || !g.resident) {
                         __syncwarp();
                         if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
@@ -375,17 +412,11 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                         phase ^= 1u;
                     }
                 }
-                r = RefSum{-minus.x, s2.x + s2.y};
-#pragma unroll
-                for (int o = 16; o; o >>= 1) {
-                    const float om = __shfl_xor_sync(0xFFFFFFFFu, r.m, o), os = __shfl_xor_sync(0xFFFFFFFFu, r.s, o);
-                    r.join(om, os, c);
-                }
+                r = join_lanes<32>(RefSum{-minus.x, s2.x + s2.y}, c);
                 if (lane == 0) warps_sum[b][warp] = make_float2(r.m, r.s);
                 bar_sync(1, kWorkers);
-                r = RefSum{warps_sum[b][0].x, warps_sum[b][0].y};
-#pragma unroll
-                for (int w = 1; w < kWorkers / 32; ++w) r.join(warps_sum[b][w].x, warps_sum[b][w].y, c);
+                const float2 mine = warps_sum[b][lane % (kWorkers / 32)];
+                r = join_lanes<kWorkers / 32>(RefSum{mine.x, mine.y}, c);
                 // (the teacher's logits are read before any block goes on to write the gradient, perhaps in the logits' place)
                 wait(ready[b], n >> 1 & 1u);
                 if (g.blocks > 1) {
@@ -401,8 +432,9 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                             : "memory");
                     }
                     wait(met[b], n >> 1 & 1u);
-                    r = RefSum{blocks_sum[b][0].x, blocks_sum[b][0].y};
-                    for (int k = 1; k < g.blocks; ++k) r.join(blocks_sum[b][k].x, blocks_sum[b][k].y, c);
+                    const float2 theirs = lane < g.blocks ? blocks_sum[b][lane] : make_float2(kNoReference, 0.f);
+                    r = join_lanes<kRowMostBlocks>(RefSum{theirs.x, theirs.y}, c);
+                    r = RefSum{__shfl_sync(0xFFFFFFFFu, r.m, 0), __shfl_sync(0xFFFFFFFFu, r.s, 0)};
                 }
                 M = r.m;
                 S = r.s;
@@ -415,29 +447,29 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             if (tid == 0) result[b] = make_float2(M, S);
             if (MODE != kLossOnly) {
                 if (g.resident && MODE == kLossAndGrad) stage = stage0;
-                const float m = mass[b];
-                const float f = m == 0.f ? 0.f : weight * g.inv_tau * m / S;
+                // (a row without a teacher has zeros, whatever it holds)
+                const float m = mass[b], f = m == 0.f ? 0.f : weight * g.inv_tau * m / S;
                 const float2 ff = make_float2(f, f), minus = make_float2(-M, -M);
+                G *out = dx + sl.a + ((long long)sl.v0 + tid) * VEC;
                 for (int v = sl.v0; v < sl.v1; v += kPieceVecs) {
-                    if (MODE == kGradOnly || !g.resident) {
-                        wait(full[stage], phase);
-                    }
-                    const uint4 *piece = reinterpret_cast<const uint4 *>(smem + stage * kPiece);
-                    const int vecs = min(kPieceVecs, sl.v1 - v);
+                    if (MODE == kGradOnly || !g.resident) wait(full[stage], phase);
+                    const uint4 *piece = reinterpret_cast<const uint4 *>(smem + stage * kPiece) + tid;
+                    const int vecs = sl.v1 - v;
+                    if (vecs >= kPieceVecs && wide && m != 0.f) {
 #pragma unroll
-                    for (int i = 0; i < kPieceVecs / kWorkers; ++i) {
-                        const int at = tid + i * kWorkers;
-                        if (at < vecs) {
+                        for (int i = 0; i < kPieceVecs / kWorkers; ++i) {
                             float2 e[VEC / 2];
-                            Vec<X>::open(piece[at], e);
-#pragma unroll
-                            for (int j = 0; j < VEC / 2; ++j) {
-                                const float2 y = __fmul2_rn(__fadd2_rn(e[j], minus), cc);
-                                e[j] = m == 0.f ? make_float2(0.f, 0.f) : __fmul2_rn(make_float2(exp2_fast(y.x), exp2_fast(y.y)), ff);
-                            }
-                            store_vec<G, VEC>(dx + sl.a + (long long)(v + at) * VEC, wide, e);
+                            gradients<X>(piece[i * kWorkers], minus, cc, ff, e);
+                            store_vec<G, VEC>(out + i * kWorkers * VEC, true, e);
+                        }
+                    } else {
+                        for (int at = tid; at < min(vecs, kPieceVecs); at += kWorkers) {
+                            float2 e[VEC / 2] = {};
+                            if (m != 0.f) gradients<X>(piece[at - tid], minus, cc, ff, e);
+                            store_vec<G, VEC>(out + (at - tid) * VEC, wide, e);
                         }
                     }
+                    out += kPieceVecs * VEC;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
                     if (++stage == g.stages) {
