@@ -29,14 +29,15 @@ struct DistillArgs {
     int normalize;
     float tau, inv_tau, c;             // c = log2(e) / tau
     int blocks;                        // of a row
-    int stages;                        // of the ring
-    int resident;                      // a slice fits the ring: it is copied once for both passes
+    int teachers;                      // warps
     int teacher_at, map_at, map_words; // in shared memory: behind the ring the teacher's arrays, and the map of listed tokens
     int32_t *status;
 };
 
-constexpr int kWorkers = 128, kDistillThreads = kWorkers + 64;
-constexpr int kPiece = 8192, kPieceVecs = kPiece / 16, kMostStages = 27;
+constexpr int kWorkers = 128, kMostTeachers = 3;   // threads of the sums and gradients, warps of the teacher
+constexpr int kDistillThreads = kWorkers + 32 + 32 * kMostTeachers;
+constexpr int kPiece = 8192, kPieceVecs = kPiece / 16, kStages = 5;
+constexpr int kTogether = 4;            // listed tokens of a lane at a time
 constexpr float kNoReference = -3.4e38f;
 
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -154,20 +155,21 @@ template <typename G, int N> __device__ __forceinline__ void store_vec(G *p, boo
     }
 }
 
-template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const __grid_constant__ DistillArgs g)
+template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const __grid_constant__ DistillArgs g)
 {
     constexpr int VEC = Vec<X>::n;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ unsigned long long full[kMostStages], empty[kMostStages], ready[2], met[2];
-    __shared__ float2 blocks_sum[2][kRowMostBlocks];                   // written by the cluster's blocks
+    __shared__ unsigned long long full[kStages], empty[kStages], ready[2], met[2];
+    __shared__ float4 blocks_sum[2][kRowMostBlocks];                   // written by the cluster's blocks: M, S, the teacher's two
     __shared__ float2 warps_sum[2][kWorkers / 32];
-    __shared__ float2 result[2];
-    __shared__ float mass[2];
+    __shared__ float4 result[2], taught[2];                            // M, S, the teacher's two; K, xr, the teacher's two
+    __shared__ float teams[5][kMostTeachers];
+    __shared__ int teams_twice[kMostTeachers], counts[2][kMostTeachers];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)cluster_rank();
     const long long first_row = blockIdx.x / g.blocks, row_step = gridDim.x / g.blocks;
     if (tid == 0) {
-        for (int s = 0; s < g.stages; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             mbar_init(smem_u32(&full[s]), 1);
             mbar_init(smem_u32(&empty[s]), kWorkers / 32);
         }
@@ -177,17 +179,23 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    for (int i = tid; i < g.map_words; i += kDistillThreads) reinterpret_cast<unsigned int *>(smem + g.map_at)[i] = 0;
+    for (int i = tid; i < g.map_words; i += blockDim.x) reinterpret_cast<unsigned int *>(smem + g.map_at)[i] = 0;
     __syncthreads();
     cluster_sync();
     // Every wait is bounded; once one has given up the others are passed over, and all roles still run to their ends.
     bool ok = true;
+    // (asked for a row ahead: the answer takes a microsecond)
+    auto weight_of = [&](long long row) { return g.weight && row < g.rows ? g.weight[row] : 1.f; };
+    float weight_next = weight_of(first_row);
     auto wait = [&](unsigned long long &bar, uint32_t parity) {
         if (ok && !mbar_wait_bounded(smem_u32(&bar), parity)) {
             ok = false;
             report_status(g.status, FPSK_ERR_TIMEOUT);
         }
     };
+
+    // the teacher's mass, from what it says: normalized its largest logit and 1 / s, else the mass itself
+    auto mass_of = [&](float a0, float a1) { return g.normalize ? (a1 == 0.f ? 0.f : 1.f) : a0; };
 
     if (warp == kWorkers / 32) {
         // ------------------------------------------------------------ copies
@@ -196,11 +204,13 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             int stage = 0;
             uint32_t phase = 0;
             for (long long row = first_row; row < g.rows && ok; row += row_step) {
-                if (g.weight && g.weight[row] == 0.f) continue;
+                const float weight = weight_next;
+                weight_next = weight_of(row + row_step);
+                if (weight == 0.f) continue;
                 const X *x = static_cast<const X *>(g.x) + row * g.xs;
                 const Slice sl(x, g.vocab, g.blocks, rank, X());
                 const char *from = reinterpret_cast<const char *>(x + sl.a);
-                for (int pass = 0; pass < (MODE == kLossAndGrad && !g.resident ? 2 : 1); ++pass) {
+                for (int pass = 0; pass < (MODE == kLossAndGrad ? 2 : 1); ++pass) {
                     for (int v = sl.v0; v < sl.v1; v += kPieceVecs) {
                         wait(empty[stage], phase ^ 1u);
                         if (!ok) break;
@@ -208,7 +218,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                         mbar_expect_tx(bar, bytes);
                         bulk_g2s(smem_u32(smem) + stage * kPiece, from + 16LL * v, bytes, bar);
                         ++k;
-                        if (++stage == g.stages) {
+                        if (++stage == kStages) {
                             stage = 0;
                             phase ^= 1u;
                         }
@@ -216,132 +226,237 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 }
             }
             // no copy is left in flight
-            for (unsigned int back = min(k, (unsigned int)g.stages); back; --back) {
+            for (unsigned int back = min(k, (unsigned int)kStages); back; --back) {
                 const unsigned int piece = k - back;
-                mbar_wait_bounded(smem_u32(&full[piece % g.stages]), piece / g.stages & 1u);
+                mbar_wait_bounded(smem_u32(&full[piece % kStages]), piece / kStages & 1u);
             }
         }
-    } else if (warp == kWorkers / 32 + 1) {
+    } else if (warp > kWorkers / 32) {
         // ------------------------------------------------------------ the teacher
-        float *arrays = reinterpret_cast<float *>(smem + g.teacher_at);
+        const int me = tid - kWorkers - 32, all = 32 * g.teachers, my_warp = me >> 5;
         unsigned int *map = reinterpret_cast<unsigned int *>(smem + g.map_at);
-        // of two rows at a time: token, log p, p, logit
-        auto array = [&](int which, int b) { return arrays + (which * 2 + b) * g.top; };
+        // Of two rows at a time, for each of the teacher's warps: the listed tokens that are this block's, their t and logit.
+        const int room = (g.top + all - 1) / all * 32;
+        auto list = [&](int which, int b, int w) { return reinterpret_cast<float *>(smem + g.teacher_at) + ((which * 2 + b) * g.teachers + w) * room; };
+        // over the teacher's warps, in their order
+        auto total = [&](float v, int slot) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+            if (g.teachers == 1) return v;
+            if (lane == 0) teams[slot][my_warp] = v;
+            bar_sync(4, all);
+            v = teams[slot][0];
+            for (int w = 1; w < g.teachers; ++w) v += teams[slot][w];
+            return v;
+        };
+        auto largest = [&](float v, int slot) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+            if (g.teachers == 1) return v;
+            if (lane == 0) teams[slot][my_warp] = v;
+            bar_sync(4, all);
+            v = teams[slot][0];
+            for (int w = 1; w < g.teachers; ++w) v = fmaxf(v, teams[slot][w]);
+            return v;
+        };
+        auto from_first = [&](float v, int slot) {
+            v = __shfl_sync(0xFFFFFFFFu, v, 0);
+            if (g.teachers == 1) return v;
+            if (me == 0) teams[slot][0] = v;
+            bar_sync(4, all);
+            return teams[slot][0];
+        };
+        // a token's place among this block's of a row, or -1
+        auto place = [&](const Slice &sl, int t) {
+            if (t < 0) return -1;
+            if (t < sl.a) return rank == 0 ? t : -1;
+            if (t >= sl.tail) return rank == g.blocks - 1 ? 8 + t - sl.tail : -1;
+            const int v = (t - sl.a) / VEC;
+            return v >= sl.v0 && v < sl.v1 ? 16 + t - sl.a - sl.v0 * VEC : -1;
+        };
+        // The first kTogether listed tokens of each lane are asked for a row ahead, and their logits brought into L2 half a row
+        // ahead: the chain weight, token, logit takes as long as a row otherwise.
+        int token[kTogether];
+        float t[kTogether];
+        auto ask = [&](long long row, int j0) {
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                const int j = j0 + all * i;
+                token[i] = -1;
+                t[i] = -INFINITY;
+                if (row < g.rows && j < g.top) {
+                    const long long v = g.tok_bytes == 4 ? (long long)static_cast<const int *>(g.tok)[row * g.toks + j]
+                                                         : static_cast<const long long *>(g.tok)[row * g.toks + j];
+                    if (v >= 0 && v < g.vocab) token[i] = (int)v;
+                    const long long at = row * g.ts + j;
+                    t[i] = g.t_type == FPSK_ELEM_FP32 ? static_cast<const float *>(g.t)[at]
+                           : g.t_type == FPSK_ELEM_FP16 ? __half2float(static_cast<const __half *>(g.t)[at])
+                                                        : __bfloat162float(static_cast<const __nv_bfloat16 *>(g.t)[at]);
+                }
+            }
+        };
+        // The sums over the list and the loss are the first block's, a token's gradient that of the block that has the token.  (Where
+        // the blocks exchange nothing each sums for itself.)
+        const bool sums = MODE == kGradOnly || rank == 0, losses = MODE != kGradOnly && rank == 0;
+        const float ct = g.normalize ? g.c : kLog2e;
+        auto bring = [&](long long row) {
+            if (row >= g.rows) return;
+            const X *x = static_cast<const X *>(g.x) + row * g.xs;
+            const Slice sl(x, g.vocab, g.blocks, rank, X());
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i)
+                if (losses ? token[i] >= 0 : MODE != kLossOnly && place(sl, token[i]) >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + token[i]));
+        };
+        // loss = sum p (log p - log q) = K + m ((M - xr) / tau + ln S), with a listed logit xr as reference; normalized, with
+        // e = 2^((t - u) c), s = sum e, m = 1 and a listed tr:  K = sum e ((t - tr) - (x - xr)) / (tau s) + (tr - u) / tau - ln s;
+        // else with e = 2^(t log2(e)), m = sum e:               K = sum e (t - (x - xr) / tau).
         auto prepare = [&](long long row, int b) {
             const X *x = static_cast<const X *>(g.x) + row * g.xs;
-            int *tok = reinterpret_cast<int *>(array(0, b));
-            float *logp = array(1, b), *prob = array(2, b), *xs = array(3, b);
-            float most = -INFINITY;
-            for (int j = lane; j < g.top; j += 32) {
-                const long long token = g.tok_bytes == 4 ? (long long)static_cast<const int *>(g.tok)[row * g.toks + j]
-                                                         : static_cast<const long long *>(g.tok)[row * g.toks + j];
-                const bool in = token >= 0 && token < g.vocab;
-                const long long at = row * g.ts + j;
-                const float t = g.t_type == FPSK_ELEM_FP32 ? static_cast<const float *>(g.t)[at]
-                                : g.t_type == FPSK_ELEM_FP16 ? __half2float(static_cast<const __half *>(g.t)[at])
-                                                             : __bfloat162float(static_cast<const __nv_bfloat16 *>(g.t)[at]);
-                const float l = !in ? -INFINITY : g.normalize ? t * g.inv_tau : t;
-                tok[j] = in ? (int)token : -1;
-                xs[j] = in ? Elem<X>::to_f(x[token]) : 0.f;
-                logp[j] = l;
-                most = fmaxf(most, l);
-            }
-            if (g.normalize) {
+            const Slice sl(x, g.vocab, g.blocks, rank, X());
+            float u = kNoReference, s = 0.f, d = 0.f, tr = 0.f, xr = 0.f;
+            int count = 0;
+            for (int j0 = me; j0 - lane < g.top; j0 += all * kTogether) {
+                if (j0 != me) ask(row, j0);
+                int at[kTogether];
+                float l[kTogether];
 #pragma unroll
-                for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-                float s = 0.f;
-                for (int j = lane; j < g.top; j += 32) s += logp[j] == -INFINITY ? 0.f : expf(logp[j] - most);
+                for (int i = 0; i < kTogether; ++i) {
+                    at[i] = MODE != kLossOnly && t[i] != -INFINITY ? place(sl, token[i]) : -1;
+                    l[i] = at[i] >= 0 || (losses && token[i] >= 0) ? Elem<X>::to_f(x[token[i]]) : 0.f;
+                }
+                if (MODE != kLossOnly) {
 #pragma unroll
-                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-                const float ln = logf(s);
-                for (int j = lane; j < g.top; j += 32)
-                    if (logp[j] != -INFINITY) logp[j] = logp[j] - most - ln;
-            }
-            float sum = 0.f;
-            for (int j = lane; j < g.top; j += 32) {
-                const float p = logp[j] == -INFINITY ? 0.f : expf(logp[j]);
-                prob[j] = p;
-                sum += p;
-            }
+                    for (int i = 0; i < kTogether; ++i) {
+                        const unsigned int own = __ballot_sync(0xFFFFFFFFu, at[i] >= 0);
+                        if (at[i] >= 0) {
+                            const int k = count + __popc(own & ((1u << lane) - 1u));
+                            reinterpret_cast<int *>(list(0, b, my_warp))[k] = token[i];
+                            list(1, b, my_warp)[k] = t[i];
+                            list(2, b, my_warp)[k] = l[i];
+                        }
+                        count += __popc(own);
+                    }
+                }
+                if (sums) {
+                    float top = u;
 #pragma unroll
-            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            if (lane == 0) mass[b] = sum;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ready[b]));
-        };
-        auto finish = [&](long long row, int b) {
-            const int *tok = reinterpret_cast<const int *>(array(0, b));
-            const float *logp = array(1, b), *prob = array(2, b), *xs = array(3, b);
-            bar_sync(2 + b, kWorkers + 32);                            // the row's gradient is written
-            const float M = result[b].x, S = result[b].y;
-            if (MODE != kGradOnly && rank == 0) {
-                const float ln = logf(S);
-                float l = 0.f;
-                for (int j = lane; j < g.top; j += 32)
-                    if (logp[j] != -INFINITY) l = fmaf(prob[j], logp[j] - fmaf(xs[j] - M, g.inv_tau, -ln), l);
+                    for (int i = 0; i < kTogether; ++i)
+                        if (token[i] >= 0) top = fmaxf(top, t[i]);
+                    if (losses && j0 == me) {
+                        tr = from_first(t[0], 0);
+                        xr = from_first(l[0], 1);
+                        if (!(fabsf(tr) < 3e38f) || !g.normalize) tr = 0.f;
+                        if (!(fabsf(xr) < 3e38f)) xr = 0.f;
+                    }
+                    if (!g.normalize) {
+                        top = 0.f;
+                    } else {
+                        const float f = exp2_fast((u - top) * ct);
+                        s *= f;
+                        d *= f;
+                    }
+                    u = top;
 #pragma unroll
-                for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-                if (lane == 0) {
-                    g.loss[row] = l;
-                    if (g.lse) g.lse[row] = fmaf(M, g.inv_tau, ln);
+                    for (int i = 0; i < kTogether; ++i) {
+                        if (token[i] < 0 || t[i] == -INFINITY) continue;
+                        const float e = exp2_fast((t[i] - u) * ct);
+                        s += e;
+                        if (losses && e != 0.f) d = fmaf(e, g.normalize ? (t[i] - tr) - (l[i] - xr) : t[i] - (l[i] - xr) * g.inv_tau, d);
+                    }
                 }
             }
-            if (MODE != kLossOnly && mass[b] != 0.f) {
-                const X *x = static_cast<const X *>(g.x) + row * g.xs;
-                const Slice sl(x, g.vocab, g.blocks, rank, X());
-                // a listed token's place among this block's, or -1
-                auto place = [&](int t) {
-                    if (t < 0) return -1;
-                    if (t < sl.a) return rank == 0 ? t : -1;
-                    if (t >= sl.tail) return rank == g.blocks - 1 ? 8 + t - sl.tail : -1;
-                    const int v = (t - sl.a) / VEC;
-                    return v >= sl.v0 && v < sl.v1 ? 16 + t - sl.a - sl.v0 * VEC : -1;
-                };
+            if (MODE != kLossOnly && lane == 0) counts[b][my_warp] = count;
+            if (sums) {
+                if (g.normalize) {
+                    const float top = largest(u, 2), f = exp2_fast((u - top) * ct);
+                    s *= f;
+                    d *= f;
+                    u = top;
+                }
+                s = total(s, 3);
+                if (losses) d = total(d, 4);
+                if (me == 0) {
+                    float4 v = make_float4(0.f, xr, 0.f, 0.f);
+                    if (!g.normalize) v = make_float4(d, xr, s, 1.f);
+                    else if (s != 0.f) v = make_float4(d / s * g.inv_tau + (tr - u) * g.inv_tau - logf(s), xr, u, 1.f / s);
+                    taught[b] = v;
+                }
+            }
+            if (g.teachers == 1) __syncwarp();
+            else bar_sync(4, all);
+            if (me == 0) mbar_arrive(smem_u32(&ready[b]));
+        };
+        float weight_before = 1.f;
+        auto finish = [&](long long row, float weight, int b) {
+            bar_sync(2 + b, kWorkers + all);                           // the row's gradient is written
+            const float M = result[b].x, S = result[b].y, u = g.normalize ? result[b].z : 0.f, over = result[b].w;
+            const float m = mass_of(result[b].z, over);
+            if (losses && me == 0) {
+                const float ln = logf(S);
+                g.loss[row] = m == 0.f ? 0.f : fmaf(m, fmaf(M - taught[b].y, g.inv_tau, ln), taught[b].x);
+                if (g.lse) g.lse[row] = fmaf(M, g.inv_tau, ln);
+            }
+            if (MODE != kLossOnly && m != 0.f) {
+                const Slice sl(static_cast<const X *>(g.x) + row * g.xs, g.vocab, g.blocks, rank, X());
+                const int *tok = reinterpret_cast<const int *>(list(0, b, my_warp));
+                const int count = counts[b][my_warp];
                 bool twice = false;
-                for (int j = lane; j < g.top; j += 32) {
-                    const int at = place(tok[j]);
-                    if (at >= 0 && atomicOr(&map[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u) twice = true;
+                for (int j = lane; j < count; j += 32) {
+                    const int at = place(sl, tok[j]);
+                    if (atomicOr(&map[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u) twice = true;
                 }
                 twice = __any_sync(0xFFFFFFFFu, twice);
-                __syncwarp();
-                const float wt = (g.weight ? g.weight[row] : 1.f) * g.inv_tau, f = wt * mass[b] / S;
+                if (g.teachers > 1) {
+                    if (lane == 0) teams_twice[my_warp] = twice;
+                    bar_sync(4, all);
+                    for (int w = 0; w < g.teachers; ++w) twice |= teams_twice[w] != 0;
+                }
+                const float wt = weight * g.inv_tau, f = wt * m / S;
                 G *dx = static_cast<G *>(g.dx) + row * g.dxs;
-                for (int j = lane; j < g.top; j += 32) {
-                    const int at = place(tok[j]);
-                    if (at < 0) continue;
+                for (int j = lane; j < count; j += 32) {
+                    const int at = place(sl, tok[j]);
                     map[at >> 5] = 0;
-                    float p = prob[j];
+                    float p = exp2_fast((list(1, b, my_warp)[j] - u) * ct) * over;
                     bool first = true;
                     if (twice) {                                       // the first of those that list a token writes it
                         p = 0.f;
-                        for (int i = 0; i < g.top; ++i)
-                            if (tok[i] == tok[j]) {
-                                if (i < j) first = false;
-                                p += prob[i];
-                            }
+                        for (int w = 0; w < g.teachers; ++w)
+                            for (int i = 0; i < counts[b][w]; ++i)
+                                if (reinterpret_cast<const int *>(list(0, b, w))[i] == tok[j]) {
+                                    if (w < my_warp || (w == my_warp && i < j)) first = false;
+                                    p += exp2_fast((list(1, b, w)[i] - u) * ct) * over;
+                                }
                     }
-                    if (first) dx[tok[j]] = Elem<G>::from_f(fmaf(f, exp2_fast((xs[j] - M) * g.c), -wt * p));
+                    if (first) dx[tok[j]] = Elem<G>::from_f(fmaf(f, exp2_fast((list(2, b, my_warp)[j] - M) * g.c), -wt * p));
                 }
-                __syncwarp();
+                if (g.teachers == 1) __syncwarp();
+                else bar_sync(4, all);
             }
         };
         // one row ahead
         long long before = -1;
         unsigned int n = 0;
+        ask(first_row, me);
         for (long long row = first_row; row < g.rows; row += row_step) {
-            if (g.weight && g.weight[row] == 0.f) {
-                if (MODE != kGradOnly && rank == 0 && lane == 0) {
+            const float weight = weight_next;
+            weight_next = weight_of(row + row_step);
+            if (weight == 0.f) {
+                if (MODE != kGradOnly && rank == 0 && me == 0) {
                     g.loss[row] = 0.f;
                     if (g.lse) g.lse[row] = 0.f;
                 }
+                ask(row + row_step, me);
                 continue;
             }
             prepare(row, n & 1);
-            if (before >= 0) finish(before, (n - 1) & 1);
+            ask(row + row_step, me);
+            if (before >= 0) finish(before, weight_before, (n - 1) & 1);
+            bring(row + row_step);
             before = row;
+            weight_before = weight;
             ++n;
         }
-        if (before >= 0) finish(before, (n - 1) & 1);
+        if (before >= 0) finish(before, weight_before, (n - 1) & 1);
     } else {
         // ------------------------------------------------------------ sums and gradients
         unsigned int n = 0;                                            // rows so far
@@ -349,9 +464,12 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
         uint32_t phase = 0;
         const float c = g.c;
         const float2 cc = make_float2(c, c);
+        float lse_next = MODE == kGradOnly && first_row < g.rows ? g.lse[first_row] : 0.f;
         for (long long row = first_row; row < g.rows; row += row_step) {
             const X *x = static_cast<const X *>(g.x) + row * g.xs;
-            const float weight = g.weight ? g.weight[row] : 1.f;
+            const float weight = weight_next, lse = lse_next;
+            weight_next = weight_of(row + row_step);
+            if (MODE == kGradOnly && row + row_step < g.rows) lse_next = g.lse[row + row_step];
             const Slice sl(x, g.vocab, g.blocks, rank, X());
             // the elements in front of the first vector and behind the last: the first block's and the last block's, one to a lane
             int loose = -1;
@@ -370,7 +488,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             const int b = n & 1;
             const float x_loose = loose >= 0 ? Elem<X>::to_f(x[loose]) : -INFINITY;
             float M, S;
-            const int stage0 = stage;
+            float2 said;                                               // by the teacher
             if (MODE != kGradOnly) {
                 RefSum r = {kNoReference, 0.f};
                 if (loose >= 0 && x_loose != -INFINITY) r = RefSum{x_loose, x_loose == x_loose ? 1.f : x_loose};
@@ -403,11 +521,9 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                         for (int at = tid; at < min(vecs, kPieceVecs); at += kWorkers) add_powers<X>(piece[at - tid], minus, cc, sum);
                     }
                     s2 = __fadd2_rn(s2, sum);
-                    if (MODE == kLossOnly || !g.resident) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
-                    }
-                    if (++stage == g.stages) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
+                    if (++stage == kStages) {
                         stage = 0;
                         phase ^= 1u;
                     }
@@ -419,20 +535,22 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 r = join_lanes<kWorkers / 32>(RefSum{mine.x, mine.y}, c);
                 // (the teacher's logits are read before any block goes on to write the gradient, perhaps in the logits' place)
                 wait(ready[b], n >> 1 & 1u);
+                said = make_float2(taught[b].z, taught[b].w);
                 if (g.blocks > 1) {
                     if (tid < g.blocks) {
-                        if (tid == 0) mbar_expect_tx(smem_u32(&met[b]), 8u * g.blocks);
+                        if (tid == 0) mbar_expect_tx(smem_u32(&met[b]), 16u * g.blocks);
                         const uint32_t at = smem_u32(&blocks_sum[b][rank]), bar = smem_u32(&met[b]);
                         asm volatile(
                             "{\n\t.reg .b32 a, m;\n\t"
                             "mapa.shared::cluster.u32 a, %0, %2;\n\t"
                             "mapa.shared::cluster.u32 m, %1, %2;\n\t"
-                            "st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [a], {%3, %4}, [m];\n\t}"
-                            ::"r"(at), "r"(bar), "r"(tid), "f"(r.m), "f"(r.s)
+                            "st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %6}, [m];\n\t}"
+                            ::"r"(at), "r"(bar), "r"(tid), "f"(r.m), "f"(r.s), "f"(said.x), "f"(said.y)
                             : "memory");
                     }
                     wait(met[b], n >> 1 & 1u);
-                    const float2 theirs = lane < g.blocks ? blocks_sum[b][lane] : make_float2(kNoReference, 0.f);
+                    const float4 theirs = lane < g.blocks ? blocks_sum[b][lane] : make_float4(kNoReference, 0.f, 0.f, 0.f);
+                    said = make_float2(blocks_sum[b][0].z, blocks_sum[b][0].w);
                     r = join_lanes<kRowMostBlocks>(RefSum{theirs.x, theirs.y}, c);
                     r = RefSum{__shfl_sync(0xFFFFFFFFu, r.m, 0), __shfl_sync(0xFFFFFFFFu, r.s, 0)};
                 }
@@ -440,19 +558,18 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 S = r.s;
             } else {
                 wait(ready[b], n >> 1 & 1u);
-                const float lse = g.lse[row];
+                said = make_float2(taught[b].z, taught[b].w);
                 M = lse * g.tau;
                 S = expf(fmaf(-M, g.inv_tau, lse));                    // what M's rounding left of it
             }
-            if (tid == 0) result[b] = make_float2(M, S);
+            if (tid == 0) result[b] = make_float4(M, S, said.x, said.y);
             if (MODE != kLossOnly) {
-                if (g.resident && MODE == kLossAndGrad) stage = stage0;
                 // (a row without a teacher has zeros, whatever it holds)
-                const float m = mass[b], f = m == 0.f ? 0.f : weight * g.inv_tau * m / S;
+                const float m = mass_of(said.x, said.y), f = m == 0.f ? 0.f : weight * g.inv_tau * m / S;
                 const float2 ff = make_float2(f, f), minus = make_float2(-M, -M);
                 G *out = dx + sl.a + ((long long)sl.v0 + tid) * VEC;
                 for (int v = sl.v0; v < sl.v1; v += kPieceVecs) {
-                    if (MODE == kGradOnly || !g.resident) wait(full[stage], phase);
+                    wait(full[stage], phase);
                     const uint4 *piece = reinterpret_cast<const uint4 *>(smem + stage * kPiece) + tid;
                     const int vecs = sl.v1 - v;
                     if (vecs >= kPieceVecs && wide && m != 0.f) {
@@ -472,14 +589,14 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                     out += kPieceVecs * VEC;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
-                    if (++stage == g.stages) {
+                    if (++stage == kStages) {
                         stage = 0;
-                        if (MODE == kGradOnly || !g.resident) phase ^= 1u;
+                        phase ^= 1u;
                     }
                 }
                 if (loose >= 0) dx[loose] = Elem<G>::from_f(m == 0.f ? 0.f : f * exp2_fast((x_loose - M) * c));
             }
-            bar_arrive(2 + b, kWorkers + 32);
+            bar_arrive(2 + b, kWorkers + 32 * g.teachers);
             ++n;
         }
     }
@@ -492,7 +609,7 @@ static int clusters_at_once(const void *kernel, const cudaLaunchConfig_t &cfg, i
 {
     struct Key {
         const void *kernel;
-        int device, blocks;
+        int device, blocks, threads;
         size_t bytes;
     };
     static std::mutex lock;
@@ -504,46 +621,43 @@ static int clusters_at_once(const void *kernel, const cudaLaunchConfig_t &cfg, i
     const int blocks = (int)cfg.attrs[0].val.clusterDim.x;
     std::lock_guard<std::mutex> hold(lock);
     for (int i = 0; i < (used < 64 ? used : 64); ++i)
-        if (keys[i].kernel == kernel && keys[i].device == device && keys[i].blocks == blocks && keys[i].bytes == cfg.dynamicSmemBytes) {
+        if (keys[i].kernel == kernel && keys[i].device == device && keys[i].blocks == blocks && keys[i].threads == (int)cfg.blockDim.x && keys[i].bytes == cfg.dynamicSmemBytes) {
             *out = values[i];
             return cudaSuccess;
         }
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 2048);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(out, kernel, &cfg);
     if (e != cudaSuccess) return e;
     if (*out < 1) *out = 1;
-    keys[used % 64] = Key{kernel, device, blocks, cfg.dynamicSmemBytes};
+    keys[used % 64] = Key{kernel, device, blocks, (int)cfg.blockDim.x, cfg.dynamicSmemBytes};
     values[used % 64] = *out;
     ++used;
     return cudaSuccess;
 }
 
-constexpr int kMostBytes = 227 * 1024 - 2048, kThirdBytes = 74 * 1024;
+constexpr long long kRowsInL2 = 40LL << 20, kLongRowsInL2 = 60LL << 20;
 
 template <typename X, typename G, int MODE> static fpsk_status launch_distill(DistillArgs g, cudaStream_t st)
 {
     const int vecs = (g.vocab + Vec<X>::n - 1) / Vec<X>::n;
     auto slice_pieces = [&](int blocks) { return ((vecs + blocks - 1) / blocks + kPieceVecs - 1) / kPieceVecs; };
-    const int teacher = (int)align_up((size_t)8 * g.top * sizeof(float), 128);
+    g.teachers = g.top <= 128 ? 1 : kMostTeachers;
+    const int teacher = MODE == kLossOnly ? 0 : (int)align_up((size_t)6 * (g.top + 32 * g.teachers) * sizeof(float), 128);
     auto map_bytes = [&](int blocks) { return MODE == kLossOnly ? 0 : (int)align_up((size_t)((vecs + blocks - 1) / blocks * Vec<X>::n + 16 + 31) / 32 * 4, 128); };
-    // Slices of 64 KB at most, so that three blocks share an SM and one computes while another's copies arrive; smaller ones where there
-    // are few rows.
+    // One block to a row, unless there are too few rows for all SMs, or the rows at work at a time (four blocks to an SM) would take
+    // more than kRowsInL2, so that the second look at them finds them gone from L2.
+    const long long row_bytes = (long long)vecs * 16;
     g.blocks = 1;
-    while (g.blocks < kRowMostBlocks && (slice_pieces(g.blocks) > 8 || (g.rows * g.blocks < 3 * kSms && slice_pieces(g.blocks) > 1))) g.blocks *= 2;
-    const int pieces = slice_pieces(g.blocks), fixed = teacher + map_bytes(g.blocks);
-    int stages = (kThirdBytes - fixed) / kPiece;
-    if (MODE == kLossAndGrad && stages < pieces) stages = (113 * 1024 - 2048 - fixed) / kPiece;
-    if (MODE == kLossAndGrad && stages < pieces) stages = (kMostBytes - fixed) / kPiece;
-    if (stages < 4) stages = 4;                                        // (a map of the largest vocabulary leaves room for them)
-    if (stages > kMostStages) stages = kMostStages;
-    g.stages = stages;
-    g.resident = pieces <= stages;
-    g.teacher_at = stages * kPiece;
+    while (g.blocks < kRowMostBlocks && slice_pieces(g.blocks) > 1 &&
+           (g.rows * g.blocks < 3 * kSms || (MODE == kLossAndGrad && 4 * kSms / g.blocks * row_bytes > kRowsInL2)))
+        g.blocks *= 2;
+    g.teacher_at = kStages * kPiece;
     g.map_at = g.teacher_at + teacher;
     g.map_words = map_bytes(g.blocks) / 4;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)g.blocks);
-    cfg.blockDim = dim3(kDistillThreads);
+    cfg.blockDim = dim3(kWorkers + 32 + 32 * g.teachers);
     cfg.dynamicSmemBytes = (size_t)g.map_at + map_bytes(g.blocks);
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
@@ -555,6 +669,9 @@ template <typename X, typename G, int MODE> static fpsk_status launch_distill(Di
     auto kernel = distill_kernel<X, G, MODE>;
     int most = 1;
     FPSK_CUDA_OK((cudaError_t)clusters_at_once(reinterpret_cast<const void *>(kernel), cfg, &most));
+    // (rows too long for that even with the most blocks each: fewer at a time)
+    if (MODE == kLossAndGrad && g.blocks == kRowMostBlocks && most > kLongRowsInL2 / row_bytes) most = (int)(kLongRowsInL2 / row_bytes);
+    if (most < 1) most = 1;
     cfg.gridDim = dim3((unsigned)((g.rows < most ? g.rows : most) * g.blocks));
     FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, g));
     FPSK_LAUNCH_CHECK();
