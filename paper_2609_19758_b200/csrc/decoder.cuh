@@ -3,6 +3,9 @@
 #pragma once
 #include "attention.cuh"
 #include "fpsk_decoder.h"
+#include "stream_pipe.cuh"
+
+#include <type_traits>
 
 namespace fpsk {
 
@@ -76,7 +79,7 @@ inline bool row_wide(const void *p, int type, long long stride, int bytes = 16)
 }
 
 // ---------------------------------------------------------------- rows of a vocabulary: a cluster of blocks to a row
-constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32, kRowMostBlocks = 8;
+constexpr int kRowMostBlocks = 8;
 constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ float exp2_fast(float x)
@@ -85,6 +88,8 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("barrier.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ unsigned int cluster_rank()
 {
     unsigned int r;
@@ -95,34 +100,89 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-// a value of another block's shared memory, at the place that it has in this one's
-__device__ __forceinline__ float cluster_load(const float *p, unsigned int rank)
+constexpr float kNoReference = -3.4e38f;
+// 2^((x - M) c) summed
+struct RefSum {
+    float m, s;
+};
+// Joined over a warp's first LANES lanes (the others hold no reference), in a fixed order; every lane has the result.
+template <int LANES> __device__ __forceinline__ RefSum join_lanes(RefSum r, float c)
 {
-    uint32_t at = (uint32_t)__cvta_generic_to_shared(p);
-    float v;
-    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(at), "r"(rank) : "memory");
-    return v;
+    float top = r.m;
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    float s = r.s * exp2_fast((r.m - top) * c);
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    return RefSum{top, s};
 }
 
-// The sum of 2^(y - m) over some y, m the largest of them (0 where that is -inf).
-struct PowerSum {
-    float m, s;                        // m may be -inf: nothing yet
-    __device__ __forceinline__ void add(float y)
+// A vector of 16 bytes as pairs.
+template <typename X> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int n = 4;
+    static __device__ __forceinline__ void open(const uint4 &u, float2 (&v)[2])
     {
-        if (y > m) {
-            s = s * exp2_fast(m - y) + 1.f;                            // (m = -inf, s = 0: 0 + 1)
-            m = y;
-        } else {
-            s += y == m ? (m == -INFINITY ? 0.f : 1.f) : exp2_fast(y - m);     // (a NaN reaches s)
-        }
-    }
-    __device__ __forceinline__ void join(float om, float os)
-    {
-        const float top = fmaxf(m, om), ref = top == -INFINITY ? 0.f : top;
-        s = s * (m == ref ? 1.f : exp2_fast(m - ref)) + os * (om == ref ? 1.f : exp2_fast(om - ref));       // (infinities alike)
-        m = top;
+        v[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+        v[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
     }
 };
-__device__ __forceinline__ float log2_of(const PowerSum &p) { return p.m == -INFINITY && p.s == 0.f ? -INFINITY : p.m + log2f(p.s); }
+template <typename X> struct Vec16 {
+    static constexpr int n = 8;
+    static __device__ __forceinline__ void open(const uint4 &u, float2 (&v)[4])
+    {
+        v[0] = HalfTraits<X>::unpack2(u.x);
+        v[1] = HalfTraits<X>::unpack2(u.y);
+        v[2] = HalfTraits<X>::unpack2(u.z);
+        v[3] = HalfTraits<X>::unpack2(u.w);
+    }
+};
+template <> struct Vec<__half> : Vec16<__half> {};
+template <> struct Vec<__nv_bfloat16> : Vec16<__nv_bfloat16> {};
+
+// Where the 16-byte vectors of a row lie: `a` elements in front of the first, `n` vectors, of which a block has [v0, v1).
+struct Slice {
+    int a, n, v0, v1, tail;            // tail: first element behind the vectors
+    template <typename X> __device__ __forceinline__ Slice(const X *row, int vocab, int blocks, int rank, X)
+    {
+        const int per = Vec<X>::n;
+        a = min(vocab, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(X));
+        n = (vocab - a) / per;
+        tail = a + n * per;
+        const int each = (n + blocks - 1) / blocks;
+        v0 = min(n, rank * each);
+        v1 = min(n, v0 + each);
+    }
+};
+
+// Stores the gradients of one vector's elements.
+template <typename G, int N> __device__ __forceinline__ void store_vec(G *p, bool wide, const float2 (&v)[N / 2])
+{
+    if (wide) {
+        if (sizeof(G) == 4) {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) reinterpret_cast<float4 *>(p)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
+        } else if (N == 8) {
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = round_pair<typename std::conditional<sizeof(G) == 2, G, __half>::type>(v[i % (N / 2)].x, v[i % (N / 2)].y);
+            *reinterpret_cast<uint4 *>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+        } else {
+            uint32_t u[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) u[i] = round_pair<typename std::conditional<sizeof(G) == 2, G, __half>::type>(v[i].x, v[i].y);
+            *reinterpret_cast<uint2 *>(p) = make_uint2(u[0], u[1]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        p[2 * i] = Elem<G>::from_f(v[i].x);
+        p[2 * i + 1] = Elem<G>::from_f(v[i].y);
+    }
+}
+
+// How many clusters of a launch fit the device side by side (decoder.cu: asked once for each shape of launch).
+cudaError_t clusters_at_once(const void *kernel, const cudaLaunchConfig_t &cfg, int *out);
 
 }  // namespace fpsk

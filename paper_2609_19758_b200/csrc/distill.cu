@@ -10,9 +10,6 @@
 // through the cluster's shared memory, and write the gradient, freeing the pieces as they go for the next row's copies; one warp prepares the
 // teacher's probabilities for the next row and takes them off the gradient of the one before, so that neither is waited for.
 #include "decoder.cuh"
-#include "stream_pipe.cuh"
-
-#include <mutex>
 
 namespace fpsk {
 
@@ -38,49 +35,7 @@ constexpr int kWorkers = 128, kMostTeachers = 3;   // threads of the sums and gr
 constexpr int kDistillThreads = kWorkers + 32 + 32 * kMostTeachers;
 constexpr int kPiece = 8192, kPieceVecs = kPiece / 16, kStages = 5;
 constexpr int kTogether = 4;            // listed tokens of a lane at a time
-constexpr float kNoReference = -3.4e38f;
 
-__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("barrier.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
-// 2^((x - M) c) summed
-struct RefSum {
-    float m, s;
-};
-// Joined over a warp's first LANES lanes (the others hold no reference), in a fixed order; every lane has the result.
-template <int LANES> __device__ __forceinline__ RefSum join_lanes(RefSum r, float c)
-{
-    float top = r.m;
-#pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    float s = r.s * exp2_fast((r.m - top) * c);
-#pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    return RefSum{top, s};
-}
-
-// A vector of 16 bytes as pairs.
-template <typename X> struct Vec;
-template <> struct Vec<float> {
-    static constexpr int n = 4;
-    static __device__ __forceinline__ void open(const uint4 &u, float2 (&v)[2])
-    {
-        v[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
-        v[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
-    }
-};
-template <typename X> struct Vec16 {
-    static constexpr int n = 8;
-    static __device__ __forceinline__ void open(const uint4 &u, float2 (&v)[4])
-    {
-        v[0] = HalfTraits<X>::unpack2(u.x);
-        v[1] = HalfTraits<X>::unpack2(u.y);
-        v[2] = HalfTraits<X>::unpack2(u.z);
-        v[3] = HalfTraits<X>::unpack2(u.w);
-    }
-};
-template <> struct Vec<__half> : Vec16<__half> {};
-template <> struct Vec<__nv_bfloat16> : Vec16<__nv_bfloat16> {};
 
 template <typename X> __device__ __forceinline__ float vec_max(const uint4 &u)
 {
@@ -110,48 +65,6 @@ template <typename X> __device__ __forceinline__ void gradients(const uint4 &u, 
     for (int j = 0; j < Vec<X>::n / 2; ++j) {
         const float2 y = __fmul2_rn(__fadd2_rn(e[j], minus), cc);
         e[j] = __fmul2_rn(make_float2(exp2_fast(y.x), exp2_fast(y.y)), ff);
-    }
-}
-
-// Where the 16-byte vectors of a row lie: `a` elements in front of the first, `n` vectors, of which a block has [v0, v1).
-struct Slice {
-    int a, n, v0, v1, tail;            // tail: first element behind the vectors
-    template <typename X> __device__ __forceinline__ Slice(const X *row, int vocab, int blocks, int rank, X)
-    {
-        const int per = Vec<X>::n;
-        a = min(vocab, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(X));
-        n = (vocab - a) / per;
-        tail = a + n * per;
-        const int each = (n + blocks - 1) / blocks;
-        v0 = min(n, rank * each);
-        v1 = min(n, v0 + each);
-    }
-};
-
-// Stores the gradients of one vector's elements.
-template <typename G, int N> __device__ __forceinline__ void store_vec(G *p, bool wide, const float2 (&v)[N / 2])
-{
-    if (wide) {
-        if (sizeof(G) == 4) {
-#pragma unroll
-            for (int i = 0; i < N / 4; ++i) reinterpret_cast<float4 *>(p)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
-        } else if (N == 8) {
-            uint32_t u[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = round_pair<typename std::conditional<sizeof(G) == 2, G, __half>::type>(v[i % (N / 2)].x, v[i % (N / 2)].y);
-            *reinterpret_cast<uint4 *>(p) = make_uint4(u[0], u[1], u[2], u[3]);
-        } else {
-            uint32_t u[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) u[i] = round_pair<typename std::conditional<sizeof(G) == 2, G, __half>::type>(v[i].x, v[i].y);
-            *reinterpret_cast<uint2 *>(p) = make_uint2(u[0], u[1]);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        p[2 * i] = Elem<G>::from_f(v[i].x);
-        p[2 * i + 1] = Elem<G>::from_f(v[i].y);
     }
 }
 
@@ -604,38 +517,6 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
     cluster_sync();                                                    // no block leaves before what the others send it
 }
 
-// Clusters of a launch that fit the device side by side, asked once for each shape of launch.
-static int clusters_at_once(const void *kernel, const cudaLaunchConfig_t &cfg, int *out)
-{
-    struct Key {
-        const void *kernel;
-        int device, blocks, threads;
-        size_t bytes;
-    };
-    static std::mutex lock;
-    static Key keys[64];
-    static int values[64], used = 0;
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    const int blocks = (int)cfg.attrs[0].val.clusterDim.x;
-    std::lock_guard<std::mutex> hold(lock);
-    for (int i = 0; i < (used < 64 ? used : 64); ++i)
-        if (keys[i].kernel == kernel && keys[i].device == device && keys[i].blocks == blocks && keys[i].threads == (int)cfg.blockDim.x && keys[i].bytes == cfg.dynamicSmemBytes) {
-            *out = values[i];
-            return cudaSuccess;
-        }
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 2048);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(out, kernel, &cfg);
-    if (e != cudaSuccess) return e;
-    if (*out < 1) *out = 1;
-    keys[used % 64] = Key{kernel, device, blocks, (int)cfg.blockDim.x, cfg.dynamicSmemBytes};
-    values[used % 64] = *out;
-    ++used;
-    return cudaSuccess;
-}
-
 constexpr long long kRowsInL2 = 40LL << 20, kLongRowsInL2 = 60LL << 20;
 
 template <typename X, typename G, int MODE> static fpsk_status launch_distill(DistillArgs g, cudaStream_t st)
@@ -668,7 +549,7 @@ template <typename X, typename G, int MODE> static fpsk_status launch_distill(Di
     cfg.numAttrs = 1;
     auto kernel = distill_kernel<X, G, MODE>;
     int most = 1;
-    FPSK_CUDA_OK((cudaError_t)clusters_at_once(reinterpret_cast<const void *>(kernel), cfg, &most));
+    FPSK_CUDA_OK(clusters_at_once(reinterpret_cast<const void *>(kernel), cfg, &most));
     // (rows too long for that even with the most blocks each: fewer at a time)
     if (MODE == kLossAndGrad && g.blocks == kRowMostBlocks && most > kLongRowsInL2 / row_bytes) most = (int)(kLongRowsInL2 / row_bytes);
     if (most < 1) most = 1;

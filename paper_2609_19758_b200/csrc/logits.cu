@@ -2,8 +2,14 @@
 //
 // For a token v of a row: z = l_v; seen: z > 0 ? z / rep : z rep; z -= freq c + pres where c > 0; z += biases; masked: -inf.
 //
-// A cluster of blocks takes a row, each a slice of the vocabulary.  Which of a chunk's tokens the history and the biases touch is
-// gathered in shared memory first.
+// What bounds it is memory, the logits once and the result once; for a row or two it is the chain of steps.  A cluster of blocks takes
+// a row, each a slice of the vocabulary.  One warp of a block copies pieces of 8 KB into a ring, passing over those that a mask forbids
+// as a whole; four warps first count in shared memory, a word to a token, which tokens the history touches, adjust those, 32 at a
+// time, and note in a map of bits which tokens are left to the stream; then they go through the pieces, with one look for a larger logit and one
+// vote for 16 or 32 tokens of a thread.  An in-place call without token or lse copies nothing: only what changes is read or written.
+//
+// (Touched tokens adjusted where the stream meets them took 75 us for 96 rows of 131072 with histories of 4096: some lane of a warp
+// meets one in almost every vector, and all wait for its division.)
 #include "decoder.cuh"
 
 namespace fpsk {
@@ -12,7 +18,7 @@ struct LogitsArgs {
     const void *x;
     void *out;
     long long xs, os, rows;
-    int vocab, out_type;
+    int vocab;
     const int *history, *history_len, *prompt_len;
     long long history_stride;
     int history_width;
@@ -24,162 +30,563 @@ struct LogitsArgs {
     long long mask_stride, n_masks;
     int *token;
     float *lse;
-    int blocks;                        // of a row
-    int slice;                         // tokens of a block, a multiple of the chunk
+    int blocks, log_blocks;            // of a row
+    int chunk;                         // vectors whose tokens have words at a time, a multiple of a piece
+    int in_place;                      // and neither token nor lse wanted: what stays as it is is left alone
+    int words_at;                      // in shared memory, behind the ring
     int32_t *status;
 };
 
-constexpr int kChunk = 4096;
-constexpr unsigned int kInPrompt = 0x80000000u;
+// Threads that work: the history's counting is bound by its latency.
+template <bool WORDS> struct Workers {
+    static constexpr int n = WORDS ? 256 : 128, threads = n + 32, stages = WORDS ? 3 : 4;       // (three blocks to an SM, five)
+};
+constexpr int kRowPiece = 8192, kRowPieceVecs = kRowPiece / 16;
+constexpr int kWordBytes = 32 * 1024;  // of the words of a chunk, at most
+constexpr int kMostChunk = 32768;      // tokens of a chunk without words, at most
 
-// the order of argmax: a NaN above all, -0 like 0, the lowest token of equal ones
+// What a block has of a row: `a` elements in front of the first 16-byte vector, `n` vectors, of whose pieces every blocks-th is the
+// block's (what is frequent has low numbers in many vocabularies: a slice of its own would be most of the work).  Its own vectors
+// and their tokens are numbered from 0, `mine` of them.
+template <typename X> struct Share {
+    static constexpr int N = Vec<X>::n, kTokens = kRowPieceVecs * N;
+    int a, n, tail, mine, rank, log;   // tail: first element behind the vectors; log: of the blocks' number
+    __device__ __forceinline__ Share(const X *row, int vocab, int log_blocks, int rank_) : rank(rank_), log(log_blocks)
+    {
+        a = min(vocab, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(X));
+        n = (vocab - a) / N;
+        tail = a + n * N;
+        const int pieces = (n + kRowPieceVecs - 1) / kRowPieceVecs, own = (pieces - rank + (1 << log) - 1) >> log;
+        mine = own <= 0 ? 0 : (own - 1) * kRowPieceVecs + min(kRowPieceVecs, n - (((own - 1) << log) + rank) * kRowPieceVecs);
+    }
+    // the vector of the row, the token, behind a number of the block's own
+    __device__ __forceinline__ int vec(int own) const { return ((own / kRowPieceVecs) << log | rank) * kRowPieceVecs + own % kRowPieceVecs; }
+    __device__ __forceinline__ int token(int own) const { return a + ((own / kTokens) << log | rank) * kTokens + own % kTokens; }
+    // its own number of a token, or -1
+    __device__ __forceinline__ int own_of(int v) const
+    {
+        const unsigned int t = (unsigned int)(v - a), piece = t / kTokens;
+        if (t >= (unsigned int)(n * N) || (int)(piece & ((1u << log) - 1u)) != rank) return -1;
+        return (int)((piece >> log) * kTokens + t % kTokens);
+    }
+};
+
+// A token's word: how often it comes behind the prompt, and from the top whether it is in the prompt, has a bias, has several.  16 bits
+// where the history is short enough.
+template <typename W> struct Word {
+    static constexpr unsigned int kInPrompt = 1u << (8 * sizeof(W) - 1), kBiased = kInPrompt >> 1, kBiasedTwice = kInPrompt >> 2, kTimes = kBiasedTwice - 1;
+    static __device__ __forceinline__ int shift(int at) { return sizeof(W) == 2 ? 16 * (at & 1) : 0; }
+    static __device__ __forceinline__ unsigned int *home(W *words, int at) { return reinterpret_cast<unsigned int *>(words) + (sizeof(W) == 2 ? at >> 1 : at); }
+    static __device__ __forceinline__ void count(W *words, int at) { atomicAdd(home(words, at), 1u << shift(at)); }
+    static __device__ __forceinline__ unsigned int mark(W *words, int at, unsigned int bits) { return atomicOr(home(words, at), bits << shift(at)) >> shift(at); }
+    // which of N tokens have a word that is not 0; `at` is a multiple of N
+    template <int N> static __device__ __forceinline__ unsigned int some(const W *words, int at)
+    {
+        unsigned int w[N * sizeof(W) / 4], any = 0, which = 0;
+        if (sizeof(W) * N == 8) {
+            const uint2 u = *reinterpret_cast<const uint2 *>(words + at);
+            w[0] = u.x; w[1] = u.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)(N * sizeof(W) / 16); ++i) {
+                const uint4 u = reinterpret_cast<const uint4 *>(words + at)[i];
+                w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < (int)(N * sizeof(W) / 4); ++i) any |= w[i];
+        if (any) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (sizeof(W) == 2 ? w[j / 2] >> 16 * (j & 1) & 0xFFFFu : w[j % (N * sizeof(W) / 4)]) which |= 1u << j;
+        }
+        return which;
+    }
+};
+
+// the order of argmax: a NaN above all, the lowest token of equal ones
 __device__ __forceinline__ unsigned long long pick_key(float z, int v)
 {
-    const unsigned int b = __float_as_uint(z + 0.f);
+    const unsigned int b = __float_as_uint(z + 0.f);                   // (-0 is 0)
     const unsigned int k = z != z ? 0xFFFFFFFFu : b & 0x80000000u ? ~b : b | 0x80000000u;
     return (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned int)v);
 }
-constexpr unsigned int kKeyNothing = 0x007FFFFFu;                      // of -inf
-
-__device__ __forceinline__ void store_elem(void *p, int type, long long at, float v)
+constexpr unsigned int kKeyNothing = 0x007FFFFFu, kKeyInfinity = 0xFF800000u, kKeyNan = 0xFFFFFFFFu;
+__device__ __forceinline__ float max_nan(float a, float b)
 {
-    if (type == FPSK_ELEM_FP32) static_cast<float *>(p)[at] = v;
-    else if (type == FPSK_ELEM_FP16) static_cast<__half *>(p)[at] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16 *>(p)[at] = __float2bfloat16_rn(v);
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
 }
 
-template <typename X> __global__ void __launch_bounds__(kRowThreads) adjust_logits_kernel(const __grid_constant__ LogitsArgs g)
+// A warp's largest so far and its token, the same in all lanes, and each lane's sum of powers with a reference that follows the largest
+// at a distance.
+struct Picked {
+    float best, m, s;
+    int at;
+    __device__ __forceinline__ void follow()
+    {
+        if ((best - m) * kLog2e > 60.f) {
+            s *= exp2_fast((m - best) * kLog2e);
+            m = best;
+        }
+    }
+    // K vectors of N values of each lane; the first values of a lane's vectors are the tokens v, v + step, ..  Tokens rise from lane to
+    // lane, vector to vector and call to call.
+    template <int K, int N> __device__ __forceinline__ void add(const float2 (&z)[K][N / 2], int v, int step, bool sum)
+    {
+        float tops[K], top;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            tops[k] = max_nan(z[k][0].x, z[k][0].y);
+#pragma unroll
+            for (int i = 1; i < N / 2; ++i) tops[k] = max_nan(tops[k], max_nan(z[k][i].x, z[k][i].y));
+        }
+        top = tops[0];
+#pragma unroll
+        for (int k = 1; k < K; ++k) top = max_nan(top, tops[k]);
+        if (__any_sync(0xFFFFFFFFu, !(top <= best))) {
+            float most = top;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) most = max_nan(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+            const bool nan = most != most;
+            if (nan ? best == best : most > best) {
+                bool found = false;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const unsigned int who = __ballot_sync(0xFFFFFFFFu, nan ? tops[k] != tops[k] : tops[k] == most);
+                    if (who && !found) {
+                        found = true;
+                        int first = 0;                                 // the place of the lane's first such value
+#pragma unroll
+                        for (int i = N - 1; i >= 0; --i) {
+                            const float x = i & 1 ? z[k][i / 2].y : z[k][i / 2].x;
+                            if (nan ? x != x : x == most) first = i;
+                        }
+                        at = __shfl_sync(0xFFFFFFFFu, v + k * step + first, __ffs(who) - 1);
+                    }
+                }
+                best = most;
+                follow();
+            }
+        }
+        if (sum) {
+            const float2 minus = make_float2(-m, -m), c = make_float2(kLog2e, kLog2e);
+            float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    const float2 y = __fmul2_rn(__fadd2_rn(z[k][i], minus), c);
+                    t = __fadd2_rn(t, make_float2(exp2_fast(y.x), exp2_fast(y.y)));
+                }
+            s += t.x + t.y;
+        }
+    }
+};
+
+// The same of a lane's single tokens, in any order.
+struct Single {
+    float best, m, s;
+    int at;
+    __device__ __forceinline__ void add(float z, int v, bool sum)
+    {
+        if (z != z ? best == best : z > best) {
+            best = z;
+            at = v;
+            if ((best - m) * kLog2e > 60.f) {
+                s *= exp2_fast((m - best) * kLog2e);
+                m = best;
+            }
+        } else if (v < at && (z == best || z != z)) {
+            at = v;
+        }
+        if (sum) s += exp2_fast((z - m) * kLog2e);
+    }
+};
+
+// the bits of N tokens from `e` on
+template <int N> __device__ __forceinline__ unsigned int mask_bits(const int *mask, int e)
 {
-    __shared__ unsigned int said[kChunk];                              // times behind the prompt, and whether in it
-    __shared__ float bias[kChunk];
-    __shared__ unsigned long long keys[kRowWarps];
-    __shared__ float tops[kRowWarps], sums[kRowWarps];
-    __shared__ float mine[4];                                          // key (two halves), largest, sum: read by the first block
+    const int w = e >> 5, s = e & 31;
+    unsigned int b = (unsigned int)mask[w] >> s;
+    if (s + N > 32) b |= (unsigned int)mask[w + 1] << (32 - s);
+    return b & ((1u << N) - 1u);
+}
+// O: the type of the result, or void.  W: of the words, void where there are neither histories nor biases.
+template <typename X, typename O, typename W> __global__ void __launch_bounds__(Workers<!std::is_void<W>::value>::threads, std::is_void<W>::value ? 5 : 3) adjust_logits_kernel(const __grid_constant__ LogitsArgs g)
+{
+    constexpr int N = Vec<X>::n, kRowWorkers = Workers<!std::is_void<W>::value>::n, kRowWarps = kRowWorkers / 32, kEachVecs = kRowPieceVecs / kRowWorkers;
+    constexpr int kRowStages = Workers<!std::is_void<W>::value>::stages;
+    constexpr bool OUT = !std::is_void<O>::value, WORDS = !std::is_void<W>::value;
+    constexpr unsigned int kAll = (1u << N) - 1u;
+    using Out = typename std::conditional<OUT, O, float>::type;
+    using Wd = typename std::conditional<WORDS, W, unsigned int>::type;
+    using F = Word<Wd>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ unsigned long long full[kRowStages], empty[kRowStages], met[2];
+    __shared__ unsigned long long keys[2][kRowWarps];
+    __shared__ float2 sums[2][kRowWarps];
+    __shared__ float4 blocks_sum[2][kRowMostBlocks];                   // written by the cluster's blocks: key (two halves), reference, sum
+    // vectors with tokens that the history touches, of each warp until there is one for each lane
+    __shared__ uint4 raw[WORDS ? kRowWarps : 1][WORDS ? 64 : 1];
+    __shared__ int touched[WORDS ? kRowWarps : 1][WORDS ? 64 : 1];
+    Wd *words = reinterpret_cast<Wd *>(smem + g.words_at);             // of a chunk's tokens, of 8 in front of the row's vectors, 8 behind
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned int rank = cluster_rank();
-    const int lo = (int)min((long long)g.vocab, (long long)rank * g.slice), hi = (int)min((long long)g.vocab, (long long)lo + g.slice);
-    for (long long row = blockIdx.x / g.blocks; row < g.rows; row += gridDim.x / g.blocks) {
-        const X *x = static_cast<const X *>(g.x) + row * g.xs;
-        const int *history = g.history ? g.history + row * g.history_stride : nullptr;
-        int n_hist = history ? g.history_width : 0;
-        if (history && g.history_len) n_hist = max(0, min(n_hist, g.history_len[row]));
-        const int n_prompt = history && g.prompt_len ? g.prompt_len[row] : 0;
-        const float rep = g.rep ? g.rep[row] : 1.f, freq = g.freq ? g.freq[row] : 0.f, pres = g.pres ? g.pres[row] : 0.f;
-        long long b0 = 0, b1 = 0;
-        if (g.bias_ptr) {
-            b0 = max(0LL, (long long)g.bias_ptr[row]);
-            b1 = min(g.n_biases, (long long)g.bias_ptr[row + 1]);
+    const int rank = (int)cluster_rank();
+    const bool pick = g.token || g.lse, sum = g.lse != nullptr;
+    const long long first_row = blockIdx.x / g.blocks, row_step = gridDim.x / g.blocks;
+    if (tid == 0) {
+        for (int s = 0; s < kRowStages; ++s) {
+            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&empty[s]), kRowWarps);
         }
-        const int *mask = nullptr;
-        bool nothing = false;
-        if (g.mask) {
-            const long long m = g.mask_row ? (long long)g.mask_row[row] : row;
-            if (m >= g.n_masks) {
-                nothing = true;
-                if (tid == 0) report_status(g.status, FPSK_ERR_PARAM);
-            } else if (m >= 0) {
-                mask = g.mask + m * g.mask_stride;
-            }
+        mbar_init(smem_u32(&met[0]), 1);
+        mbar_init(smem_u32(&met[1]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    cluster_sync();
+    // Every wait is bounded; once one has given up the others are passed over, and all roles still run to their ends.
+    bool ok = true;
+    auto wait = [&](unsigned long long &bar, uint32_t parity) {
+        if (ok && !mbar_wait_bounded(smem_u32(&bar), parity)) {
+            ok = false;
+            report_status(g.status, FPSK_ERR_TIMEOUT);
         }
-        unsigned long long best = 0;
-        PowerSum p = {-INFINITY, 0.f};
-        for (int c0 = lo; c0 < hi; c0 += kChunk) {
-            const int n = min(kChunk, hi - c0);
-            __syncthreads();
-            for (int i = tid; i < kChunk; i += kRowThreads) {
-                said[i] = 0;
-                bias[i] = 0.f;
-            }
-            __syncthreads();
-            for (int i = tid; i < n_hist; i += kRowThreads) {
-                const unsigned int at = (unsigned int)history[i] - (unsigned int)c0;
-                if (at < (unsigned int)n) {
-                    if (i < n_prompt) atomicOr(&said[at], kInPrompt);
-                    else atomicAdd(&said[at], 1u);
+    };
+    // a row's mask (NULL: none), and whether the one that it asks for is missing
+    auto mask_of = [&](long long row, bool &missing) -> const int * {
+        missing = false;
+        if (!g.mask) return nullptr;
+        const long long m = g.mask_row ? (long long)g.mask_row[row] : row;
+        missing = m >= g.n_masks;
+        return m >= 0 && !missing ? g.mask + m * g.mask_stride : nullptr;
+    };
+
+    if (warp == kRowWarps) {
+        // ------------------------------------------------------------ copies
+        unsigned int k = 0;                                            // pieces so far
+        int stage = 0;
+        uint32_t phase = 0;
+        for (long long row = first_row; row < g.rows && !g.in_place; row += row_step) {
+            const X *x = static_cast<const X *>(g.x) + row * g.xs;
+            const Share<X> sl(x, g.vocab, g.log_blocks, rank);
+            bool missing;
+            const int *mask = mask_of(row, missing);
+            const char *from = reinterpret_cast<const char *>(x + sl.a);
+            for (int own = 0; own < sl.mine; own += kRowPieceVecs) {
+                const int vecs = min(kRowPieceVecs, sl.mine - own), v = sl.vec(own);
+                bool needed = !missing;
+                if (mask) {
+                    const int w0 = (sl.a + v * N) >> 5, w1 = (sl.a + (v + vecs) * N - 1) >> 5;
+                    unsigned int any = 0;
+                    for (int w = w0 + lane; w <= w1; w += 32) any |= (unsigned int)mask[w];
+                    needed = __any_sync(0xFFFFFFFFu, any != 0);
+                }
+                if (lane == 0) {
+                    wait(empty[stage], phase ^ 1u);
+                    const uint32_t bar = smem_u32(&full[stage]);
+                    if (ok && needed) {
+                        mbar_expect_tx(bar, 16u * (uint32_t)vecs);
+                        bulk_g2s(smem_u32(smem) + stage * kRowPiece, from + 16LL * v, 16u * (uint32_t)vecs, bar);
+                    } else {
+                        mbar_arrive(bar);
+                    }
+                }
+                ++k;
+                if (++stage == kRowStages) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
-            if (warp == 0 && b0 < b1) {
-                // in the list's order, whatever comes twice
-                for (long long i0 = b0; i0 < b1; i0 += 32) {
-                    const long long i = i0 + lane;
-                    const unsigned int at = i < b1 ? (unsigned int)g.bias_token[i] - (unsigned int)c0 : 0xFFFFFFFFu;
-                    const bool in = at < (unsigned int)n;
-                    const float value = in ? g.bias_value[i] : 0.f;
-                    const unsigned int same = __match_any_sync(0xFFFFFFFFu, in ? (int)at : -1 - lane);
-                    if (__any_sync(0xFFFFFFFFu, __popc(same) > 1)) {
-                        for (int l = 0; l < 32; ++l) {
-                            if (l == lane && in) bias[at] += value;
-                            __syncwarp();
+        }
+        // no copy is left in flight
+        if (lane == 0)
+            for (unsigned int back = min(k, (unsigned int)kRowStages); back; --back) {
+                const unsigned int piece = k - back;
+                mbar_wait_bounded(smem_u32(&full[piece % kRowStages]), piece / kRowStages & 1u);
+            }
+    } else {
+        unsigned int n_rows = 0;
+        int stage = 0;
+        uint32_t phase = 0;
+        const int chunk_tokens = g.chunk * N;
+        for (long long row = first_row; row < g.rows; row += row_step, ++n_rows) {
+            const X *x = static_cast<const X *>(g.x) + row * g.xs;
+            Out *out = OUT ? static_cast<Out *>(g.out) + row * g.os : nullptr;
+            const Share<X> sl(x, g.vocab, g.log_blocks, rank);
+            const bool wide = OUT && reinterpret_cast<uintptr_t>(out + sl.a) % (N * sizeof(Out) < 16 ? N * sizeof(Out) : 16) == 0;
+            const int buf = n_rows & 1;
+
+            // the row's parameters, asked for together; the history's first tokens before their number is known
+            const int *history = WORDS && g.history ? g.history + row * g.history_stride : nullptr;
+            constexpr int kEarly = 8;
+            int early[kEarly];
+            auto first_of_history = [&] {
+#pragma unroll
+                for (int i = 0; i < kEarly; ++i) early[i] = history && tid + i * kRowWorkers < g.history_width ? history[tid + i * kRowWorkers] : -1;
+            };
+            first_of_history();
+            int n_hist = history ? g.history_width : 0, n_prompt = 0;
+            if (history && g.history_len) n_hist = max(0, min(n_hist, g.history_len[row]));
+            if (history && g.prompt_len) n_prompt = g.prompt_len[row];
+            const float rep = WORDS && g.rep ? g.rep[row] : 1.f, freq = WORDS && g.freq ? g.freq[row] : 0.f, pres = WORDS && g.pres ? g.pres[row] : 0.f;
+            long long b0 = 0, b1 = 0;
+            if (WORDS && g.bias_ptr) {
+                b0 = max(0LL, (long long)g.bias_ptr[row]);
+                b1 = min(g.n_biases, (long long)g.bias_ptr[row + 1]);
+            }
+            bool nothing;
+            const int *mask = mask_of(row, nothing);
+            if (nothing && tid == 0) report_status(g.status, FPSK_ERR_PARAM);
+            const bool masks = mask || nothing;
+            auto allowed = [&](int e) { return nothing ? 0u : mask ? mask_bits<N>(mask, e) : kAll; };
+            // z of a token, all but its biases and the mask; c: its word
+            auto adjusted = [&](float z, unsigned int c) {
+                if (c & (F::kInPrompt | F::kTimes)) z = z > 0.f ? __fdiv_rn(z, rep) : __fmul_rn(z, rep);
+                if (c & F::kTimes) z = __fsub_rn(z, __fadd_rn(__fmul_rn((float)(c & F::kTimes), freq), pres));
+                return z;
+            };
+
+            Picked p = {-INFINITY, kNoReference, 0.f, -1};
+            Single own = {-INFINITY, kNoReference, 0.f, -1};
+            auto single = [&](int v, float z) {
+                if (masks && (nothing || !(mask[v >> 5] >> (v & 31) & 1))) z = -INFINITY;
+                if (OUT) out[v] = Elem<Out>::from_f(z);
+                if (pick) own.add(z, v, sum);
+            };
+            for (int c0 = 0; c0 < sl.mine || c0 == 0; c0 += g.chunk) {
+                const int c1 = min(sl.mine, c0 + g.chunk);             // the chunk's vectors
+                // The elements in front of the row's first vector and behind its last go with the first chunk of the first and the last block.
+                const bool front = c0 == 0 && rank == 0, back = c0 == 0 && rank == g.blocks - 1;
+                int loose = -1;
+                if (warp == 0 && front && lane < sl.a) loose = lane;
+                if (warp == 0 && back && lane >= 16 && sl.tail + lane - 16 < g.vocab) loose = sl.tail + lane - 16;
+                // a token's word of this chunk, or -1
+                const bool edges = sl.a > 0 || sl.tail < g.vocab;
+                auto slot = [&](int v) {
+                    const int own = sl.own_of(v);
+                    if (own >= c0 * N && own < c1 * N) return own - c0 * N;
+                    if (!edges) return -1;
+                    if (front && v >= 0 && v < sl.a) return chunk_tokens + v;
+                    if (back && v >= sl.tail && v < g.vocab) return chunk_tokens + 8 + v - sl.tail;
+                    return -1;
+                };
+                if (WORDS) {
+                    bar_sync(1, kRowWorkers);                          // the chunk in front is done with
+                    if (c0) first_of_history();
+                    for (int i = tid; i < (chunk_tokens + 16) * (int)sizeof(Wd) / 16; i += kRowWorkers) reinterpret_cast<uint4 *>(words)[i] = make_uint4(0u, 0u, 0u, 0u);
+                    bar_sync(1, kRowWorkers);
+                    auto count = [&](int i, int v) {
+                        const int at = slot(v);
+                        if (at < 0) return;
+                        if (i < n_prompt) F::mark(words, at, F::kInPrompt);
+                        else F::count(words, at);
+                    };
+                    for (int i0 = tid; i0 < n_hist; i0 += kEarly * kRowWorkers) {
+                        int now[kEarly];
+#pragma unroll
+                        for (int i = 0; i < kEarly; ++i) {             // the next ones set out before these are counted
+                            const int next = i0 + (kEarly + i) * kRowWorkers;
+                            now[i] = early[i];
+                            early[i] = next < n_hist ? history[next] : -1;
                         }
-                    } else if (in) {
-                        bias[at] += value;
+#pragma unroll
+                        for (int i = 0; i < kEarly; ++i)
+                            if (i0 + i * kRowWorkers < n_hist && now[i] >= 0) count(i0 + i * kRowWorkers, now[i]);
+                    }
+                    for (long long i = b0 + tid; i < b1; i += kRowWorkers) {
+                        const int at = slot(g.bias_token[i]);
+                        if (at >= 0 && F::mark(words, at, F::kBiased) & F::kBiased) F::mark(words, at, F::kBiasedTwice);
+                    }
+                    bar_sync(1, kRowWorkers);
+                }
+                // Touched vectors wait, as they are, until there is one for each lane.
+                int n_touched = 0;
+                auto adjust = [&](int n) {
+                    __syncwarp();
+                    n_touched -= n;
+                    const int own_vec = lane < n ? touched[warp][n_touched + lane] : c0, e = sl.token(own_vec * N);
+                    const Wd *w = words + (own_vec - c0) * N;
+                    const X *l = reinterpret_cast<const X *>(&raw[warp][n_touched + (lane < n ? lane : 0)]);
+                    unsigned int rest = lane < n ? F::template some<N>(words, (own_vec - c0) * N) : 0u;
+                    while (rest) {                                     // (as often as the most touched of the vectors asks)
+                        const int j = __ffs(rest) - 1;
+                        rest &= rest - 1;
+                        const unsigned int c = w[j];
+                        if (!(c & F::kBiased)) single(e + j, adjusted(Elem<X>::to_f(l[j]), c));
                     }
                     __syncwarp();
-                }
-            }
-            __syncthreads();
-            for (int i = tid; i < n; i += kRowThreads) {
-                const int v = c0 + i;
-                float z = Elem<X>::to_f(x[v]);
-                const unsigned int c = said[i];
-                if (c) z = z > 0.f ? __fdiv_rn(z, rep) : __fmul_rn(z, rep);
-                if (c & ~kInPrompt) z = __fsub_rn(z, __fadd_rn(__fmul_rn((float)(c & ~kInPrompt), freq), pres));
-                if (b0 < b1) z += bias[i];
-                if (nothing || (mask && !(mask[v >> 5] >> (v & 31) & 1))) z = -INFINITY;
-                if (g.out) store_elem(g.out, g.out_type, row * g.os + v, z);
-                if (g.token || g.lse) {
-                    best = max(best, pick_key(z, v));
-                    p.add(z * kLog2e);
-                }
-            }
-        }
-        if (!g.token && !g.lse) continue;
+                };
+                // (all lanes) a vector that has touched tokens
+                auto put_off = [&](bool some, int own_vec, const uint4 &u) {
+                    const unsigned int who = __ballot_sync(0xFFFFFFFFu, some);
+                    if (some) {
+                        const int at = n_touched + __popc(who & ((1u << lane) - 1u));
+                        touched[warp][at] = own_vec;
+                        raw[warp][at] = u;
+                    }
+                    n_touched += __popc(who);
+                    if (n_touched >= 32) adjust(32);
+                };
+                if (g.in_place) {
+                    for (int v0 = c0; v0 < c1; v0 += kRowWorkers) {
+                        const int v = v0 + tid, e = sl.token(v0 * N) + tid * N;
+                        const bool here = v < c1;
+                        const unsigned int some = WORDS && here ? F::template some<N>(words, (v - c0) * N) : 0u;
+                        if (WORDS) put_off(some, v, some ? *reinterpret_cast<const uint4 *>(x + e) : make_uint4(0u, 0u, 0u, 0u));
+                        const unsigned int bits = here ? allowed(e) : kAll;
+                        if (OUT && bits != kAll) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            best = max(best, __shfl_xor_sync(0xFFFFFFFFu, best, o));
-            const float om = __shfl_xor_sync(0xFFFFFFFFu, p.m, o), os = __shfl_xor_sync(0xFFFFFFFFu, p.s, o);
-            p.join(om, os);
-        }
-        if (lane == 0) {
-            keys[warp] = best;
-            tops[warp] = p.m;
-            sums[warp] = p.s;
-        }
-        __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < kRowWarps; ++w) {
-                best = max(best, keys[w]);
-                p.join(tops[w], sums[w]);
+                            for (int j = 0; j < N; ++j)
+                                if (!((bits | some) >> j & 1u)) out[e + j] = Elem<Out>::from_f(-INFINITY);
+                        }
+                    }
+                } else {
+                    for (int v0 = c0; v0 < c1; v0 += kRowPieceVecs) {
+                        wait(full[stage], phase);
+                        const uint4 *piece = reinterpret_cast<const uint4 *>(smem + stage * kRowPiece) + tid;
+                        const int v = v0 + tid, e = sl.token(v0 * N) + tid * N;
+                        float2 z[kEachVecs][N / 2];
+                        if (v0 + kRowPieceVecs <= c1 && !WORDS && !masks) {
+#pragma unroll
+                            for (int k = 0; k < kEachVecs; ++k) {
+                                Vec<X>::open(piece[k * kRowWorkers], z[k]);
+                                if (OUT) store_vec<Out, N>(out + e + k * kRowWorkers * N, wide, z[k]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < kEachVecs; ++k) {
+                                const int vk = v + k * kRowWorkers, ek = e + k * kRowWorkers * N;
+                                const bool here = vk < c1;
+                                const unsigned int bits = !here ? 0u : masks ? allowed(ek) : kAll;
+                                const uint4 u = piece[k * kRowWorkers];
+                                const unsigned int some = WORDS && here ? F::template some<N>(words, (vk - c0) * N) : 0u;
+                                if (WORDS && __any_sync(0xFFFFFFFFu, some != 0)) put_off(some, vk, u);
+                                Vec<X>::open(u, z[k]);
+                                if (bits != kAll) {
+#pragma unroll
+                                    for (int j = 0; j < N; ++j)
+                                        if (!(bits >> j & 1u)) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
+                                }
+                                if (OUT && here) {
+                                    if (!some) {
+                                        store_vec<Out, N>(out + ek, wide, z[k]);
+                                    } else {
+#pragma unroll
+                                        for (int j = 0; j < N; ++j)
+                                            if (!(some >> j & 1u)) out[ek + j] = Elem<Out>::from_f(j & 1 ? z[k][j / 2].y : z[k][j / 2].x);
+                                    }
+                                }
+                                if (some && pick) {
+#pragma unroll
+                                    for (int j = 0; j < N; ++j)
+                                        if (some >> j & 1u) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
+                                }
+                            }
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
+                        if (++stage == kRowStages) {
+                            stage = 0;
+                            phase ^= 1u;
+                        }
+                        if (pick) p.add<kEachVecs, N>(z, e, kRowWorkers * N, sum);
+                    }
+                }
+                if (WORDS && n_touched) adjust(n_touched);
+                if (WORDS) {
+                    for (long long i = b0 + tid; i < b1; i += kRowWorkers) {
+                        const int v = g.bias_token[i], where = slot(v);
+                        if (where < 0) continue;
+                        float b = g.bias_value[i];
+                        if (words[where] & F::kBiasedTwice) {          // the first of its entries does it, in the list's order
+                            bool mine_to_do = true;
+                            b = 0.f;
+                            for (long long k = b0; k < b1; ++k)
+                                if (g.bias_token[k] == v) {
+                                    if (k < i) mine_to_do = false;
+                                    b += g.bias_value[k];
+                                }
+                            if (!mine_to_do) continue;
+                        }
+                        single(v, adjusted(Elem<X>::to_f(x[v]), words[where]) + b);
+                    }
+                }
+                if (loose >= 0) {
+                    const unsigned int c = WORDS ? words[slot(loose)] : 0u;
+                    if (!(c & F::kBiased)) single(loose, adjusted(Elem<X>::to_f(x[loose]), c));
+                }
             }
-            mine[0] = __uint_as_float((unsigned int)(best >> 32));
-            mine[1] = __uint_as_float((unsigned int)best);
-            mine[2] = p.m;
-            mine[3] = p.s;
-        }
-        cluster_sync();
-        if (rank == 0 && tid == 0) {
-            for (int b = 1; b < g.blocks; ++b) {
-                const unsigned long long k = (unsigned long long)__float_as_uint(cluster_load(&mine[0], b)) << 32 | __float_as_uint(cluster_load(&mine[1], b));
-                best = max(best, k);
-                p.join(cluster_load(&mine[2], b), cluster_load(&mine[3], b));
+            if (!pick) continue;
+            unsigned long long key = max(p.at < 0 ? 0ull : pick_key(p.best, p.at), own.at < 0 ? 0ull : pick_key(own.best, own.at));
+#pragma unroll
+            for (int o = 16; o; o >>= 1) key = max(key, __shfl_xor_sync(0xFFFFFFFFu, key, o));
+            const float top = fmaxf(p.m, own.m);
+            RefSum r = join_lanes<32>(RefSum{top, p.s * exp2_fast((p.m - top) * kLog2e) + own.s * exp2_fast((own.m - top) * kLog2e)}, kLog2e);
+            if (lane == 0) {
+                keys[buf][warp] = key;
+                sums[buf][warp] = make_float2(r.m, r.s);
             }
-            if (g.token) g.token[row] = (unsigned int)(best >> 32) <= kKeyNothing ? -1 : (int)(0xFFFFFFFFu - (unsigned int)best);
-            if (g.lse) g.lse[row] = log2_of(p) * kLn2;
+            bar_sync(1, kRowWorkers);
+            if (warp == 0) {
+                const float2 t = sums[buf][lane % kRowWarps];
+                r = join_lanes<kRowWarps>(RefSum{t.x, t.y}, kLog2e);
+                key = keys[buf][lane % kRowWarps];
+#pragma unroll
+                for (int o = kRowWarps / 2; o; o >>= 1) key = max(key, __shfl_xor_sync(0xFFFFFFFFu, key, o));
+                if (g.blocks > 1) {
+                    // (all hear of all, so that none is two rows ahead of another)
+                    if (lane == 0) mbar_expect_tx(smem_u32(&met[buf]), 16u * g.blocks);
+                    if (lane < g.blocks) {
+                        asm volatile(
+                            "{\n\t.reg .b32 a, m;\n\t"
+                            "mapa.shared::cluster.u32 a, %0, %2;\n\t"
+                            "mapa.shared::cluster.u32 m, %1, %2;\n\t"
+                            "st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %6}, [m];\n\t}"
+                            ::"r"(smem_u32(&blocks_sum[buf][rank])), "r"(smem_u32(&met[buf])), "r"(lane), "f"(__uint_as_float((unsigned int)(key >> 32))),
+                            "f"(__uint_as_float((unsigned int)key)), "f"(r.m), "f"(r.s)
+                            : "memory");
+                    }
+                    wait(met[buf], n_rows >> 1 & 1u);
+                    const float4 theirs = lane < g.blocks ? blocks_sum[buf][lane] : make_float4(0.f, 0.f, kNoReference, 0.f);
+                    key = (unsigned long long)__float_as_uint(theirs.x) << 32 | __float_as_uint(theirs.y);
+                    r = join_lanes<kRowMostBlocks>(RefSum{theirs.z, theirs.w}, kLog2e);
+#pragma unroll
+                    for (int o = kRowMostBlocks / 2; o; o >>= 1) key = max(key, __shfl_xor_sync(0xFFFFFFFFu, key, o));
+                }
+                if (rank == 0 && lane == 0) {
+                    const unsigned int k = (unsigned int)(key >> 32);
+                    if (g.token) g.token[row] = k <= kKeyNothing ? -1 : (int)(0xFFFFFFFFu - (unsigned int)key);
+                    if (g.lse) g.lse[row] = k == kKeyNan ? __uint_as_float(0x7FC00000u) : k == kKeyInfinity ? INFINITY : r.m + logf(r.s);
+                }
+            }
         }
-        cluster_sync();
     }
+    __syncthreads();
+    cluster_sync();                                                    // no block leaves before what the others send it
 }
 
-template <typename X> static fpsk_status launch_logits(LogitsArgs g, cudaStream_t st)
+template <typename X, typename O, typename W> static fpsk_status launch_logits(LogitsArgs g, cudaStream_t st)
 {
-    const int chunks = (g.vocab + kChunk - 1) / kChunk;
+    constexpr int N = Vec<X>::n;
+    constexpr bool WORDS = !std::is_void<W>::value;
+    using Wd = typename std::conditional<WORDS, W, char>::type;
+    const int chunk_tokens = WORDS ? kWordBytes / (int)sizeof(Wd) : kMostChunk;
+    // Blocks of a row: as many as make slices of one chunk, and more where there are too few rows for the SMs.
     g.blocks = 1;
-    while (g.blocks < kRowMostBlocks && 2 * g.blocks <= chunks && g.rows * g.blocks < 4 * kSms) g.blocks *= 2;
-    g.slice = (chunks + g.blocks - 1) / g.blocks * kChunk;
-    const long long most = 1 << 20;
+    while (g.blocks < kRowMostBlocks && ((WORDS && g.vocab > g.blocks * chunk_tokens) || (g.rows * g.blocks < 3 * kSms && g.vocab > g.blocks * 4096))) {
+        g.blocks *= 2;
+        ++g.log_blocks;
+    }
+    const int vecs = (g.vocab + N - 1) / N, pieces = ((vecs + kRowPieceVecs - 1) / kRowPieceVecs + g.blocks - 1) / g.blocks;
+    g.chunk = (pieces < chunk_tokens / N / kRowPieceVecs ? pieces : chunk_tokens / N / kRowPieceVecs) * kRowPieceVecs;
+    g.words_at = g.in_place ? 0 : Workers<WORDS>::stages * kRowPiece;
+    auto kernel = adjust_logits_kernel<X, O, W>;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((g.rows < most ? g.rows : most) * g.blocks));
-    cfg.blockDim = dim3(kRowThreads);
+    cfg.blockDim = dim3(Workers<WORDS>::threads);
+    cfg.dynamicSmemBytes = (size_t)g.words_at + (WORDS ? (g.chunk * N + 16) * sizeof(Wd) : 0);
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -187,9 +594,24 @@ template <typename X> static fpsk_status launch_logits(LogitsArgs g, cudaStream_
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, adjust_logits_kernel<X>, g));
+    cfg.gridDim = dim3((unsigned)g.blocks);
+    int most = 1;
+    FPSK_CUDA_OK(clusters_at_once(reinterpret_cast<const void *>(kernel), cfg, &most));
+    cfg.gridDim = dim3((unsigned)((g.rows < most ? g.rows : most) * g.blocks));
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, g));
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
+}
+template <typename X> static fpsk_status launch_logits_typed(const LogitsArgs &g, int out_type, cudaStream_t st)
+{
+    // (16 bits: three of them flags)
+    const bool words = g.history || g.bias_ptr, narrow = !g.history || g.history_width < (int)Word<uint16_t>::kBiasedTwice;
+#define FPSK_OUT(O) (!words ? launch_logits<X, O, void>(g, st) : narrow ? launch_logits<X, O, uint16_t>(g, st) : launch_logits<X, O, uint32_t>(g, st))
+    if (!g.out) return FPSK_OUT(void);
+    if (out_type == FPSK_ELEM_FP32) return FPSK_OUT(float);
+    if (out_type == FPSK_ELEM_FP16) return FPSK_OUT(__half);
+    return FPSK_OUT(__nv_bfloat16);
+#undef FPSK_OUT
 }
 
 }  // namespace fpsk
@@ -204,6 +626,8 @@ extern "C" fpsk_status fpsk_adjust_logits(const fpsk_logits *a, int32_t *d_statu
     if (a->n_rows == 0) return FPSK_OK;
     if (!a->logits || (!a->out && !a->token && !a->lse)) return FPSK_ERR_NULL;
     if (a->logits_stride < 0 || (a->out && a->n_rows > 1 && a->out_stride < a->vocab)) return FPSK_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(a->logits) % elem_bytes(a->logits_type) || (a->out && reinterpret_cast<uintptr_t>(a->out) % elem_bytes(a->out_type)))
+        return FPSK_ERR_ALIGN;
     if (a->history && (a->history_width < 0 || a->history_stride < 0)) return FPSK_ERR_SHAPE;
     if (!a->history && (a->history_len || a->prompt_len || a->repetition || a->frequency || a->presence)) return FPSK_ERR_NULL;
     if (a->bias_ptr && (a->n_biases < 0 || (a->n_biases > 0 && (!a->bias_token || !a->bias_value)))) return FPSK_ERR_NULL;
@@ -211,7 +635,7 @@ extern "C" fpsk_status fpsk_adjust_logits(const fpsk_logits *a, int32_t *d_statu
     if (!a->mask && a->mask_row) return FPSK_ERR_NULL;
     LogitsArgs g = {};
     g.x = a->logits; g.out = a->out; g.xs = a->logits_stride; g.os = a->out_stride; g.rows = a->n_rows;
-    g.vocab = a->vocab; g.out_type = a->out_type;
+    g.vocab = a->vocab;
     g.history = a->history; g.history_len = a->history_len; g.prompt_len = a->prompt_len;
     g.history_stride = a->history_stride; g.history_width = a->history_width;
     g.rep = a->repetition; g.freq = a->frequency; g.pres = a->presence;
@@ -219,7 +643,8 @@ extern "C" fpsk_status fpsk_adjust_logits(const fpsk_logits *a, int32_t *d_statu
     g.mask = a->mask; g.mask_row = a->mask_row; g.mask_stride = a->mask_stride; g.n_masks = a->n_masks;
     g.token = a->token; g.lse = a->lse; g.status = d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a->logits_type == FPSK_ELEM_FP32) return launch_logits<float>(g, st);
-    if (a->logits_type == FPSK_ELEM_FP16) return launch_logits<__half>(g, st);
-    return launch_logits<__nv_bfloat16>(g, st);
+    g.in_place = a->out == a->logits && a->out_type == a->logits_type && (a->n_rows == 1 || a->out_stride == a->logits_stride) && !g.token && !g.lse;
+    if (a->logits_type == FPSK_ELEM_FP32) return launch_logits_typed<float>(g, a->out_type, st);
+    if (a->logits_type == FPSK_ELEM_FP16) return launch_logits_typed<__half>(g, a->out_type, st);
+    return launch_logits_typed<__nv_bfloat16>(g, a->out_type, st);
 }
