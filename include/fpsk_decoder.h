@@ -42,7 +42,7 @@ typedef struct {
     int32_t group;               /* 0 (the whole row), 32, 64, 128 or 256                              */
     float eps;
 } fpsk_add_norm;
-fpsk_status fpsk_add_rms_norm(const fpsk_add_norm *a, void *stream);
+fpsk_status fpsk_add_rms_norm(const fpsk_add_norm *a, int32_t *d_status, void *stream);
 
 /* Its backward pass, from the sum h (residual_out, or x where there was no residual), the gradient dy of y and the gradient dh that
  * arrives at the sum from elsewhere (NULL: none).  With n = h r and g = dy w:
@@ -62,7 +62,7 @@ typedef struct {
     float eps;
 } fpsk_add_norm_grad;
 size_t fpsk_add_norm_workspace_bytes(int32_t dim);
-fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, void *workspace, size_t ws_bytes, void *stream);
+fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, void *workspace, size_t ws_bytes, int32_t *d_status, void *stream);
 
 #define FPSK_MAX_VOCAB (1 << 23)
 

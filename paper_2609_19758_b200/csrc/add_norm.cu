@@ -149,8 +149,9 @@ template <typename X, typename R, bool WIDE> __global__ void __launch_bounds__(1
                 scale = e4m3_scale(top);
                 if (n > 0 && c % g.group == 0) g.scale[row * g.ss + c / g.group] = scale;
             }
+            const float over = __frcp_rn(scale);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = __fdiv_rn(y[i], scale);
+            for (int i = 0; i < 8; ++i) y[i] *= over;
             unsigned char *out = static_cast<unsigned char *>(g.y) + row * g.ys + c;
             const unsigned int lo = e4m3_pair(y[0], y[1]) | e4m3_pair(y[2], y[3]) << 16, hi = e4m3_pair(y[4], y[5]) | e4m3_pair(y[6], y[7]) << 16;
             if (WIDE && n == 8) *reinterpret_cast<uint2 *>(out) = make_uint2(lo, hi);
@@ -256,8 +257,453 @@ static int warps_of(int dim)
     return w;
 }
 
-template <typename X, typename R> static fpsk_status launch_norm(const NormArgs &g, bool wide, cudaStream_t st)
+// ---------------------------------------------------------------- rows through a ring
+// For many rows of 513 to 16384 channels: one warp of a block copies whole rows into a ring of stages, so that what is in flight does
+// not depend on the other warps' registers, and those take a row each pass: sums over the row's threads, one barrier, the result.
+// Rows that start off 16 bytes come as their aligned middles, and their first and last elements by plain loads a stage ahead.
+struct RingRows {
+    const char *base;
+    long long stride;                  // bytes from row to row
+    int bytes, size;                   // of a row, of an element
+    int at;                            // in a row's part of a stage
+};
+struct RingArgs {
+    NormArgs f;
+    NormGradArgs b;
+    RingRows in[3];
+    int inputs;
+    int row_bytes, stage_bytes, stages;
+    int teams, log_teams;              // rows of a stage
+    long long n, steps;
+    int32_t *status;
+};
+constexpr int kRingMost = 8, kRingEdges = 6;
+
+// team of W warps: sums of two values, the same order everywhere; slots of the team alternate from row to row
+__device__ __forceinline__ float2 ring_sum(float2 v, int warps, int team, float2 *slots)
 {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+        v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+    }
+    if (lane == 0) slots[(threadIdx.x >> 5) - team * warps] = v;
+    bar_sync(1 + team, 32 * warps);
+    v = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+        v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+    }
+    return v;
+}
+
+// The copying warp.
+template <bool WIDE> __device__ __forceinline__ void ring_copy(const RingArgs &g, uint32_t smem, unsigned long long *full, unsigned long long *empty)
+{
+    const int lane = threadIdx.x & 31;
+    bool ok = true;
+    int slot = 0;
+    uint32_t phase = 0;
+    unsigned int k = 0;
+    const int mine = lane < g.teams * g.inputs ? lane : -1, my_row = mine >= 0 ? mine & (g.teams - 1) : 0, my_in = mine >= 0 ? mine >> g.log_teams : 0;
+    // edge i of this lane: element e < 8 in front of the aligned middle, or e - 8 behind it
+    unsigned int edge[kRingEdges];
+    auto edge_of = [&](int i, long long step, const char *&from, uint32_t &to, int &size) {
+        const int at = lane + 32 * i, e = at & 15, row = at >> 4 & (g.teams - 1), in = at >> (4 + g.log_teams);
+        const long long r = (step << g.log_teams) + row;
+        if (in >= g.inputs || step >= g.steps || r >= g.n) return false;
+        const RingRows &p = g.in[in];
+        size = p.size;
+        const char *start = p.base + r * p.stride;
+        const int shift = (int)(reinterpret_cast<uintptr_t>(start) & 15), head = min(p.bytes, 16 - shift & 15), tail = (p.bytes - head) & 15;
+        const int off = e < 8 ? e * p.size : p.bytes - tail + (e - 8) * p.size;
+        if (e < 8 ? off >= head : off >= p.bytes) return false;
+        from = start + off;
+        to = smem + row * g.row_bytes + p.at + shift + off;
+        return true;
+    };
+    auto ask = [&](long long step) {
+        if (WIDE) return;
+#pragma unroll
+        for (int i = 0; i < kRingEdges; ++i) {
+            const char *from;
+            uint32_t to;
+            int size;
+            edge[i] = 0;
+            if (edge_of(i, step, from, to, size)) edge[i] = size == 4 ? *reinterpret_cast<const unsigned int *>(from) : *reinterpret_cast<const unsigned short *>(from);
+        }
+    };
+    ask(blockIdx.x);
+    for (long long step = blockIdx.x; step < g.steps; step += gridDim.x) {
+        if (ok && !mbar_wait_bounded(smem_u32(&empty[slot]), phase ^ 1u)) {
+            ok = false;
+            report_status(g.status, FPSK_ERR_TIMEOUT);
+        }
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        const uint32_t bar = smem_u32(&full[slot]), stage = slot * g.stage_bytes;
+        int bytes = 0, shift = 0, head = 0;
+        const char *start = nullptr;
+        const RingRows &p = g.in[my_in];
+        const long long r = (step << g.log_teams) + my_row;
+        if (mine >= 0 && r < g.n) {
+            start = p.base + r * p.stride;
+            if (!WIDE) {
+                shift = (int)(reinterpret_cast<uintptr_t>(start) & 15);
+                head = min(p.bytes, 16 - shift & 15);
+            }
+            bytes = (p.bytes - head) & ~15;
+        }
+        const int all = __reduce_add_sync(0xFFFFFFFFu, bytes);
+        if (!WIDE) {
+#pragma unroll
+            for (int i = 0; i < kRingEdges; ++i) {
+                const char *from;
+                uint32_t to;
+                int size;
+                if (edge_of(i, step, from, to, size)) {
+                    if (size == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + stage), "r"(edge[i]) : "memory");
+                    else asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + stage), "h"((unsigned short)edge[i]) : "memory");
+                }
+            }
+            __syncwarp();
+        }
+        if (lane == 0) mbar_expect_tx(bar, (uint32_t)all);
+        __syncwarp();
+        if (bytes) bulk_g2s(smem + stage + my_row * g.row_bytes + p.at + shift + head, start + head, (uint32_t)bytes, bar);
+        ask(step + gridDim.x);
+        ++k;
+        if (++slot == g.stages) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+    // no copy is left in flight
+    if (lane == 0)
+        for (unsigned int back = min(k, (unsigned int)g.stages); back; --back) {
+            const unsigned int piece = k - back;
+            mbar_wait_bounded(smem_u32(&full[piece % g.stages]), piece / g.stages & 1u);
+        }
+}
+
+// Vector j of a thread's channels: WIDE eight neighbours, j vectors of `lanes` threads on, else eight single ones, `lanes` apart.
+template <bool WIDE> __device__ __forceinline__ int channel(int lane, int lanes, int j, int i) { return WIDE ? 8 * (lane + j * lanes) + i : lane + (8 * j + i) * lanes; }
+// It from a row in shared memory, as pairs (0 behind the row).
+template <bool WIDE> __device__ __forceinline__ void ring_load(const float *row, int lane, int lanes, int j, int dim, float2 (&v)[4])
+{
+    if (WIDE) {
+        const int c = 8 * (lane + j * lanes);
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        if (c < dim) {
+            a = *reinterpret_cast<const float4 *>(row + c);
+            b = *reinterpret_cast<const float4 *>(row + c + 4);
+        }
+        v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w);
+        v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = channel<false>(lane, lanes, j, 2 * i);
+        v[i] = make_float2(c < dim ? row[c] : 0.f, c + lanes < dim ? row[c + lanes] : 0.f);
+    }
+}
+template <bool WIDE, typename T> __device__ __forceinline__ void ring_load(const T *row, int lane, int lanes, int j, int dim, float2 (&v)[4])
+{
+    if (WIDE) {
+        const int c = 8 * (lane + j * lanes);
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        if (c < dim) u = *reinterpret_cast<const uint4 *>(row + c);
+        v[0] = HalfTraits<T>::unpack2(u.x); v[1] = HalfTraits<T>::unpack2(u.y);
+        v[2] = HalfTraits<T>::unpack2(u.z); v[3] = HalfTraits<T>::unpack2(u.w);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = channel<false>(lane, lanes, j, 2 * i);
+        v[i] = make_float2(c < dim ? Elem<T>::to_f(row[c]) : 0.f, c + lanes < dim ? Elem<T>::to_f(row[c + lanes]) : 0.f);
+    }
+}
+template <bool WIDE> __device__ __forceinline__ void ring_weights(const void *w, int type, int lane, int lanes, int j, int dim, float2 (&v)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = make_float2(1.f, 1.f);
+    if (!w) return;
+    float t[8];
+    const int c = channel<WIDE>(lane, lanes, j, 0);
+    if (WIDE) {
+        if (c >= dim) return;
+        load8_any<true>(w, type, c, 8, t);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int ci = c + i * lanes;
+            t[i] = ci >= dim ? 0.f
+                   : type == FPSK_ELEM_FP32 ? static_cast<const float *>(w)[ci]
+                   : type == FPSK_ELEM_FP16 ? __half2float(static_cast<const __half *>(w)[ci])
+                                            : __bfloat162float(static_cast<const __nv_bfloat16 *>(w)[ci]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = make_float2(t[2 * i], t[2 * i + 1]);
+}
+template <bool WIDE, typename T> __device__ __forceinline__ void ring_store(T *row, int lane, int lanes, int j, int dim, const float2 (&v)[4])
+{
+    const int c = channel<WIDE>(lane, lanes, j, 0);
+    if (WIDE) {
+        if (c < dim) store_vec<T, 8>(row + c, true, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i * lanes < dim) row[c + i * lanes] = Elem<T>::from_f(i & 1 ? v[i / 2].y : v[i / 2].x);
+}
+template <bool WIDE> __device__ __forceinline__ void ring_store_any(void *p, int type, long long at, int lane, int lanes, int j, int dim, const float2 (&v)[4])
+{
+    if (type == FPSK_ELEM_FP32) ring_store<WIDE>(static_cast<float *>(p) + at, lane, lanes, j, dim, v);
+    else if (type == FPSK_ELEM_FP16) ring_store<WIDE>(static_cast<__half *>(p) + at, lane, lanes, j, dim, v);
+    else ring_store<WIDE>(static_cast<__nv_bfloat16 *>(p) + at, lane, lanes, j, dim, v);
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Threads of a row's channels: J vectors of eight each; MOST: of the largest block.  The weights and their gradients stay in registers.
+template <typename X, typename R, bool WIDE, bool GRAD, int J, int MOST, int PER_SM>
+__global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __grid_constant__ RingArgs g)
+{
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ unsigned long long full[kRingMost], empty[kRingMost];
+    __shared__ float2 sums[2][4][16];                                  // of the teams' warps
+    __shared__ unsigned int tops[2][4][16];
+    const int workers = (int)blockDim.x - 32, warps = workers / 32 >> g.log_teams;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < g.stages; ++s) {
+            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&empty[s]), workers / 32);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if ((int)threadIdx.x >= workers) {
+        ring_copy<WIDE>(g, smem_u32(smem), full, empty);
+        return;
+    }
+    const int team = (int)(threadIdx.x >> 5) / warps, lanes = 32 * warps, lane = (int)threadIdx.x - team * lanes;
+    const int dim = GRAD ? g.b.dim : g.f.dim;
+    const float eps = GRAD ? g.b.eps : g.f.eps, inv_dim = GRAD ? g.b.inv_dim : g.f.inv_dim;
+    float2 w[J][4], acc[GRAD ? J : 1][4] = {};
+#pragma unroll
+    for (int j = 0; j < J; ++j) ring_weights<WIDE>(GRAD ? g.b.w : g.f.w, GRAD ? g.b.wtype : g.f.wtype, lane, lanes, j, dim, w[j]);
+    bool ok = true;
+    int slot = 0, turn = 0;
+    uint32_t phase = 0;
+    for (long long step = blockIdx.x; step < g.steps; step += gridDim.x, turn ^= 1) {
+        const long long row = (step << g.log_teams) + team;
+        const bool live = row < g.n;
+        const int here = live ? dim : 0;
+        if (ok && !mbar_wait_bounded(smem_u32(&full[slot]), phase)) ok = false;           // (the copying warp tells)
+        auto input = [&](int i) {
+            const int shift = WIDE ? 0 : (int)(reinterpret_cast<uintptr_t>(g.in[i].base + row * g.in[i].stride) & 15);
+            return smem + slot * g.stage_bytes + team * g.row_bytes + g.in[i].at + shift;
+        };
+        auto release = [&] {
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&empty[slot]));
+        };
+        const X *first = reinterpret_cast<const X *>(input(0));
+        const R *second = reinterpret_cast<const R *>(input(1));
+        float2 sh = both(0.f), sg = both(0.f);
+        if (GRAD) {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                float2 h[4], d[4];
+                ring_load<WIDE>(first, lane, lanes, j, here, h);
+                ring_load<WIDE>(second, lane, lanes, j, here, d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sh = __ffma2_rn(h[i], h[i], sh);
+                    sg = __ffma2_rn(h[i], __fmul2_rn(d[i], w[j][i]), sg);
+                }
+            }
+            const float2 s = ring_sum(make_float2(sh.x + sh.y, sg.x + sg.y), warps, team, sums[turn][team]);
+            const float r = rsqrtf(fmaf(s.x, inv_dim, eps));
+            // dx = (dy w - h r^2 mean(dy w h)) r + dh
+            const float2 rr = both(r), off = both(-s.y * r * inv_dim * r);
+            const R *third = g.b.dh ? reinterpret_cast<const R *>(input(2)) : nullptr;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                float2 h[4], d[4];
+                ring_load<WIDE>(first, lane, lanes, j, here, h);
+                ring_load<WIDE>(second, lane, lanes, j, here, d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    acc[j][i] = __ffma2_rn(d[i], live ? __fmul2_rn(h[i], rr) : both(0.f), acc[j][i]);
+                    d[i] = __fmul2_rn(rr, __ffma2_rn(h[i], off, __fmul2_rn(d[i], w[j][i])));
+                }
+                if (third) {
+                    ring_load<WIDE>(third, lane, lanes, j, here, h);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[i] = __fadd2_rn(d[i], h[i]);
+                }
+                if (j == J - 1) release();
+                if (live) ring_store<WIDE>(static_cast<R *>(g.b.dx) + row * g.b.dxs, lane, lanes, j, dim, d);
+            }
+        } else {
+            float2 h[J][4];
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                ring_load<WIDE>(first, lane, lanes, j, here, h[j]);
+                if (g.f.res) {
+                    float2 b[4];
+                    ring_load<WIDE>(second, lane, lanes, j, here, b);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[j][i] = __fadd2_rn(h[j][i], b[i]);
+                }
+                if (j == J - 1) release();
+                if (live && g.f.hout) ring_store<WIDE>(static_cast<R *>(g.f.hout) + row * g.f.hs, lane, lanes, j, dim, h[j]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sh = __ffma2_rn(h[j][i], h[j][i], sh);
+            }
+            const float2 s = ring_sum(make_float2(sh.x + sh.y, 0.f), warps, team, sums[turn][team]);
+            const float2 rr = both(rsqrtf(fmaf(s.x, inv_dim, eps)));
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[j][i] = __fmul2_rn(__fmul2_rn(h[j][i], rr), w[j][i]);
+            if (g.f.ytype != FPSK_ELEM_E4M3) {
+                if (live) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) ring_store_any<WIDE>(g.f.y, g.f.ytype, row * g.f.ys, lane, lanes, j, dim, h[j]);
+                }
+            } else if (WIDE) {
+                // (a vector's eight channels are in one group, and a group's vectors in neighbouring lanes)
+                unsigned int top[J], most = 0;
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    top[j] = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top[j] = max(top[j], max(magnitude(h[j][i].x), magnitude(h[j][i].y)));
+                    if (8 * (lane + j * lanes) >= here) top[j] = 0;
+                    most = max(most, top[j]);
+                }
+                float whole = 1.f;
+                if (g.f.group == 0) {
+                    most = __reduce_max_sync(0xFFFFFFFFu, most);
+                    if ((threadIdx.x & 31) == 0) tops[turn][team][lane >> 5] = most;
+                    bar_sync(1 + team, lanes);
+                    most = __reduce_max_sync(0xFFFFFFFFu, (lane & 31) < warps ? tops[turn][team][lane & 31] : 0u);
+                    whole = e4m3_scale(most);
+                    if (live && lane == 0) g.f.scale[row * g.f.ss] = whole;
+                }
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int c = 8 * (lane + j * lanes);
+                    float scale = whole;
+                    if (g.f.group) {
+                        for (int o = 1; o < g.f.group / 8; o <<= 1) top[j] = max(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], o));
+                        scale = e4m3_scale(top[j]);
+                        if (c < here && (c & (g.f.group - 1)) == 0) g.f.scale[row * g.f.ss + c / g.f.group] = scale;
+                    }
+                    const float2 over = both(__frcp_rn(scale));
+                    unsigned int q[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 y = __fmul2_rn(h[j][i], over);
+                        q[i] = e4m3_pair(y.x, y.y);
+                    }
+                    if (c < here) *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(g.f.y) + row * g.f.ys + c) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+                }
+            }
+        }
+        if (++slot == g.stages) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+    if (!GRAD || !g.b.part) return;
+    float *part = g.b.part + (((long long)blockIdx.x << g.log_teams) + team) * dim;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = channel<WIDE>(lane, lanes, j, i);
+            if (c < dim) part[c] = i & 1 ? acc[GRAD ? j : 0][i / 2].y : acc[GRAD ? j : 0][i / 2].x;
+        }
+}
+
+// Whether the ring takes a call, and how.  A thread has sixteen channels, or 32 where a row would take more than sixteen warps; a block
+// has four to eight warps that work, and one row for each eight of them.  Up to 4096 channels two blocks share an SM, above one has it.
+constexpr int kRingOne = 220 * 1024, kRingHalf = 110 * 1024;
+static bool ring_plan(RingArgs &g, int dim, bool wide, int &threads)
+{
+    if (dim <= 512 || dim > 16384) return false;
+    int warps = 2;
+    while (warps < 16 && 32 * 16 * warps < dim) warps *= 2;
+    g.log_teams = warps >= 8 ? 0 : warps == 4 ? 1 : 2;
+    g.teams = 1 << g.log_teams;
+    threads = 32 * (warps * g.teams + 1);
+    g.row_bytes = 0;
+    for (int i = 0; i < g.inputs; ++i) {
+        g.in[i].at = g.row_bytes;
+        g.row_bytes += (g.in[i].bytes + 15) / 16 * 16 + (wide ? 0 : 16);
+    }
+    g.stage_bytes = (int)align_up((size_t)g.row_bytes * g.teams, 128);
+    g.stages = (warps < 16 ? kRingHalf : kRingOne) / g.stage_bytes;
+    if (g.stages < 2) return false;
+    if (g.stages > kRingMost) g.stages = kRingMost;
+    g.steps = (g.n + g.teams - 1) >> g.log_teams;
+    return g.steps >= 2 * kSms;
+}
+static unsigned ring_blocks(const RingArgs &g, int threads)
+{
+    const long long most = (long long)kSms * (threads > 288 ? 1 : 2);
+    return (unsigned)(g.steps < most ? g.steps : most);
+}
+
+template <typename X, typename R, bool GRAD> static fpsk_status launch_ring(const RingArgs &g, bool wide, int dim, int threads, cudaStream_t st)
+{
+    const size_t bytes = (size_t)g.stages * g.stage_bytes;
+#define FPSK_RING(WIDE, J, MOST, PER_SM)                                                                                                         \
+    do {                                                                                                                                         \
+        auto kernel = add_norm_ring_kernel<X, R, WIDE, GRAD, J, MOST, PER_SM>;                                                                   \
+        FPSK_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingOne));                                       \
+        kernel<<<ring_blocks(g, threads), threads, bytes, st>>>(g);                                                                              \
+    } while (0)
+    if (threads <= 288) {
+        if (wide) FPSK_RING(true, 2, 288, 2);
+        else FPSK_RING(false, 2, 288, 2);
+    } else if (dim <= 8192) {
+        if (wide) FPSK_RING(true, 2, 544, 1);
+        else FPSK_RING(false, 2, 544, 1);
+    } else {
+        if (wide) FPSK_RING(true, 4, 544, 1);
+        else FPSK_RING(false, 4, 544, 1);
+    }
+#undef FPSK_RING
+    FPSK_LAUNCH_CHECK();
+    return FPSK_OK;
+}
+static RingRows ring_rows(const void *p, long long stride, int dim, int type)
+{
+    const int size = elem_bytes(type);
+    return RingRows{static_cast<const char *>(p), stride * size, dim * size, size, 0};
+}
+
+template <typename X, typename R> static fpsk_status launch_norm(const NormArgs &g, bool wide, int xtype, int rtype, int32_t *d_status, cudaStream_t st)
+{
+    if (wide || g.ytype != FPSK_ELEM_E4M3) {
+        RingArgs r = {};
+        const bool whole = wide && g.dim % 8 == 0;
+        r.f = g;
+        r.in[0] = ring_rows(g.x, g.xs, g.dim, xtype);
+        r.in[1] = ring_rows(g.res, g.rs, g.dim, rtype);
+        r.inputs = g.res ? 2 : 1;
+        r.n = g.n;
+        r.status = d_status;
+        int threads;
+        if ((whole || g.ytype != FPSK_ELEM_E4M3) && ring_plan(r, g.dim, whole, threads)) return launch_ring<X, R, false>(r, whole, g.dim, threads, st);
+    }
     const int threads = g.warps > 8 ? 32 * g.warps : kNormThreads, teams = threads / 32 / g.warps;
     const long long steps = (g.n + teams - 1) / teams, most = 1LL << 20;
     const unsigned blocks = (unsigned)(steps < most ? steps : most);
@@ -275,8 +721,25 @@ static int grad_rows(int dim)
     return kNormGradBlocks * (w > 8 ? 1 : 8 / w);
 }
 
-template <typename X, typename G> static fpsk_status launch_norm_grad(NormGradArgs g, bool wide, float *dw, cudaStream_t st)
+template <typename X, typename G> static fpsk_status launch_norm_grad(NormGradArgs g, bool wide, float *dw, int htype, int gtype, int32_t *d_status, cudaStream_t st)
 {
+    RingArgs r = {};
+    const bool whole = wide && g.dim % 8 == 0;
+    r.b = g;
+    r.in[0] = ring_rows(g.h, g.hs, g.dim, htype);
+    r.in[1] = ring_rows(g.dy, g.dys, g.dim, gtype);
+    r.in[2] = ring_rows(g.dh, g.dhs, g.dim, gtype);
+    r.inputs = g.dh ? 3 : 2;
+    r.n = g.n;
+    r.status = d_status;
+    int ring_threads;
+    if (ring_plan(r, g.dim, whole, ring_threads)) {
+        const fpsk_status rc = launch_ring<X, G, true>(r, whole, g.dim, ring_threads, st);
+        if (rc != FPSK_OK || !dw) return rc;
+        add_norm_sum_kernel<<<(unsigned)(g.dim + 31) / 32, 1024, 0, st>>>(g.part, (int)ring_blocks(r, ring_threads) * r.teams, g.dim, dw);
+        FPSK_LAUNCH_CHECK();
+        return FPSK_OK;
+    }
     const int threads = g.warps > 8 ? 32 * g.warps : kNormThreads, teams = threads / 32 / g.warps;
     const long long steps = (g.n + teams - 1) / teams;
     const unsigned blocks = (unsigned)(steps < kNormGradBlocks ? steps : kNormGradBlocks);
@@ -303,7 +766,7 @@ using namespace fpsk;
 
 static bool rows_ok(long long n, int dim, long long stride) { return n < 2 || stride >= dim; }
 
-extern "C" fpsk_status fpsk_add_rms_norm(const fpsk_add_norm *a, void *stream)
+extern "C" fpsk_status fpsk_add_rms_norm(const fpsk_add_norm *a, int32_t *d_status, void *stream)
 {
     if (!a) return FPSK_ERR_NULL;
     if (a->n_tokens < 0 || a->n_tokens > (1LL << 40) || a->dim < 1 || a->dim > FPSK_MAX_NORM_DIM) return FPSK_ERR_SHAPE;
@@ -332,8 +795,8 @@ extern "C" fpsk_status fpsk_add_rms_norm(const fpsk_add_norm *a, void *stream)
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int rt = a->residual || a->residual_out ? a->residual_type : FPSK_ELEM_FP32;
 #define FPSK_RES(X)                                                      \
-    (rt == FPSK_ELEM_FP32 ? launch_norm<X, float>(g, wide, st)           \
-                          : rt == FPSK_ELEM_FP16 ? launch_norm<X, __half>(g, wide, st) : launch_norm<X, __nv_bfloat16>(g, wide, st))
+    (rt == FPSK_ELEM_FP32 ? launch_norm<X, float>(g, wide, a->x_type, rt, d_status, st)           \
+                          : rt == FPSK_ELEM_FP16 ? launch_norm<X, __half>(g, wide, a->x_type, rt, d_status, st) : launch_norm<X, __nv_bfloat16>(g, wide, a->x_type, rt, d_status, st))
     if (a->x_type == FPSK_ELEM_FP32) return FPSK_RES(float);
     if (a->x_type == FPSK_ELEM_FP16) return FPSK_RES(__half);
     return FPSK_RES(__nv_bfloat16);
@@ -346,7 +809,7 @@ extern "C" size_t fpsk_add_norm_workspace_bytes(int32_t dim)
     return align_up((size_t)grad_rows(dim) * dim * sizeof(float), 256);
 }
 
-extern "C" fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, void *workspace, size_t ws_bytes, void *stream)
+extern "C" fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, void *workspace, size_t ws_bytes, int32_t *d_status, void *stream)
 {
     if (!a) return FPSK_ERR_NULL;
     if (a->n_tokens < 0 || a->n_tokens > (1LL << 40) || a->dim < 1 || a->dim > FPSK_MAX_NORM_DIM) return FPSK_ERR_SHAPE;
@@ -371,9 +834,9 @@ extern "C" fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, v
                       row_wide(g.dx, a->grad_type, g.dxs) && row_wide(g.w, a->weight_type, 0);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 #define FPSK_IN(G)                                                                              \
-    (a->h_type == FPSK_ELEM_FP32 ? launch_norm_grad<float, G>(g, wide, a->dweight, st)          \
-                                 : a->h_type == FPSK_ELEM_FP16 ? launch_norm_grad<__half, G>(g, wide, a->dweight, st)  \
-                                                               : launch_norm_grad<__nv_bfloat16, G>(g, wide, a->dweight, st))
+    (a->h_type == FPSK_ELEM_FP32 ? launch_norm_grad<float, G>(g, wide, a->dweight, a->h_type, a->grad_type, d_status, st)          \
+                                 : a->h_type == FPSK_ELEM_FP16 ? launch_norm_grad<__half, G>(g, wide, a->dweight, a->h_type, a->grad_type, d_status, st)  \
+                                                               : launch_norm_grad<__nv_bfloat16, G>(g, wide, a->dweight, a->h_type, a->grad_type, d_status, st))
     if (a->grad_type == FPSK_ELEM_FP32) return FPSK_IN(float);
     if (a->grad_type == FPSK_ELEM_FP16) return FPSK_IN(__half);
     return FPSK_IN(__nv_bfloat16);

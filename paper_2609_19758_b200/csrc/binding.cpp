@@ -400,10 +400,10 @@ int32_t small(int64_t n, const char *what)
     return (int32_t)n;
 }
 
-// x, residual, weight, y, residual_out, scale, group, eps, stream
+// x, residual, weight, y, residual_out, scale, group, eps, status, stream
 PyObject *py_add_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return call(n, 9, [&] {
+    return call(n, 10, [&] {
         const int device = device_of(needed(a[0], "x"), "x");
         const at::Tensor &x = rows_of(a[0], -1, -1, device, "x");
         const int64_t rows = x.size(0), dim = x.size(1);
@@ -447,13 +447,13 @@ PyObject *py_add_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         t.eps = (float)number(a[7]);
         const OnDevice on(device);
-        return lib.add_norm(&t, stream_ptr(a[8]));
+        return lib.add_norm(&t, status_ptr(a[8], device), stream_ptr(a[9]));
     });
 }
-// h, dy, weight, dx, dweight, ws, dh, eps, stream
+// h, dy, weight, dx, dweight, ws, dh, eps, status, stream
 PyObject *py_add_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return call(n, 9, [&] {
+    return call(n, 10, [&] {
         const int device = device_of(needed(a[0], "h"), "h");
         const at::Tensor &h = rows_of(a[0], -1, -1, device, "h");
         const int64_t rows = h.size(0), dim = h.size(1);
@@ -479,7 +479,7 @@ PyObject *py_add_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (ws && (!ws->is_cuda() || ws->get_device() != device || !ws->is_contiguous())) refuse(PyExc_ValueError, "ws: on cuda:%d expected", device);
         t.eps = (float)number(a[7]);
         const OnDevice on(device);
-        return lib.add_norm_backward(&t, ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->nbytes() : 0, stream_ptr(a[8]));
+        return lib.add_norm_backward(&t, ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->nbytes() : 0, status_ptr(a[8], device), stream_ptr(a[9]));
     });
 }
 // logits, out, history, history_len, prompt_len, repetition, frequency, presence, bias pointers, tokens, values, mask, mask_row, token,

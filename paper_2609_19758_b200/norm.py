@@ -19,11 +19,11 @@ from .fpsk import ERR_SHAPE, FpskError
 
 def add_rms_norm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: Optional[torch.Tensor], y: torch.Tensor,
                  residual_out: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, group: int = 0, eps: float = 1e-6,
-                 stream=None) -> None:
+                 status: Optional[torch.Tensor] = None, stream=None) -> None:
     """h = x + residual (tokens, dim), stored to residual_out (which may be residual); y = h rsqrt(mean(h^2) + eps) weight, rounded once.
     A float8_e4m3fn y holds y / scale, with scale (tokens, groups) filled for each `group` channels (32, 64, 128 or 256; 0: the row)."""
     b = A._binding or A._bind()
-    A._check(b.add_rms_norm(x, residual, weight, y, residual_out, scale, group, eps, A._stream(b.device(x), stream)), "fpsk_add_rms_norm")
+    A._check(b.add_rms_norm(x, residual, weight, y, residual_out, scale, group, eps, status, A._stream(b.device(x), stream)), "fpsk_add_rms_norm")
 
 
 def add_rms_norm_workspace(dim: int, device=None) -> torch.Tensor:
@@ -37,11 +37,11 @@ def add_rms_norm_workspace(dim: int, device=None) -> torch.Tensor:
 
 def add_rms_norm_backward(h: torch.Tensor, dy: torch.Tensor, weight: Optional[torch.Tensor], dx: torch.Tensor,
                           dweight: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None,
-                          eps: float = 1e-6, stream=None) -> None:
+                          eps: float = 1e-6, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """Backward pass of add_rms_norm from the sum h: dx (the type of dy), the gradient of x and of the residual alike, from dy and from
     dh, what arrives at the sum through the residual stream; and the FP32 gradient of the weight (overwritten; it needs ws)."""
     b = A._binding or A._bind()
-    A._check(b.add_rms_norm_backward(h, dy, weight, dx, dweight, ws, dh, eps, A._stream(b.device(h), stream)), "fpsk_add_rms_norm_backward")
+    A._check(b.add_rms_norm_backward(h, dy, weight, dx, dweight, ws, dh, eps, status, A._stream(b.device(h), stream)), "fpsk_add_rms_norm_backward")
 
 
 class AddRMSNorm(torch.autograd.Function):

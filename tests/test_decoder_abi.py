@@ -16,8 +16,8 @@ P = 4096                                                               # never r
 def lib():
     B.build()
     L = fpsk.lib()
-    L.fpsk_add_rms_norm.argtypes = [vp, vp]
-    L.fpsk_add_rms_norm_backward.argtypes = [vp, vp, sz, vp]
+    L.fpsk_add_rms_norm.argtypes = [vp, vp, vp]
+    L.fpsk_add_rms_norm_backward.argtypes = [vp, vp, sz, vp, vp]
     L.fpsk_add_norm_workspace_bytes.argtypes, L.fpsk_add_norm_workspace_bytes.restype = [C.c_int32], sz
     L.fpsk_adjust_logits.argtypes = [vp, vp, vp]
     L.fpsk_distill_loss.argtypes = L.fpsk_distill_loss_backward.argtypes = [vp, vp, vp]
@@ -26,9 +26,9 @@ def lib():
 
 def test_add_norm(lib):
     def call(x=P, res=0, w=0, hout=0, y=P, scale=0, strides=(64, 64, 64, 64, 1), n=2, dim=64, types=(F32, F32, F32, F32), group=0, eps=1e-6):
-        return lib.fpsk_add_rms_norm(struct.pack("@PPPPPPqqqqqqiiiiiif", x, res, w, hout, y, scale, *strides, n, dim, *types, group, eps), None)
+        return lib.fpsk_add_rms_norm(struct.pack("@PPPPPPqqqqqqiiiiiif", x, res, w, hout, y, scale, *strides, n, dim, *types, group, eps), None, None)
 
-    assert lib.fpsk_add_rms_norm(None, None) == fpsk.ERR_NULL
+    assert lib.fpsk_add_rms_norm(None, None, None) == fpsk.ERR_NULL
     assert call(n=-1) == call(dim=0) == call(dim=32769) == call(strides=(64, 64, 64, 63, 1)) == call(strides=(-1, 64, 64, 64, 1)) == fpsk.ERR_SHAPE
     assert call(hout=P, strides=(64, 64, 60, 64, 1)) == fpsk.ERR_SHAPE
     assert call(types=(E4M3, 0, 0, 0)) == call(res=P, types=(F32, 3, 0, 0)) == call(w=P, types=(F32, 0, 4, 0)) == call(types=(F32, 0, 0, 4)) == fpsk.ERR_DTYPE
@@ -41,9 +41,9 @@ def test_add_norm(lib):
 
 def test_add_norm_backward(lib):
     def call(h=P, dy=P, dh=0, w=0, dx=P, dw=0, strides=(64, 64, 64, 64), n=2, dim=64, types=(F32, F32, F32), eps=1e-6, ws=0, ws_bytes=0):
-        return lib.fpsk_add_rms_norm_backward(struct.pack("@PPPPPPqqqqqiiiif", h, dy, dh, w, dx, dw, *strides, n, dim, *types, eps), ws, ws_bytes, None)
+        return lib.fpsk_add_rms_norm_backward(struct.pack("@PPPPPPqqqqqiiiif", h, dy, dh, w, dx, dw, *strides, n, dim, *types, eps), ws, ws_bytes, None, None)
 
-    assert lib.fpsk_add_rms_norm_backward(None, None, 0, None) == fpsk.ERR_NULL
+    assert lib.fpsk_add_rms_norm_backward(None, None, 0, None, None) == fpsk.ERR_NULL
     assert lib.fpsk_add_norm_workspace_bytes(0) == lib.fpsk_add_norm_workspace_bytes(32769) == 0 < lib.fpsk_add_norm_workspace_bytes(64)
     assert call(n=-1) == call(dim=0) == call(strides=(64, 64, 64, 8)) == call(strides=(64, -64, 64, 64)) == fpsk.ERR_SHAPE
     assert call(types=(E4M3, 0, 0)) == call(types=(F32, E4M3, 0)) == call(w=P, types=(F32, F32, 7)) == fpsk.ERR_DTYPE
