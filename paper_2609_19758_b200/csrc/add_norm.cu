@@ -65,12 +65,19 @@ __device__ __forceinline__ unsigned int team_max(unsigned int v, int warps, unsi
     return s;
 }
 __device__ __forceinline__ unsigned int magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
-// the scale of a group whose largest magnitude has these bits
+// The scale of a group whose largest magnitude has these bits, and one over it: a product and an approximate reciprocal (one unit), as
+// two divisions for every eight channels took a fifth of the kernel.
 __device__ __forceinline__ float e4m3_scale(unsigned int top)
 {
-    const float t = __uint_as_float(top);
     if (top == 0) return 1.f;
-    return t < 448.f * 1.17549435e-38f ? 1.17549435e-38f : __fdiv_rn(t, 448.f);       // (a NaN divides)
+    const float s = __uint_as_float(top) * (1.f / 448.f);
+    return s < 1.17549435e-38f ? 1.17549435e-38f : s;                  // (a NaN stays)
+}
+__device__ __forceinline__ float over(float scale)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(scale));
+    return r;
 }
 __device__ __forceinline__ unsigned int e4m3_pair(float a, float b)
 {
@@ -81,6 +88,8 @@ template <typename X, typename R, bool WIDE> __global__ void __launch_bounds__(1
 {
     __shared__ float2 sums[32];
     __shared__ unsigned int tops[32];
+    let_the_next();
+    behind_the_last();
     const int teams = (int)(blockDim.x >> 5) / g.warps, team = (int)(threadIdx.x >> 5) / g.warps;
     const int lanes = 32 * g.warps, lane = (int)threadIdx.x - team * lanes;
     for (long long row0 = (long long)blockIdx.x * teams; row0 < g.n; row0 += (long long)gridDim.x * teams) {
@@ -149,9 +158,9 @@ template <typename X, typename R, bool WIDE> __global__ void __launch_bounds__(1
                 scale = e4m3_scale(top);
                 if (n > 0 && c % g.group == 0) g.scale[row * g.ss + c / g.group] = scale;
             }
-            const float over = __frcp_rn(scale);
+            const float by = over(scale);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] *= over;
+            for (int i = 0; i < 8; ++i) y[i] *= by;
             unsigned char *out = static_cast<unsigned char *>(g.y) + row * g.ys + c;
             const unsigned int lo = e4m3_pair(y[0], y[1]) | e4m3_pair(y[2], y[3]) << 16, hi = e4m3_pair(y[4], y[5]) | e4m3_pair(y[6], y[7]) << 16;
             if (WIDE && n == 8) *reinterpret_cast<uint2 *>(out) = make_uint2(lo, hi);
@@ -171,6 +180,8 @@ template <typename X, typename G, bool WIDE, int MOST> __global__ void __launch_
     __shared__ float2 sums[32];
     const int teams = (int)(blockDim.x >> 5) / g.warps, team = (int)(threadIdx.x >> 5) / g.warps;
     const int lanes = 32 * g.warps, lane = (int)threadIdx.x - team * lanes;
+    let_the_next();
+    behind_the_last();
     float acc[kGradVecs][8] = {};
     for (long long row0 = (long long)blockIdx.x * teams; row0 < g.n; row0 += (long long)gridDim.x * teams) {
         const long long row = row0 + team;
@@ -233,20 +244,35 @@ template <typename X, typename G, bool WIDE, int MOST> __global__ void __launch_
     }
 }
 
-// dw[c] = sum of `rows` rows of partial gradients: a warp's lanes take neighbouring channels, the warps rows 32 apart.
+// dw[c] = sum of `rows` rows of partial gradients: a warp's lanes take neighbouring channels, the warps rows 32 apart, eight at a time.
 __global__ void __launch_bounds__(1024) add_norm_sum_kernel(const float *part, int rows, int dim, float *dw)
 {
     __shared__ float sums[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float s = 0.f;
+    let_the_next();
+    behind_the_last();
     if (c < dim)
-        for (int r = warp; r < rows; r += 32) s += part[(long long)r * dim + c];
+        for (int r = warp; r < rows; r += 32 * 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = r + 32 * i < rows ? part[(long long)(r + 32 * i) * dim + c] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];
+        }
     sums[warp][lane] = s;
     __syncthreads();
     s = sums[lane][warp];
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
     if (lane == 0 && blockIdx.x * 32 + warp < dim) dw[blockIdx.x * 32 + warp] = s;
+}
+static fpsk_status launch_sum(const float *part, int rows, int dim, float *dw, cudaStream_t st)
+{
+    Launch launch((unsigned)(dim + 31) / 32, 1024, 0, 1, st);
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&launch.cfg, add_norm_sum_kernel, part, rows, dim, dw));
+    FPSK_LAUNCH_CHECK();
+    return FPSK_OK;
 }
 
 // warps of a row: a thread takes two vectors of eight channels, four where that would be more than 32 warps
@@ -261,10 +287,11 @@ static int warps_of(int dim)
 // For many rows of 513 to 16384 channels: one warp of a block copies whole rows into a ring of stages, so that what is in flight does
 // not depend on the other warps' registers, and those take a row each pass: sums over the row's threads, one barrier, the result.
 // Rows that start off 16 bytes come as their aligned middles, and their first and last elements by plain loads a stage ahead.
+// Above 8192 channels a row is divided among a cluster of blocks, which tell each other their sums.
 struct RingRows {
     const char *base;
     long long stride;                  // bytes from row to row
-    int bytes, size;                   // of a row, of an element
+    int size;                          // of an element
     int at;                            // in a row's part of a stage
 };
 struct RingArgs {
@@ -274,10 +301,11 @@ struct RingArgs {
     int inputs;
     int row_bytes, stage_bytes, stages;
     int teams, log_teams;              // rows of a stage
+    int blocks, slice;                 // a row's blocks, and how many channels each but the last has
     long long n, steps;
     int32_t *status;
 };
-constexpr int kRingMost = 8, kRingEdges = 6;
+constexpr int kRingMost = 8, kRingEdges = 6, kRingTeams = 8, kRingMostBlocks = 4;
 
 // team of W warps: sums of two values, the same order everywhere; slots of the team alternate from row to row
 __device__ __forceinline__ float2 ring_sum(float2 v, int warps, int team, float2 *slots)
@@ -289,6 +317,7 @@ __device__ __forceinline__ float2 ring_sum(float2 v, int warps, int team, float2
         v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
     }
     if (lane == 0) slots[(threadIdx.x >> 5) - team * warps] = v;
+    if (warps == 1) return v;
     bar_sync(1 + team, 32 * warps);
     v = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
 #pragma unroll
@@ -300,7 +329,8 @@ __device__ __forceinline__ float2 ring_sum(float2 v, int warps, int team, float2
 }
 
 // The copying warp.
-template <bool WIDE> __device__ __forceinline__ void ring_copy(const RingArgs &g, uint32_t smem, unsigned long long *full, unsigned long long *empty)
+template <bool WIDE>
+__device__ __forceinline__ void ring_copy(const RingArgs &g, int c0, int dim, long long first, long long stride, uint32_t smem, unsigned long long *full, unsigned long long *empty)
 {
     const int lane = threadIdx.x & 31;
     bool ok = true;
@@ -316,10 +346,10 @@ template <bool WIDE> __device__ __forceinline__ void ring_copy(const RingArgs &g
         if (in >= g.inputs || step >= g.steps || r >= g.n) return false;
         const RingRows &p = g.in[in];
         size = p.size;
-        const char *start = p.base + r * p.stride;
-        const int shift = (int)(reinterpret_cast<uintptr_t>(start) & 15), head = min(p.bytes, 16 - shift & 15), tail = (p.bytes - head) & 15;
-        const int off = e < 8 ? e * p.size : p.bytes - tail + (e - 8) * p.size;
-        if (e < 8 ? off >= head : off >= p.bytes) return false;
+        const char *start = p.base + r * p.stride + (long long)c0 * p.size;
+        const int all = dim * p.size, shift = (int)(reinterpret_cast<uintptr_t>(start) & 15), head = min(all, (16 - shift) & 15), tail = (all - head) & 15;
+        const int off = e < 8 ? e * p.size : all - tail + (e - 8) * p.size;
+        if (e < 8 ? off >= head : off >= all) return false;
         from = start + off;
         to = smem + row * g.row_bytes + p.at + shift + off;
         return true;
@@ -335,8 +365,8 @@ template <bool WIDE> __device__ __forceinline__ void ring_copy(const RingArgs &g
             if (edge_of(i, step, from, to, size)) edge[i] = size == 4 ? *reinterpret_cast<const unsigned int *>(from) : *reinterpret_cast<const unsigned short *>(from);
         }
     };
-    ask(blockIdx.x);
-    for (long long step = blockIdx.x; step < g.steps; step += gridDim.x) {
+    ask(first);
+    for (long long step = first; step < g.steps; step += stride) {
         if (ok && !mbar_wait_bounded(smem_u32(&empty[slot]), phase ^ 1u)) {
             ok = false;
             report_status(g.status, FPSK_ERR_TIMEOUT);
@@ -349,12 +379,12 @@ template <bool WIDE> __device__ __forceinline__ void ring_copy(const RingArgs &g
         const RingRows &p = g.in[my_in];
         const long long r = (step << g.log_teams) + my_row;
         if (mine >= 0 && r < g.n) {
-            start = p.base + r * p.stride;
+            start = p.base + r * p.stride + (long long)c0 * p.size;
             if (!WIDE) {
                 shift = (int)(reinterpret_cast<uintptr_t>(start) & 15);
-                head = min(p.bytes, 16 - shift & 15);
+                head = min(dim * p.size, (16 - shift) & 15);
             }
-            bytes = (p.bytes - head) & ~15;
+            bytes = (dim * p.size - head) & ~15;
         }
         const int all = __reduce_add_sync(0xFFFFFFFFu, bytes);
         if (!WIDE) {
@@ -373,13 +403,14 @@ template <bool WIDE> __device__ __forceinline__ void ring_copy(const RingArgs &g
         if (lane == 0) mbar_expect_tx(bar, (uint32_t)all);
         __syncwarp();
         if (bytes) bulk_g2s(smem + stage + my_row * g.row_bytes + p.at + shift + head, start + head, (uint32_t)bytes, bar);
-        ask(step + gridDim.x);
+        ask(step + stride);
         ++k;
         if (++slot == g.stages) {
             slot = 0;
             phase ^= 1u;
         }
     }
+    let_the_next();
     // no copy is left in flight
     if (lane == 0)
         for (unsigned int back = min(k, (unsigned int)g.stages); back; --back) {
@@ -469,42 +500,85 @@ template <bool WIDE> __device__ __forceinline__ void ring_store_any(void *p, int
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // Threads of a row's channels: J vectors of eight each; MOST: of the largest block.  The weights and their gradients stay in registers.
-template <typename X, typename R, bool WIDE, bool GRAD, int J, int MOST, int PER_SM>
+template <typename X, typename R, bool WIDE, bool GRAD, int MOST, int PER_SM>
 __global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __grid_constant__ RingArgs g)
 {
+    constexpr int J = 2;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ unsigned long long full[kRingMost], empty[kRingMost];
-    __shared__ float2 sums[2][4][16];                                  // of the teams' warps
-    __shared__ unsigned int tops[2][4][16];
+    __shared__ unsigned long long full[kRingMost], empty[kRingMost], met[2];
+    __shared__ float2 sums[2][kRingTeams][16];                         // of the teams' warps
+    __shared__ unsigned int tops[2][kRingTeams][16];
+    __shared__ float4 blocks_sum[2][kRingMostBlocks];                  // written by the row's blocks
     const int workers = (int)blockDim.x - 32, warps = workers / 32 >> g.log_teams;
     if (threadIdx.x == 0) {
         for (int s = 0; s < g.stages; ++s) {
             mbar_init(smem_u32(&full[s]), 1);
             mbar_init(smem_u32(&empty[s]), workers / 32);
         }
+        mbar_init(smem_u32(&met[0]), 1);
+        mbar_init(smem_u32(&met[1]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    const bool shared_row = g.blocks > 1;
+    if (shared_row) cluster_sync();
+    behind_the_last();
+    const int rank = shared_row ? (int)cluster_rank() : 0, c0 = rank * g.slice;
+    const int row_dim = GRAD ? g.b.dim : g.f.dim, dim = min(g.slice, row_dim - c0);
+    const long long first_step = blockIdx.x / g.blocks, step_stride = gridDim.x / g.blocks;
     if ((int)threadIdx.x >= workers) {
-        ring_copy<WIDE>(g, smem_u32(smem), full, empty);
+        ring_copy<WIDE>(g, c0, dim, first_step, step_stride, smem_u32(smem), full, empty);
+        if (shared_row) cluster_sync();
         return;
     }
     const int team = (int)(threadIdx.x >> 5) / warps, lanes = 32 * warps, lane = (int)threadIdx.x - team * lanes;
-    const int dim = GRAD ? g.b.dim : g.f.dim;
     const float eps = GRAD ? g.b.eps : g.f.eps, inv_dim = GRAD ? g.b.inv_dim : g.f.inv_dim;
     float2 w[J][4], acc[GRAD ? J : 1][4] = {};
+    {
+        const void *weights = GRAD ? g.b.w : g.f.w;
+        const int type = GRAD ? g.b.wtype : g.f.wtype;
+        if (weights) weights = static_cast<const char *>(weights) + c0 * elem_bytes(type);
 #pragma unroll
-    for (int j = 0; j < J; ++j) ring_weights<WIDE>(GRAD ? g.b.w : g.f.w, GRAD ? g.b.wtype : g.f.wtype, lane, lanes, j, dim, w[j]);
+        for (int j = 0; j < J; ++j) ring_weights<WIDE>(weights, type, lane, lanes, j, dim, w[j]);
+    }
     bool ok = true;
     int slot = 0, turn = 0;
-    uint32_t phase = 0;
-    for (long long step = blockIdx.x; step < g.steps; step += gridDim.x, turn ^= 1) {
+    uint32_t phase = 0, meeting = 0;
+    // this block's part of a row's sums (or largest), joined with the others' in their order
+    auto meet = [&](float2 mine, unsigned int top) {
+        float4 r = make_float4(mine.x, mine.y, __uint_as_float(top), 0.f);
+        if (!shared_row) return r;
+        const int at = meeting & 1;
+        if ((int)threadIdx.x < g.blocks) {                             // (one row at a time: one team)
+            if (threadIdx.x == 0) mbar_expect_tx(smem_u32(&met[at]), 16u * g.blocks);
+            asm volatile(
+                "{\n\t.reg .b32 a, m;\n\t"
+                "mapa.shared::cluster.u32 a, %0, %2;\n\t"
+                "mapa.shared::cluster.u32 m, %1, %2;\n\t"
+                "st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %5}, [m];\n\t}"
+                ::"r"(smem_u32(&blocks_sum[at][rank])), "r"(smem_u32(&met[at])), "r"(threadIdx.x), "f"(r.x), "f"(r.y), "f"(r.z)
+                : "memory");
+        }
+        if (ok && !mbar_wait_bounded(smem_u32(&met[at]), meeting >> 1 & 1u)) {
+            ok = false;
+            report_status(g.status, FPSK_ERR_TIMEOUT);
+        }
+        ++meeting;
+        r = blocks_sum[at][0];
+        for (int b = 1; b < g.blocks; ++b) {
+            const float4 o = blocks_sum[at][b];
+            r = make_float4(r.x + o.x, r.y + o.y, __uint_as_float(max(__float_as_uint(r.z), __float_as_uint(o.z))), 0.f);
+        }
+        return r;
+    };
+    const int log_group = GRAD ? 0 : 31 - __clz(max(g.f.group, 1));
+    for (long long step = first_step; step < g.steps; step += step_stride, turn ^= 1) {
         const long long row = (step << g.log_teams) + team;
         const bool live = row < g.n;
         const int here = live ? dim : 0;
         if (ok && !mbar_wait_bounded(smem_u32(&full[slot]), phase)) ok = false;           // (the copying warp tells)
         auto input = [&](int i) {
-            const int shift = WIDE ? 0 : (int)(reinterpret_cast<uintptr_t>(g.in[i].base + row * g.in[i].stride) & 15);
+            const int shift = WIDE ? 0 : (int)(reinterpret_cast<uintptr_t>(g.in[i].base + row * g.in[i].stride + (long long)c0 * g.in[i].size) & 15);
             return smem + slot * g.stage_bytes + team * g.row_bytes + g.in[i].at + shift;
         };
         auto release = [&] {
@@ -526,7 +600,7 @@ __global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __gri
                     sg = __ffma2_rn(h[i], __fmul2_rn(d[i], w[j][i]), sg);
                 }
             }
-            const float2 s = ring_sum(make_float2(sh.x + sh.y, sg.x + sg.y), warps, team, sums[turn][team]);
+            const float4 s = meet(ring_sum(make_float2(sh.x + sh.y, sg.x + sg.y), warps, team, sums[turn][team]), 0u);
             const float r = rsqrtf(fmaf(s.x, inv_dim, eps));
             // dx = (dy w - h r^2 mean(dy w h)) r + dh
             const float2 rr = both(r), off = both(-s.y * r * inv_dim * r);
@@ -547,7 +621,7 @@ __global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __gri
                     for (int i = 0; i < 4; ++i) d[i] = __fadd2_rn(d[i], h[i]);
                 }
                 if (j == J - 1) release();
-                if (live) ring_store<WIDE>(static_cast<R *>(g.b.dx) + row * g.b.dxs, lane, lanes, j, dim, d);
+                if (live) ring_store<WIDE>(static_cast<R *>(g.b.dx) + row * g.b.dxs + c0, lane, lanes, j, dim, d);
             }
         } else {
             float2 h[J][4];
@@ -561,11 +635,11 @@ __global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __gri
                     for (int i = 0; i < 4; ++i) h[j][i] = __fadd2_rn(h[j][i], b[i]);
                 }
                 if (j == J - 1) release();
-                if (live && g.f.hout) ring_store<WIDE>(static_cast<R *>(g.f.hout) + row * g.f.hs, lane, lanes, j, dim, h[j]);
+                if (live && g.f.hout) ring_store<WIDE>(static_cast<R *>(g.f.hout) + row * g.f.hs + c0, lane, lanes, j, dim, h[j]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sh = __ffma2_rn(h[j][i], h[j][i], sh);
             }
-            const float2 s = ring_sum(make_float2(sh.x + sh.y, 0.f), warps, team, sums[turn][team]);
+            const float4 s = meet(ring_sum(make_float2(sh.x + sh.y, 0.f), warps, team, sums[turn][team]), 0u);
             const float2 rr = both(rsqrtf(fmaf(s.x, inv_dim, eps)));
 #pragma unroll
             for (int j = 0; j < J; ++j)
@@ -574,7 +648,7 @@ __global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __gri
             if (g.f.ytype != FPSK_ELEM_E4M3) {
                 if (live) {
 #pragma unroll
-                    for (int j = 0; j < J; ++j) ring_store_any<WIDE>(g.f.y, g.f.ytype, row * g.f.ys, lane, lanes, j, dim, h[j]);
+                    for (int j = 0; j < J; ++j) ring_store_any<WIDE>(g.f.y, g.f.ytype, row * g.f.ys + c0, lane, lanes, j, dim, h[j]);
                 }
             } else if (WIDE) {
                 // (a vector's eight channels are in one group, and a group's vectors in neighbouring lanes)
@@ -588,31 +662,39 @@ __global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __gri
                     most = max(most, top[j]);
                 }
                 float whole = 1.f;
-                if (g.f.group == 0) {
+                if (g.f.group) {
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1)
+                        if (8 * o < g.f.group) {
+#pragma unroll
+                            for (int j = 0; j < J; ++j) top[j] = max(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], o));
+                        }
+                } else {
                     most = __reduce_max_sync(0xFFFFFFFFu, most);
-                    if ((threadIdx.x & 31) == 0) tops[turn][team][lane >> 5] = most;
-                    bar_sync(1 + team, lanes);
-                    most = __reduce_max_sync(0xFFFFFFFFu, (lane & 31) < warps ? tops[turn][team][lane & 31] : 0u);
-                    whole = e4m3_scale(most);
-                    if (live && lane == 0) g.f.scale[row * g.f.ss] = whole;
+                    if (warps > 1) {
+                        if ((threadIdx.x & 31) == 0) tops[turn][team][lane >> 5] = most;
+                        bar_sync(1 + team, lanes);
+                        most = __reduce_max_sync(0xFFFFFFFFu, (lane & 31) < warps ? tops[turn][team][lane & 31] : 0u);
+                    }
+                    whole = e4m3_scale(__float_as_uint(meet(both(0.f), most).z));
+                    if (live && lane == 0 && rank == 0) g.f.scale[row * g.f.ss] = whole;
                 }
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     const int c = 8 * (lane + j * lanes);
                     float scale = whole;
                     if (g.f.group) {
-                        for (int o = 1; o < g.f.group / 8; o <<= 1) top[j] = max(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], o));
                         scale = e4m3_scale(top[j]);
-                        if (c < here && (c & (g.f.group - 1)) == 0) g.f.scale[row * g.f.ss + c / g.f.group] = scale;
+                        if (c < here && (c & (g.f.group - 1)) == 0) g.f.scale[row * g.f.ss + (c0 + c >> log_group)] = scale;
                     }
-                    const float2 over = both(__frcp_rn(scale));
+                    const float2 by = both(over(scale));
                     unsigned int q[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float2 y = __fmul2_rn(h[j][i], over);
+                        const float2 y = __fmul2_rn(h[j][i], by);
                         q[i] = e4m3_pair(y.x, y.y);
                     }
-                    if (c < here) *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(g.f.y) + row * g.f.ys + c) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+                    if (c < here) *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(g.f.y) + row * g.f.ys + c0 + c) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
                 }
             }
         }
@@ -621,73 +703,68 @@ __global__ void __launch_bounds__(MOST, PER_SM) add_norm_ring_kernel(const __gri
             phase ^= 1u;
         }
     }
-    if (!GRAD || !g.b.part) return;
-    float *part = g.b.part + (((long long)blockIdx.x << g.log_teams) + team) * dim;
+    if (GRAD && g.b.part) {
+        float *part = g.b.part + ((first_step << g.log_teams) + team) * row_dim + c0;
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+        for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = channel<WIDE>(lane, lanes, j, i);
-            if (c < dim) part[c] = i & 1 ? acc[GRAD ? j : 0][i / 2].y : acc[GRAD ? j : 0][i / 2].x;
-        }
+            for (int i = 0; i < 8; ++i) {
+                const int c = channel<WIDE>(lane, lanes, j, i);
+                if (c < dim) part[c] = i & 1 ? acc[GRAD ? j : 0][i / 2].y : acc[GRAD ? j : 0][i / 2].x;
+            }
+    }
+    if (shared_row) cluster_sync();                                    // no block leaves before what the others send it
 }
 
-// Whether the ring takes a call, and how.  A thread has sixteen channels, or 32 where a row would take more than sixteen warps; a block
-// has four to eight warps that work, and one row for each eight of them.  Up to 4096 channels two blocks share an SM, above one has it.
-constexpr int kRingOne = 220 * 1024, kRingHalf = 110 * 1024;
+// Whether the ring takes a call, and how.  A thread has sixteen channels and a block up to eight warps that work, two blocks to an SM:
+// one row, or as many short ones as fill them.  Above 4096 channels a row has sixteen warps of a block that has its SM to itself, above 8192 two or
+// four such blocks.  (Two blocks of eight warps for 8192 channels would leave each a ring of two stages.)
+constexpr int kRingOne = 218 * 1024, kRingHalf = 108 * 1024;
 static bool ring_plan(RingArgs &g, int dim, bool wide, int &threads)
 {
-    if (dim <= 512 || dim > 16384) return false;
-    int warps = 2;
-    while (warps < 16 && 32 * 16 * warps < dim) warps *= 2;
-    g.log_teams = warps >= 8 ? 0 : warps == 4 ? 1 : 2;
+    if (dim <= 128) return false;
+    g.blocks = dim <= 8192 ? 1 : dim <= 16384 ? 2 : 4;
+    // (a multiple of the largest group of channels with one scale)
+    g.slice = g.blocks == 1 ? dim : ((dim + g.blocks - 1) / g.blocks + 255) / 256 * 256;
+    const int warps = (g.slice + 511) / 512;
+    if (warps == 1 && !wide) return false;                             // (eight rows' edges are too many for the copying warp)
+    g.log_teams = warps > 4 ? 0 : warps > 2 ? 1 : warps > 1 ? 2 : 3;
     g.teams = 1 << g.log_teams;
     threads = 32 * (warps * g.teams + 1);
     g.row_bytes = 0;
     for (int i = 0; i < g.inputs; ++i) {
         g.in[i].at = g.row_bytes;
-        g.row_bytes += (g.in[i].bytes + 15) / 16 * 16 + (wide ? 0 : 16);
+        g.row_bytes += (g.slice * g.in[i].size + 15) / 16 * 16 + (wide ? 0 : 16);
     }
     g.stage_bytes = (int)align_up((size_t)g.row_bytes * g.teams, 128);
-    g.stages = (warps < 16 ? kRingHalf : kRingOne) / g.stage_bytes;
+    g.stages = (warps <= 8 ? kRingHalf : kRingOne) / g.stage_bytes;
     if (g.stages < 2) return false;
     if (g.stages > kRingMost) g.stages = kRingMost;
     g.steps = (g.n + g.teams - 1) >> g.log_teams;
-    return g.steps >= 2 * kSms;
+    return g.steps * g.blocks >= 2 * kSms;
 }
-static unsigned ring_blocks(const RingArgs &g, int threads)
-{
-    const long long most = (long long)kSms * (threads > 288 ? 1 : 2);
-    return (unsigned)(g.steps < most ? g.steps : most);
-}
+// rows of partial weight gradients at most
+static int ring_most(const RingArgs &g, int threads) { return kSms * (threads > 288 ? 1 : 2) / g.blocks; }
 
-template <typename X, typename R, bool GRAD> static fpsk_status launch_ring(const RingArgs &g, bool wide, int dim, int threads, cudaStream_t st)
+template <typename X, typename R, bool GRAD> static fpsk_status launch_ring(const RingArgs &g, bool wide, int threads, int &rows, cudaStream_t st)
 {
-    const size_t bytes = (size_t)g.stages * g.stage_bytes;
-#define FPSK_RING(WIDE, J, MOST, PER_SM)                                                                                                         \
-    do {                                                                                                                                         \
-        auto kernel = add_norm_ring_kernel<X, R, WIDE, GRAD, J, MOST, PER_SM>;                                                                   \
-        FPSK_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingOne));                                       \
-        kernel<<<ring_blocks(g, threads), threads, bytes, st>>>(g);                                                                              \
-    } while (0)
-    if (threads <= 288) {
-        if (wide) FPSK_RING(true, 2, 288, 2);
-        else FPSK_RING(false, 2, 288, 2);
-    } else if (dim <= 8192) {
-        if (wide) FPSK_RING(true, 2, 544, 1);
-        else FPSK_RING(false, 2, 544, 1);
-    } else {
-        if (wide) FPSK_RING(true, 4, 544, 1);
-        else FPSK_RING(false, 4, 544, 1);
-    }
-#undef FPSK_RING
+    Launch launch((unsigned)g.blocks, threads, (size_t)g.stages * g.stage_bytes, g.blocks, st);
+    void (*kernel)(RingArgs) = threads <= 288 ? (wide ? add_norm_ring_kernel<X, R, true, GRAD, 288, 2> : add_norm_ring_kernel<X, R, false, GRAD, 288, 2>)
+                                              : (wide ? add_norm_ring_kernel<X, R, true, GRAD, 544, 1> : add_norm_ring_kernel<X, R, false, GRAD, 544, 1>);
+    int most = 1;
+    FPSK_CUDA_OK(clusters_at_once(reinterpret_cast<const void *>(kernel), launch.cfg, &most));
+    if (most > ring_most(g, threads)) most = ring_most(g, threads);
+    if (most > g.steps) most = (int)g.steps;
+    rows = most * g.teams;
+    launch.cfg.gridDim = dim3((unsigned)(most * g.blocks));
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&launch.cfg, kernel, g));
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
-static RingRows ring_rows(const void *p, long long stride, int dim, int type)
+static RingRows ring_rows(const void *p, long long stride, int type)
 {
     const int size = elem_bytes(type);
-    return RingRows{static_cast<const char *>(p), stride * size, dim * size, size, 0};
+    return RingRows{static_cast<const char *>(p), stride * size, size, 0};
 }
 
 template <typename X, typename R> static fpsk_status launch_norm(const NormArgs &g, bool wide, int xtype, int rtype, int32_t *d_status, cudaStream_t st)
@@ -696,19 +773,19 @@ template <typename X, typename R> static fpsk_status launch_norm(const NormArgs 
         RingArgs r = {};
         const bool whole = wide && g.dim % 8 == 0;
         r.f = g;
-        r.in[0] = ring_rows(g.x, g.xs, g.dim, xtype);
-        r.in[1] = ring_rows(g.res, g.rs, g.dim, rtype);
+        r.in[0] = ring_rows(g.x, g.xs, xtype);
+        r.in[1] = ring_rows(g.res, g.rs, rtype);
         r.inputs = g.res ? 2 : 1;
         r.n = g.n;
         r.status = d_status;
-        int threads;
-        if ((whole || g.ytype != FPSK_ELEM_E4M3) && ring_plan(r, g.dim, whole, threads)) return launch_ring<X, R, false>(r, whole, g.dim, threads, st);
+        int threads, rows;
+        if ((whole || g.ytype != FPSK_ELEM_E4M3) && ring_plan(r, g.dim, whole, threads)) return launch_ring<X, R, false>(r, whole, threads, rows, st);
     }
     const int threads = g.warps > 8 ? 32 * g.warps : kNormThreads, teams = threads / 32 / g.warps;
     const long long steps = (g.n + teams - 1) / teams, most = 1LL << 20;
     const unsigned blocks = (unsigned)(steps < most ? steps : most);
-    if (wide) add_norm_kernel<X, R, true><<<blocks, threads, 0, st>>>(g);
-    else add_norm_kernel<X, R, false><<<blocks, threads, 0, st>>>(g);
+    Launch launch(blocks, threads, 0, 1, st);
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&launch.cfg, wide ? add_norm_kernel<X, R, true> : add_norm_kernel<X, R, false>, g));
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
@@ -726,38 +803,29 @@ template <typename X, typename G> static fpsk_status launch_norm_grad(NormGradAr
     RingArgs r = {};
     const bool whole = wide && g.dim % 8 == 0;
     r.b = g;
-    r.in[0] = ring_rows(g.h, g.hs, g.dim, htype);
-    r.in[1] = ring_rows(g.dy, g.dys, g.dim, gtype);
-    r.in[2] = ring_rows(g.dh, g.dhs, g.dim, gtype);
+    r.in[0] = ring_rows(g.h, g.hs, htype);
+    r.in[1] = ring_rows(g.dy, g.dys, gtype);
+    r.in[2] = ring_rows(g.dh, g.dhs, gtype);
     r.inputs = g.dh ? 3 : 2;
     r.n = g.n;
     r.status = d_status;
-    int ring_threads;
+    int ring_threads, rows;
     if (ring_plan(r, g.dim, whole, ring_threads)) {
-        const fpsk_status rc = launch_ring<X, G, true>(r, whole, g.dim, ring_threads, st);
-        if (rc != FPSK_OK || !dw) return rc;
-        add_norm_sum_kernel<<<(unsigned)(g.dim + 31) / 32, 1024, 0, st>>>(g.part, (int)ring_blocks(r, ring_threads) * r.teams, g.dim, dw);
-        FPSK_LAUNCH_CHECK();
-        return FPSK_OK;
+        const fpsk_status rc = launch_ring<X, G, true>(r, whole, ring_threads, rows, st);
+        return rc != FPSK_OK || !dw ? rc : launch_sum(g.part, rows, g.dim, dw, st);
     }
     const int threads = g.warps > 8 ? 32 * g.warps : kNormThreads, teams = threads / 32 / g.warps;
     const long long steps = (g.n + teams - 1) / teams;
     const unsigned blocks = (unsigned)(steps < kNormGradBlocks ? steps : kNormGradBlocks);
     if (blocks) {
-        if (threads > 512) {
-            if (wide) add_norm_grad_kernel<X, G, true, 1024><<<blocks, threads, 0, st>>>(g);
-            else add_norm_grad_kernel<X, G, false, 1024><<<blocks, threads, 0, st>>>(g);
-        } else {
-            if (wide) add_norm_grad_kernel<X, G, true, 512><<<blocks, threads, 0, st>>>(g);
-            else add_norm_grad_kernel<X, G, false, 512><<<blocks, threads, 0, st>>>(g);
-        }
+        Launch launch(blocks, threads, 0, 1, st);
+        FPSK_CUDA_OK(cudaLaunchKernelEx(&launch.cfg,
+                                        threads > 512 ? (wide ? add_norm_grad_kernel<X, G, true, 1024> : add_norm_grad_kernel<X, G, false, 1024>)
+                                                      : (wide ? add_norm_grad_kernel<X, G, true, 512> : add_norm_grad_kernel<X, G, false, 512>),
+                                        g));
         FPSK_LAUNCH_CHECK();
     }
-    if (dw) {
-        add_norm_sum_kernel<<<(unsigned)(g.dim + 31) / 32, 1024, 0, st>>>(g.part, (int)blocks * teams, g.dim, dw);
-        FPSK_LAUNCH_CHECK();
-    }
-    return FPSK_OK;
+    return dw ? launch_sum(g.part, (int)blocks * teams, g.dim, dw, st) : FPSK_OK;
 }
 
 }  // namespace fpsk

@@ -95,6 +95,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
     for (int i = tid; i < g.map_words; i += blockDim.x) reinterpret_cast<unsigned int *>(smem + g.map_at)[i] = 0;
     __syncthreads();
     cluster_sync();
+    behind_the_last();
     // Every wait is bounded; once one has given up the others are passed over, and all roles still run to their ends.
     bool ok = true;
     // (asked for a row ahead: the answer takes a microsecond)
@@ -138,6 +139,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                     }
                 }
             }
+            let_the_next();
             // no copy is left in flight
             for (unsigned int back = min(k, (unsigned int)kStages); back; --back) {
                 const unsigned int piece = k - back;
@@ -536,25 +538,15 @@ template <typename X, typename G, int MODE> static fpsk_status launch_distill(Di
     g.teacher_at = kStages * kPiece;
     g.map_at = g.teacher_at + teacher;
     g.map_words = map_bytes(g.blocks) / 4;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)g.blocks);
-    cfg.blockDim = dim3(kWorkers + 32 + 32 * g.teachers);
-    cfg.dynamicSmemBytes = (size_t)g.map_at + map_bytes(g.blocks);
-    cfg.stream = st;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = g.blocks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    Launch launch((unsigned)g.blocks, kWorkers + 32 + 32 * g.teachers, (size_t)g.map_at + map_bytes(g.blocks), g.blocks, st);
     auto kernel = distill_kernel<X, G, MODE>;
     int most = 1;
-    FPSK_CUDA_OK(clusters_at_once(reinterpret_cast<const void *>(kernel), cfg, &most));
+    FPSK_CUDA_OK(clusters_at_once(reinterpret_cast<const void *>(kernel), launch.cfg, &most));
     // (rows too long for that even with the most blocks each: fewer at a time)
     if (MODE == kLossAndGrad && g.blocks == kRowMostBlocks && most > kLongRowsInL2 / row_bytes) most = (int)(kLongRowsInL2 / row_bytes);
     if (most < 1) most = 1;
-    cfg.gridDim = dim3((unsigned)((g.rows < most ? g.rows : most) * g.blocks));
-    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, g));
+    launch.cfg.gridDim = dim3((unsigned)((g.rows < most ? g.rows : most) * g.blocks));
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&launch.cfg, kernel, g));
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }

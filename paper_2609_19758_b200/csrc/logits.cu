@@ -247,6 +247,7 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
     }
     __syncthreads();
     cluster_sync();
+    behind_the_last();
     // Every wait is bounded; once one has given up the others are passed over, and all roles still run to their ends.
     bool ok = true;
     auto wait = [&](unsigned long long &bar, uint32_t parity) {
@@ -301,6 +302,7 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                 }
             }
         }
+        let_the_next();
         // no copy is left in flight
         if (lane == 0)
             for (unsigned int back = min(k, (unsigned int)kRowStages); back; --back) {
@@ -584,21 +586,11 @@ template <typename X, typename O, typename W> static fpsk_status launch_logits(L
     g.chunk = (pieces < chunk_tokens / N / kRowPieceVecs ? pieces : chunk_tokens / N / kRowPieceVecs) * kRowPieceVecs;
     g.words_at = g.in_place ? 0 : Workers<WORDS>::stages * kRowPiece;
     auto kernel = adjust_logits_kernel<X, O, W>;
-    cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(Workers<WORDS>::threads);
-    cfg.dynamicSmemBytes = (size_t)g.words_at + (WORDS ? (g.chunk * N + 16) * sizeof(Wd) : 0);
-    cfg.stream = st;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = g.blocks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3((unsigned)g.blocks);
+    Launch launch((unsigned)g.blocks, Workers<WORDS>::threads, (size_t)g.words_at + (WORDS ? (g.chunk * N + 16) * sizeof(Wd) : 0), g.blocks, st);
     int most = 1;
-    FPSK_CUDA_OK(clusters_at_once(reinterpret_cast<const void *>(kernel), cfg, &most));
-    cfg.gridDim = dim3((unsigned)((g.rows < most ? g.rows : most) * g.blocks));
-    FPSK_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, g));
+    FPSK_CUDA_OK(clusters_at_once(reinterpret_cast<const void *>(kernel), launch.cfg, &most));
+    launch.cfg.gridDim = dim3((unsigned)((g.rows < most ? g.rows : most) * g.blocks));
+    FPSK_CUDA_OK(cudaLaunchKernelEx(&launch.cfg, kernel, g));
     FPSK_LAUNCH_CHECK();
     return FPSK_OK;
 }
