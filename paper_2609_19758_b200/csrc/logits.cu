@@ -323,7 +323,7 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
 
             // the row's parameters, asked for together; the history's first tokens before their number is known
             const int *history = WORDS && g.history ? g.history + row * g.history_stride : nullptr;
-            constexpr int kEarly = 8;
+            constexpr int kEarly = 4;
             int early[kEarly];
             auto first_of_history = [&] {
 #pragma unroll
@@ -338,6 +338,14 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
             if (WORDS && g.bias_ptr) {
                 b0 = max(0LL, (long long)g.bias_ptr[row]);
                 b1 = min(g.n_biases, (long long)g.bias_ptr[row + 1]);
+            }
+            // the first biases and their logits as well
+            int bias_v = -1;
+            float bias_b = 0.f, bias_l = 0.f;
+            if (WORDS && b0 + tid < b1) {
+                bias_v = g.bias_token[b0 + tid];
+                bias_b = g.bias_value[b0 + tid];
+                if (sl.own_of(bias_v) >= 0) bias_l = Elem<X>::to_f(x[bias_v]);
             }
             bool nothing;
             const int *mask = mask_of(row, nothing);
@@ -399,7 +407,7 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                             if (i0 + i * kRowWorkers < n_hist && now[i] >= 0) count(i0 + i * kRowWorkers, now[i]);
                     }
                     for (long long i = b0 + tid; i < b1; i += kRowWorkers) {
-                        const int at = slot(g.bias_token[i]);
+                        const int at = slot(i == b0 + tid ? bias_v : g.bias_token[i]);
                         if (at >= 0 && F::mark(words, at, F::kBiased) & F::kBiased) F::mark(words, at, F::kBiasedTwice);
                     }
                     bar_sync(1, kRowWorkers);
@@ -458,34 +466,34 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                                 if (OUT) store_vec<Out, N>(out + e + k * kRowWorkers * N, wide, z[k]);
                             }
                         } else {
+                            int waiting = 0;
 #pragma unroll
                             for (int k = 0; k < kEachVecs; ++k) {
                                 const int vk = v + k * kRowWorkers, ek = e + k * kRowWorkers * N;
                                 const bool here = vk < c1;
                                 const unsigned int bits = !here ? 0u : masks ? allowed(ek) : kAll;
                                 const uint4 u = piece[k * kRowWorkers];
-                                const unsigned int some = WORDS && here ? F::template some<N>(words, (vk - c0) * N) : 0u;
-                                if (WORDS && __any_sync(0xFFFFFFFFu, some != 0)) put_off(some, vk, u);
                                 Vec<X>::open(u, z[k]);
                                 if (bits != kAll) {
 #pragma unroll
                                     for (int j = 0; j < N; ++j)
                                         if (!(bits >> j & 1u)) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
                                 }
-                                if (OUT && here) {
-                                    if (!some) {
-                                        store_vec<Out, N>(out + ek, wide, z[k]);
-                                    } else {
+                                // (touched tokens as they are: their turn comes)
+                                if (OUT && here) store_vec<Out, N>(out + ek, wide, z[k]);
+                                if (WORDS) {
+                                    const unsigned int some = here ? F::template some<N>(words, (vk - c0) * N) : 0u;
+                                    if (pick && some) {
 #pragma unroll
                                         for (int j = 0; j < N; ++j)
-                                            if (!(some >> j & 1u)) out[ek + j] = Elem<Out>::from_f(j & 1 ? z[k][j / 2].y : z[k][j / 2].x);
+                                            if (some >> j & 1u) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
                                     }
+                                    waiting |= (some != 0) << k;
                                 }
-                                if (some && pick) {
-#pragma unroll
-                                    for (int j = 0; j < N; ++j)
-                                        if (some >> j & 1u) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
-                                }
+                            }
+                            if (WORDS && __any_sync(0xFFFFFFFFu, waiting != 0)) {
+#pragma unroll 1
+                                for (int k = 0; k < kEachVecs; ++k) put_off(waiting >> k & 1, v + k * kRowWorkers, piece[k * kRowWorkers]);
                             }
                         }
                         __syncwarp();
@@ -498,11 +506,13 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                     }
                 }
                 if (WORDS && n_touched) adjust(n_touched);
-                if (WORDS) {
+                if (WORDS && b0 < b1) {
+                    bar_sync(1, kRowWorkers);                          // (the stream has stored them as they were)
                     for (long long i = b0 + tid; i < b1; i += kRowWorkers) {
-                        const int v = g.bias_token[i], where = slot(v);
+                        const bool known = i == b0 + tid;
+                        const int v = known ? bias_v : g.bias_token[i], where = slot(v);
                         if (where < 0) continue;
-                        float b = g.bias_value[i];
+                        float b = known ? bias_b : g.bias_value[i];
                         if (words[where] & F::kBiasedTwice) {          // the first of its entries does it, in the list's order
                             bool mine_to_do = true;
                             b = 0.f;
@@ -513,7 +523,7 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                                 }
                             if (!mine_to_do) continue;
                         }
-                        single(v, adjusted(Elem<X>::to_f(x[v]), words[where]) + b);
+                        single(v, adjusted(known && where < chunk_tokens ? bias_l : Elem<X>::to_f(x[v]), words[where]) + b);
                     }
                 }
                 if (loose >= 0) {
