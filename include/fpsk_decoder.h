@@ -10,7 +10,8 @@
  * without a host synchronisation, errors are return codes, nothing throws.  Strides are in ELEMENTS between rows; the elements
  * of a row are contiguous.  Types are fpsk_elem; a row may start anywhere that its type may.  Rows of 0 do nothing.  Sums, norms
  * and exponentials are FP32 in a fixed order: a call gives the same bits each time on one device.  d_status is a device int32 or
- * NULL, to which the kernels only ever write an fpsk_status other than FPSK_OK (FPSK_ERR_TIMEOUT: a device-side wait gave up).
+ * NULL, to which the kernels only ever write an fpsk_status other than FPSK_OK (FPSK_ERR_TIMEOUT: a device-side wait gave up, and
+ * what the call wrote is not to be used).
  */
 #ifndef FPSK_DECODER_H
 #define FPSK_DECODER_H
@@ -65,6 +66,7 @@ size_t fpsk_add_norm_workspace_bytes(int32_t dim);
 fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, void *workspace, size_t ws_bytes, int32_t *d_status, void *stream);
 
 #define FPSK_MAX_VOCAB (1 << 23)
+#define FPSK_MAX_HISTORY (1 << 28)
 
 /* What is done to a row of logits before a token is picked, in this order, in FP32:
  *   tokens that the row's history holds:      z > 0 ? z / repetition : z * repetition

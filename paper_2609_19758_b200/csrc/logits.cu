@@ -630,7 +630,7 @@ extern "C" fpsk_status fpsk_adjust_logits(const fpsk_logits *a, int32_t *d_statu
     if (a->logits_stride < 0 || (a->out && a->n_rows > 1 && a->out_stride < a->vocab)) return FPSK_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(a->logits) % elem_bytes(a->logits_type) || (a->out && reinterpret_cast<uintptr_t>(a->out) % elem_bytes(a->out_type)))
         return FPSK_ERR_ALIGN;
-    if (a->history && (a->history_width < 0 || a->history_stride < 0)) return FPSK_ERR_SHAPE;
+    if (a->history && (a->history_width < 0 || a->history_width > FPSK_MAX_HISTORY || a->history_stride < 0)) return FPSK_ERR_SHAPE;
     if (!a->history && (a->history_len || a->prompt_len || a->repetition || a->frequency || a->presence)) return FPSK_ERR_NULL;
     if (a->bias_ptr && (a->n_biases < 0 || (a->n_biases > 0 && (!a->bias_token || !a->bias_value)))) return FPSK_ERR_NULL;
     if (a->mask && (a->n_masks < 0 || a->mask_stride < 0 || (!a->mask_row && a->n_masks < a->n_rows))) return FPSK_ERR_SHAPE;

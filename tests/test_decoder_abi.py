@@ -36,6 +36,7 @@ def test_add_norm(lib):
     assert call(types=(F32, 0, 0, E4M3), group=48, scale=P) == call(types=(F32, 0, 0, E4M3), group=-32, scale=P) == fpsk.ERR_PARAM
     assert call(x=0) == call(y=0) == call(types=(F32, 0, 0, E4M3)) == fpsk.ERR_NULL
     assert call(types=(F32, 0, 0, E4M3), group=32, scale=P, strides=(64, 64, 64, 64, 1)) == fpsk.ERR_SHAPE
+    assert call(x=P + 2) == call(res=P + 1) == call(w=P + 1) == call(y=P + 2) == fpsk.ERR_ALIGN
     assert call(n=0, x=0, y=0) == fpsk.STATUS_OK
 
 
@@ -51,6 +52,7 @@ def test_add_norm_backward(lib):
     assert call(h=0) == call(dy=0) == call(dx=0) == call(dw=P) == fpsk.ERR_NULL
     assert call(dw=P, ws=P + 16, ws_bytes=1 << 30) == fpsk.ERR_ALIGN
     assert call(dw=P, ws=P, ws_bytes=255) == fpsk.ERR_WORKSPACE
+    assert call(h=P + 2) == call(dy=P + 1) == call(dh=P + 2) == call(dx=P + 3) == fpsk.ERR_ALIGN
     assert call(n=0, h=0, dy=0, dx=0) == fpsk.STATUS_OK
 
 
@@ -65,7 +67,8 @@ def test_adjust_logits(lib):
     assert call(n=-1) == call(n=1 << 31) == call(vocab=0) == call(vocab=(1 << 23) + 1) == call(strides=(100, 99)) == call(strides=(-1, 100)) == fpsk.ERR_SHAPE
     assert call(types=(E4M3, F32)) == call(types=(F32, E4M3)) == fpsk.ERR_DTYPE
     assert call(x=0) == call(out=0) == call(penalties=(P, 0, 0)) == call(history=(0, P, 0)) == call(bias=(P, 0, P), n_biases=3) == call(mask=(0, P)) == fpsk.ERR_NULL
-    assert call(history=(P, 0, 0), width=-1) == call(mask=(P, 0), mask_stride=-1) == fpsk.ERR_SHAPE
+    assert call(x=P + 2) == call(out=P + 1) == fpsk.ERR_ALIGN
+    assert call(history=(P, 0, 0), width=-1) == call(history=(P, 0, 0), width=(1 << 28) + 1) == call(mask=(P, 0), mask_stride=-1) == fpsk.ERR_SHAPE
     assert call(mask=(P, 0), mask_stride=4, n_masks=1) == fpsk.ERR_SHAPE            # fewer masks than rows, and nothing says whose
     assert call(n=0, x=0) == fpsk.STATUS_OK
 
@@ -79,6 +82,7 @@ def test_distill(lib):
         assert call(f, n=-1) == call(f, vocab=0) == call(f, top=-1) == call(f, top=1025) == call(f, strides=(100, 4, 4, 99)) == call(f, strides=(-1, 4, 4, 100)) == fpsk.ERR_SHAPE
         assert call(f, types=(E4M3, 4, F32, F32)) == call(f, types=(F32, 2, F32, F32)) == call(f, types=(F32, 8, E4M3, F32)) == call(f, types=(F32, 8, F32, E4M3)) == fpsk.ERR_DTYPE
         assert call(f, tau=0.0) == call(f, tau=-1.0) == call(f, tau=float("nan")) == call(f, tau=float("inf")) == call(f, tau=1e-39) == fpsk.ERR_PARAM
+        assert call(f, x=P + 2) == call(f, dx=P + 2) == fpsk.ERR_ALIGN
         assert call(f, x=0) == call(f, tok=0) == call(f, t=0) == fpsk.ERR_NULL
         assert call(f, n=0, x=0) == fpsk.STATUS_OK
     assert call(lib.fpsk_distill_loss, loss=0) == call(lib.fpsk_distill_loss_backward, lse=0) == call(lib.fpsk_distill_loss_backward, dx=0) == fpsk.ERR_NULL
