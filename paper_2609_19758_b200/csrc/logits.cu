@@ -39,7 +39,7 @@ struct LogitsArgs {
 
 // Threads that work: the history's counting is bound by its latency.
 template <bool WORDS> struct Workers {
-    static constexpr int n = WORDS ? 256 : 128, threads = n + 32, stages = WORDS ? 3 : 4;       // (three blocks to an SM, five)
+    static constexpr int n = WORDS ? 256 : 128, threads = n + 32, stages = 4;       // (three blocks to an SM, or five)
 };
 constexpr int kRowPiece = 8192, kRowPieceVecs = kRowPiece / 16;
 constexpr int kWordBytes = 32 * 1024;  // of the words of a chunk, at most
@@ -79,28 +79,20 @@ template <typename W> struct Word {
     static __device__ __forceinline__ unsigned int *home(W *words, int at) { return reinterpret_cast<unsigned int *>(words) + (sizeof(W) == 2 ? at >> 1 : at); }
     static __device__ __forceinline__ void count(W *words, int at) { atomicAdd(home(words, at), 1u << shift(at)); }
     static __device__ __forceinline__ unsigned int mark(W *words, int at, unsigned int bits) { return atomicOr(home(words, at), bits << shift(at)) >> shift(at); }
-    // which of N tokens have a word that is not 0; `at` is a multiple of N
-    template <int N> static __device__ __forceinline__ unsigned int some(const W *words, int at)
+    // whether any of N tokens has a word that is not 0; `at` is a multiple of N
+    template <int N> static __device__ __forceinline__ bool any(const W *words, int at)
     {
-        unsigned int w[N * sizeof(W) / 4], any = 0, which = 0;
         if (sizeof(W) * N == 8) {
             const uint2 u = *reinterpret_cast<const uint2 *>(words + at);
-            w[0] = u.x; w[1] = u.y;
-        } else {
-#pragma unroll
-            for (int i = 0; i < (int)(N * sizeof(W) / 16); ++i) {
-                const uint4 u = reinterpret_cast<const uint4 *>(words + at)[i];
-                w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
-            }
+            return u.x | u.y;
         }
+        unsigned int some = 0;
 #pragma unroll
-        for (int i = 0; i < (int)(N * sizeof(W) / 4); ++i) any |= w[i];
-        if (any) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (sizeof(W) == 2 ? w[j / 2] >> 16 * (j & 1) & 0xFFFFu : w[j % (N * sizeof(W) / 4)]) which |= 1u << j;
+        for (int i = 0; i < (int)(sizeof(W) * N / 16); ++i) {
+            const uint4 u = reinterpret_cast<const uint4 *>(words + at)[i];
+            some |= u.x | u.y | u.z | u.w;
         }
-        return which;
+        return some;
     }
 };
 
@@ -228,9 +220,6 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
     __shared__ unsigned long long keys[2][kRowWarps];
     __shared__ float2 sums[2][kRowWarps];
     __shared__ float4 blocks_sum[2][kRowMostBlocks];                   // written by the cluster's blocks: key (two halves), reference, sum
-    // vectors with tokens that the history touches, of each warp until there is one for each lane
-    __shared__ uint4 raw[WORDS ? kRowWarps : 1][WORDS ? 64 : 1];
-    __shared__ int touched[WORDS ? kRowWarps : 1][WORDS ? 64 : 1];
     Wd *words = reinterpret_cast<Wd *>(smem + g.words_at);             // of a chunk's tokens, of 8 in front of the row's vectors, 8 behind
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_rank();
@@ -352,11 +341,12 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
             if (nothing && tid == 0) report_status(g.status, FPSK_ERR_PARAM);
             const bool masks = mask || nothing;
             auto allowed = [&](int e) { return nothing ? 0u : mask ? mask_bits<N>(mask, e) : kAll; };
-            // z of a token, all but its biases and the mask; c: its word
+            // z of a token, all but its biases and the mask; c: its word.  (By one over the repetition: a unit at most from the quotient.)
+            const float inv_rep = 1.f / rep;
             auto adjusted = [&](float z, unsigned int c) {
-                if (c & (F::kInPrompt | F::kTimes)) z = z > 0.f ? __fdiv_rn(z, rep) : __fmul_rn(z, rep);
-                if (c & F::kTimes) z = __fsub_rn(z, __fadd_rn(__fmul_rn((float)(c & F::kTimes), freq), pres));
-                return z;
+                const float less = __fadd_rn(__fmul_rn((float)(c & F::kTimes), freq), pres);
+                if (c & (F::kInPrompt | F::kTimes)) z = __fmul_rn(z, z > 0.f ? inv_rep : rep);
+                return c & F::kTimes ? __fsub_rn(z, less) : z;
             };
 
             Picked p = {-INFINITY, kNoReference, 0.f, -1};
@@ -412,45 +402,33 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                     }
                     bar_sync(1, kRowWorkers);
                 }
-                // Touched vectors wait, as they are, until there is one for each lane.
-                int n_touched = 0;
-                auto adjust = [&](int n) {
-                    __syncwarp();
-                    n_touched -= n;
-                    const int own_vec = lane < n ? touched[warp][n_touched + lane] : c0, e = sl.token(own_vec * N);
+                // A vector's touched tokens; which of them have biases and wait for those.
+                auto adjust = [&](float2 (&z)[N / 2], int own_vec) {
                     const Wd *w = words + (own_vec - c0) * N;
-                    const X *l = reinterpret_cast<const X *>(&raw[warp][n_touched + (lane < n ? lane : 0)]);
-                    unsigned int rest = lane < n ? F::template some<N>(words, (own_vec - c0) * N) : 0u;
-                    while (rest) {                                     // (as often as the most touched of the vectors asks)
-                        const int j = __ffs(rest) - 1;
-                        rest &= rest - 1;
+                    unsigned int biased = 0;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
                         const unsigned int c = w[j];
-                        if (!(c & F::kBiased)) single(e + j, adjusted(Elem<X>::to_f(l[j]), c));
+                        float &y = j & 1 ? z[j / 2].y : z[j / 2].x;
+                        if (c & F::kBiased) biased |= 1u << j;
+                        else y = adjusted(y, c);
                     }
-                    __syncwarp();
-                };
-                // (all lanes) a vector that has touched tokens
-                auto put_off = [&](bool some, int own_vec, const uint4 &u) {
-                    const unsigned int who = __ballot_sync(0xFFFFFFFFu, some);
-                    if (some) {
-                        const int at = n_touched + __popc(who & ((1u << lane) - 1u));
-                        touched[warp][at] = own_vec;
-                        raw[warp][at] = u;
-                    }
-                    n_touched += __popc(who);
-                    if (n_touched >= 32) adjust(32);
+                    return biased;
                 };
                 if (g.in_place) {
                     for (int v0 = c0; v0 < c1; v0 += kRowWorkers) {
                         const int v = v0 + tid, e = sl.token(v0 * N) + tid * N;
                         const bool here = v < c1;
-                        const unsigned int some = WORDS && here ? F::template some<N>(words, (v - c0) * N) : 0u;
-                        if (WORDS) put_off(some, v, some ? *reinterpret_cast<const uint4 *>(x + e) : make_uint4(0u, 0u, 0u, 0u));
+                        const bool some = WORDS && here && F::template any<N>(words, (v - c0) * N);
                         const unsigned int bits = here ? allowed(e) : kAll;
-                        if (OUT && bits != kAll) {
+                        if (OUT && (some || bits != kAll)) {
+                            float2 z[N / 2];
+                            Vec<X>::open(*reinterpret_cast<const uint4 *>(x + e), z);
+                            if (WORDS && some) adjust(z, v);
 #pragma unroll
                             for (int j = 0; j < N; ++j)
-                                if (!((bits | some) >> j & 1u)) out[e + j] = Elem<Out>::from_f(-INFINITY);
+                                if (!(bits >> j & 1u)) (j & 1 ? z[j / 2].y : z[j / 2].x) = -INFINITY;
+                            store_vec<Out, N>(out + e, wide, z);
                         }
                     }
                 } else {
@@ -466,34 +444,26 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                                 if (OUT) store_vec<Out, N>(out + e + k * kRowWorkers * N, wide, z[k]);
                             }
                         } else {
-                            int waiting = 0;
 #pragma unroll
                             for (int k = 0; k < kEachVecs; ++k) {
                                 const int vk = v + k * kRowWorkers, ek = e + k * kRowWorkers * N;
                                 const bool here = vk < c1;
+                                Vec<X>::open(piece[k * kRowWorkers], z[k]);
+                                unsigned int biased = 0;
+                                if (WORDS && here && F::template any<N>(words, (vk - c0) * N)) biased = adjust(z[k], vk);
                                 const unsigned int bits = !here ? 0u : masks ? allowed(ek) : kAll;
-                                const uint4 u = piece[k * kRowWorkers];
-                                Vec<X>::open(u, z[k]);
                                 if (bits != kAll) {
 #pragma unroll
                                     for (int j = 0; j < N; ++j)
                                         if (!(bits >> j & 1u)) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
                                 }
-                                // (touched tokens as they are: their turn comes)
+                                // (biased tokens as they are: their turn comes)
                                 if (OUT && here) store_vec<Out, N>(out + ek, wide, z[k]);
-                                if (WORDS) {
-                                    const unsigned int some = here ? F::template some<N>(words, (vk - c0) * N) : 0u;
-                                    if (pick && some) {
+                                if (WORDS && pick && biased) {
 #pragma unroll
-                                        for (int j = 0; j < N; ++j)
-                                            if (some >> j & 1u) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
-                                    }
-                                    waiting |= (some != 0) << k;
+                                    for (int j = 0; j < N; ++j)
+                                        if (biased >> j & 1u) (j & 1 ? z[k][j / 2].y : z[k][j / 2].x) = -INFINITY;
                                 }
-                            }
-                            if (WORDS && __any_sync(0xFFFFFFFFu, waiting != 0)) {
-#pragma unroll 1
-                                for (int k = 0; k < kEachVecs; ++k) put_off(waiting >> k & 1, v + k * kRowWorkers, piece[k * kRowWorkers]);
                             }
                         }
                         __syncwarp();
@@ -505,7 +475,6 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                         if (pick) p.add<kEachVecs, N>(z, e, kRowWorkers * N, sum);
                     }
                 }
-                if (WORDS && n_touched) adjust(n_touched);
                 if (WORDS && b0 < b1) {
                     bar_sync(1, kRowWorkers);                          // (the stream has stored them as they were)
                     for (long long i = b0 + tid; i < b1; i += kRowWorkers) {
