@@ -4,8 +4,8 @@
 // Backwards: n = h r, g = dy w, dx = r (g - n sum(g n) / d) + dh, dw = sum over the rows of dy n.
 //
 // The forms here read a row from memory again for what they computed its sums from (it is in L1 or L2 by then).  They take what the ring
-// (add_norm_ring.cuh) does not: few rows, where one token of 4096 channels takes 3.6 us, the launch; up to 128 channels; rows too long for two
-// stages.
+// (add_norm_ring.cuh) does not: few rows, where one token of 4096 channels takes 3.6 us, the launch; up to 32 channels, or 512 in rows that start off
+// 16 bytes; rows too long for two stages.
 #include "add_norm.cuh"
 
 namespace fpsk {

@@ -575,7 +575,7 @@ template <typename X, typename O, typename W> static fpsk_status launch_logits(L
 }
 template <typename X> static fpsk_status launch_logits_typed(const LogitsArgs &g, int out_type, cudaStream_t st)
 {
-    // (16 bits: three of them flags)
+    // (16 bits: three of them flags.  96 rows of 131072 with histories of 4096 take 43 us with them and 52 with 32, 640 of 50257 93 and 140)
     const bool words = g.history || g.bias_ptr, narrow = !g.history || g.history_width < (int)Word<uint16_t>::kBiasedTwice;
 #define FPSK_OUT(O) (!words ? launch_logits<X, O, void>(g, st) : narrow ? launch_logits<X, O, uint16_t>(g, st) : launch_logits<X, O, uint32_t>(g, st))
     if (!g.out) return FPSK_OUT(void);
