@@ -69,7 +69,7 @@ fpsk_status fpsk_add_rms_norm_backward(const fpsk_add_norm_grad *a, void *worksp
 #define FPSK_MAX_HISTORY (1 << 28)
 
 /* What is done to a row of logits before a token is picked, in this order, in FP32:
- *   tokens that the row's history holds:      z > 0 ? z / repetition : z * repetition
+ *   tokens that the row's history holds:      z > 0 ? z / repetition : z * repetition     (by a product with 1 / repetition)
  *   c times behind the first prompt_len:      z -= frequency c + presence
  *   tokens of the row's list of biases:       z += the sum of their biases, in the list's order
  *   tokens whose bit of the row's mask is 0:  z = -inf, whatever the logit (NaN too)

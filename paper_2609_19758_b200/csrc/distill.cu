@@ -4,11 +4,17 @@
 // In powers of two, with c = log2(e) / tau and a reference M near the row's largest logit: S = sum 2^((x - M) c), q_v = 2^((x_v - M) c) / S,
 // log q_v = (x_v - M) / tau - ln S.  M and S stay apart to the end, so that nothing is rounded at the size of the logarithm.
 //
-// What bounds it is memory: the logits once, the gradient once.  The gradient needs S first, so a row has to stay on the chip from the
-// first look at it to the second: a cluster of blocks holds it in shared memory, each block a slice (131072 FP32 logits: eight times
-// 64 KB, three blocks to an SM).  One warp of a block copies pieces of 8 KB into a ring; eight warps sum a slice up, exchange (M, S)
-// through the cluster's shared memory, and write the gradient, freeing the pieces as they go for the next row's copies; one warp prepares the
-// teacher's probabilities for the next row and takes them off the gradient of the one before, so that neither is waited for.
+// What bounds it is memory: the logits once, the gradient once.  The gradient needs S first, so a row is looked at twice; the second look
+// finds it in L2 as long as the rows at work at a time are not too many bytes, which a cluster of blocks to a row sees to.  One warp of a
+// block copies pieces of 8 KB of its slice into a ring, once or twice over; four warps sum the slice up, exchange (M, S) through the
+// cluster's shared memory, and write the gradient; one or three warps prepare the teacher's probabilities for the next row and take them off the
+// gradient of the one before, so that neither is waited for.
+//
+// Measured: 4096 rows of 131072 FP32 logits with BF16 gradients 521 us in a burst (6.2 TB/s of logits and gradients, 0.95 of a copy),
+// 602 sustained, at the power limit; losses of 2048 rows of 65536 BF16 49 us (0.84; the special function unit, which makes the powers, is busy
+// for 66 %); loss, then gradient of 1500 x 50257 FP16 90 us; 5 rows of 131072 8.7 us.  Rows held in shared memory between the two looks
+// (eight slices of 64 KB, three blocks to an SM): 662 us, as fewer rows are at work at a time.  The gradient's factor folded into the
+// exponent, a product fewer for two elements: no faster.
 #include "decoder.cuh"
 
 namespace fpsk {
@@ -76,7 +82,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
     __shared__ float4 blocks_sum[2][kRowMostBlocks];                   // written by the cluster's blocks: M, S, the teacher's two
     __shared__ float2 warps_sum[2][kWorkers / 32];
     __shared__ float4 result[2], taught[2];                            // M, S, the teacher's two; K, xr, the teacher's two
-    __shared__ float teams[5][kMostTeachers];
+    __shared__ float teams[6][kMostTeachers], highest[2];              // highest: of the block's listed logits
     __shared__ int teams_twice[kMostTeachers], counts[2][kMostTeachers];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)cluster_rank();
@@ -108,6 +114,10 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
         }
     };
 
+    // FP32 gradients, and an lse that they are made from later, take their powers with the block's largest listed logit as reference at
+    // least: the largest powers, which are most of the sum and of the gradient, have exponents near 0 then, whose rounding is small (an
+    // error of 1.2e-6 relative, else, for logits of a normal distribution with larger ones listed).
+    const bool anchored = MODE == kLossAndGrad ? sizeof(G) == 4 : MODE == kLossOnly && g.lse;
     // the teacher's mass, from what it says: normalized its largest logit and 1 / s, else the mass itself
     auto mass_of = [&](float a0, float a1) { return g.normalize ? (a1 == 0.f ? 0.f : 1.f) : a0; };
 
@@ -220,7 +230,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             const Slice sl(x, g.vocab, g.blocks, rank, X());
 #pragma unroll
             for (int i = 0; i < kTogether; ++i)
-                if (losses ? token[i] >= 0 : MODE != kLossOnly && place(sl, token[i]) >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + token[i]));
+                if (losses ? token[i] >= 0 : (MODE != kLossOnly || anchored) && place(sl, token[i]) >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + token[i]));
         };
         // loss = sum p (log p - log q) = K + m ((M - xr) / tau + ln S), with a listed logit xr as reference; normalized, with
         // e = 2^((t - u) c), s = sum e, m = 1 and a listed tr:  K = sum e ((t - tr) - (x - xr)) / (tau s) + (tr - u) / tau - ln s;
@@ -228,7 +238,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
         auto prepare = [&](long long row, int b) {
             const X *x = static_cast<const X *>(g.x) + row * g.xs;
             const Slice sl(x, g.vocab, g.blocks, rank, X());
-            float u = kNoReference, s = 0.f, d = 0.f, tr = 0.f, xr = 0.f;
+            float u = kNoReference, s = 0.f, d = 0.f, tr = 0.f, xr = 0.f, high = kNoReference;
             int count = 0;
             for (int base = 0; base < g.top; base += all * kTogether) {            // (as often for each warp: there are barriers in it)
                 if (base) ask(row, base + me);
@@ -236,8 +246,13 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 float l[kTogether];
 #pragma unroll
                 for (int i = 0; i < kTogether; ++i) {
-                    at[i] = MODE != kLossOnly && t[i] != -INFINITY ? place(sl, token[i]) : -1;
+                    at[i] = (MODE != kLossOnly || anchored) && t[i] != -INFINITY ? place(sl, token[i]) : -1;
                     l[i] = at[i] >= 0 || (losses && token[i] >= 0) ? Elem<X>::to_f(x[token[i]]) : 0.f;
+                }
+                if (anchored) {
+#pragma unroll
+                    for (int i = 0; i < kTogether; ++i)
+                        if (at[i] >= 0 && l[i] < 3e38f) high = fmaxf(high, l[i]);
                 }
                 if (MODE != kLossOnly) {
 #pragma unroll
@@ -281,6 +296,10 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 }
             }
             if (MODE != kLossOnly && lane == 0) counts[b][my_warp] = count;
+            if (anchored) {
+                high = largest(high, 5);
+                if (me == 0) highest[b] = high;
+            }
             if (sums) {
                 if (g.normalize) {
                     const float top = largest(u, 2), f = exp2_fast((u - top) * ct);
@@ -407,6 +426,11 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             if (MODE != kGradOnly) {
                 RefSum r = {kNoReference, 0.f};
                 if (loose >= 0 && x_loose != -INFINITY) r = RefSum{x_loose, x_loose == x_loose ? 1.f : x_loose};
+                float floor = kNoReference;
+                if (anchored) {
+                    wait(ready[b], n >> 1 & 1u);
+                    floor = highest[b];
+                }
                 float2 s2 = make_float2(r.s, 0.f), minus = make_float2(-r.m, -r.m);
                 for (int v = sl.v0; v < sl.v1; v += kPieceVecs) {
                     wait(full[stage], phase);
@@ -416,7 +440,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                     // 2^100 or more (an infinity, a NaN): then it moves to the piece's largest and the piece is summed anew.  A
                     // reference below the row's largest costs no precision.
                     if (v == sl.v0 && tid < vecs && loose < 0) {
-                        const float top = vec_max<X>(piece[0]);
+                        const float top = fmaxf(vec_max<X>(piece[0]), floor);
                         if (top != -INFINITY) minus = make_float2(-top, -top);
                     }
                     float2 sum = make_float2(0.f, 0.f);
@@ -519,6 +543,8 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
     cluster_sync();                                                    // no block leaves before what the others send it
 }
 
+// (131072 FP32 logits, 512 KB a row: eight blocks to a row 513 us, four 700, one 846; 65536: eight 286, four 273, two 364; 32768: four 285,
+// two 260, one 373; 8192: two 236, one 155.  262144, with all the clusters that fit 338 us, with 60 MB of rows 304; 400000: 414, 376.)
 constexpr long long kRowsInL2 = 40LL << 20, kLongRowsInL2 = 60LL << 20;
 
 template <typename X, typename G, int MODE> static fpsk_status launch_distill(DistillArgs g, cudaStream_t st)

@@ -2,14 +2,17 @@
 //
 // For a token v of a row: z = l_v; seen: z > 0 ? z / rep : z rep; z -= freq c + pres where c > 0; z += biases; masked: -inf.
 //
-// What bounds it is memory, the logits once and the result once; for a row or two it is the chain of steps.  A cluster of blocks takes
-// a row, each a slice of the vocabulary.  One warp of a block copies pieces of 8 KB into a ring, passing over those that a mask forbids
-// as a whole; four warps first count in shared memory, a word to a token, which tokens the history touches, adjust those, 32 at a
-// time, and note in a map of bits which tokens are left to the stream; then they go through the pieces, with one look for a larger logit and one
-// vote for 16 or 32 tokens of a thread.  An in-place call without token or lse copies nothing: only what changes is read or written.
+// What bounds it is memory, the logits once and the result once, where there is no history; with one it is the instructions and barriers
+// of finding out what it touches.  A cluster of blocks takes a row, whose pieces of 8 KB go to the blocks in turn.  One warp of a block
+// copies them into a ring, passing over those that a mask forbids as a whole; the others count in shared memory, a word to a token, how
+// often the history has each, and then go through the pieces: touched tokens are adjusted in place, and the largest is looked for
+// with one vote of a warp for all its tokens of a piece.  Tokens with biases are stored as they were and done behind the stream, one to a thread.
+// An in-place call without token or lse copies nothing: only what changes is read or written.
 //
-// (Touched tokens adjusted where the stream meets them took 75 us for 96 rows of 131072 with histories of 4096: some lane of a warp
-// meets one in almost every vector, and all wait for its division.)
+// Measured: 2000 rows of 32000 FP32 logits without histories, token and log-sum-exp, 51 us (0.77 of a copy); 96 rows of 131072 with histories
+// of 4096, biases and masks 43 us (17 without them, floor 8): a block's 16384 tokens take some 20 us, of which the history's counting is 4 and
+// the words' looking through 3, three blocks to an SM; 640 rows of 50257 BF16 to FP32 93 us (46, floor 30); one row of 32000 with a history of
+// 1000 7 us.  Tokens adjusted by divided threads of their own, in lists of 32, took 52 and 113 us, with a map of bits for the stream 60.
 #include "decoder.cuh"
 
 namespace fpsk {
@@ -37,7 +40,7 @@ struct LogitsArgs {
     int32_t *status;
 };
 
-// Threads that work: the history's counting is bound by its latency.
+// Threads that work: the history's counting is bound by its latency (96 rows of 131072 with histories of 4096: 43 us with 256, 52 with 128).
 template <bool WORDS> struct Workers {
     static constexpr int n = WORDS ? 256 : 128, threads = n + 32, stages = 4;       // (three blocks to an SM, or five)
 };
@@ -555,7 +558,7 @@ template <typename X, typename O, typename W> static fpsk_status launch_logits(L
     constexpr bool WORDS = !std::is_void<W>::value;
     using Wd = typename std::conditional<WORDS, W, char>::type;
     const int chunk_tokens = WORDS ? kWordBytes / (int)sizeof(Wd) : kMostChunk;
-    // Blocks of a row: as many as make slices of one chunk, and more where there are too few rows for the SMs.
+    // Blocks of a row: as many as make shares of one chunk, and more, down to 4096 tokens each, where there are too few rows for the SMs.
     g.blocks = 1;
     while (g.blocks < kRowMostBlocks && ((WORDS && g.vocab > g.blocks * chunk_tokens) || (g.rows * g.blocks < 3 * kSms && g.vocab > g.blocks * 4096))) {
         g.blocks *= 2;
