@@ -10,9 +10,10 @@
 // cluster's shared memory, and write the gradient; one or three warps prepare the teacher's probabilities for the next row and take them off the
 // gradient of the one before, so that neither is waited for.
 //
-// Measured: 4096 rows of 131072 FP32 logits with BF16 gradients 521 us in a burst (6.2 TB/s of logits and gradients, 0.95 of a copy),
-// 602 sustained, at the power limit; losses of 2048 rows of 65536 BF16 49 us (0.84; the special function unit, which makes the powers, is busy
-// for 66 %); loss, then gradient of 1500 x 50257 FP16 90 us; 5 rows of 131072 8.7 us.  Rows held in shared memory between the two looks
+// Measured: 4096 rows of 131072 FP32 logits with BF16 gradients 537 us in a burst (6.0 TB/s of logits and gradients, 0.92 of a copy),
+// 632 sustained, at the power limit; losses of 2048 rows of 65536 BF16 52 us (0.79; the special function unit, which makes the powers, is busy
+// for 66 %); loss, then gradient of 1500 x 50257 FP16 94 us; 5 rows of 131072 11 us.  (Without the
+// largest listed logit as reference 521, 49 and 9 us.)  Rows held in shared memory between the two looks
 // (eight slices of 64 KB, three blocks to an SM): 662 us, as fewer rows are at work at a time.  The gradient's factor folded into the
 // exponent, a product fewer for two elements: no faster.
 #include "decoder.cuh"
@@ -114,10 +115,10 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
         }
     };
 
-    // FP32 gradients, and an lse that they are made from later, take their powers with the block's largest listed logit as reference at
-    // least: the largest powers, which are most of the sum and of the gradient, have exponents near 0 then, whose rounding is small (an
-    // error of 1.2e-6 relative, else, for logits of a normal distribution with larger ones listed).
-    const bool anchored = MODE == kLossAndGrad ? sizeof(G) == 4 : MODE == kLossOnly && g.lse;
+    // A row's sum takes its powers with the block's largest listed logit as reference at least: the largest powers, which are most of the
+    // sum and of the gradient, have exponents near 0 then, whose rounding is small (an error of 1.2e-6 relative in an FP32 gradient, else,
+    // for logits of a normal distribution with larger ones listed, and of 4e-6 in a small loss of few rows).
+    constexpr bool anchored = MODE != kGradOnly;
     // the teacher's mass, from what it says: normalized its largest logit and 1 / s, else the mass itself
     auto mass_of = [&](float a0, float a1) { return g.normalize ? (a1 == 0.f ? 0.f : 1.f) : a0; };
 
@@ -230,7 +231,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             const Slice sl(x, g.vocab, g.blocks, rank, X());
 #pragma unroll
             for (int i = 0; i < kTogether; ++i)
-                if (losses ? token[i] >= 0 : (MODE != kLossOnly || anchored) && place(sl, token[i]) >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + token[i]));
+                if (losses ? token[i] >= 0 : place(sl, token[i]) >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + token[i]));
         };
         // loss = sum p (log p - log q) = K + m ((M - xr) / tau + ln S), with a listed logit xr as reference; normalized, with
         // e = 2^((t - u) c), s = sum e, m = 1 and a listed tr:  K = sum e ((t - tr) - (x - xr)) / (tau s) + (tr - u) / tau - ln s;
@@ -246,7 +247,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 float l[kTogether];
 #pragma unroll
                 for (int i = 0; i < kTogether; ++i) {
-                    at[i] = (MODE != kLossOnly || anchored) && t[i] != -INFINITY ? place(sl, token[i]) : -1;
+                    at[i] = t[i] != -INFINITY ? place(sl, token[i]) : -1;
                     l[i] = at[i] >= 0 || (losses && token[i] >= 0) ? Elem<X>::to_f(x[token[i]]) : 0.f;
                 }
                 if (anchored) {

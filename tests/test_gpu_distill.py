@@ -202,6 +202,21 @@ def test_repeatable_captured_and_on_another_stream():
             assert torch.equal(a, b) and torch.equal(a, c)
 
 
+@pytest.mark.parametrize("vocab", [700, 5000, 131072])
+@pytest.mark.parametrize("grad", [None, F32, BF16])
+def test_a_learnt_token_costs_no_precision(vocab, grad):
+    """One listed logit stands 40 to 60 above the others: the loss is ln(1 + sum e^(x_v - x_0)), below 1e-12.  Its exponent is 0 when it is the
+    reference, and S then 1 with two units of the power and one rounding of a sum or a logarithm each: 2^-23 (2 + 1) at the most.  With
+    another logit as reference the exponent, up to 86 in powers of two, is rounded by up to 2^-18."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    x = torch.randn(64, vocab, generator=g, device="cuda")
+    token = torch.randint(0, vocab, (64, 1), generator=g, device="cuda", dtype=torch.int32)
+    x.scatter_(1, token.long(), 45.0 + 15.0 * torch.rand(64, 1, generator=g, device="cuda"))
+    loss, dx = torch.empty(64, device="cuda"), None if grad is None else torch.empty(64, vocab, device="cuda", dtype=grad)
+    L.distill_loss(x, token, torch.zeros(64, 1, device="cuda"), loss, dlogits=dx)
+    assert float(loss.abs().max()) <= 3 * 2.0 ** -23
+
+
 def test_no_rows():
     x = torch.empty(0, 100, device="cuda")
     L.distill_loss(x, torch.empty(0, 4, dtype=torch.int32, device="cuda"), torch.empty(0, 4, device="cuda"), torch.empty(0, device="cuda"), dlogits=torch.empty_like(x))
