@@ -544,6 +544,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
     cluster_sync();                                                    // no block leaves before what the others send it
 }
 
+constexpr int kMostShared = 224 * 1024;         // dynamic, of a block (227 KB less what is static)
 // (131072 FP32 logits, 512 KB a row: eight blocks to a row 513 us, four 700, one 846; 65536: eight 286, four 273, two 364; 32768: four 285,
 // two 260, one 373; 8192: two 236, one 155.  262144, with all the clusters that fit 338 us, with 60 MB of rows 304; 400000: 414, 376.)
 constexpr long long kRowsInL2 = 40LL << 20, kLongRowsInL2 = 60LL << 20;
@@ -556,15 +557,16 @@ template <typename X, typename G, int MODE> static fpsk_status launch_distill(Di
     g.teachers = g.top <= 160 ? 1 : kMostTeachers;
     const int teacher = MODE == kLossOnly ? 0 : (int)align_up((size_t)6 * (g.top + 32 * g.teachers) * sizeof(float), 128);
     auto map_bytes = [&](int blocks) { return MODE == kLossOnly ? 0 : (int)align_up((size_t)((vecs + blocks - 1) / blocks * Vec<X>::n + 16 + 31) / 32 * 4, 128); };
+    g.teacher_at = kStages * kPiece;
+    g.map_at = g.teacher_at + teacher;
     // One block to a row, unless there are too few rows for all SMs, or the rows at work at a time (four blocks to an SM) would take
-    // more than kRowsInL2, so that the second look at them finds them gone from L2.
+    // more than kRowsInL2, so that the second look at them finds them gone from L2, or a block's map of its tokens has no room (from
+    // 1.3 million tokens a block on; the most blocks always have it).
     const long long row_bytes = (long long)vecs * 16;
     g.blocks = 1;
     while (g.blocks < kRowMostBlocks && slice_pieces(g.blocks) > 1 &&
-           (g.rows * g.blocks < 3 * kSms || (MODE == kLossAndGrad && 4 * kSms / g.blocks * row_bytes > kRowsInL2)))
+           (g.rows * g.blocks < 3 * kSms || (MODE == kLossAndGrad && 4 * kSms / g.blocks * row_bytes > kRowsInL2) || g.map_at + map_bytes(g.blocks) > kMostShared))
         g.blocks *= 2;
-    g.teacher_at = kStages * kPiece;
-    g.map_at = g.teacher_at + teacher;
     g.map_words = map_bytes(g.blocks) / 4;
     Launch launch((unsigned)g.blocks, kWorkers + 32 + 32 * g.teachers, (size_t)g.map_at + map_bytes(g.blocks), g.blocks, st);
     auto kernel = distill_kernel<X, G, MODE>;
