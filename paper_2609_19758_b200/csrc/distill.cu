@@ -185,13 +185,6 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             for (int w = 1; w < g.teachers; ++w) v = fmaxf(v, teams[slot][w]);
             return v;
         };
-        auto from_first = [&](float v, int slot) {
-            v = __shfl_sync(0xFFFFFFFFu, v, 0);
-            if (g.teachers == 1) return v;
-            if (me == 0) teams[slot][0] = v;
-            bar_sync(4, all);
-            return teams[slot][0];
-        };
         // a token's place among this block's of a row, or -1
         auto place = [&](const Slice &sl, int t) {
             if (t < 0) return -1;
@@ -233,13 +226,22 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             for (int i = 0; i < kTogether; ++i)
                 if (losses ? token[i] >= 0 : place(sl, token[i]) >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + token[i]));
         };
-        // loss = sum p (log p - log q) = K + m ((M - xr) / tau + ln S), with a listed logit xr as reference; normalized, with
-        // e = 2^((t - u) c), s = sum e, m = 1 and a listed tr:  K = sum e ((t - tr) - (x - xr)) / (tau s) + (tr - u) / tau - ln s;
-        // else with e = 2^(t log2(e)), m = sum e:               K = sum e (t - (x - xr) / tau).
+        // loss = sum p (log p - log q) = K + m ((M - xr) / tau + ln S), with the largest listed t as reference u, and the student's logit of
+        // its token as xr; normalized, with e = 2^((t - u) c), s = sum e, m = 1:  K = sum e ((t - u) - (x - xr)) / (tau s) - ln s;
+        // else with e = 2^(t log2(e)), m = sum e:                                 K = sum e (t - (x - xr) / tau).
+        // (Another entry as reference may be one that a large negative number masks, there or in the student, and takes all precision
+        // from the sums; the largest one has a share of p.)  Each lane has a reference of its own, which moves with its largest t.
         auto prepare = [&](long long row, int b) {
             const X *x = static_cast<const X *>(g.x) + row * g.xs;
             const Slice sl(x, g.vocab, g.blocks, rank, X());
-            float u = kNoReference, s = 0.f, d = 0.f, tr = 0.f, xr = 0.f, high = kNoReference;
+            float u = kNoReference, xr = 0.f, s = 0.f, d = 0.f, high = kNoReference;
+            auto refer = [&](float top, float x_top) {                 // the sums so far, with another reference
+                const float f = g.normalize ? exp2_fast((u - top) * ct) : 1.f, more = g.normalize ? (u - top) + (x_top - xr) : (x_top - xr) * g.inv_tau;
+                d = s == 0.f || f == 0.f ? 0.f : fmaf(s, more, d) * f;
+                s *= f;
+                u = top;
+                xr = x_top;
+            };
             int count = 0;
             for (int base = 0; base < g.top; base += all * kTogether) {            // (as often for each warp: there are barriers in it)
                 if (base) ask(row, base + me);
@@ -269,30 +271,20 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                     }
                 }
                 if (sums) {
-                    float top = u;
+                    float top = u, x_top = xr;
 #pragma unroll
                     for (int i = 0; i < kTogether; ++i)
-                        if (token[i] >= 0) top = fmaxf(top, t[i]);
-                    if (losses && base == 0) {
-                        tr = from_first(t[0], 0);
-                        xr = from_first(l[0], 1);
-                        if (!(fabsf(tr) < 3e38f) || !g.normalize) tr = 0.f;
-                        if (!(fabsf(xr) < 3e38f)) xr = 0.f;
-                    }
-                    if (!g.normalize) {
-                        top = 0.f;
-                    } else {
-                        const float f = exp2_fast((u - top) * ct);
-                        s *= f;
-                        d *= f;
-                    }
-                    u = top;
+                        if (token[i] >= 0 && t[i] > top) {
+                            top = t[i];
+                            x_top = fabsf(l[i]) < 3e38f ? l[i] : 0.f;
+                        }
+                    refer(top, x_top);
 #pragma unroll
                     for (int i = 0; i < kTogether; ++i) {
                         if (token[i] < 0 || t[i] == -INFINITY) continue;
-                        const float e = exp2_fast((t[i] - u) * ct);
+                        const float e = exp2_fast(g.normalize ? (t[i] - u) * ct : t[i] * ct);
                         s += e;
-                        if (losses && e != 0.f) d = fmaf(e, g.normalize ? (t[i] - tr) - (l[i] - xr) : t[i] - (l[i] - xr) * g.inv_tau, d);
+                        if (losses && e != 0.f) d = fmaf(e, g.normalize ? (t[i] - u) - (l[i] - xr) : t[i] - (l[i] - xr) * g.inv_tau, d);
                     }
                 }
             }
@@ -302,18 +294,30 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 if (me == 0) highest[b] = high;
             }
             if (sums) {
-                if (g.normalize) {
-                    const float top = largest(u, 2), f = exp2_fast((u - top) * ct);
-                    s *= f;
-                    d *= f;
-                    u = top;
+                // (the lowest lane of the largest t, and of the lowest warp)
+                float top = u;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                float x_top = __shfl_sync(0xFFFFFFFFu, xr, __ffs(__ballot_sync(0xFFFFFFFFu, u == top)) - 1);
+                if (g.teachers > 1) {
+                    if (lane == 0) {
+                        teams[0][my_warp] = top;
+                        teams[1][my_warp] = x_top;
+                    }
+                    bar_sync(4, all);
+                    for (int w = g.teachers - 1; w >= 0; --w)
+                        if (teams[0][w] >= top) {
+                            top = teams[0][w];
+                            x_top = teams[1][w];
+                        }
                 }
+                refer(top, x_top);
                 s = total(s, 3);
                 if (losses) d = total(d, 4);
                 if (me == 0) {
                     float4 v = make_float4(0.f, xr, 0.f, 0.f);
                     if (!g.normalize) v = make_float4(d, xr, s, 1.f);
-                    else if (s != 0.f) v = make_float4(d / s * g.inv_tau + (tr - u) * g.inv_tau - logf(s), xr, u, 1.f / s);
+                    else if (s != 0.f) v = make_float4(d / s * g.inv_tau - logf(s), xr, u, 1.f / s);
                     taught[b] = v;
                 }
             }

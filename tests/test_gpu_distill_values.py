@@ -7,7 +7,7 @@ import torch
 from oracle import decoder_oracle as D
 from paper_2609_19758_b200 import build as B
 from paper_2609_19758_b200 import logits as L
-from test_gpu_distill import check, np64
+from test_gpu_distill import check, lse_bound, np64
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +41,46 @@ def test_the_gradient_alone_of_wide_vocabularies(rows, vocab, top):
     del x
     dx[live] = 0.0
     assert not bool(dx.any())
+
+
+@pytest.mark.parametrize("top", [1, 8, 100, 600])
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("ttype,low", [(F32, -1e9), (F32, -1e30), (F16, -65504.0), (BF16, -1e4)])
+def test_listed_entries_that_a_finite_number_masks(top, normalize, ttype, low):
+    """Entries that a mask has set to a large negative number add nothing, wherever they stand in the list, and whatever the student's logit
+    of them is; the others keep their precision (the bounds of `test_gpu_distill.check` for the logits that are not masked)."""
+    g = torch.Generator(device="cuda").manual_seed(top)
+    rows, vocab = 12, 5003
+    x = 2.0 * torch.randn(rows, vocab, generator=g, device="cuda")
+    token = torch.stack([torch.randperm(vocab, generator=g, device="cuda")[:top] for _ in range(rows)]).to(torch.int32)
+    t = 2.0 * torch.randn(rows, top, generator=g, device="cuda")
+    if not normalize:
+        t = torch.log_softmax(t, 1) - 0.1
+    t = t.to(ttype)
+    kept = t.clone()
+    t[:4, 0] = low
+    t[4:8, :top // 2] = low
+    t[8:10, :max(top - 1, 0)] = low                                    # the last one counts
+    t[10, ::2] = low
+    t[11] = low                                                        # all of them: as likely as each other, or (as given) not at all
+    if top == 600:
+        t[8, :] = low
+        t[8, 450] = kept[8, 450]
+    # half of the rows: the student's logits of those tokens masked as well
+    for r in range(0, rows - 1, 2):
+        x[r, token[r][t[r] == low].long()] = -1e9
+    loss, lse, dx = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+    L.distill_loss(x, token, t, loss, lse=lse, dlogits=dx, normalize=normalize, temperature=1.25)
+    alone = torch.empty_like(loss)
+    L.distill_loss(x, token, t, alone, normalize=normalize, temperature=1.25)
+    for r in range(rows):
+        raw, tl = np64(x[r]), np64(t[r])
+        if normalize and np.all(tl == tl[0]) and tl[0] < -1e3:
+            tl = np.zeros(top)                                         # (the same row, where 64 bits hold its logarithms and the bounds are not the mask's size)
+        l, d, s, mag, dmag = D.distill(raw, token[r].tolist(), tl, 1.25, normalize)
+        off = lse_bound(raw[raw > -1e8], 1.25, vocab)
+        mass = 1.0 if normalize else np.exp(tl).sum()
+        assert abs(float(lse[r]) - s) <= off
+        assert max(abs(float(loss[r]) - l), abs(float(alone[r]) - l)) <= 64 * E * mag + off * mass
+        y = np.where(raw > -1e8, np.abs(raw / 1.25), 0.0)
+        assert np.all(np.abs(np64(dx[r]) - d) <= (off + E * (3 * y + 3 * abs(s) + 1540)) * dmag + 2.0 ** -126)
