@@ -100,7 +100,7 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-constexpr float kNoReference = -3.4e38f;
+constexpr float kMostFloat = 3.402823466e38f, kNoReference = -kMostFloat;      // (a row may hold nothing but the lowest number: its powers are 1)
 // 2^((x - M) c) summed
 struct RefSum {
     float m, s;

@@ -274,9 +274,9 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                     float top = u, x_top = xr;
 #pragma unroll
                     for (int i = 0; i < kTogether; ++i)
-                        if (token[i] >= 0 && t[i] > top) {
+                        if (token[i] >= 0 && t[i] >= top) {
                             top = t[i];
-                            x_top = fabsf(l[i]) < 3e38f ? l[i] : 0.f;
+                            x_top = fabsf(l[i]) <= kMostFloat ? l[i] : 0.f;
                         }
                     refer(top, x_top);
 #pragma unroll

@@ -84,3 +84,30 @@ def test_listed_entries_that_a_finite_number_masks(top, normalize, ttype, low):
         assert max(abs(float(loss[r]) - l), abs(float(alone[r]) - l)) <= 64 * E * mag + off * mass
         y = np.where(raw > -1e8, np.abs(raw / 1.25), 0.0)
         assert np.all(np.abs(np64(dx[r]) - d) <= (off + E * (3 * y + 3 * abs(s) + 1540)) * dmag + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_rows_of_the_types_lowest_value(dtype):
+    """A mask of the type's lowest value over everything leaves tokens that are as likely as each other."""
+    rows, vocab, top = 3, 3001, 9
+    low = torch.finfo(dtype).min
+    x = torch.full((rows, vocab), low, dtype=dtype, device="cuda")
+    x[1, 77] = 0.5                                                     # but one
+    token = torch.arange(70, 70 + top, device="cuda", dtype=torch.int32).repeat(rows, 1)
+    t = torch.randn(rows, top, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0))
+    t[1] = -float("inf")
+    t[1, 7] = 2.0
+    t[2] = torch.finfo(F32).min                                        # the teacher's as well
+    loss, dx = torch.empty(rows, device="cuda"), torch.empty(rows, vocab, device="cuda")
+    L.distill_loss(x, token, t, loss, dlogits=dx)
+    p = torch.softmax(t.double(), 1)
+    p[2] = 1.0 / top
+    want = torch.full((rows, vocab), 1.0 / vocab, dtype=torch.float64, device="cuda")
+    want[1] = 0.0
+    want[1, 77] = 1.0
+    want.scatter_add_(1, token.long(), -p)
+    # powers of 0 are 1: a rounding for each of some 16 sums and 24 joins, a product, a quotient
+    assert float((dx.double() - want).abs().max()) <= 64 * E
+    held = np.log(vocab) + (torch.special.xlogy(p, p)).sum(1)
+    held[1] = 0.0
+    assert float((loss.double() - held).abs().max()) <= 64 * E * 10
