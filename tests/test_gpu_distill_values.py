@@ -111,3 +111,27 @@ def test_rows_of_the_types_lowest_value(dtype):
     held = np.log(vocab) + (torch.special.xlogy(p, p)).sum(1)
     held[1] = 0.0
     assert float((loss.double() - held).abs().max()) <= 64 * E * 10
+
+
+@pytest.mark.parametrize("rows,vocab", [(128, 5000), (128, 5003), (24, 131072), (600, 20001)])
+@pytest.mark.parametrize("temperature", [1.0, 0.5])
+def test_an_outlier_that_is_not_listed_costs_no_precision(rows, vocab, temperature):
+    """One logit 30 to 50 (in units of the temperature) above the others, anywhere in the row, first and last elements among them.
+
+    A power 2^y with |y| <= 8 is off by the difference x - M (below 8 temperatures: 4 E of the power), by y's own rounding (4 E ln 2) and by the
+    powers' two units (4 E); the sum as much, and by 16 roundings of additions and joins; the factor by 5 roundings: 48 E.  A logit d
+    below the largest: its exponent is rounded at its size, twice: 2 d E more.  The teacher's probabilities are equal (2 E)."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    x = torch.randn(rows, vocab, generator=g, device="cuda")
+    at = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    at[:8] = torch.tensor([0, 1, 2, 3, vocab - 1, vocab - 2, vocab - 3, vocab - 4], device="cuda")
+    x[torch.arange(rows, device="cuda"), at] = 30.0 + 20.0 * torch.rand(rows, generator=g, device="cuda")
+    x *= temperature
+    token = torch.randint(0, vocab, (rows, 6), generator=g, device="cuda", dtype=torch.int32)
+    t = torch.zeros(rows, 6, device="cuda")
+    loss, dx = torch.empty(rows, device="cuda"), torch.empty_like(x)
+    L.distill_loss(x, token, t, loss, dlogits=dx, temperature=temperature)
+    for i in range(rows):
+        _, d, lse, _, mag = D.distill(np64(x[i]), token[i].tolist(), [0.0] * 6, temperature, True)
+        below = (np64(x[i]).max() - np64(x[i])) / temperature
+        assert np.all(np.abs(np64(dx[i]) - d) <= (50 + 2 * below) * E * mag + 2.0 ** -126), i
