@@ -129,6 +129,12 @@ typedef struct {
 } fpsk_distill;
 fpsk_status fpsk_distill_loss(const fpsk_distill *a, int32_t *d_status, void *stream);
 fpsk_status fpsk_distill_loss_backward(const fpsk_distill *a, int32_t *d_status, void *stream);
+/* The two for a gradient that is not rounded at the size of the log-sum-exp: `sums` (device, two floats a row; NULL: as above) takes a
+ * number M near each row's largest logit and S = sum_v exp((x_v - M) / temperature), so that lse = M / temperature + ln S.  The backward
+ * pass reads them in place of lse, which may be NULL.  (From an FP32 lse a gradient is off by lse's rounding, relative: 5e-7 at 10, 3e-5
+ * at 700.) */
+fpsk_status fpsk_distill_loss_sums(const fpsk_distill *a, float *sums, int32_t *d_status, void *stream);
+fpsk_status fpsk_distill_loss_backward_sums(const fpsk_distill *a, const float *sums, int32_t *d_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -38,7 +38,7 @@ def _bind():
         L.fpsk_add_norm_workspace_bytes.restype, L.fpsk_add_norm_workspace_bytes.argtypes = sz, [C.c_int32]
         b.bind(*(C.cast(getattr(L, n), vp).value for n in (
             "fpsk_qk_norm_rope", "fpsk_qk_norm_rope_backward", "fpsk_paged_append", "fpsk_paged_attention", "fpsk_add_rms_norm",
-            "fpsk_add_rms_norm_backward", "fpsk_adjust_logits", "fpsk_distill_loss", "fpsk_distill_loss_backward")))
+            "fpsk_add_rms_norm_backward", "fpsk_adjust_logits", "fpsk_distill_loss_sums", "fpsk_distill_loss_backward_sums")))
         _binding = b
     return _binding
 

@@ -21,8 +21,8 @@ struct Library {
     decltype(&fpsk_add_rms_norm) add_norm;
     decltype(&fpsk_add_rms_norm_backward) add_norm_backward;
     decltype(&fpsk_adjust_logits) adjust_logits;
-    decltype(&fpsk_distill_loss) distill;
-    decltype(&fpsk_distill_loss_backward) distill_backward;
+    decltype(&fpsk_distill_loss_sums) distill;
+    decltype(&fpsk_distill_loss_backward_sums) distill_backward;
 } lib;
 
 struct Refused {};                       // a Python error is set
@@ -546,10 +546,10 @@ PyObject *py_adjust_logits(PyObject *, PyObject *const *a, Py_ssize_t n)
         return lib.adjust_logits(&t, status_ptr(a[15], device), stream_ptr(a[16]));
     });
 }
-// logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, status, stream
+// logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, sums, status, stream
 template <bool BACKWARD> PyObject *py_distill(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return call(n, 11, [&] {
+    return call(n, 12, [&] {
         const int device = device_of(needed(a[0], "logits"), "logits");
         const at::Tensor &x = rows_of(a[0], -1, -1, device, "logits");
         const int64_t rows = x.size(0), vocab = x.size(1);
@@ -580,8 +580,15 @@ template <bool BACKWARD> PyObject *py_distill(PyObject *, PyObject *const *a, Py
         if (!(tau > 0) || tau > 3.4e38 || tau < 1e-38) refuse(PyExc_ValueError, "temperature must be positive and finite");
         t.temperature = (float)tau;
         t.normalize = truth(a[8]);
+        float *sums = nullptr;
+        if (a[9] != Py_None) {
+            const at::Tensor &s = rows_of(a[9], rows, 2, device, "sums");
+            if (s.scalar_type() != at::kFloat || !s.is_contiguous()) refuse(PyExc_ValueError, "sums: contiguous (%lld, 2) float32 expected", (long long)rows);
+            sums = static_cast<float *>(s.data_ptr());
+        }
         const OnDevice on(device);
-        return (BACKWARD ? lib.distill_backward : lib.distill)(&t, status_ptr(a[9], device), stream_ptr(a[10]));
+        return BACKWARD ? lib.distill_backward(&t, sums, status_ptr(a[10], device), stream_ptr(a[11]))
+                        : lib.distill(&t, sums, status_ptr(a[10], device), stream_ptr(a[11]));
     });
 }
 

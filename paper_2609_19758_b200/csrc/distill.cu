@@ -25,7 +25,7 @@ enum { kLossOnly = 0, kLossAndGrad = 1, kGradOnly = 2 };
 struct DistillArgs {
     const void *x, *tok, *t;
     const float *weight;
-    float *loss, *lse;
+    float *loss, *lse, *sums;          // sums: M and S of each row, written by the loss, read by the gradient alone where they are given
     void *dx;
     long long xs, toks, ts, dxs, rows;
     int vocab, top;
@@ -337,6 +337,10 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 const float ln = logf(S);
                 g.loss[row] = m == 0.f ? 0.f : fmaf(m, fmaf(M - taught[b].y, g.inv_tau, ln), taught[b].x);
                 if (g.lse) g.lse[row] = fmaf(M, g.inv_tau, ln);
+                if (g.sums) {
+                    g.sums[2 * row] = M;
+                    g.sums[2 * row + 1] = S;
+                }
             }
             if (MODE != kLossOnly && m != 0.f) {
                 const Slice sl(static_cast<const X *>(g.x) + row * g.xs, g.vocab, g.blocks, rank, X());
@@ -386,6 +390,10 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 if (MODE != kGradOnly && rank == 0 && me == 0) {
                     g.loss[row] = 0.f;
                     if (g.lse) g.lse[row] = 0.f;
+                    if (g.sums) {
+                        g.sums[2 * row] = 0.f;
+                        g.sums[2 * row + 1] = 1.f;
+                    }
                 }
                 ask(row + row_step, me);
                 continue;
@@ -406,12 +414,18 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
         uint32_t phase = 0;
         const float c = g.c;
         const float2 cc = make_float2(c, c);
-        float lse_next = MODE == kGradOnly && first_row < g.rows ? g.lse[first_row] : 0.f;
+        // what the loss kept of a row: M and S, or the log-sum-exp
+        auto kept_of = [&](long long row) {
+            if (MODE != kGradOnly || row >= g.rows) return make_float2(0.f, 0.f);
+            return g.sums ? make_float2(g.sums[2 * row], g.sums[2 * row + 1]) : make_float2(g.lse[row], 0.f);
+        };
+        float2 kept_next = kept_of(first_row);
         for (long long row = first_row; row < g.rows; row += row_step) {
             const X *x = static_cast<const X *>(g.x) + row * g.xs;
-            const float weight = weight_next, lse = lse_next;
+            const float weight = weight_next;
+            const float2 kept = kept_next;
             weight_next = weight_of(row + row_step);
-            if (MODE == kGradOnly && row + row_step < g.rows) lse_next = g.lse[row + row_step];
+            kept_next = kept_of(row + row_step);
             const Slice sl(x, g.vocab, g.blocks, rank, X());
             // the elements in front of the first vector and behind the last: the first block's and the last block's, one to a lane
             int loose = -1;
@@ -503,8 +517,12 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
             } else {
                 wait(ready[b], n >> 1 & 1u);
                 said = make_float2(taught[b].z, taught[b].w);
-                M = lse * g.tau;
-                S = expf(fmaf(-M, g.inv_tau, lse));                    // what M's rounding left of it
+                M = kept.x;
+                S = kept.y;
+                if (!g.sums) {
+                    M = kept.x * g.tau;
+                    S = expf(fmaf(-M, g.inv_tau, kept.x));             // what M's rounding left of it
+                }
             }
             if (tid == 0) result[b] = make_float4(M, S, said.x, said.y);
             if (MODE != kLossOnly) {
@@ -598,7 +616,7 @@ template <typename X> static fpsk_status launch_distill_typed(const DistillArgs 
 
 using namespace fpsk;
 
-static fpsk_status distill(const fpsk_distill *a, bool backward, int32_t *d_status, void *stream)
+static fpsk_status distill(const fpsk_distill *a, float *sums, bool backward, int32_t *d_status, void *stream)
 {
     if (!a) return FPSK_ERR_NULL;
     if (a->n_rows < 0 || a->n_rows > 0x7FFFFFFFLL || a->vocab < 1 || a->vocab > FPSK_MAX_VOCAB || a->top < 0 || a->top > FPSK_MAX_TOP) return FPSK_ERR_SHAPE;
@@ -607,15 +625,16 @@ static fpsk_status distill(const fpsk_distill *a, bool backward, int32_t *d_stat
     if (!(a->temperature > 0.f) || a->temperature > 3.4e38f) return FPSK_ERR_PARAM;
     if (a->n_rows == 0) return FPSK_OK;
     if (!a->logits || (a->top > 0 && (!a->teacher_token || !a->teacher_logit))) return FPSK_ERR_NULL;
-    if (backward ? !a->lse || !a->dlogits : !a->loss) return FPSK_ERR_NULL;
+    if (backward ? (!a->lse && !sums) || !a->dlogits : !a->loss) return FPSK_ERR_NULL;
     if (a->logits_stride < 0 || a->token_stride < 0 || a->teacher_stride < 0 || (a->dlogits && a->n_rows > 1 && a->dlogits_stride < a->vocab)) return FPSK_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(a->logits) % elem_bytes(a->logits_type) || (a->dlogits && reinterpret_cast<uintptr_t>(a->dlogits) % elem_bytes(a->grad_type)))
         return FPSK_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(sums) % sizeof(float)) return FPSK_ERR_ALIGN;
     const double inv = 1.0 / (double)a->temperature;
     if (inv > 3.4e38) return FPSK_ERR_PARAM;
     DistillArgs g = {};
     g.x = a->logits; g.tok = a->teacher_token; g.t = a->teacher_logit; g.weight = a->row_weight;
-    g.loss = a->loss; g.lse = a->lse; g.dx = a->dlogits;
+    g.loss = a->loss; g.lse = a->lse; g.sums = sums; g.dx = a->dlogits;
     g.xs = a->logits_stride; g.toks = a->token_stride; g.ts = a->teacher_stride; g.dxs = a->dlogits_stride;
     g.rows = a->n_rows; g.vocab = a->vocab; g.top = a->top;
     g.tok_bytes = a->token_bytes; g.t_type = a->teacher_type;
@@ -630,5 +649,10 @@ static fpsk_status distill(const fpsk_distill *a, bool backward, int32_t *d_stat
     return launch_distill_typed<__nv_bfloat16>(g, a->grad_type, backward, st);
 }
 
-extern "C" fpsk_status fpsk_distill_loss(const fpsk_distill *a, int32_t *d_status, void *stream) { return distill(a, false, d_status, stream); }
-extern "C" fpsk_status fpsk_distill_loss_backward(const fpsk_distill *a, int32_t *d_status, void *stream) { return distill(a, true, d_status, stream); }
+extern "C" fpsk_status fpsk_distill_loss(const fpsk_distill *a, int32_t *d_status, void *stream) { return distill(a, nullptr, false, d_status, stream); }
+extern "C" fpsk_status fpsk_distill_loss_backward(const fpsk_distill *a, int32_t *d_status, void *stream) { return distill(a, nullptr, true, d_status, stream); }
+extern "C" fpsk_status fpsk_distill_loss_sums(const fpsk_distill *a, float *sums, int32_t *d_status, void *stream) { return distill(a, sums, false, d_status, stream); }
+extern "C" fpsk_status fpsk_distill_loss_backward_sums(const fpsk_distill *a, const float *sums, int32_t *d_status, void *stream)
+{
+    return distill(a, const_cast<float *>(sums), true, d_status, stream);
+}

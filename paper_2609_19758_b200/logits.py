@@ -35,22 +35,25 @@ def adjust_logits(logits: torch.Tensor, out: Optional[torch.Tensor] = None, hist
 
 def distill_loss(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, loss: torch.Tensor,
                  row_weight: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
-                 temperature: float = 1.0, normalize: bool = True, status: Optional[torch.Tensor] = None, stream=None) -> None:
+                 temperature: float = 1.0, normalize: bool = True, status: Optional[torch.Tensor] = None, stream=None,
+                 sums: Optional[torch.Tensor] = None) -> None:
     """loss (rows,): sum_j p_j (log p_j - log q_j) of each row of logits (rows, vocab), q = softmax(logits / temperature), against the
     teacher's logits for the tokens teacher_token (rows, top): p = softmax(teacher_logit / temperature) over them, or exp(teacher_logit)
     with normalize=False (logarithms of probabilities).  Tokens outside the vocabulary (-1) are left out.  dlogits (rows, vocab) gets the gradient of
-    sum(row_weight * loss) in the same launch; it may be logits.  Rows of weight 0 are not read: loss 0, gradient 0."""
+    sum(row_weight * loss) in the same launch; it may be logits.  Rows of weight 0 are not read: loss 0, gradient 0.  lse (rows,) and sums
+    (rows, 2), both FP32, keep the rows' log-sum-exps for distill_loss_backward."""
     b = A._binding or A._bind()
-    A._check(b.distill_loss(logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, status,
+    A._check(b.distill_loss(logits, teacher_token, teacher_logit, loss, row_weight, lse, dlogits, temperature, normalize, sums, status,
                             A._stream(b.device(logits), stream)), "fpsk_distill_loss")
 
 
-def distill_loss_backward(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, lse: torch.Tensor,
+def distill_loss_backward(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, lse: Optional[torch.Tensor],
                           dloss: torch.Tensor, dlogits: torch.Tensor, temperature: float = 1.0, normalize: bool = True,
-                          status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """The gradient of distill_loss alone, from the lse of the forward pass and the gradients dloss (rows,) of the rows' losses."""
+                          status: Optional[torch.Tensor] = None, stream=None, sums: Optional[torch.Tensor] = None) -> None:
+    """The gradient of distill_loss alone, from the sums (or the lse, which costs its rounding) of the forward pass and the gradients dloss
+    (rows,) of the rows' losses."""
     b = A._binding or A._bind()
-    A._check(b.distill_loss_backward(logits, teacher_token, teacher_logit, None, dloss, lse, dlogits, temperature, normalize, status,
+    A._check(b.distill_loss_backward(logits, teacher_token, teacher_logit, None, dloss, lse, dlogits, temperature, normalize, sums, status,
                                      A._stream(b.device(logits), stream)), "fpsk_distill_loss_backward")
 
 
@@ -60,16 +63,16 @@ class DistillLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, teacher_token, teacher_logit, temperature, normalize):
-        loss, lse = (torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device) for _ in range(2))
-        distill_loss(logits, teacher_token, teacher_logit, loss, lse=lse, temperature=temperature, normalize=normalize)
-        ctx.save_for_backward(logits, teacher_token, teacher_logit, lse)
+        loss, sums = (torch.empty(logits.shape[0], *more, dtype=torch.float32, device=logits.device) for more in ((), (2,)))
+        distill_loss(logits, teacher_token, teacher_logit, loss, temperature=temperature, normalize=normalize, sums=sums)
+        ctx.save_for_backward(logits, teacher_token, teacher_logit, sums)
         ctx.more = (temperature, normalize)
         return loss
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dloss):
-        logits, teacher_token, teacher_logit, lse = ctx.saved_tensors
+        logits, teacher_token, teacher_logit, sums = ctx.saved_tensors
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        distill_loss_backward(logits, teacher_token, teacher_logit, lse, dloss.float().contiguous(), dlogits, *ctx.more)
+        distill_loss_backward(logits, teacher_token, teacher_logit, None, dloss.float().contiguous(), dlogits, *ctx.more, sums=sums)
         return dlogits, None, None, None, None

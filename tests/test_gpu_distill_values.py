@@ -135,3 +135,47 @@ def test_an_outlier_that_is_not_listed_costs_no_precision(rows, vocab, temperatu
         _, d, lse, _, mag = D.distill(np64(x[i]), token[i].tolist(), [0.0] * 6, temperature, True)
         below = (np64(x[i]).max() - np64(x[i])) / temperature
         assert np.all(np.abs(np64(dx[i]) - d) <= (50 + 2 * below) * E * mag + 2.0 ** -126), i
+
+
+@pytest.mark.parametrize("shift", [0.0, 300.0, -5000.0])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_autograd_does_not_round_at_the_logarithms_size(shift, normalize):
+    """The gradient of DistillLoss for rows whose log-sum-exp is large, as exact as that of the fused call: the bounds of the outliers' test
+    without an outlier, with 40 E more for p = e^t of t between -20 and 0, twice rounded."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows, vocab = 40, 20003
+    x = (2.0 * torch.randn(rows, vocab, generator=g, device="cuda") + shift).requires_grad_()
+    token = torch.stack([torch.randperm(vocab, generator=g, device="cuda")[:12] for _ in range(rows)])
+    t = 2.0 * torch.randn(rows, 12, generator=g, device="cuda")
+    if not normalize:
+        t = torch.log_softmax(t, 1) - 0.1
+    w = torch.rand(rows, generator=g, device="cuda")
+    w[3] = 0.0
+    (L.DistillLoss.apply(x, token, t, 1.0, normalize) * w).sum().backward()
+    fused, loss = torch.empty(rows, vocab, device="cuda"), torch.empty(rows, device="cuda")
+    L.distill_loss(x.detach(), token, t, loss, row_weight=w, dlogits=fused, normalize=normalize)
+    for i in range(rows):
+        raw = np64(x.detach()[i])
+        _, d, _, _, mag = D.distill(raw, token[i].tolist(), t[i].tolist(), 1.0, normalize)
+        for got in (x.grad[i], fused[i]):
+            assert np.all(np.abs(np64(got) - float(w[i]) * d) <= float(w[i]) * (90 + 2 * (raw.max() - raw)) * E * mag + 2.0 ** -126), i
+
+
+def test_sums_that_are_refused_and_rows_without_weight():
+    x, token, t = torch.randn(3, 500, device="cuda"), torch.zeros(3, 2, dtype=torch.int32, device="cuda"), torch.zeros(3, 2, device="cuda")
+    loss, dx, weight = torch.empty(3, device="cuda"), torch.empty(3, 500, device="cuda"), torch.tensor([1.0, 0.0, 1.0], device="cuda")
+    sums = torch.full((3, 2), 7.0, device="cuda")
+    for bad in (sums[:2], sums[:, :1], sums.double(), sums.t().contiguous().t(), torch.zeros(3, 4, device="cuda")[:, :2], sums.cpu()):
+        with pytest.raises(ValueError):
+            L.distill_loss(x, token, t, loss, sums=bad)
+    with pytest.raises(RuntimeError):
+        L.distill_loss_backward(x, token, t, None, loss, dx)           # neither sums nor lse
+    assert bool((sums == 7.0).all())
+    lse = torch.empty(3, device="cuda")
+    L.distill_loss(x, token, t, loss, row_weight=weight, lse=lse, sums=sums)
+    assert sums[1].tolist() == [0.0, 1.0] and float(lse[1]) == 0.0
+    assert float((sums[:, 0] + sums[:, 1].log() - lse).abs().max()) <= 4 * E * 10
+    L.distill_loss_backward(x, token, t, None, weight, dx, sums=sums)
+    check(x, token, t, 1.0, True, weight, loss, lse, dx)
+    empty = torch.empty(0, 500, device="cuda")
+    L.distill_loss(empty, token[:0], t[:0], loss[:0], sums=sums[:0])
