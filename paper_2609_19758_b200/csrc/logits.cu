@@ -114,14 +114,14 @@ __device__ __forceinline__ float max_nan(float a, float b)
     return m;
 }
 
-// A warp's largest so far and its token, the same in all lanes, and each lane's sum of powers with a reference that follows the largest
-// at a distance.
+// A warp's largest so far and its token, the same in all lanes, and each lane's sum of powers with the largest as reference.  (One that
+// followed it at a distance of 2^60 left log-sum-exps 3e-6 off: exponents are rounded at their own size.  It took as long.)
 struct Picked {
     float best, m, s;
     int at;
     __device__ __forceinline__ void follow()
     {
-        if ((best - m) * kLog2e > 60.f) {
+        if (best > m) {
             s *= exp2_fast((m - best) * kLog2e);
             m = best;
         }
@@ -189,7 +189,7 @@ struct Single {
         if (z != z ? best == best : z > best) {
             best = z;
             at = v;
-            if ((best - m) * kLog2e > 60.f) {
+            if (best > m) {
                 s *= exp2_fast((m - best) * kLog2e);
                 m = best;
             }

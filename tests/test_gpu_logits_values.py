@@ -31,3 +31,20 @@ def test_rows_of_the_lowest_value():
         assert lse.tolist()[1] == 1.0
         for r, n in ((0, 4001), (2, 4000)):
             assert float(lse[r]) == pytest.approx(low + np.log(n), rel=4 * E)
+
+
+@pytest.mark.parametrize("base", [-40.0, -35.0, -28.0])
+@pytest.mark.parametrize("vocab", [3000, 3001, 60000])
+def test_a_late_largest_costs_no_precision(base, vocab):
+    """Three logits near 0 behind a row of others 28 to 40 below.  Their powers have exponents below 4 with the largest as reference: the
+    difference (below 2) and the exponent are rounded by 2 E and 2 E ln 2 at most, the power by two units (4 E), sums and joins by some 12 E
+    (what is far below the largest adds less than E in all); the logarithm of at most 3 and the sum with the largest by 3 E."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    x = base + torch.randn(64, vocab, generator=g, device="cuda")
+    x = torch.minimum(x, torch.full_like(x, base + 4))
+    at = torch.stack([vocab // 2 + torch.randperm(vocab - vocab // 2, generator=g, device="cuda")[:3] for _ in range(64)])
+    x.scatter_(1, at, 0.3 * torch.randn(64, 3, generator=g, device="cuda"))
+    lse = torch.empty(64, device="cuda")
+    L.adjust_logits(x, lse=lse)
+    want = torch.logsumexp(x.double(), 1)
+    assert float((lse.double() - want).abs().max()) <= 24 * E
