@@ -284,7 +284,6 @@ template <typename X, typename G> static fpsk_status launch_norm_grad(const Norm
 using namespace fpsk;
 
 static bool rows_ok(long long n, int dim, long long stride) { return n < 2 || stride >= dim; }
-static bool aligned(const void *p, int type) { return reinterpret_cast<uintptr_t>(p) % elem_bytes(type) == 0; }
 
 extern "C" fpsk_status fpsk_add_rms_norm(const fpsk_add_norm *a, int32_t *d_status, void *stream)
 {

@@ -72,6 +72,7 @@ template <bool WIDE> __device__ __forceinline__ void store8_any(void *p, int typ
 }
 
 __host__ __device__ __forceinline__ int elem_bytes(int type) { return type == FPSK_ELEM_FP32 ? 4 : type == FPSK_ELEM_E4M3 ? 1 : 2; }
+inline bool aligned(const void *p, int type) { return reinterpret_cast<uintptr_t>(p) % elem_bytes(type) == 0; }
 // rows of 16-byte vectors: the base and the stride
 inline bool row_wide(const void *p, int type, long long stride, int bytes = 16)
 {

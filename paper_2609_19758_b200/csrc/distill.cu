@@ -627,9 +627,10 @@ static fpsk_status distill(const fpsk_distill *a, float *sums, bool backward, in
     if (!a->logits || (a->top > 0 && (!a->teacher_token || !a->teacher_logit))) return FPSK_ERR_NULL;
     if (backward ? (!a->lse && !sums) || !a->dlogits : !a->loss) return FPSK_ERR_NULL;
     if (a->logits_stride < 0 || a->token_stride < 0 || a->teacher_stride < 0 || (a->dlogits && a->n_rows > 1 && a->dlogits_stride < a->vocab)) return FPSK_ERR_SHAPE;
-    if (reinterpret_cast<uintptr_t>(a->logits) % elem_bytes(a->logits_type) || (a->dlogits && reinterpret_cast<uintptr_t>(a->dlogits) % elem_bytes(a->grad_type)))
+    if (!aligned(a->logits, a->logits_type) || (a->dlogits && !aligned(a->dlogits, a->grad_type)) || reinterpret_cast<uintptr_t>(a->teacher_token) % a->token_bytes ||
+        !aligned(a->teacher_logit, a->teacher_type) || !aligned(a->row_weight, FPSK_ELEM_FP32) || !aligned(a->loss, FPSK_ELEM_FP32) || !aligned(a->lse, FPSK_ELEM_FP32) ||
+        !aligned(sums, FPSK_ELEM_FP32))
         return FPSK_ERR_ALIGN;
-    if (reinterpret_cast<uintptr_t>(sums) % sizeof(float)) return FPSK_ERR_ALIGN;
     const double inv = 1.0 / (double)a->temperature;
     if (inv > 3.4e38) return FPSK_ERR_PARAM;
     DistillArgs g = {};

@@ -600,8 +600,11 @@ extern "C" fpsk_status fpsk_adjust_logits(const fpsk_logits *a, int32_t *d_statu
     if (a->n_rows == 0) return FPSK_OK;
     if (!a->logits || (!a->out && !a->token && !a->lse)) return FPSK_ERR_NULL;
     if (a->logits_stride < 0 || (a->out && a->n_rows > 1 && a->out_stride < a->vocab)) return FPSK_ERR_SHAPE;
-    if (reinterpret_cast<uintptr_t>(a->logits) % elem_bytes(a->logits_type) || (a->out && reinterpret_cast<uintptr_t>(a->out) % elem_bytes(a->out_type)))
-        return FPSK_ERR_ALIGN;
+    if (!aligned(a->logits, a->logits_type) || (a->out && !aligned(a->out, a->out_type))) return FPSK_ERR_ALIGN;
+    const void *values[] = {a->history, a->history_len, a->prompt_len, a->repetition, a->frequency, a->presence, a->bias_ptr, a->bias_token, a->bias_value,
+                           a->mask, a->mask_row, a->token, a->lse};
+    for (const void *p : values)
+        if (!aligned(p, FPSK_ELEM_FP32)) return FPSK_ERR_ALIGN;
     if (a->history && (a->history_width < 0 || a->history_width > FPSK_MAX_HISTORY || a->history_stride < 0)) return FPSK_ERR_SHAPE;
     if (!a->history && (a->history_len || a->prompt_len || a->repetition || a->frequency || a->presence)) return FPSK_ERR_NULL;
     if (a->bias_ptr && (a->n_biases < 0 || (a->n_biases > 0 && (!a->bias_token || !a->bias_value)))) return FPSK_ERR_NULL;
