@@ -125,7 +125,7 @@ typedef struct {
     int32_t vocab, top;          /* 1 .. FPSK_MAX_VOCAB, 0 .. FPSK_MAX_TOP                             */
     int32_t logits_type, token_bytes, teacher_type, grad_type;
     int32_t normalize;
-    float temperature;           /* positive and finite                                                */
+    float temperature;           /* positive and finite, 5e-39 at least                                */
 } fpsk_distill;
 fpsk_status fpsk_distill_loss(const fpsk_distill *a, int32_t *d_status, void *stream);
 fpsk_status fpsk_distill_loss_backward(const fpsk_distill *a, int32_t *d_status, void *stream);

@@ -521,6 +521,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                 S = kept.y;
                 if (!g.sums) {
                     M = kept.x * g.tau;
+                    if (fabsf(kept.x) <= kMostFloat) M = fminf(fmaxf(M, -kMostFloat), kMostFloat);     // (any M will do)
                     S = expf(fmaf(-M, g.inv_tau, kept.x));             // what M's rounding left of it
                 }
             }
@@ -632,7 +633,7 @@ static fpsk_status distill(const fpsk_distill *a, float *sums, bool backward, in
         !aligned(sums, FPSK_ELEM_FP32))
         return FPSK_ERR_ALIGN;
     const double inv = 1.0 / (double)a->temperature;
-    if (inv > 3.4e38) return FPSK_ERR_PARAM;
+    if (inv * 1.4426950408889634 > 3.4e38) return FPSK_ERR_PARAM;      // (c)
     DistillArgs g = {};
     g.x = a->logits; g.tok = a->teacher_token; g.t = a->teacher_logit; g.weight = a->row_weight;
     g.loss = a->loss; g.lse = a->lse; g.sums = sums; g.dx = a->dlogits;

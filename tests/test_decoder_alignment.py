@@ -1,4 +1,5 @@
-"""Host-side checks of the decoder operators' C ABI: pointers that their types may not have are refused before a launch."""
+"""Host-side checks of the decoder operators' C ABI: pointers that their types may not have are refused before a launch, temperatures whose
+powers FP32 does not hold as well."""
 import ctypes as C
 import struct
 
@@ -47,3 +48,10 @@ def test_distill(lib):
         assert distill(lambda s, status, stream: f(s, P + 2, status, stream)) == fpsk.ERR_ALIGN
         assert f(None, P, None, None) == fpsk.ERR_NULL
     assert distill(lambda s, status, stream: lib.fpsk_distill_loss_backward_sums(s, None, status, stream), lse=0) == fpsk.ERR_NULL
+
+
+def test_temperatures_whose_powers_fp32_does_not_hold(lib):
+    """1 / tau is representable from 3e-39 on, log2(e) / tau, by which a logit becomes an exponent, from 4.3e-39."""
+    for f in (lib.fpsk_distill_loss, lib.fpsk_distill_loss_backward):
+        for tau in (3e-39, 4.2e-39):
+            assert distill(f, tau=tau) == fpsk.ERR_PARAM

@@ -179,3 +179,22 @@ def test_sums_that_are_refused_and_rows_without_weight():
     check(x, token, t, 1.0, True, weight, loss, lse, dx)
     empty = torch.empty(0, 500, device="cuda")
     L.distill_loss(empty, token[:0], t[:0], loss[:0], sums=sums[:0])
+
+
+def test_the_highest_temperatures():
+    """The log-sum-exp times the temperature is beyond FP32, its powers are not.  A factor of 1 / temperature below the normal numbers is off by
+    2^-149 / 1e-38, twice."""
+    x = torch.randn(4, 5001, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0))
+    token = torch.arange(8, device="cuda", dtype=torch.int32).repeat(4, 1)
+    t = torch.zeros(4, 8, device="cuda")
+    weight = torch.full((4,), 1e30, device="cuda")
+    want = torch.full((4, 5001), 1.0 / 5001, dtype=torch.float64, device="cuda")
+    want[:, :8] -= 0.125
+    for tau in (1e6, 1e37, 1e38):
+        loss, lse, dx, back = torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+        L.distill_loss(x, token, t, loss, row_weight=weight, lse=lse, dlogits=dx, temperature=tau)
+        L.distill_loss_backward(x, token, t, lse, weight, back, temperature=tau)
+        scale = 1e30 / tau
+        for got in (dx, back):
+            # the logits themselves move a probability by 5 / tau
+            assert float((got.double() / scale - want).abs().max()) <= (1.0 / 5001 + 0.125) * (64 * E + 3e-7 + 5 / tau)
