@@ -79,8 +79,9 @@ class VerifiedAttention:
         self.cos, self.sin = A.rotary_tables(n_pos, dim if rot_dim is None else rot_dim, device=dev)
         self.ws = A.attention_workspace(dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
-        self.state = fpsk.new_probe_state(dev)
-        self.result = fpsk.new_probe_result()
+        with torch.cuda.device(dev):
+            self.state = fpsk.new_probe_state(dev)
+        self.result = fpsk.new_probe_result(dev)
         self.probe_ws = {}
         self.last = None                                               # sequences and new tokens of the last step
 
@@ -90,10 +91,11 @@ class VerifiedAttention:
         if fault is not None:
             c[fault[0], fault[1]] += fault[2]
         key = (w.shape[0], w.shape[1])
-        if key not in self.probe_ws:                                   # (its size does not depend on the rows of x)
-            self.probe_ws[key] = fpsk.probe_workspace(1, *key)
-        fpsk.probe(x, w, c, self.probe_ws[key], self.result)
-        fpsk.probe_accumulate(self.result, self.state)
+        with torch.cuda.device(w.device):                              # (the probe runs on the current device)
+            if key not in self.probe_ws:                               # (its size does not depend on the rows of x)
+                self.probe_ws[key] = fpsk.probe_workspace(1, *key, device=w.device)
+            fpsk.probe(x, w, c, self.probe_ws[key], self.result)
+            fpsk.probe_accumulate(self.result, self.state)
         return c
 
     def step(self, x: torch.Tensor, seqs: Sequence[int], new: Sequence[int], fault=None) -> torch.Tensor:
@@ -141,7 +143,8 @@ class VerifiedAttention:
         """Whether any product since the last call was dirty (where a step is read on the host).  What the kernels of the append and the
         attention reported since then, a page outside the cache or a wait that gave up, is raised."""
         s = fpsk.read_probe_state(self.state)
-        fpsk.reset_probe_state(self.state)
+        with torch.cuda.device(self.state.device):
+            fpsk.reset_probe_state(self.state)
         reported = int(self.status)
         if reported != fpsk.STATUS_OK:
             self.status.zero_()

@@ -21,7 +21,8 @@ class VerifiedHead:
 
     def __init__(self, weight: torch.Tensor):
         self.weight = weight
-        self.state = fpsk.new_probe_state(weight.device)
+        with torch.cuda.device(weight.device):
+            self.state = fpsk.new_probe_state(weight.device)
         self.result = fpsk.new_probe_result(weight.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=weight.device)
         self.probe_ws = {}
@@ -32,10 +33,11 @@ class VerifiedHead:
         if fault is not None:
             c[fault[0], fault[1]] += fault[2]
         key = (b.shape[0], b.shape[1])
-        if key not in self.probe_ws:                                   # (its size does not depend on the rows of a)
-            self.probe_ws[key] = fpsk.probe_workspace(1, *key)
-        fpsk.probe(a, b, c, self.probe_ws[key], self.result)
-        fpsk.probe_accumulate(self.result, self.state)
+        with torch.cuda.device(b.device):                              # (the probe runs on the current device)
+            if key not in self.probe_ws:                               # (its size does not depend on the rows of a)
+                self.probe_ws[key] = fpsk.probe_workspace(1, *key, device=b.device)
+            fpsk.probe(a, b, c, self.probe_ws[key], self.result)
+            fpsk.probe_accumulate(self.result, self.state)
         return c
 
     def next_tokens(self, x: torch.Tensor, fault=None, **how) -> torch.Tensor:
@@ -63,7 +65,8 @@ class VerifiedHead:
     def fired(self) -> bool:
         """Whether any product since the last call was dirty.  What the kernels reported since then is raised."""
         s = fpsk.read_probe_state(self.state)
-        fpsk.reset_probe_state(self.state)
+        with torch.cuda.device(self.state.device):
+            fpsk.reset_probe_state(self.state)
         reported = int(self.status)
         if reported != fpsk.STATUS_OK:
             self.status.zero_()

@@ -1,0 +1,57 @@
+"""The host's part of the verified decoder, on tensors of the host with the library's calls replaced: devices, verdicts, sequences."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2609_19758_b200 import attention_layer as L
+from paper_2609_19758_b200 import decoder as M
+from paper_2609_19758_b200 import fpsk
+
+
+class Calls:
+    """Stands in for the library's calls and notes the device that is current (None: the caller's) and the one that each is given."""
+
+    def __init__(self, monkeypatch):
+        self.current, self.made = [None], []
+
+        @contextlib.contextmanager
+        def device(d):
+            self.current.append(torch.device(d).type)
+            yield
+            self.current.pop()
+
+        monkeypatch.setattr(torch.cuda, "device", device)
+        for name in ("new_probe_state", "new_probe_result", "probe_workspace", "probe", "probe_accumulate", "reset_probe_state", "read_probe_state"):
+            monkeypatch.setattr(fpsk, name, self.stand_in(name))
+        for module in (M, L):
+            monkeypatch.setattr(module.harness, "vendor_gemm_fp32", lambda a, b: a @ b)
+
+    def stand_in(self, name):
+        def f(*args, **kw):
+            given = kw.get("device", args[0] if name in ("new_probe_state", "new_probe_result") and args else None)
+            self.made.append((name, self.current[-1], None if given is None else torch.device(given).type))
+            return fpsk.ProbeState() if name == "read_probe_state" else torch.zeros(64, dtype=torch.uint8)
+        return f
+
+
+def test_verified_products_run_on_their_tensors_device(monkeypatch):
+    """The probe launches on the current device: that is the tensors' for the time of a call, and workspaces and verdicts lie there."""
+    calls = Calls(monkeypatch)
+    head = M.VerifiedHead(torch.ones(4, 6))
+    head.product(torch.ones(3, 4), head.weight)
+    assert not head.fired()
+    layer = L.VerifiedAttention.__new__(L.VerifiedAttention)
+    monkeypatch.setattr(L.A, "PagedCache", lambda k, v: None)
+    monkeypatch.setattr(L.A, "rotary_tables", lambda *a, **kw: (torch.zeros(1, 1), torch.zeros(1, 1)))
+    monkeypatch.setattr(L.A, "attention_workspace", lambda d: torch.zeros(1))
+    layer.__init__(torch.ones(4, 6), torch.ones(2, 4), 1, 1, 2, n_pages=1, n_pos=1)
+    layer._verified(torch.ones(3, 4), layer.qkv_weight)
+    assert not layer.fired()
+    names = [name for name, _, _ in calls.made]
+    assert all(names.count(n) == 2 for n in set(names)) and len(set(names)) == 7
+    for name, current, given in calls.made:
+        if name not in ("new_probe_result", "read_probe_state"):       # (these launch nothing of the library's)
+            assert current == "cpu", name
+        if name in ("new_probe_state", "new_probe_result", "probe_workspace"):
+            assert given == "cpu", name
