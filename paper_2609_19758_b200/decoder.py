@@ -25,18 +25,23 @@ class VerifiedHead:
             self.state = fpsk.new_probe_state(weight.device)
         self.result = fpsk.new_probe_result(weight.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=weight.device)
-        self.probe_ws = {}
+        self.probe_ws = []                                             # (the last one serves; graphs may hold those that it has replaced)
+
+    def _workspace(self, k: int, n: int) -> torch.Tensor:
+        """One for all products: training steps of many lengths have as many shapes of the weight's gradient.  Each is twice the one before at
+        least, so that all together are less than twice the last."""
+        held = self.probe_ws[-1].numel() if self.probe_ws else 0
+        if held < int(fpsk.lib().fpsk_probe_workspace_bytes(1, k, n)):  # (it does not depend on the rows of the other operand)
+            self.probe_ws.append(fpsk.probe_workspace(1, k, n, device=self.weight.device, room=2 * held))
+        return self.probe_ws[-1]
 
     def product(self, a: torch.Tensor, b: torch.Tensor, fault=None) -> torch.Tensor:
         """a b with the accumulator in FP32, probed; `fault`: (row, column, what to add), for trying the probe."""
         c = harness.vendor_gemm_fp32(a, b)
         if fault is not None:
             c[fault[0], fault[1]] += fault[2]
-        key = (b.shape[0], b.shape[1])
         with torch.cuda.device(b.device):                              # (the probe runs on the current device)
-            if key not in self.probe_ws:                               # (its size does not depend on the rows of a)
-                self.probe_ws[key] = fpsk.probe_workspace(1, *key, device=b.device)
-            fpsk.probe(a, b, c, self.probe_ws[key], self.result)
+            fpsk.probe(a, b, c, self._workspace(b.shape[0], b.shape[1]), self.result)
             fpsk.probe_accumulate(self.result, self.state)
         return c
 

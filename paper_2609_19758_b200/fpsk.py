@@ -272,9 +272,10 @@ def plan(m: int, k: int, n: int, dtype: int, sigma_hat: float, rms_c: float, m_c
     return ml.value, r.value, B.value
 
 
-def probe_workspace(m: int, k: int, n: int, device=None, stream=None) -> torch.Tensor:
-    """Allocate and prepare a probe workspace (torch owns the memory)."""
-    nbytes = int(lib().fpsk_probe_workspace_bytes(m, k, n))
+def probe_workspace(m: int, k: int, n: int, device=None, stream=None, room: int = 0) -> torch.Tensor:
+    """Allocate and prepare a probe workspace of `room` bytes at least (torch owns the memory).  It serves every shape that it is large
+    enough for, one call at a time."""
+    nbytes = max(int(lib().fpsk_probe_workspace_bytes(m, k, n)), room)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device or "cuda")
     rc = lib().fpsk_probe_init(ws.data_ptr(), nbytes, _stream_ptr(stream))
     if rc != STATUS_OK:

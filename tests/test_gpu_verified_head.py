@@ -1,0 +1,37 @@
+"""The verified head over many steps: its workspaces do not grow with the lengths of the batches, and serve all of its products."""
+import pytest
+import torch
+
+from paper_2609_19758_b200 import build as B
+from paper_2609_19758_b200 import decoder as M
+from paper_2609_19758_b200 import fpsk
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    B.build()
+
+
+def test_workspaces_do_not_grow_with_the_batches_lengths():
+    g = torch.Generator(device="cuda").manual_seed(0)
+    head = M.VerifiedHead((torch.randn(256, 1000, generator=g, device="cuda") / 16).half())
+    before = torch.cuda.memory_allocated()
+    lengths = list(range(8, 600, 8))
+    for rows in lengths + lengths[::-1]:
+        x = torch.randn(rows, 256, generator=g, device="cuda").half()
+        token = torch.randint(0, 1000, (rows, 4), generator=g, device="cuda", dtype=torch.int32)
+        head.distill(x, token, torch.zeros(rows, 4, device="cuda"))
+        head.next_tokens(x)
+        assert not head.fired()
+    need = max(int(fpsk.lib().fpsk_probe_workspace_bytes(1, k, n)) for k, n in [(256, 1000), (1000, 256)] + [(rows, 256) for rows in lengths])
+    del x, token
+    held = torch.cuda.memory_allocated() - before
+    assert held <= 4 * need, (held, need)                              # (the last is below twice what is needed, all below twice the last)
+    # a fault is seen in a product of each shape
+    for a, b in ((torch.randn(40, 256, device="cuda").half(), head.weight), (torch.randn(1000, 592, device="cuda").half(), torch.randn(592, 256, device="cuda").half())):
+        head.product(a, b, fault=(3, 5, 1e4))
+        assert head.fired()
+        head.product(a, b)
+        assert not head.fired()
