@@ -128,13 +128,21 @@ class VerifiedDecoder:
         self.stepped = 0
 
     def fired(self) -> bool:
-        """Whether any product since the last call was dirty (one host read a layer).  What the kernels reported is raised."""
-        fired = [layer.fired() for layer in self.layers] + [self.head.fired()]
+        """Whether any product since the last call was dirty (one host read a layer).  What the kernels reported is raised, after all verdicts
+        have been read: the next call's are those of what comes next."""
+        fired, raised = False, None
+        for part in [*self.layers, self.head]:
+            try:
+                fired |= part.fired()
+            except fpsk.FpskError as e:
+                raised = raised or e
         reported = int(self.status)
         if reported != fpsk.STATUS_OK:
             self.status.zero_()
-            raise fpsk.FpskError(reported, "verified decoder")
-        return any(fired)
+            raised = raised or fpsk.FpskError(reported, "verified decoder")
+        if raised is not None:
+            raise raised
+        return fired
 
     def generate(self, prompts: Sequence[Sequence[int]], steps: int, repetition: float = 1.0, frequency: float = 0.0, presence: float = 0.0,
                  mask: Optional[torch.Tensor] = None, fault_at: int = -1) -> List[List[int]]:

@@ -55,3 +55,38 @@ def test_verified_products_run_on_their_tensors_device(monkeypatch):
             assert current == "cpu", name
         if name in ("new_probe_state", "new_probe_result", "probe_workspace"):
             assert given == "cpu", name
+
+
+class Layer:
+    """A layer whose verdicts and pages are lists."""
+
+    def __init__(self, verdicts=(), opened=0):
+        self.verdicts, self.pages = list(verdicts), L.PageTable(4, 16)
+        for _ in range(opened):
+            self.pages.open()
+
+    def fired(self):
+        v = self.verdicts.pop(0)
+        if isinstance(v, Exception):
+            raise v
+        return v
+
+
+def decoder(layers, head=None):
+    return M.VerifiedDecoder(torch.zeros(5, 8), layers, [torch.ones(8)] * (len(layers) + 1), head)
+
+
+def test_all_verdicts_are_read_before_one_is_raised():
+    """A verdict that stays unread would be the next step's."""
+    dirty, bad = fpsk.FpskError(fpsk.ERR_TIMEOUT, "attention layer"), fpsk.FpskError(fpsk.ERR_PARAM, "verified head")
+    d = decoder([Layer([dirty, False, False]), Layer([True, False, True])], Layer([bad, False, False]))
+    d.status.fill_(fpsk.ERR_PARAM)
+    with pytest.raises(fpsk.FpskError) as e:
+        d.fired()
+    assert e.value is dirty
+    assert d.fired() is False and d.fired() is True
+    d = decoder([Layer([True, False])], Layer([False, False]))
+    d.status.fill_(fpsk.ERR_PARAM)
+    with pytest.raises(fpsk.FpskError, match="decoder"):
+        d.fired()
+    assert d.fired() is False
