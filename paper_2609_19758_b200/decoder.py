@@ -83,15 +83,20 @@ class VerifiedDecoder:
     """Token embeddings (vocab, hidden), attention layers with a norm weight (hidden,) in front of each, a last norm weight, a head."""
 
     def __init__(self, embedding: torch.Tensor, layers: Sequence[VerifiedAttention], norm_weights: Sequence[torch.Tensor], head: VerifiedHead, eps: float = 1e-6):
-        if len(norm_weights) != len(layers) + 1:
-            raise ValueError("a norm weight for each layer and one for the head")
+        if not layers or len(norm_weights) != len(layers) + 1:
+            raise ValueError("a norm weight for each layer, of which there is one at least, and one for the head")
         self.embedding, self.layers, self.norm_weights, self.head, self.eps = embedding, list(layers), list(norm_weights), head, eps
         self.status = torch.zeros(1, dtype=torch.int32, device=embedding.device)
         self.stepped = 0
 
     def open(self) -> int:
         """A new sequence."""
-        return [layer.pages.open() for layer in self.layers][0]
+        seqs = [layer.pages.open() for layer in self.layers]
+        if len(set(seqs)) > 1:                                         # (one number stands for all layers: another's sequence would be written to)
+            for layer, seq in zip(self.layers, seqs):
+                layer.pages.close(seq)
+            raise RuntimeError("the layers have had different numbers of sequences: they serve one decoder, and in one place")
+        return seqs[0]
 
     def close(self, seq: int) -> None:
         for layer in self.layers:

@@ -90,3 +90,16 @@ def test_all_verdicts_are_read_before_one_is_raised():
     with pytest.raises(fpsk.FpskError, match="decoder"):
         d.fired()
     assert d.fired() is False
+
+
+def test_layers_that_are_not_at_the_same_sequence_are_refused():
+    """A sequence has one number in all layers: a layer that has been used by itself, or stands in two places, gives another."""
+    d = decoder([Layer(), Layer()])
+    assert [d.open(), d.open()] == [0, 1]
+    for layers in ([Layer(opened=1), Layer()], [Layer()] * 2):
+        d = decoder(layers)
+        with pytest.raises(RuntimeError, match="sequences"):
+            d.open()
+        assert all(layer.pages.length == [0] * len(layer.pages.rows) for layer in layers)
+    with pytest.raises(ValueError):
+        decoder([])
