@@ -20,6 +20,9 @@ fpsk_status fpsk_selftest_bounded_wait(uint32_t *d_flag, fpsk_probe_result *d_re
 /* Number of kernels launched by this library since load (all entry points, all threads). */
 uint64_t fpsk_launch_count(void);
 
+/* How many of those were the form for many rows of the residual addition and norm, forward or backward (fpsk_decoder.h). */
+uint64_t fpsk_norm_ring_count(void);
+
 /* Number of auxiliary stream sets and pinned buffers the library has created by itself since load (calls made
  * with a context create none). */
 uint64_t fpsk_lazy_resource_count(void);

@@ -49,6 +49,7 @@ __device__ __forceinline__ unsigned int e4m3_pair(float a, float b)
 
 // add_norm_ring.cu, add_norm_ring_grad.cu: true where the ring takes the call (*rc is its status then); `rows` of partial weight gradients
 // are left in g.part.
+void count_ring();
 bool norm_ring(const NormArgs &g, bool wide, int x_type, int res_type, int32_t *d_status, cudaStream_t st, fpsk_status *rc);
 bool norm_grad_ring(const NormGradArgs &g, bool wide, int h_type, int grad_type, int32_t *d_status, cudaStream_t st, fpsk_status *rc, int *rows);
 

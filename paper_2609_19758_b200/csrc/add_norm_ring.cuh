@@ -495,6 +495,7 @@ template <typename X, typename R, bool GRAD> static fpsk_status launch_ring(cons
     launch.cfg.gridDim = dim3((unsigned)(most * g.blocks));
     FPSK_CUDA_OK(cudaLaunchKernelEx(&launch.cfg, kernel, g));
     FPSK_LAUNCH_CHECK();
+    count_ring();
     return FPSK_OK;
 }
 static RingRows ring_rows(const void *p, long long stride, int type)

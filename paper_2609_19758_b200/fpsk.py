@@ -156,6 +156,8 @@ def lib() -> C.CDLL:
         L.fpsk_selftest_bounded_wait.argtypes = [vp, vp, vp]
         L.fpsk_launch_count.restype = u64
         L.fpsk_launch_count.argtypes = []
+        L.fpsk_norm_ring_count.restype = u64
+        L.fpsk_norm_ring_count.argtypes = []
         L.fpsk_lazy_resource_count.restype = u64
         L.fpsk_lazy_resource_count.argtypes = []
         L.fpsk_debug_bounds_report.restype = i32

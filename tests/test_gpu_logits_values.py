@@ -17,7 +17,6 @@ def _built():
     B.build()
 
 
-
 def test_rows_of_the_lowest_value():
     """Logits that a mask has set to the type's lowest value are numbers still: the first of them is the token, their log-sum-exp that value."""
     for dtype in (F32, BF16, F16):
