@@ -487,13 +487,10 @@ template <typename X, typename O, typename W> __global__ void __launch_bounds__(
                         float b = known ? bias_b : g.bias_value[i];
                         if (words[where] & F::kBiasedTwice) {          // the first of its entries does it, in the list's order
                             bool mine_to_do = true;
-                            b = 0.f;
-                            for (long long k = b0; k < b1; ++k)
-                                if (g.bias_token[k] == v) {
-                                    if (k < i) mine_to_do = false;
-                                    b += g.bias_value[k];
-                                }
+                            for (long long k = b0; k < i && mine_to_do; ++k) mine_to_do = g.bias_token[k] != v;
                             if (!mine_to_do) continue;
+                            for (long long k = i + 1; k < b1; ++k)
+                                if (g.bias_token[k] == v) b += g.bias_value[k];
                         }
                         single(v, adjusted(known && where < chunk_tokens ? bias_l : Elem<X>::to_f(x[v]), words[where]) + b);
                     }

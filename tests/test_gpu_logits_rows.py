@@ -53,3 +53,21 @@ def test_in_place_with_the_token_and_the_log_sum_exp(rows, vocab, width, biases,
         assert torch.equal(y, out) and bool((whole[:, vocab:] == 7.0).all())
         assert "token" not in want or torch.equal(t2, token)
         assert "lse" not in want or torch.equal(l2, lse)
+
+
+def test_a_long_list_that_names_one_token_again_and_again():
+    """Entries behind a token's first one are done with as soon as they have met it: a list of n entries of one token takes n steps of one thread, not
+    n for each entry (the other blocks of the row wait, and give up after a second)."""
+    n, vocab = 200000, 40000
+    r = np.random.default_rng(0)
+    values = r.integers(-8, 9, n).astype(np.float32)                   # (sums that FP32 holds)
+    tokens = np.full(n, 777, dtype=np.int64)
+    tokens[::1000] = np.arange(200) * 150
+    x = torch.zeros(2, vocab, device="cuda")
+    out, token, status = torch.empty_like(x), torch.empty(2, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    bias = tuple(torch.tensor(a, dtype=t, device="cuda") for a, t in ((np.array([0, n, n]), torch.int32), (tokens, torch.int32), (values, F32)))
+    L.adjust_logits(x, out, bias=bias, token=token, status=status)
+    want = np.zeros(vocab)
+    np.add.at(want, tokens, values.astype(np.float64))
+    assert int(status) == 0 and np.array_equal(out[0].double().cpu().numpy(), want) and bool((out[1] == 0).all())
+    assert token.tolist() == [int(want.argmax()), 0]
