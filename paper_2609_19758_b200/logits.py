@@ -58,21 +58,25 @@ def distill_loss_backward(logits: torch.Tensor, teacher_token: torch.Tensor, tea
 
 
 class DistillLoss(torch.autograd.Function):
-    """distill_loss for autograd: ``apply(logits, teacher_token, teacher_logit, temperature, normalize)`` returns the rows' losses.  The
-    teacher gets no gradient; a second derivative is refused."""
+    """distill_loss for autograd: ``apply(logits, teacher_token, teacher_logit, temperature, normalize, row_weight=None)`` returns the rows'
+    losses.  Rows whose row_weight is 0 (padding) are not read: their loss and gradient are 0, whatever they hold; the other losses come
+    as they are, for the caller to weight.  The teacher gets no gradient; a second derivative is refused."""
 
     @staticmethod
-    def forward(ctx, logits, teacher_token, teacher_logit, temperature, normalize):
+    def forward(ctx, logits, teacher_token, teacher_logit, temperature, normalize, row_weight=None):
         loss, sums = (torch.empty(logits.shape[0], *more, dtype=torch.float32, device=logits.device) for more in ((), (2,)))
-        distill_loss(logits, teacher_token, teacher_logit, loss, temperature=temperature, normalize=normalize, sums=sums)
-        ctx.save_for_backward(logits, teacher_token, teacher_logit, sums)
+        distill_loss(logits, teacher_token, teacher_logit, loss, row_weight=row_weight, temperature=temperature, normalize=normalize, sums=sums)
+        ctx.save_for_backward(logits, teacher_token, teacher_logit, sums, row_weight)
         ctx.more = (temperature, normalize)
         return loss
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dloss):
-        logits, teacher_token, teacher_logit, sums = ctx.saved_tensors
+        logits, teacher_token, teacher_logit, sums, row_weight = ctx.saved_tensors
+        dloss = dloss.float().contiguous()
+        if row_weight is not None:
+            dloss = dloss.masked_fill(row_weight == 0, 0.0)
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        distill_loss_backward(logits, teacher_token, teacher_logit, None, dloss.float().contiguous(), dlogits, *ctx.more, sums=sums)
-        return dlogits, None, None, None, None
+        distill_loss_backward(logits, teacher_token, teacher_logit, None, dloss, dlogits, *ctx.more, sums=sums)
+        return dlogits, None, None, None, None, None

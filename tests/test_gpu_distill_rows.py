@@ -86,3 +86,24 @@ def test_gradients_of_a_learnt_token(vocab, grad):
         l, d, _, mag, dmag = D.distill(raw, token[i].tolist(), t[i].tolist(), 1.0, True)
         assert l > 1e-3 and abs(float(loss[i]) - l) <= 64 * E * mag
         assert np.all(np.abs(np64(dx[i]) - d) <= u * np.abs(d) + (70 + 2 * (raw.max() - raw)) * E * dmag + 2.0 ** -126)
+
+
+def test_padding_in_autograd():
+    """Rows without weight hold NaN and infinities, which reach neither the weighted sum nor the gradient."""
+    x, token, t, weight = listed(9, 300, 4001, 12, F32, True)
+    pad = weight == 0
+    x[pad] = float("nan")
+    x[pad.nonzero()[0]] = float("inf")
+    t[pad] = float("nan")
+    assert 50 < int(pad.sum()) < 150
+    x.requires_grad_()
+    loss = L.DistillLoss.apply(x, token, t, 1.0, True, weight)
+    (loss * weight).sum().backward()
+    check(x.detach(), token, t, 1.0, True, weight, loss.detach(), None, x.grad)
+    x.grad = None
+    L.DistillLoss.apply(x, token, t, 1.0, True, weight).sum().backward()                 # (whatever gradient a loss of padding gets)
+    check(x.detach(), token, t, 1.0, True, (~pad).float(), None, None, x.grad)
+    # as before without it
+    y = x.detach()[~pad].requires_grad_()
+    L.DistillLoss.apply(y, token[~pad], t[~pad], 1.0, True).sum().backward()
+    check(y.detach(), token[~pad], t[~pad], 1.0, True, None, None, None, y.grad)
