@@ -64,6 +64,22 @@ template <typename X> __device__ __forceinline__ void add_powers(const uint4 &u,
         sum = __fadd2_rn(sum, make_float2(exp2_fast(y.x), exp2_fast(y.y)));
     }
 }
+// 2^((x - M) c) summed, joined over a warp's first LANES lanes like join_lanes, in 64 bits: what is rounded at the size of the whole sum is
+// rounded once, so that the order of the additions, which goes by a row's alignment, rarely shows.
+struct LongSum {
+    float m;
+    double s;
+};
+template <int LANES> __device__ __forceinline__ LongSum join_long(LongSum r, float c)
+{
+    float top = r.m;
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    double s = r.s * (double)exp2_fast((r.m - top) * c);
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    return LongSum{top, s};
+}
 // f 2^((x - M) c)
 template <typename X> __device__ __forceinline__ void gradients(const uint4 &u, float2 minus, float2 cc, float2 ff, float2 (&e)[Vec<X>::n / 2])
 {
@@ -81,7 +97,7 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ unsigned long long full[kStages], empty[kStages], ready[2], met[2];
     __shared__ float4 blocks_sum[2][kRowMostBlocks];                   // written by the cluster's blocks: M, S, the teacher's two
-    __shared__ float2 warps_sum[2][kWorkers / 32];
+    __shared__ LongSum warps_sum[2][kWorkers / 32];
     __shared__ float4 result[2], taught[2];                            // M, S, the teacher's two; K, xr, the teacher's two
     __shared__ float teams[6][kMostTeachers], highest[2];              // highest: of the block's listed logits
     __shared__ int teams_twice[kMostTeachers], counts[2][kMostTeachers];
@@ -486,11 +502,10 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                         phase ^= 1u;
                     }
                 }
-                RefSum r = join_lanes<32>(RefSum{-minus.x, s2.x + s2.y}, c);
-                if (lane == 0) warps_sum[b][warp] = make_float2(r.m, r.s);
+                LongSum r = join_long<32>(LongSum{-minus.x, (double)s2.x + (double)s2.y}, c);
+                if (lane == 0) warps_sum[b][warp] = r;
                 bar_sync(1, kWorkers);
-                const float2 mine = warps_sum[b][lane % (kWorkers / 32)];
-                r = join_lanes<kWorkers / 32>(RefSum{mine.x, mine.y}, c);
+                r = join_long<kWorkers / 32>(warps_sum[b][lane % (kWorkers / 32)], c);
                 // (the teacher's logits are read before any block goes on to write the gradient, perhaps in the logits' place)
                 wait(ready[b], n >> 1 & 1u);
                 said = make_float2(taught[b].z, taught[b].w);
@@ -503,17 +518,17 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                             "mapa.shared::cluster.u32 a, %0, %2;\n\t"
                             "mapa.shared::cluster.u32 m, %1, %2;\n\t"
                             "st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %6}, [m];\n\t}"
-                            ::"r"(at), "r"(bar), "r"(tid), "f"(r.m), "f"(r.s), "f"(said.x), "f"(said.y)
+                            ::"r"(at), "r"(bar), "r"(tid), "f"(r.m), "f"((float)r.s), "f"(said.x), "f"(said.y)
                             : "memory");
                     }
                     wait(met[b], n >> 1 & 1u);
                     const float4 theirs = lane < g.blocks ? blocks_sum[b][lane] : make_float4(kNoReference, 0.f, 0.f, 0.f);
                     said = make_float2(blocks_sum[b][0].z, blocks_sum[b][0].w);
-                    r = join_lanes<kRowMostBlocks>(RefSum{theirs.x, theirs.y}, c);
-                    r = RefSum{__shfl_sync(0xFFFFFFFFu, r.m, 0), __shfl_sync(0xFFFFFFFFu, r.s, 0)};
+                    r = join_long<kRowMostBlocks>(LongSum{theirs.x, theirs.y}, c);
+                    r = LongSum{__shfl_sync(0xFFFFFFFFu, r.m, 0), __shfl_sync(0xFFFFFFFFu, r.s, 0)};
                 }
                 M = r.m;
-                S = r.s;
+                S = (float)r.s;
             } else {
                 wait(ready[b], n >> 1 & 1u);
                 said = make_float2(taught[b].z, taught[b].w);
