@@ -2,7 +2,8 @@
 //
 // q = softmax(x / tau), p over the listed tokens; loss = sum_j p_j (log p_j - log q_j); d/dx_v = (m q_v - p_v) / tau, m = sum p.
 // In powers of two, with c = log2(e) / tau and a reference M near the row's largest logit: S = sum 2^((x - M) c), q_v = 2^((x_v - M) c) / S,
-// log q_v = (x_v - M) / tau - ln S.  M and S stay apart to the end, so that nothing is rounded at the size of the logarithm.
+// log q_v = (x_v - M) / tau - ln S.  M and S stay apart to the end, and from the loss to a gradient that comes later, so that nothing is
+// rounded at the size of the logarithm.
 //
 // What bounds it is memory: the logits once, the gradient once.  The gradient needs S first, so a row is looked at twice; the second look
 // finds it in L2 as long as the rows at work at a time are not too many bytes, which a cluster of blocks to a row sees to.  One warp of a
@@ -10,7 +11,7 @@
 // cluster's shared memory, and write the gradient; one or three warps prepare the teacher's probabilities for the next row and take them off the
 // gradient of the one before, so that neither is waited for.
 //
-// Measured: 4096 rows of 131072 FP32 logits with BF16 gradients 537 us in a burst (6.0 TB/s of logits and gradients, 0.92 of a copy),
+// Measured: 4096 rows of 131072 FP32 logits with BF16 gradients 541 us in a burst (6.0 TB/s of logits and gradients, 0.91 of a copy),
 // 632 sustained, at the power limit; losses of 2048 rows of 65536 BF16 52 us (0.79; the special function unit, which makes the powers, is busy
 // for 66 %); loss, then gradient of 1500 x 50257 FP16 94 us; 5 rows of 131072 11 us.  (Without the
 // largest listed logit as reference 521, 49 and 9 us.)  Rows held in shared memory between the two looks

@@ -45,9 +45,9 @@ def add_rms_norm_backward(h: torch.Tensor, dy: torch.Tensor, weight: Optional[to
 
 
 class AddRMSNorm(torch.autograd.Function):
-    """add_rms_norm with its gradients for autograd: ``apply(x, residual, weight, out_dtype, eps)`` returns y in out_dtype and the sum h
-    in the residual's type (in x's where residual is None).  The gradient is computed and rounded once in the type of x where all types
-    agree, else in FP32; a second derivative is refused."""
+    """add_rms_norm with its gradients for autograd: ``apply(x, residual, weight, out_dtype, eps)`` returns y in out_dtype (16 bits or FP32: an
+    8-bit y, which wants scales, is add_rms_norm's alone) and the sum h in the residual's type (in x's where residual is None).  The
+    gradient is computed and rounded once in the type of x where all types agree, else in FP32; a second derivative is refused."""
 
     @staticmethod
     def forward(ctx, x, residual, weight, out_dtype, eps):
