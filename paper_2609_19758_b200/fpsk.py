@@ -247,7 +247,8 @@ def _mat_args(A: torch.Tensor, B: torch.Tensor, Cm: torch.Tensor, b_transposed: 
     """(A, lda, B, ldb, C, ldc, m, k, n, dtype); with b_transposed, B is the weight W = B^T of shape (n, k)."""
     assert A.is_cuda and B.is_cuda and Cm.is_cuda, "A, B, C must be device tensors"
     assert A.dim() == 2 and B.dim() == 2 and Cm.dim() == 2
-    assert A.stride(1) == 1 and B.stride(1) == 1 and Cm.stride(1) == 1, "row-major (unit column stride) required"
+    # (a single column has any stride: the transpose of one row, which is contiguous as it is, says the row's length)
+    assert all(t.stride(1) == 1 or t.shape[1] == 1 for t in (A, B, Cm)), "row-major (unit column stride) required"
     m, k = A.shape
     if b_transposed:
         n, k2 = B.shape

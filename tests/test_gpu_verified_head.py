@@ -35,3 +35,27 @@ def test_workspaces_do_not_grow_with_the_batches_lengths():
         assert head.fired()
         head.product(a, b)
         assert not head.fired()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [1, 2, 7])
+def test_few_rows_and_rows_without_weight(rows, dtype):
+    """A training step of one position, whose logits' gradient is a single column when it is transposed, and one without any weight."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    head = M.VerifiedHead((torch.randn(256, 3000, generator=g, device="cuda") / 16).to(dtype))
+    x = torch.randn(rows, 256, generator=g, device="cuda").to(dtype)
+    token = torch.randint(0, 3000, (rows, 5), generator=g, device="cuda", dtype=torch.int32)
+    t = torch.randn(rows, 5, generator=g, device="cuda")
+    loss, dx, dw = head.distill(x, token, t)
+    assert not head.fired() and dx.shape == x.shape and dw.shape == head.weight.shape
+    xd, wd = x.double().requires_grad_(), head.weight.double().requires_grad_()
+    logq, logp = torch.log_softmax(xd @ wd, -1), torch.log_softmax(t.double(), -1)
+    want = (logp.exp() * (logp - logq.gather(1, token.long()))).sum(-1)
+    want.sum().backward()
+    # as in the decoder's own test: the logits' gradient is rounded to 16 bits, the products are FP32
+    u = torch.finfo(dtype).eps / 2
+    assert float((loss.double() - want.detach()).abs().max()) <= 2.0 ** -16 * float(want.detach().abs().max())
+    for got, ref in ((dx, xd.grad), (dw, wd.grad)):
+        assert float((got.double() - ref).norm() / ref.norm()) <= 2 * u + 2.0 ** -16
+    loss, dx, dw = head.distill(x, token, t, torch.zeros(rows, device="cuda"))
+    assert not head.fired() and not bool(loss.any()) and not bool(dx.any()) and not bool(dw.any())
