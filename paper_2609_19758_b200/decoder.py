@@ -58,14 +58,23 @@ class VerifiedHead:
         sum(row_weight * loss) with respect to x and the weight.  Three products, all verified; the gradient of the logits is made
         in the operands' type in the pass that makes the losses."""
         c = self.product(x, self.weight)
+        # FP16 ends at 6e-8, which probabilities times the weights of a mean are below: the logits' gradient is made for weights whose
+        # largest, by the temperature, is 2^8 to 2^9, and the products are scaled back.  (Powers of two, made on the device.)
+        back = None
+        if x.dtype == torch.float16:
+            most = torch.ones(1, device=x.device) if row_weight is None else row_weight.abs().amax().view(1)
+            scale = torch.exp2(8 - torch.floor(torch.log2((most / temperature).clamp(2.0 ** -100, 2.0 ** 100))))
+            row_weight, back = scale.expand(x.shape[0]).contiguous() if row_weight is None else row_weight * scale, 1 / scale
         loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
         dlogits = torch.empty(c.shape, dtype=x.dtype, device=x.device)
         logits.distill_loss(c, teacher_token, teacher_logit, loss, row_weight=row_weight, dlogits=dlogits, temperature=temperature, normalize=normalize,
                             status=self.status)
         # The probe compares the columns' sums of an error with their mean: the products are laid out so that the logits' gradient, whose
         # columns differ by orders of magnitude between tokens that are listed and others, has the rows, not the columns.
-        dx = self.product(dlogits, self.weight.t().contiguous())
-        return loss, dx, self.product(dlogits.t().contiguous(), x).t()
+        dx, dw = self.product(dlogits, self.weight.t().contiguous()), self.product(dlogits.t().contiguous(), x).t()
+        if back is not None:
+            dx, dw = dx.mul_(back), dw.mul_(back)
+        return loss, dx, dw
 
     def fired(self) -> bool:
         """Whether any product since the last call was dirty.  What the kernels reported since then is raised."""

@@ -59,3 +59,29 @@ def test_few_rows_and_rows_without_weight(rows, dtype):
         assert float((got.double() - ref).norm() / ref.norm()) <= 2 * u + 2.0 ** -16
     loss, dx, dw = head.distill(x, token, t, torch.zeros(rows, device="cuda"))
     assert not head.fired() and not bool(loss.any()) and not bool(dx.any()) and not bool(dw.any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab,weight", [(160, 3000, 1.0 / 4096), (64, 40000, 1.0 / 65536), (3, 3000, 1e-3), (1, 3000, 1e-3), (2, 3000, 1e-12), (40, 3000, 3e4)])
+def test_weights_of_any_size(rows, vocab, weight, dtype):
+    """Gradients of a mean over many positions (or of a scaled loss): the logits' gradient is rounded relative to itself, not to what FP16 can
+    hold.  Bounds as for weights of 1."""
+    g = torch.Generator(device="cuda").manual_seed(vocab + rows)
+    head = M.VerifiedHead((torch.randn(256, vocab, generator=g, device="cuda") / 16).to(dtype))
+    x = torch.randn(rows, 256, generator=g, device="cuda").to(dtype)
+    token = torch.randint(0, vocab, (rows, 6), generator=g, device="cuda", dtype=torch.int32)
+    t = torch.randn(rows, 6, generator=g, device="cuda")
+    w = weight * (0.5 + torch.rand(rows, generator=g, device="cuda"))
+    if rows > 8:
+        w[::5] = 0.0
+    loss, dx, dw = head.distill(x, token, t, w, temperature=1.5)
+    assert not head.fired()
+    xd, wd = x.double().requires_grad_(), head.weight.double().requires_grad_()
+    logq, logp = torch.log_softmax(xd @ wd / 1.5, -1), torch.log_softmax(t.double() / 1.5, -1)
+    want = (logp.exp() * (logp - logq.gather(1, token.long()))).sum(-1)
+    (want * w.double()).sum().backward()
+    u = torch.finfo(dtype).eps / 2
+    live = w != 0
+    assert float((loss.double() - want.detach())[live].abs().max()) <= 2.0 ** -16 * float(want.detach().abs().max())
+    for got, ref in ((dx, xd.grad), (dw, wd.grad)):
+        assert float((got.double() - ref).norm() / ref.norm()) <= 2 * u + 2.0 ** -16
