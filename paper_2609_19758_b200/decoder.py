@@ -16,6 +16,16 @@ from . import fpsk, harness, logits, norm
 from .attention_layer import VerifiedAttention
 
 
+MOST_PROBED = 1 << 17      # columns of a product that are probed together, and half of the channels that it sums over (a probe takes 1.15 times as many)
+
+
+def _parts(n: int, most: int):
+    """The ranges of 0 .. n of at most `most`, as long as each other but for multiples of 8."""
+    step = -(-n // (-(-n // most)))
+    step += -step % 8
+    return [(i, min(n, i + step)) for i in range(0, n, step)]
+
+
 class VerifiedHead:
     """The product of a model's last states with a weight (hidden, vocab), verified, and what follows it."""
 
@@ -37,12 +47,19 @@ class VerifiedHead:
 
     def product(self, a: torch.Tensor, b: torch.Tensor, fault=None) -> torch.Tensor:
         """a b with the accumulator in FP32, probed; `fault`: (row, column, what to add), for trying the probe."""
+        if b.shape[0] > 2 * MOST_PROBED:                               # (a sum over a wide vocabulary: parts of it, added up)
+            (first, last), *rest = _parts(b.shape[0], 2 * MOST_PROBED)
+            c = self.product(a[:, first:last], b[first:last], fault)
+            for first, last in rest:
+                c += self.product(a[:, first:last], b[first:last])
+            return c
         c = harness.vendor_gemm_fp32(a, b)
         if fault is not None:
             c[fault[0], fault[1]] += fault[2]
         with torch.cuda.device(b.device):                              # (the probe runs on the current device)
-            fpsk.probe(a, b, c, self._workspace(b.shape[0], b.shape[1]), self.result)
-            fpsk.probe_accumulate(self.result, self.state)
+            for first, last in _parts(b.shape[1], MOST_PROBED):
+                fpsk.probe(a, b[:, first:last], c[:, first:last], self._workspace(b.shape[0], last - first), self.result)
+                fpsk.probe_accumulate(self.result, self.state)
         return c
 
     def next_tokens(self, x: torch.Tensor, fault=None, **how) -> torch.Tensor:

@@ -103,3 +103,11 @@ def test_layers_that_are_not_at_the_same_sequence_are_refused():
         assert all(layer.pages.length == [0] * len(layer.pages.rows) for layer in layers)
     with pytest.raises(ValueError):
         decoder([])
+
+
+def test_parts_of_wide_products():
+    for n in [1, 7, 8, 9, 131071, 131072, 131073, 151936, 262145, 300000, (1 << 23) - 1, 1 << 23]:
+        parts = M._parts(n, M.MOST_PROBED)
+        assert parts[0][0] == 0 and parts[-1][1] == n and all(a[1] == b[0] for a, b in zip(parts, parts[1:]))
+        assert all(0 < b - a <= M.MOST_PROBED and a % 8 == 0 for a, b in parts) and len(parts) == -(-n // M.MOST_PROBED)
+        assert min(b - a for a, b in parts) > max(b - a for a, b in parts) - 8 * len(parts) - 8

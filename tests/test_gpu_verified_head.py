@@ -85,3 +85,34 @@ def test_weights_of_any_size(rows, vocab, weight, dtype):
     assert float((loss.double() - want.detach())[live].abs().max()) <= 2.0 ** -16 * float(want.detach().abs().max())
     for got, ref in ((dx, xd.grad), (dw, wd.grad)):
         assert float((got.double() - ref).norm() / ref.norm()) <= 2 * u + 2.0 ** -16
+
+
+@pytest.mark.parametrize("vocab", [131080, 151936, 200001, 300000])
+def test_wide_vocabularies(vocab):
+    """More columns, or channels to sum over, than one probe takes: the product is probed in parts, and a fault is seen in each."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    rows, hidden = 24, 64
+    head = M.VerifiedHead((torch.randn(hidden, vocab, generator=g, device="cuda") / 8).half())
+    x = torch.randn(rows, hidden, generator=g, device="cuda").half()
+    picked = head.next_tokens(x)
+    assert not head.fired()
+    z = x.double() @ head.weight.double()
+    # (products of FP16 are exact in FP32, sums of 64 of them off by 64 roundings of at most 64 x 4 x 4 / 8)
+    assert float((z.amax(1) - z.gather(1, picked.long()[:, None])[:, 0]).abs().max()) <= 2 * 64 * 2.0 ** -24 * 128
+    for column in (0, vocab // 2, vocab - 1):
+        head.next_tokens(x, fault=(5, column, 30.0))
+        assert head.fired()
+    token = torch.randint(0, vocab, (rows, 6), generator=g, device="cuda", dtype=torch.int32)
+    t = torch.randn(rows, 6, generator=g, device="cuda")
+    loss, dx, dw = head.distill(x, token, t)
+    assert not head.fired()
+    xd, wd = x.double().requires_grad_(), head.weight.double().requires_grad_()
+    logq, logp = torch.log_softmax(xd @ wd, -1), torch.log_softmax(t.double(), -1)
+    (logp.exp() * (logp - logq.gather(1, token.long()))).sum().backward()
+    for got, ref in ((dx, xd.grad), (dw, wd.grad)):
+        assert float((got.double() - ref).norm() / ref.norm()) <= 2.0 ** -10 + 2.0 ** -16
+    a = torch.randn(40, vocab, generator=g, device="cuda").half()
+    for _ in range(2):
+        head.product(a, head.weight.t().contiguous(), fault=(3, 5, 3e4))
+        assert head.fired()
+        assert head.product(a, head.weight.t().contiguous()).shape == (40, hidden) and not head.fired()
