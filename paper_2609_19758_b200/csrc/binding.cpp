@@ -61,11 +61,13 @@ int device_of(const at::Tensor &t, const char *what)
     if (!t.is_cuda()) refuse(PyExc_ValueError, "%s: a CUDA tensor expected", what);
     return t.get_device();
 }
+// whether the last dimension is contiguous: without elements it is, whatever a gradient that was expanded from a number says
+bool contiguous_last(const at::Tensor &t) { return t.size(-1) <= 1 || t.stride(-1) == 1 || t.numel() == 0; }
 // (tokens, heads, channels) with contiguous channels
 void check_heads(const at::Tensor &t, int64_t tokens, int64_t heads, int64_t dim, at::ScalarType type, int device, const char *what)
 {
     if (t.dim() != 3 || t.size(0) != tokens || t.size(1) != heads || t.size(2) != dim || t.scalar_type() != type || !t.is_cuda() ||
-        t.get_device() != device || (dim > 1 && t.stride(2) != 1))
+        t.get_device() != device || !contiguous_last(t))
         refuse(PyExc_ValueError, "%s: expected (%lld, %lld, %lld) %s on cuda:%d with contiguous channels", what, (long long)tokens,
                (long long)heads, (long long)dim, c10::toString(type), device);
 }
@@ -380,7 +382,7 @@ const at::Tensor &rows_of(PyObject *o, int64_t rows, int64_t n, int device, cons
 {
     const at::Tensor &t = needed(o, what);
     if (t.dim() != 2 || !t.is_cuda() || t.get_device() != device || (rows >= 0 && t.size(0) != rows) || (n >= 0 && t.size(1) != n) ||
-        (t.size(1) > 1 && t.stride(1) != 1))
+        !contiguous_last(t))
         refuse(PyExc_ValueError, "%s: (%lld, %lld) on cuda:%d with contiguous rows expected (-1: any)", what, (long long)rows, (long long)n, device);
     return t;
 }
