@@ -43,7 +43,7 @@ constexpr int kWorkers = 128, kMostTeachers = 3;   // threads of the sums and gr
 constexpr int kDistillThreads = kWorkers + 32 + 32 * kMostTeachers;
 constexpr int kPiece = 8192, kPieceVecs = kPiece / 16, kStages = 5;
 constexpr int kTogether = 4;            // listed tokens of a lane at a time
-constexpr float kMostPowers = 64.f;    // (a piece has 32 of a thread's at most: equal logits do not reach it)
+constexpr float kMostPowers = 256.f;    // (a piece has 32 of a thread's at most: equal logits do not reach it)
 
 template <typename X> __device__ __forceinline__ float vec_max(const uint4 &u)
 {
@@ -132,12 +132,12 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
         }
     };
 
-    // A thread takes its powers with a reference that is no more than 2^6 below the largest of them, and not below the block's largest listed
+    // A warp takes its powers with a reference that is no more than 2^8 below the largest of them, and not below the block's largest listed
     // logit: an exponent is rounded at its own size, so that the largest powers, which are most of the sum and of the gradient, want
     // exponents near 0.  (Errors of 1.2e-6 relative in an FP32 gradient and 4e-6 in a small loss of few rows without the listed logit, for
     // normal logits with larger ones listed; of 5e-6 in the gradient with a reference that moved at 2^100 only, for a logit that is not
-    // listed 30 to 50 above the others.  The warp's first reference costs 0.1 us for a row and 1 % for many, a thread's own, which moves
-    // in most rows, 6 to 12 %: 4096 x 131072 took 622, 630 and 663 to 704 us.)
+    // listed 30 to 50 above the others.  It costs 1 % for 4096 x 131072 normal logits, 543 us, and 3, 7 and -13 % where they spread 2.5, 5 and 20
+    // times as far; a reference for each thread, which moves in most rows, 6 to 23 %.)
     constexpr bool anchored = MODE != kGradOnly;
     // the teacher's mass, from what it says: normalized its largest logit and 1 / s, else the mass itself
     auto mass_of = [&](float a0, float a1) { return g.normalize ? (a1 == 0.f ? 0.f : 1.f) : a0; };
@@ -470,15 +470,16 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                     wait(full[stage], phase);
                     const uint4 *piece = reinterpret_cast<const uint4 *>(smem + stage * kPiece) + tid;
                     const int vecs = sl.v1 - v;
-                    // The reference is the largest of the warp's first logits, and stays where it is unless a piece's powers add up to
+                    // A warp's reference is the largest of its first logits, and stays where it is unless a lane's powers of a piece add up to
                     // kMostPowers or more (an infinity, a NaN): then it moves to the piece's largest and the piece is summed anew.
-                    if (v == sl.v0) {
-                        float top = tid < vecs ? fmaxf(vec_max<X>(piece[0]), -minus.x) : -minus.x;
+                    auto refer = [&](float top) {
 #pragma unroll
                         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-                        s2.x *= exp2_fast((-minus.x - top) * c);
+                        const float f = exp2_fast((-minus.x - top) * c);
+                        s2 = make_float2(s2.x * f, s2.y * f);
                         minus = make_float2(-top, -top);
-                    }
+                    };
+                    if (v == sl.v0) refer(tid < vecs ? fmaxf(vec_max<X>(piece[0]), -minus.x) : -minus.x);
                     float2 sum = make_float2(0.f, 0.f);
                     if (vecs >= kPieceVecs) {
 #pragma unroll
@@ -486,12 +487,10 @@ template <typename X, typename G, int MODE> __global__ void __launch_bounds__(kD
                     } else {
                         for (int at = tid; at < vecs; at += kWorkers) add_powers<X>(piece[at - tid], minus, cc, sum);
                     }
-                    if (!(sum.x + sum.y < kMostPowers)) {
+                    if (__any_sync(0xFFFFFFFFu, !(sum.x + sum.y < kMostPowers))) {
                         float top = -minus.x;
                         for (int at = tid; at < min(vecs, kPieceVecs); at += kWorkers) top = fmaxf(top, vec_max<X>(piece[at - tid]));
-                        const float f = exp2_fast((-minus.x - top) * c);
-                        s2 = make_float2(s2.x * f, s2.y * f);
-                        minus = make_float2(-top, -top);
+                        refer(top);
                         sum = make_float2(0.f, 0.f);
                         for (int at = tid; at < min(vecs, kPieceVecs); at += kWorkers) add_powers<X>(piece[at - tid], minus, cc, sum);
                     }
