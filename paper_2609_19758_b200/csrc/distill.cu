@@ -11,8 +11,8 @@
 // cluster's shared memory, and write the gradient; one or three warps prepare the teacher's probabilities for the next row and take them off the
 // gradient of the one before, so that neither is waited for.
 //
-// Measured: 4096 rows of 131072 FP32 logits with BF16 gradients 541 us in a burst (6.0 TB/s of logits and gradients, 0.91 of a copy),
-// 632 sustained, at the power limit; losses of 2048 rows of 65536 BF16 52 us (0.79; the special function unit, which makes the powers, is busy
+// Measured: 4096 rows of 131072 FP32 logits with BF16 gradients 543 us in a burst (5.9 TB/s of logits and gradients, 0.91 of a copy),
+// 636 sustained, at the power limit; losses of 2048 rows of 65536 BF16 52 us (0.79; the special function unit, which makes the powers, is busy
 // for 66 %); loss, then gradient of 1500 x 50257 FP16 94 us; 5 rows of 131072 11 us.  (Without the
 // largest listed logit as reference 521, 49 and 9 us.)  Rows held in shared memory between the two looks
 // (eight slices of 64 KB, three blocks to an SM): 662 us, as fewer rows are at work at a time.  The gradient's factor folded into the
